@@ -156,6 +156,39 @@ SIGNATURES = [
      [_P(bdscan_ssd_dims), _P(bdscan_noisy), _P(bdscan_params), c_void_p, c_void_p, ctypes.c_size_t, c_void_p]),
 ]
 
+
+
+class bdscan_linear_dims(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d_in", ctypes.c_int64), ("d_out", ctypes.c_int64),
+                ("ld_x", ctypes.c_int64), ("ld_res", ctypes.c_int64), ("ld_y", ctypes.c_int64),
+                ("act", ctypes.c_int32), ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32)]
+
+
+class bdscan_lm_loss_dims(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d_model", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("ld_h", ctypes.c_int64), ("excluded", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+BDSCAN_ACT_NONE = 0
+BDSCAN_ACT_SILU = 1
+BDSCAN_ACT_GELU = 2
+
+# include/bdscan_dense.h
+DENSE_SIGNATURES = [
+    ("bdscan_linear_forward_workspace_size", ctypes.c_size_t, [_P(bdscan_linear_dims)]),
+    ("bdscan_linear_forward", ctypes.c_int,
+     [_P(bdscan_linear_dims)] + [c_void_p] * 7 + [ctypes.c_size_t, c_void_p]),
+    ("bdscan_linear_backward_workspace_size", ctypes.c_size_t, [_P(bdscan_linear_dims)]),
+    ("bdscan_linear_backward", ctypes.c_int,
+     [_P(bdscan_linear_dims)] + [c_void_p] * 8 + [ctypes.c_size_t, c_void_p]),
+    ("bdscan_lm_loss_forward_workspace_size", ctypes.c_size_t, [_P(bdscan_lm_loss_dims)]),
+    ("bdscan_lm_loss_forward", ctypes.c_int,
+     [_P(bdscan_lm_loss_dims)] + [c_void_p] * 7 + [ctypes.c_size_t, c_void_p]),
+    ("bdscan_lm_loss_backward_workspace_size", ctypes.c_size_t, [_P(bdscan_lm_loss_dims)]),
+    ("bdscan_lm_loss_backward", ctypes.c_int,
+     [_P(bdscan_lm_loss_dims)] + [c_void_p] * 9 + [ctypes.c_size_t, c_void_p]),
+]
+
 BDSCAN_NOALLOC_SCRATCH_BYTES = 32 << 20
 
 _lock = threading.Lock()
@@ -177,7 +210,7 @@ def load(build_if_missing: bool = True, debug=None):
             if not os.path.exists(path):
                 raise RuntimeError(f"libbdscan is not built ({path} missing); run paper_2607_02805_gb300/build.py")
             lib = ctypes.CDLL(path)
-            for name, res, args in SIGNATURES:
+            for name, res, args in SIGNATURES + DENSE_SIGNATURES:
                 f = getattr(lib, name)
                 f.restype = res
                 f.argtypes = args
@@ -399,6 +432,41 @@ def bdscan_ssd_full_bidir_forward(dims, noisy, params, y, workspace, workspace_b
     return load().bdscan_ssd_full_bidir_forward(_ref(dims), _ref(noisy), _ref(params), y, workspace,
                                                 workspace_bytes, stream)
 
+
+def bdscan_linear_forward_workspace_size(dims) -> int:
+    return load().bdscan_linear_forward_workspace_size(_ref(dims))
+
+
+def bdscan_linear_forward(dims, x, w, bias, residual, pre, y, workspace, workspace_bytes, stream):
+    return load().bdscan_linear_forward(_ref(dims), x, w, bias, residual, pre, y, workspace, workspace_bytes, stream)
+
+
+def bdscan_linear_backward_workspace_size(dims) -> int:
+    return load().bdscan_linear_backward_workspace_size(_ref(dims))
+
+
+def bdscan_linear_backward(dims, x, w, pre, dy, dx, dw, dbias, workspace, workspace_bytes, stream):
+    return load().bdscan_linear_backward(_ref(dims), x, w, pre, dy, dx, dw, dbias, workspace, workspace_bytes, stream)
+
+
+def bdscan_lm_loss_forward_workspace_size(dims) -> int:
+    return load().bdscan_lm_loss_forward_workspace_size(_ref(dims))
+
+
+def bdscan_lm_loss_forward(dims, h, w, target, weight, loss, lse, workspace, workspace_bytes, stream):
+    return load().bdscan_lm_loss_forward(_ref(dims), h, w, target, weight, loss, lse, workspace, workspace_bytes,
+                                         stream)
+
+
+def bdscan_lm_loss_backward_workspace_size(dims) -> int:
+    return load().bdscan_lm_loss_backward_workspace_size(_ref(dims))
+
+
+def bdscan_lm_loss_backward(dims, h, w, target, weight, lse, dloss, dh, dw, workspace, workspace_bytes, stream):
+    return load().bdscan_lm_loss_backward(_ref(dims), h, w, target, weight, lse, dloss, dh, dw, workspace,
+                                          workspace_bytes, stream)
+
+
 # ---------------------------------------------------------------------------
 # torch-tensor helpers (marshalling only)
 # ---------------------------------------------------------------------------
@@ -594,3 +662,51 @@ def ssd_backward(dims, t, states, dy_c, dy_n, dstates, g, workspace, stream=None
     _call("bdscan_ssd_backward", ctypes.byref(dims), ctypes.byref(make_clean(t)), ctypes.byref(make_noisy(t)),
           ctypes.byref(make_params(t)), _ptr(states), _ptr(dy_c), _ptr(dy_n), _ptr(dstates), ctypes.byref(gc),
           ctypes.byref(gn), ctypes.byref(gp), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+# ---------------------------------------------------------------------------
+# dense operators (include/bdscan_dense.h); x, residual, y, dy and h may have a
+# row stride of their own (the dims carry it)
+# ---------------------------------------------------------------------------
+def _ptr2(t):
+    """Address of a 2-D tensor whose rows are contiguous (any row stride)."""
+    if t is None:
+        return None
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("bdscan dense tensors must be 2-D with contiguous rows")
+    return t.data_ptr()
+
+
+def row_stride(t):
+    """The row stride that bdscan_linear_dims / bdscan_lm_loss_dims take for t."""
+    return int(t.stride(0)) if t.shape[0] > 1 else max(1, int(t.shape[1]))
+
+
+def make_linear_dims(rows, d_in, d_out, act=BDSCAN_ACT_NONE, dtype=BDSCAN_BF16, out_dtype=None, ld_x=0, ld_res=0,
+                     ld_y=0):
+    return bdscan_linear_dims(int(rows), int(d_in), int(d_out), int(ld_x), int(ld_res), int(ld_y), int(act),
+                              int(dtype), int(dtype if out_dtype is None else out_dtype))
+
+
+def linear_forward(dims, x, w, bias, residual, pre, y, workspace, stream=None):
+    _call("bdscan_linear_forward", ctypes.byref(dims), _ptr2(x), _ptr(w), _ptr(bias), _ptr2(residual), _ptr(pre),
+          _ptr2(y), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def linear_backward(dims, x, w, pre, dy, dx, dw, dbias, workspace, stream=None):
+    _call("bdscan_linear_backward", ctypes.byref(dims), _ptr2(x), _ptr(w), _ptr(pre), _ptr2(dy), _ptr(dx), _ptr(dw),
+          _ptr(dbias), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def make_lm_loss_dims(rows, d_model, vocab, dtype=BDSCAN_BF16, excluded=-1, ld_h=0):
+    return bdscan_lm_loss_dims(int(rows), int(d_model), int(vocab), int(ld_h), int(excluded), int(dtype))
+
+
+def lm_loss_forward(dims, h, w, target, weight, loss, lse, workspace, stream=None):
+    _call("bdscan_lm_loss_forward", ctypes.byref(dims), _ptr2(h), _ptr(w), _ptr(target), _ptr(weight), _ptr(loss),
+          _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def lm_loss_backward(dims, h, w, target, weight, lse, dloss, dh, dw, workspace, stream=None):
+    _call("bdscan_lm_loss_backward", ctypes.byref(dims), _ptr2(h), _ptr(w), _ptr(target), _ptr(weight), _ptr(lse),
+          _ptr(dloss), _ptr(dh), _ptr(dw), _ptr(workspace), _nbytes(workspace), _stream(stream))

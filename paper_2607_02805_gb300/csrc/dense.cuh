@@ -1,0 +1,124 @@
+// dense.cuh -- argument blocks and launchers of the dense operators
+// (include/bdscan_dense.h): the tcgen05 matrix product of gemm.cuh and the
+// passes around it.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace bds {
+
+// What a product does with its accumulators.
+constexpr int kEpiOut = 0;    // residual + act(acc + bias), or a split's partial sums
+constexpr int kEpiStats = 1;  // running maximum and sum of a row's logits, and the target's logit
+constexpr int kEpiDz = 2;     // the loss's gradient at the logits
+
+// A [m][k] or [k][m], B [n][k] or [k][n] come as tensor maps; extents in elements.
+struct GemmParams {
+  int m, n, k;
+  // Rows that count, known on the device only: limits m (1), k (2) or nothing (0).
+  const int* rows_dev;
+  int rows_axis;
+  int bn;         // columns of a tile (a multiple of 16 per CTA, at most the instance's BN)
+  int splits;     // ranges of k, each with its own partial sums
+  int group_m;    // row tiles walked together
+  // kEpiOut: out[row_map ? row_map[i] : i][j]
+  const void* bias;
+  const void* res;
+  void* out;
+  void* pre;
+  const int* row_map;
+  int64_t ld_res, ld_out, ld_pre;
+  int64_t split_stride;  // elements between the partial sums of two splits
+  int bias_f32, res_f32, out_f32, pre_f32;
+  int act;
+  int vec;               // rows of res, out and pre start on 4-element boundaries
+  int64_t out_extent;    // elements of `out` (debug build)
+  // kEpiStats / kEpiDz: rows i are the rows that count; column j is entry v0 + j
+  int v0, excluded;
+  const int* target;     // [rows] of the rows that count
+  float2* part;          // [2 * column tiles][rows] (maximum, sum of exponentials), base 2
+  float* at_target;      // [rows]
+  int64_t rows_ld;       // rows of `part`
+  const float* lse;      // [rows] of the rows that count
+  const float* gscale;   // [rows]
+  int64_t plane;         // kEpiDz with three pieces: elements between two of them
+  int* flag;             // set by a bounded wait that gave up
+};
+
+// Instances: CG 1 or 2 CTAs per tile, BN columns at most, `pieces` bf16 pieces
+// per operand (1: bf16 operands, 3: fp32 operands).
+struct GemmCfg {
+  int cg, bn, pieces;
+  bool a_mn, b_mn;  // operand rows along k (true) or along m / n (false)
+  int epi;
+};
+
+cudaError_t launch_gemm(const GemmCfg& c, const GemmParams& p, const CUtensorMap& a, const CUtensorMap& b,
+                        cudaStream_t s);
+// Sums of the partial sums of p.splits splits, then the output step of kEpiOut.
+cudaError_t launch_split_reduce(const GemmParams& p, const float* part, cudaStream_t s);
+
+// rows x cols of src (row stride ld) into `pieces` bf16 planes with row stride
+// ld_dst: the values themselves (bf16), or three pieces whose sum they are
+// (fp32). With `idx`, row i is source row idx[i] for i < *count and zero up to
+// the next multiple of 256 rows.
+struct PackParams {
+  const void* src;
+  int64_t ld, rows, cols;
+  __nv_bfloat16* dst;
+  int64_t ld_dst, plane;
+  int src_f32, pieces;
+  const int* idx;
+  const int* count;
+};
+cudaError_t launch_pack(const PackParams& p, cudaStream_t s);
+
+// dz = dy * act'(pre) in `pieces` bf16 planes, and partial column sums of the
+// unrounded values per row range.
+struct DactParams {
+  const void* dy;
+  const void* pre;
+  int64_t ld_dy, ld_pre, rows, cols;
+  int dy_f32, pre_f32, act, pieces;
+  __nv_bfloat16* dz;  // null: sums only
+  int64_t ld_dz, plane;
+  float* part;  // [ranges][cols], null: no sums
+  int ranges;
+};
+cudaError_t launch_dact(const DactParams& p, cudaStream_t s);
+cudaError_t launch_colsum(const float* part, int ranges, int64_t cols, void* out, int out_f32, cudaStream_t s);
+
+// y = res + act(x w^T + bias) for a few rows, without the tensor cores.
+constexpr int kVecRows = 8;
+struct VecParams {
+  const void *x, *w, *bias, *res;
+  void *y, *pre;
+  int64_t ld_x, ld_res, ld_y;
+  int rows, k, n, act, f32, out_f32;
+};
+cudaError_t launch_linear_vec(const VecParams& p, cudaStream_t s);
+
+// The rows of the loss that count (weight, and dloss if given, not zero, and a
+// target inside the vocabulary), in order: their number, index, target and
+// gradient scale. Rows that do not count get loss = lse = 0 where given.
+struct LossRowsParams {
+  const int64_t* target;
+  const float *weight, *dloss, *lse_in;
+  int64_t rows, vocab;
+  int *count, *idx, *tgt;
+  float *gscale, *lse_c;
+  float *loss, *lse;
+};
+cudaError_t launch_loss_rows(const LossRowsParams& p, cudaStream_t s);
+cudaError_t launch_loss_combine(const float2* part, int parts, int64_t rows_ld, const float* at_target,
+                                const int* count, const int* idx, const float* weight, float* loss, float* lse,
+                                int64_t rows, cudaStream_t s);
+// Zeroes the rows of dst that do not count.
+cudaError_t launch_zero_rows(const int64_t* target, const float* weight, const float* dloss, int64_t rows,
+                             int64_t vocab, void* dst, int64_t row_bytes, cudaStream_t s);
+
+int* ssd_wait_flag_ptr();  // ssd.cu
+
+}  // namespace bds

@@ -1,0 +1,764 @@
+// dense_api.cu -- the C ABI of the dense operators (include/bdscan_dense.h):
+// argument validation, workspace layout, the choice of tiles and splits, and
+// the launch sequences.
+#include <cudaTypedefs.h>
+
+#include <cstdio>
+#include <cstring>
+
+#include "bdscan_dense.h"
+#include "dense.cuh"
+#include "params.h"
+
+namespace bds {
+
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder();  // ssd.cu
+
+cudaError_t launch_gemm_nt(const GemmCfg&, const GemmParams&, const CUtensorMap&, const CUtensorMap&, cudaStream_t);
+cudaError_t launch_gemm_nn(const GemmCfg&, const GemmParams&, const CUtensorMap&, const CUtensorMap&, cudaStream_t);
+cudaError_t launch_gemm_tn(const GemmCfg&, const GemmParams&, const CUtensorMap&, const CUtensorMap&, cudaStream_t);
+cudaError_t launch_gemm_loss(const GemmCfg&, const GemmParams&, const CUtensorMap&, const CUtensorMap&, cudaStream_t);
+
+namespace {
+
+int fail_msg(int code, const char* fn, const char* what) {
+  char msg[384];
+  snprintf(msg, sizeof(msg), "%s: %s", fn, what);
+  return api_fail(code, msg);
+}
+int fail_arg(const char* fn, const char* name, const char* problem) {
+  char msg[384];
+  snprintf(msg, sizeof(msg), "%s: %s %s", fn, name, problem);
+  return api_fail(BDSCAN_ERR_ARG, msg);
+}
+int cuda_fail(cudaError_t e, const char* fn) { return fail_msg(BDSCAN_ERR_CUDA, fn, cudaGetErrorString(e)); }
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
+int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+#define DENSE_REQ(ptr, fn, name)                                               \
+  do {                                                                         \
+    if ((ptr) == nullptr) return fail_arg(fn, name, "is NULL");                \
+    if (!aligned16(ptr)) return fail_arg(fn, name, "is not 16-byte aligned");  \
+  } while (0)
+#define DENSE_OPT(ptr, fn, name)                                               \
+  do {                                                                         \
+    if ((ptr) != nullptr && !aligned16(ptr)) return fail_arg(fn, name, "is not 16-byte aligned"); \
+  } while (0)
+
+// Sizes above these are refused: extents of tensor maps and row indices are
+// 32-bit, and the products of two extents are 64-bit everywhere.
+constexpr int64_t kMaxRows = (int64_t)1 << 30;
+constexpr int64_t kMaxCols = (int64_t)1 << 24;
+
+// A bf16 operand in memory: `rows` rows of `inner` contiguous elements.
+struct Operand {
+  const void* base;
+  int64_t inner, rows, ld;
+  int pieces;
+  int64_t plane;
+};
+
+// Boxes of 64 elements x `box_rows` rows, 128-byte swizzle; elements outside
+// the operand read as zero.
+bool encode(CUtensorMap* m, const Operand& o, int box_rows) {
+  const cuuint64_t dims[3] = {(cuuint64_t)o.inner, (cuuint64_t)o.rows, (cuuint64_t)o.pieces};
+  const int64_t plane = o.pieces > 1 ? o.plane : up(o.ld * 8, 8);  // one piece: never stepped over
+  const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)plane * 2};
+  const cuuint32_t box[3] = {64u, (cuuint32_t)box_rows, 1u};
+  const cuuint32_t estr[3] = {1u, 1u, 1u};
+  return tensor_map_encoder()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.base), dims, strides, box,
+                              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Whether rows of `ld` elements of `dtype` can be read by TMA where they lie.
+bool in_place(int dtype, int64_t ld) { return dtype == BDSCAN_BF16 && ld % 8 == 0; }
+size_t packed_bytes(int dtype, int64_t rows, int64_t cols) {
+  return al256((size_t)rows * up(cols, 8) * 2 * (dtype == BDSCAN_F32 ? 3 : 1));
+}
+
+// Tiles and splits of a product of m x n over k. Functions of the sizes only,
+// for 152 SMs, so that workspace sizes do not depend on the device.
+struct Plan {
+  GemmCfg cfg;
+  int bn, splits, group_m;
+};
+constexpr int64_t kSms = 152;
+Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split) {
+  Plan q;
+  memset(&q, 0, sizeof(q));
+  q.cfg.pieces = pieces;
+  const int64_t pairs = ((m + 255) / 256) * ((n + 255) / 256);
+  if (pieces == 1 && m > 128 && pairs >= kSms / 4) {
+    q.cfg.cg = 2;
+    q.cfg.bn = 256;
+  } else {
+    q.cfg.cg = 1;
+    q.cfg.bn = pieces == 3 || ((m + 127) / 128) * ((n + 127) / 128) >= kSms / 2 ? 128 : 64;
+  }
+  const int64_t nt = (n + q.cfg.bn - 1) / q.cfg.bn;
+  q.bn = (int)up((n + nt - 1) / nt, 16 * q.cfg.cg);
+  const int64_t mt = (m + 128 * q.cfg.cg - 1) / (128 * q.cfg.cg);
+  const int64_t tiles = mt * ((n + q.bn - 1) / q.bn), nk = (k + 63) / 64;
+  q.group_m = q.cfg.cg == 2 ? 8 : 12;
+  q.splits = 1;
+  if (may_split && tiles > 0) {
+    int64_t s = (kSms / q.cfg.cg) / tiles;
+    if (s > nk / 4) s = nk / 4;
+    if (s > 16) s = 16;
+    if (s > 1) q.splits = (int)s;
+  }
+  return q;
+}
+size_t split_bytes(const Plan& q, int64_t m, int64_t n) {
+  return q.splits > 1 ? al256((size_t)q.splits * m * up(n, 4) * 4) : 0;
+}
+
+// The geometry of a plan's launch; the caller adds the epilogue's fields.
+GemmParams geometry(const Plan& q, int64_t m, int64_t n, int64_t k, int* flag) {
+  GemmParams p;
+  memset(&p, 0, sizeof(p));
+  p.m = (int)m;
+  p.n = (int)n;
+  p.k = (int)k;
+  p.bn = q.bn;
+  p.splits = 1;
+  p.group_m = q.group_m;
+  p.excluded = -1;
+  p.flag = flag;
+  return p;
+}
+
+cudaError_t run_product(const Plan& q, const GemmParams& p, const Operand& a, const Operand& b, cudaStream_t s) {
+  CUtensorMap am, bm;
+  const int b_rows = q.cfg.b_mn ? 64 : q.cfg.bn / q.cfg.cg;
+  if (!encode(&am, a, q.cfg.a_mn ? 64 : 128) || !encode(&bm, b, b_rows)) return cudaErrorInvalidValue;
+  cudaError_t e;
+  if (q.cfg.epi != kEpiOut) e = launch_gemm_loss(q.cfg, p, am, bm, s);
+  else if (q.cfg.a_mn) e = launch_gemm_tn(q.cfg, p, am, bm, s);
+  else if (q.cfg.b_mn) e = launch_gemm_nn(q.cfg, p, am, bm, s);
+  else e = launch_gemm_nt(q.cfg, p, am, bm, s);
+  return api_launched(e, s);
+}
+
+// A product with the output step of kEpiOut, split over k where the plan says
+// so: then the partial sums go to `part` and a second launch ends it.
+cudaError_t run_out(Plan q, bool a_mn, bool b_mn, const GemmParams& p, const Operand& a, const Operand& b, float* part,
+                    cudaStream_t s) {
+  q.cfg.a_mn = a_mn;
+  q.cfg.b_mn = b_mn;
+  q.cfg.epi = kEpiOut;
+  if (q.splits == 1) return run_product(q, p, a, b, s);
+  GemmParams g = p;
+  g.splits = q.splits;
+  g.bias = g.res = nullptr;
+  g.pre = nullptr;
+  g.row_map = nullptr;
+  g.out = part;
+  g.ld_out = up(p.n, 4);
+  g.split_stride = p.m * g.ld_out;
+  g.out_f32 = 1;
+  g.vec = 1;
+  g.act = BDSCAN_ACT_NONE;
+  g.out_extent = (int64_t)q.splits * g.split_stride;
+  cudaError_t e = run_product(q, g, a, b, s);
+  if (e != cudaSuccess) return e;
+  GemmParams r = p;
+  r.splits = q.splits;
+  r.split_stride = g.split_stride;
+  return api_launched(launch_split_reduce(r, part, s), s);
+}
+
+// The operand as the products read it: where it lies, or packed into `ws`.
+cudaError_t operand(Operand* o, int dtype, const void* src, int64_t rows, int64_t cols, int64_t ld, char* ws,
+                    cudaStream_t s) {
+  if (in_place(dtype, ld)) {
+    *o = Operand{src, cols, rows, ld, 1, 0};
+    return cudaSuccess;
+  }
+  PackParams p;
+  memset(&p, 0, sizeof(p));
+  p.src = src;
+  p.ld = ld;
+  p.rows = rows;
+  p.cols = cols;
+  p.dst = (__nv_bfloat16*)ws;
+  p.ld_dst = up(cols, 8);
+  p.plane = rows * p.ld_dst;
+  p.src_f32 = dtype == BDSCAN_F32;
+  p.pieces = p.src_f32 ? 3 : 1;
+  *o = Operand{ws, cols, rows, p.ld_dst, p.pieces, p.plane};
+  return api_launched(launch_pack(p, s), s);
+}
+
+int check_types(int dtype, int out_dtype, const char* fn) {
+  if (dtype != BDSCAN_F32 && dtype != BDSCAN_BF16) return fail_msg(BDSCAN_ERR_ARG, fn, "bad dtype");
+  if (out_dtype != BDSCAN_F32 && out_dtype != BDSCAN_BF16) return fail_msg(BDSCAN_ERR_ARG, fn, "bad out_dtype");
+  if (dtype == BDSCAN_F32 && out_dtype == BDSCAN_BF16)
+    return fail_msg(BDSCAN_ERR_UNSUPPORTED, fn, "f32 inputs with bf16 outputs are not supported");
+  return BDSCAN_OK;
+}
+
+// ---------------------------------------------------------------------------
+// linear
+// ---------------------------------------------------------------------------
+struct Lin {
+  int64_t T, K, N, ld_x, ld_res, ld_y;
+  int act, dtype, out, pieces;
+};
+int check_linear(const bdscan_linear_dims* d, Lin* l, const char* fn) {
+  api_begin();
+  if (d == nullptr) return fail_msg(BDSCAN_ERR_ARG, fn, "dims is NULL");
+  if (d->rows < 0) return fail_msg(BDSCAN_ERR_ARG, fn, "negative rows");
+  if (d->d_in <= 0 || d->d_out <= 0) return fail_msg(BDSCAN_ERR_ARG, fn, "d_in and d_out must be positive");
+  const int rc = check_types(d->dtype, d->out_dtype, fn);
+  if (rc) return rc;
+  if (d->act != BDSCAN_ACT_NONE && d->act != BDSCAN_ACT_SILU && d->act != BDSCAN_ACT_GELU)
+    return fail_msg(BDSCAN_ERR_ARG, fn, "bad act");
+  if (d->rows > kMaxRows || d->d_in > kMaxCols || d->d_out > kMaxCols)
+    return fail_msg(BDSCAN_ERR_UNSUPPORTED, fn, "rows above 2^30, or d_in or d_out above 2^24");
+  l->T = d->rows;
+  l->K = d->d_in;
+  l->N = d->d_out;
+  l->ld_x = d->ld_x ? d->ld_x : l->K;
+  l->ld_res = d->ld_res ? d->ld_res : l->N;
+  l->ld_y = d->ld_y ? d->ld_y : l->N;
+  if (l->ld_x < l->K) return fail_msg(BDSCAN_ERR_ARG, fn, "ld_x is below d_in");
+  if (l->ld_res < l->N) return fail_msg(BDSCAN_ERR_ARG, fn, "ld_res is below d_out");
+  if (l->ld_y < l->N) return fail_msg(BDSCAN_ERR_ARG, fn, "ld_y is below d_out");
+  if (l->ld_x > kMaxCols * 64 || l->ld_res > kMaxCols * 64 || l->ld_y > kMaxCols * 64)
+    return fail_msg(BDSCAN_ERR_UNSUPPORTED, fn, "a row stride above 2^30");
+  l->act = d->act;
+  l->dtype = d->dtype;
+  l->out = d->out_dtype;
+  l->pieces = d->dtype == BDSCAN_F32 ? 3 : 1;
+  return BDSCAN_OK;
+}
+
+// Byte offsets of a forward's workspace.
+struct LinFwdWs {
+  Plan q;
+  size_t x, w, part, total;
+};
+LinFwdWs lin_fwd_ws(const Lin& l) {
+  LinFwdWs w;
+  memset(&w, 0, sizeof(w));
+  if (l.T <= kVecRows) return w;
+  w.q = plan(l.T, l.N, l.K, l.pieces, true);
+  size_t o = 0;
+  w.x = o;
+  if (!in_place(l.dtype, l.ld_x)) o += packed_bytes(l.dtype, l.T, l.K);
+  w.w = o;
+  if (!in_place(l.dtype, l.K)) o += packed_bytes(l.dtype, l.N, l.K);
+  w.part = o;
+  w.total = o + split_bytes(w.q, l.T, l.N);
+  return w;
+}
+
+// Row ranges of the pass over dy: about four CTAs per SM, 32 rows at least.
+int dact_ranges(int64_t rows, int64_t cols) {
+  const int64_t strips = (cols + 127) / 128;
+  int64_t r = (4 * kSms + strips - 1) / strips;
+  if (r > (rows + 31) / 32) r = (rows + 31) / 32;
+  return (int)(r < 1 ? 1 : r);
+}
+struct LinBwdWs {
+  Plan qx, qw;
+  bool make_dz;  // dz differs from dy, or dy cannot be read by TMA
+  size_t x, w, dz, sums, part, total;
+  int ranges;
+};
+LinBwdWs lin_bwd_ws(const Lin& l) {
+  LinBwdWs w;
+  memset(&w, 0, sizeof(w));
+  w.qx = plan(l.T, l.K, l.N, l.pieces, true);
+  w.qw = plan(l.N, l.K, l.T, l.pieces, true);
+  w.make_dz = l.act != BDSCAN_ACT_NONE || l.out != BDSCAN_BF16 || !in_place(l.out, l.ld_y);
+  size_t o = 0;
+  w.x = o;
+  if (!in_place(l.dtype, l.ld_x)) o += packed_bytes(l.dtype, l.T, l.K);
+  w.w = o;
+  if (!in_place(l.dtype, l.K)) o += packed_bytes(l.dtype, l.N, l.K);
+  w.dz = o;
+  if (w.make_dz) o += packed_bytes(l.dtype, l.T, l.N);
+  w.sums = o;
+  w.ranges = dact_ranges(l.T, l.N);
+  o += al256((size_t)w.ranges * l.N * 4);
+  w.part = o;
+  const size_t a = split_bytes(w.qx, l.T, l.K), b = split_bytes(w.qw, l.N, l.K);
+  w.total = o + (a > b ? a : b);
+  return w;
+}
+
+// ---------------------------------------------------------------------------
+// loss
+// ---------------------------------------------------------------------------
+struct Loss {
+  int64_t T, K, V, ld_h, excluded;
+  int dtype, pieces;
+};
+int check_loss(const bdscan_lm_loss_dims* d, Loss* l, const char* fn) {
+  api_begin();
+  if (d == nullptr) return fail_msg(BDSCAN_ERR_ARG, fn, "dims is NULL");
+  if (d->rows < 0) return fail_msg(BDSCAN_ERR_ARG, fn, "negative rows");
+  if (d->d_model <= 0 || d->vocab <= 0) return fail_msg(BDSCAN_ERR_ARG, fn, "d_model and vocab must be positive");
+  const int rc = check_types(d->dtype, d->dtype, fn);
+  if (rc) return rc;
+  if (d->rows > kMaxRows || d->d_model > kMaxCols || d->vocab > kMaxCols)
+    return fail_msg(BDSCAN_ERR_UNSUPPORTED, fn, "rows above 2^30, or d_model or vocab above 2^24");
+  if (d->excluded < -1 || d->excluded >= d->vocab)
+    return fail_msg(BDSCAN_ERR_ARG, fn, "excluded is neither -1 nor inside the vocabulary");
+  l->T = d->rows;
+  l->K = d->d_model;
+  l->V = d->vocab;
+  l->ld_h = d->ld_h ? d->ld_h : l->K;
+  if (l->ld_h < l->K) return fail_msg(BDSCAN_ERR_ARG, fn, "ld_h is below d_model");
+  if (l->ld_h > kMaxCols * 64) return fail_msg(BDSCAN_ERR_UNSUPPORTED, fn, "a row stride above 2^30");
+  l->excluded = d->excluded;
+  l->dtype = d->dtype;
+  l->pieces = d->dtype == BDSCAN_F32 ? 3 : 1;
+  return BDSCAN_OK;
+}
+
+// The rows that count, gathered: their h (whole tiles of rows), indices,
+// targets, and in the backward their gradient scales and log sums.
+struct LossRows {
+  size_t count, idx, tgt, gscale, lse, h, end;
+  int64_t rows;  // T rounded up to whole tiles
+};
+LossRows loss_rows_ws(const Loss& l, size_t o) {
+  LossRows r;
+  r.rows = up(l.T, 256);
+  const size_t v = al256((size_t)r.rows * 4);
+  r.count = o;
+  r.idx = o + 256;
+  r.tgt = r.idx + v;
+  r.gscale = r.tgt + v;
+  r.lse = r.gscale + v;
+  r.h = r.lse + v;
+  r.end = r.h + packed_bytes(l.dtype, r.rows, l.K);
+  return r;
+}
+struct LossFwdWs {
+  Plan q;
+  LossRows r;
+  size_t w, part, at, total;
+  int parts;
+};
+LossFwdWs loss_fwd_ws(const Loss& l) {
+  LossFwdWs w;
+  memset(&w, 0, sizeof(w));
+  w.q = plan(l.T, l.V, l.K, l.pieces, false);
+  if (w.q.cfg.bn == 64) w.q = plan(1 << 20, l.V, l.K, 3, false), w.q.cfg.pieces = l.pieces;
+  w.r = loss_rows_ws(l, 0);
+  size_t o = w.r.end;
+  w.w = o;
+  if (!in_place(l.dtype, l.K)) o += packed_bytes(l.dtype, l.V, l.K);
+  w.parts = (int)(2 * ((l.V + w.q.bn - 1) / w.q.bn));
+  w.part = o;
+  o += al256((size_t)w.parts * w.r.rows * 8);
+  w.at = o;
+  w.total = o + al256((size_t)w.r.rows * 4);
+  return w;
+}
+
+// Vocabulary entries per piece of the backward: as many as 256 MiB hold of
+// the logits' gradient, in pieces of equal size.
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;
+struct LossBwdWs {
+  Plan qz, qh, qw;
+  LossRows r;
+  size_t w, dz, acc, part, total;
+  int64_t piece;  // entries, a multiple of 256 unless there is one piece
+  int pieces;
+};
+LossBwdWs loss_bwd_ws(const Loss& l) {
+  LossBwdWs w;
+  memset(&w, 0, sizeof(w));
+  w.r = loss_rows_ws(l, 0);
+  int64_t most = kPieceBytes / (w.r.rows * 2 * l.pieces) / 256 * 256;
+  if (most < 256) most = 256;
+  w.pieces = (int)((l.V + most - 1) / most);
+  w.piece = w.pieces == 1 ? l.V : up((l.V + w.pieces - 1) / w.pieces, 256);
+  w.pieces = (int)((l.V + w.piece - 1) / w.piece);
+  w.qz = plan(l.T, w.piece, l.K, l.pieces, false);
+  if (w.qz.cfg.bn == 64) w.qz = plan(1 << 20, w.piece, l.K, 3, false), w.qz.cfg.pieces = l.pieces;
+  w.qh = plan(l.T, l.K, w.piece, l.pieces, true);
+  w.qw = plan(w.piece, l.K, l.T, l.pieces, true);
+  size_t o = w.r.end;
+  w.w = o;
+  if (!in_place(l.dtype, l.K)) o += packed_bytes(l.dtype, l.V, l.K);
+  w.dz = o;
+  o += packed_bytes(l.dtype, w.r.rows, w.piece);
+  w.acc = o;
+  if (w.pieces > 1) o += al256((size_t)l.T * up(l.K, 4) * 4);
+  w.part = o;
+  const size_t a = split_bytes(w.qh, l.T, l.K), b = split_bytes(w.qw, w.piece, l.K);
+  w.total = o + (a > b ? a : b);
+  return w;
+}
+
+cudaError_t gather_h(const Loss& l, const LossRows& r, const void* h, char* ws, Operand* o, cudaStream_t s) {
+  PackParams p;
+  memset(&p, 0, sizeof(p));
+  p.src = h;
+  p.ld = l.ld_h;
+  p.rows = r.rows;
+  p.cols = l.K;
+  p.dst = (__nv_bfloat16*)(ws + r.h);
+  p.ld_dst = up(l.K, 8);
+  p.plane = r.rows * p.ld_dst;
+  p.src_f32 = l.dtype == BDSCAN_F32;
+  p.pieces = l.pieces;
+  p.idx = (const int*)(ws + r.idx);
+  p.count = (const int*)(ws + r.count);
+  *o = Operand{p.dst, l.K, r.rows, p.ld_dst, p.pieces, p.plane};
+  return api_launched(launch_pack(p, s), s);
+}
+
+int check_workspace(const void* ws, size_t have, size_t need, const char* fn) {
+  if (need == 0) return BDSCAN_OK;
+  DENSE_REQ(ws, fn, "workspace");
+  if (have < need) {
+    char msg[160];
+    snprintf(msg, sizeof(msg), "workspace of %zu bytes, %zu needed", have, need);
+    return fail_msg(BDSCAN_ERR_ARG, fn, msg);
+  }
+  return BDSCAN_OK;
+}
+int check_device(const char* fn, int** flag) {
+  if (tensor_map_encoder() == nullptr)
+    return fail_msg(BDSCAN_ERR_UNSUPPORTED, fn, "the driver has no tensor-map encoder");
+  *flag = ssd_wait_flag_ptr();
+  return *flag != nullptr ? BDSCAN_OK : fail_msg(BDSCAN_ERR_CUDA, fn, "cannot locate the device wait flag");
+}
+
+}  // namespace
+}  // namespace bds
+
+using namespace bds;
+
+extern "C" {
+
+size_t bdscan_linear_forward_workspace_size(const bdscan_linear_dims* dims) {
+  Lin l;
+  if (check_linear(dims, &l, "bdscan_linear_forward_workspace_size") != BDSCAN_OK || l.T == 0) return 0;
+  return lin_fwd_ws(l).total;
+}
+
+int bdscan_linear_forward(const bdscan_linear_dims* dims, const void* x, const void* w, const void* bias,
+                          const void* residual, void* pre, void* y, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+  const char* fn = "bdscan_linear_forward";
+  Lin l;
+  int rc = check_linear(dims, &l, fn);
+  if (rc) return rc;
+  if (l.T == 0) return api_ok();
+  DENSE_REQ(x, fn, "x");
+  DENSE_REQ(w, fn, "w");
+  DENSE_OPT(bias, fn, "bias");
+  DENSE_OPT(residual, fn, "residual");
+  DENSE_OPT(pre, fn, "pre");
+  DENSE_REQ(y, fn, "y");
+  cudaStream_t s = (cudaStream_t)stream;
+  if (l.T <= kVecRows) {
+    VecParams v{};
+    v.x = x, v.w = w, v.bias = bias, v.res = residual, v.y = y, v.pre = pre;
+    v.ld_x = l.ld_x, v.ld_res = l.ld_res, v.ld_y = l.ld_y;
+    v.rows = (int)l.T, v.k = (int)l.K, v.n = (int)l.N, v.act = l.act;
+    v.f32 = l.dtype == BDSCAN_F32, v.out_f32 = l.out == BDSCAN_F32;
+    const cudaError_t e = api_launched(launch_linear_vec(v, s), s);
+    return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+  }
+  const LinFwdWs ws = lin_fwd_ws(l);
+  if ((rc = check_workspace(workspace, workspace_bytes, ws.total, fn))) return rc;
+  int* flag;
+  if ((rc = check_device(fn, &flag))) return rc;
+  char* base = (char*)workspace;
+  Operand a, b;
+  cudaError_t e = operand(&a, l.dtype, x, l.T, l.K, l.ld_x, base + ws.x, s);
+  if (e == cudaSuccess) e = operand(&b, l.dtype, w, l.N, l.K, l.K, base + ws.w, s);
+  if (e == cudaSuccess) {
+    GemmParams p = geometry(ws.q, l.T, l.N, l.K, flag);
+    p.bias = bias;
+    p.res = residual;
+    p.pre = pre;
+    p.out = y;
+    p.ld_res = l.ld_res;
+    p.ld_out = l.ld_y;
+    p.ld_pre = l.N;
+    p.bias_f32 = p.pre_f32 = l.dtype == BDSCAN_F32;
+    p.res_f32 = p.out_f32 = l.out == BDSCAN_F32;
+    p.act = l.act;
+    p.vec = l.ld_y % 4 == 0 && (residual == nullptr || l.ld_res % 4 == 0) && (pre == nullptr || l.N % 4 == 0);
+    p.out_extent = (l.T - 1) * l.ld_y + l.N;
+    e = run_out(ws.q, false, false, p, a, b, (float*)(base + ws.part), s);
+  }
+  return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+}
+
+size_t bdscan_linear_backward_workspace_size(const bdscan_linear_dims* dims) {
+  Lin l;
+  if (check_linear(dims, &l, "bdscan_linear_backward_workspace_size") != BDSCAN_OK || l.T == 0) return 0;
+  return lin_bwd_ws(l).total;
+}
+
+int bdscan_linear_backward(const bdscan_linear_dims* dims, const void* x, const void* w, const void* pre,
+                           const void* dy, void* dx, void* dw, void* dbias, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  const char* fn = "bdscan_linear_backward";
+  Lin l;
+  int rc = check_linear(dims, &l, fn);
+  if (rc) return rc;
+  DENSE_OPT(dx, fn, "dx");
+  DENSE_OPT(dw, fn, "dw");
+  DENSE_OPT(dbias, fn, "dbias");
+  cudaStream_t s = (cudaStream_t)stream;
+  const size_t elt = l.dtype == BDSCAN_F32 ? 4 : 2;
+  if (l.T == 0) {  // sums over no rows
+    cudaError_t e = cudaSuccess;
+    if (dw != nullptr) e = cudaMemsetAsync(dw, 0, (size_t)l.N * l.K * elt, s);
+    if (dbias != nullptr && e == cudaSuccess) e = cudaMemsetAsync(dbias, 0, (size_t)l.N * elt, s);
+    return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+  }
+  if (dw != nullptr) DENSE_REQ(x, fn, "x");
+  if (dx != nullptr) DENSE_REQ(w, fn, "w");
+  if (l.act != BDSCAN_ACT_NONE) DENSE_REQ(pre, fn, "pre");
+  DENSE_REQ(dy, fn, "dy");
+  const LinBwdWs ws = lin_bwd_ws(l);
+  if ((rc = check_workspace(workspace, workspace_bytes, ws.total, fn))) return rc;
+  int* flag;
+  if ((rc = check_device(fn, &flag))) return rc;
+  char* base = (char*)workspace;
+  float* part = (float*)(base + ws.part);
+  cudaError_t e = cudaSuccess;
+  const bool products = dx != nullptr || dw != nullptr;
+  Operand dz{dy, l.N, l.T, l.ld_y, 1, 0};
+  if ((products && ws.make_dz) || dbias != nullptr) {
+    DactParams p;
+    memset(&p, 0, sizeof(p));
+    p.dy = dy;
+    p.pre = pre;
+    p.ld_dy = l.ld_y;
+    p.ld_pre = l.N;
+    p.rows = l.T;
+    p.cols = l.N;
+    p.dy_f32 = l.out == BDSCAN_F32;
+    p.pre_f32 = l.dtype == BDSCAN_F32;
+    p.act = l.act;
+    p.pieces = l.pieces;
+    p.ranges = ws.ranges;
+    if (products && ws.make_dz) {
+      p.dz = (__nv_bfloat16*)(base + ws.dz);
+      p.ld_dz = up(l.N, 8);
+      p.plane = l.T * p.ld_dz;
+      dz = Operand{p.dz, l.N, l.T, p.ld_dz, l.pieces, p.plane};
+    }
+    p.part = dbias != nullptr ? (float*)(base + ws.sums) : nullptr;
+    e = api_launched(launch_dact(p, s), s);
+    if (e == cudaSuccess && dbias != nullptr)
+      e = api_launched(launch_colsum(p.part, p.ranges, l.N, dbias, l.dtype == BDSCAN_F32, s), s);
+  }
+  if (e == cudaSuccess && dx != nullptr) {
+    Operand b;
+    e = operand(&b, l.dtype, w, l.N, l.K, l.K, base + ws.w, s);
+    if (e == cudaSuccess) {
+      GemmParams p = geometry(ws.qx, l.T, l.K, l.N, flag);
+      p.out = dx;
+      p.ld_out = l.K;
+      p.out_f32 = l.dtype == BDSCAN_F32;
+      p.vec = l.K % 4 == 0;
+      p.out_extent = l.T * l.K;
+      e = run_out(ws.qx, false, true, p, dz, b, part, s);
+    }
+  }
+  if (e == cudaSuccess && dw != nullptr) {
+    Operand b;
+    e = operand(&b, l.dtype, x, l.T, l.K, l.ld_x, base + ws.x, s);
+    if (e == cudaSuccess) {
+      GemmParams p = geometry(ws.qw, l.N, l.K, l.T, flag);
+      p.out = dw;
+      p.ld_out = l.K;
+      p.out_f32 = l.dtype == BDSCAN_F32;
+      p.vec = l.K % 4 == 0;
+      p.out_extent = l.N * l.K;
+      e = run_out(ws.qw, true, true, p, dz, b, part, s);
+    }
+  }
+  return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+}
+
+size_t bdscan_lm_loss_forward_workspace_size(const bdscan_lm_loss_dims* dims) {
+  Loss l;
+  if (check_loss(dims, &l, "bdscan_lm_loss_forward_workspace_size") != BDSCAN_OK || l.T == 0) return 0;
+  return loss_fwd_ws(l).total;
+}
+
+int bdscan_lm_loss_forward(const bdscan_lm_loss_dims* dims, const void* h, const void* w, const int64_t* target,
+                           const float* weight, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  const char* fn = "bdscan_lm_loss_forward";
+  Loss l;
+  int rc = check_loss(dims, &l, fn);
+  if (rc) return rc;
+  if (l.T == 0) return api_ok();
+  DENSE_REQ(h, fn, "h");
+  DENSE_REQ(w, fn, "w");
+  DENSE_REQ(target, fn, "target");
+  DENSE_OPT(weight, fn, "weight");
+  DENSE_REQ(loss, fn, "loss");
+  DENSE_REQ(lse, fn, "lse");
+  const LossFwdWs ws = loss_fwd_ws(l);
+  if ((rc = check_workspace(workspace, workspace_bytes, ws.total, fn))) return rc;
+  int* flag;
+  if ((rc = check_device(fn, &flag))) return rc;
+  cudaStream_t s = (cudaStream_t)stream;
+  char* base = (char*)workspace;
+  LossRowsParams rp;
+  memset(&rp, 0, sizeof(rp));
+  rp.target = target;
+  rp.weight = weight;
+  rp.rows = l.T;
+  rp.vocab = l.V;
+  rp.count = (int*)(base + ws.r.count);
+  rp.idx = (int*)(base + ws.r.idx);
+  rp.tgt = (int*)(base + ws.r.tgt);
+  rp.loss = loss;
+  rp.lse = lse;
+  cudaError_t e = api_launched(launch_loss_rows(rp, s), s);
+  Operand a, b;
+  if (e == cudaSuccess) e = gather_h(l, ws.r, h, base, &a, s);
+  if (e == cudaSuccess) e = operand(&b, l.dtype, w, l.V, l.K, l.K, base + ws.w, s);
+  if (e == cudaSuccess) {
+    Plan q = ws.q;
+    q.cfg.epi = kEpiStats;
+    GemmParams p = geometry(q, l.T, l.V, l.K, flag);
+    p.rows_dev = rp.count;
+    p.rows_axis = 1;
+    p.target = rp.tgt;
+    p.excluded = (int)l.excluded;
+    p.part = (float2*)(base + ws.part);
+    p.at_target = (float*)(base + ws.at);
+    p.rows_ld = ws.r.rows;
+    e = run_product(q, p, a, b, s);
+  }
+  if (e == cudaSuccess)
+    e = api_launched(launch_loss_combine((const float2*)(base + ws.part), ws.parts, ws.r.rows,
+                                         (const float*)(base + ws.at), rp.count, rp.idx, weight, loss, lse, l.T, s),
+                     s);
+  return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+}
+
+size_t bdscan_lm_loss_backward_workspace_size(const bdscan_lm_loss_dims* dims) {
+  Loss l;
+  if (check_loss(dims, &l, "bdscan_lm_loss_backward_workspace_size") != BDSCAN_OK || l.T == 0) return 0;
+  return loss_bwd_ws(l).total;
+}
+
+int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, const void* w, const int64_t* target,
+                            const float* weight, const float* lse, const float* dloss, void* dh, void* dw,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "bdscan_lm_loss_backward";
+  Loss l;
+  int rc = check_loss(dims, &l, fn);
+  if (rc) return rc;
+  const size_t elt = l.dtype == BDSCAN_F32 ? 4 : 2;
+  cudaStream_t s = (cudaStream_t)stream;
+  DENSE_REQ(dw, fn, "dw");
+  if (l.T == 0) {
+    const cudaError_t e = cudaMemsetAsync(dw, 0, (size_t)l.V * l.K * elt, s);
+    return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+  }
+  DENSE_REQ(h, fn, "h");
+  DENSE_REQ(w, fn, "w");
+  DENSE_REQ(target, fn, "target");
+  DENSE_OPT(weight, fn, "weight");
+  DENSE_REQ(lse, fn, "lse");
+  DENSE_OPT(dloss, fn, "dloss");
+  DENSE_REQ(dh, fn, "dh");
+  const LossBwdWs ws = loss_bwd_ws(l);
+  if ((rc = check_workspace(workspace, workspace_bytes, ws.total, fn))) return rc;
+  int* flag;
+  if ((rc = check_device(fn, &flag))) return rc;
+  char* base = (char*)workspace;
+  LossRowsParams rp;
+  memset(&rp, 0, sizeof(rp));
+  rp.target = target;
+  rp.weight = weight;
+  rp.dloss = dloss;
+  rp.lse_in = lse;
+  rp.rows = l.T;
+  rp.vocab = l.V;
+  rp.count = (int*)(base + ws.r.count);
+  rp.idx = (int*)(base + ws.r.idx);
+  rp.tgt = (int*)(base + ws.r.tgt);
+  rp.gscale = (float*)(base + ws.r.gscale);
+  rp.lse_c = (float*)(base + ws.r.lse);
+  cudaError_t e = api_launched(launch_loss_rows(rp, s), s);
+  if (e == cudaSuccess)
+    e = api_launched(launch_zero_rows(target, weight, dloss, l.T, l.V, dh, (int64_t)(l.K * elt), s), s);
+  Operand a, b;
+  if (e == cudaSuccess) e = gather_h(l, ws.r, h, base, &a, s);
+  if (e == cudaSuccess) e = operand(&b, l.dtype, w, l.V, l.K, l.K, base + ws.w, s);
+  const int64_t ld_dz = up(ws.piece, 8), ld_acc = up(l.K, 4);
+  const int f32 = l.dtype == BDSCAN_F32;
+  float* part = (float*)(base + ws.part);
+  float* acc = (float*)(base + ws.acc);
+  for (int i = 0; i < ws.pieces && e == cudaSuccess; ++i) {
+    const int64_t v0 = i * ws.piece, n = l.V - v0 < ws.piece ? l.V - v0 : ws.piece;
+    Operand bp = b;  // this piece's rows of w
+    bp.base = (const char*)b.base + v0 * b.ld * 2;
+    bp.rows = n;
+    const Operand dz{base + ws.dz, n, ws.r.rows, ld_dz, l.pieces, ws.r.rows * ld_dz};
+    // the logits' gradient
+    Plan q = ws.qz;
+    q.cfg.epi = kEpiDz;
+    GemmParams p = geometry(q, l.T, n, l.K, flag);
+    p.rows_dev = rp.count;
+    p.rows_axis = 1;
+    p.target = rp.tgt;
+    p.v0 = (int)v0;
+    p.excluded = (int)l.excluded;
+    p.lse = rp.lse_c;
+    p.gscale = rp.gscale;
+    p.out = base + ws.dz;
+    p.ld_out = ld_dz;
+    p.plane = ws.r.rows * ld_dz;
+    p.out_extent = ws.r.rows * ld_dz;
+    e = run_product(q, p, a, bp, s);
+    // this piece's rows of dw
+    if (e == cudaSuccess) {
+      GemmParams g = geometry(ws.qw, n, l.K, ws.r.rows, flag);
+      g.rows_dev = rp.count;
+      g.rows_axis = 2;
+      g.out = (char*)dw + (size_t)v0 * l.K * elt;
+      g.ld_out = l.K;
+      g.out_f32 = f32;
+      g.vec = l.K % 4 == 0;
+      g.out_extent = n * l.K;
+      e = run_out(ws.qw, true, true, g, dz, a, part, s);
+    }
+    // its part of dh: fp32 sums over the pieces, the last one writes dh
+    if (e == cudaSuccess) {
+      const bool last = i + 1 == ws.pieces;
+      GemmParams g = geometry(ws.qh, l.T, l.K, n, flag);
+      g.rows_dev = rp.count;
+      g.rows_axis = 1;
+      g.res = i > 0 ? acc : nullptr;
+      g.ld_res = ld_acc;
+      g.res_f32 = 1;
+      g.out = last ? dh : acc;
+      g.ld_out = last ? l.K : ld_acc;
+      g.out_f32 = last ? f32 : 1;
+      g.row_map = last ? rp.idx : nullptr;
+      g.vec = g.ld_out % 4 == 0;
+      g.out_extent = last ? l.T * l.K : l.T * ld_acc;
+      e = run_out(ws.qh, false, true, g, dz, bp, part, s);
+    }
+  }
+  return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+}
+
+}  // extern "C"

@@ -1,0 +1,629 @@
+// gemm.cuh -- the matrix product of the dense operators on the tcgen05 tensor
+// cores: C[m, n] = sum_k A[m, k] B[n, k], fp32 accumulators in TMEM, one of the
+// epilogues of dense.cuh.
+//
+// One CTA (CG = 1) computes tiles of 128 x BN; a pair of CTAs (CG = 2) one of
+// 256 x BN, each holding its 128 rows of A and half of the columns of B, so
+// that a byte of B staged in shared memory feeds twice the MMAs. At 128 x 256
+// per CTA and step of 64 the operands are 48 KB per 512 tensor clocks, more
+// than an SM's share of the L2; the pair takes 32 KB.
+//
+// Persistent CTAs, roles by warp: 0 issues the TMA loads of a ring of stages,
+// 1 the MMAs, 2 owns the TMEM allocation, 4 to 11 run the epilogue of one
+// accumulator while the MMAs fill the other. A stage holds 64 elements of k of
+// both operands in the 128-byte swizzled layout of umma.cuh, rows along m or n
+// (K-major) or along k (MN-major), as the operand lies in memory: no operand
+// is transposed by a pass of its own.
+//
+// fp32 operands come as three bf16 pieces each (value = p0 + p1 + p2 to 24
+// bits); the six products with the largest terms are accumulated, smallest
+// first, and after every 64 elements of k the epilogue warps add the
+// accumulator to fp32 registers: the tensor core's own accumulation truncates,
+// and over a long k that error would grow with k.
+//
+// Every wait has a poll limit. A role that gives up sets the wait flag and
+// leaves its loop; the producer then waits for its copies in flight, and TMEM
+// is freed.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "dense.cuh"
+#include "device.cuh"
+#include "params.h"
+#include "ssd_common.cuh"
+#include "umma.cuh"
+
+namespace bds {
+namespace {
+
+constexpr int kGemmThreads = 384;
+constexpr int kEpiWarps = 8;
+constexpr int kBk = 64;  // elements of k per stage: one 128-byte swizzled row
+
+template <int CG, int BN, int NP>
+struct GemmSmem {
+  static constexpr uint32_t kA = 128u * 128u;                // one piece of A
+  static constexpr uint32_t kB = (uint32_t)(BN / CG) * 128u;  // one piece of B
+  static constexpr uint32_t kStage = NP * (kA + kB);
+  static constexpr uint32_t kEpi = kEpiWarps * 4096u;
+  static constexpr int kStages = (int)((232448u - 1024u - 512u - kEpi) / kStage) > 8
+                                     ? 8
+                                     : (int)((232448u - 1024u - 512u - kEpi) / kStage);
+  static constexpr uint32_t kBytes = kStages * kStage + kEpi + 1024u;
+  static_assert(kStages >= 2, "at least two stages");
+};
+
+// ---- cluster and two-CTA forms of the pieces of umma.cuh ----
+__device__ __forceinline__ uint32_t cta_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t map_cta(uint32_t saddr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(r) : "r"(saddr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
+template <int CG>
+__device__ __forceinline__ bool gbar_wait(uint64_t* bar, uint32_t parity) {
+  if constexpr (CG == 1) {
+    return umma::bar_wait(bar, parity);
+  } else {
+    const uint32_t a = umma::smem_u32(bar);
+    for (uint32_t i = 0; i < (1u << 22); ++i) {
+      uint32_t done;
+      asm volatile(
+          "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+          " selp.u32 %0, 1, 0, p;\n}\n"
+          : "=r"(done)
+          : "r"(a), "r"(parity)
+          : "memory");
+      if (done) return true;
+    }
+    return false;
+  }
+}
+// The same by every lane of a warp, which leaves together.
+template <int CG>
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
+  return __all_sync(0xffffffffu, gbar_wait<CG>(bar, parity));
+}
+// One arrival at the barrier at this offset in the tile's first CTA.
+template <int CG>
+__device__ __forceinline__ void leader_arrive(uint64_t* bar) {
+  if constexpr (CG == 1)
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(umma::smem_u32(bar)) : "memory");
+  else
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(
+                     map_cta(umma::smem_u32(bar), 0))
+                 : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void gtma_load(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+  if constexpr (CG == 1)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
+        "[%5];\n" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, "
+        "{%2, %3, %4}], [%5];\n" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void gmma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+  if constexpr (CG == 1)
+    umma::mma_bf16(d, a, b, idesc, acc);
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc ? 1u : 0u)
+        : "memory");
+}
+// The barrier at this offset in every CTA of the tile completes a phase when
+// the MMAs issued so far have finished.
+template <int CG>
+__device__ __forceinline__ void gcommit(uint64_t* bar) {
+  if constexpr (CG == 1)
+    umma::mma_commit(bar);
+  else
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n" ::"r"(
+            umma::smem_u32(bar)),
+        "h"((uint16_t)3)
+        : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void gtmem_alloc(uint32_t* slot, uint32_t cols) {
+  if constexpr (CG == 1)
+    asm volatile(
+        "tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n"
+        "tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::"r"(umma::smem_u32(slot)),
+        "r"(cols)
+        : "memory");
+  else
+    asm volatile(
+        "tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n"
+        "tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::"r"(umma::smem_u32(slot)),
+        "r"(cols)
+        : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void gtmem_dealloc(uint32_t tm, uint32_t cols) {
+  if constexpr (CG == 1)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tm), "r"(cols));
+  else
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tm), "r"(cols));
+}
+
+// ---- activations ----
+// GELU is its tanh form, z (1 + tanh u) / 2 = z sigmoid(2 u): one exponential
+// and one reciprocal on the MUFU unit instead of a polynomial per element. The
+// argument is clamped to +-16, where the sigmoid is 0 or 1 in fp32, so that the
+// cube cannot overflow.
+constexpr int kActNone = 0, kActSilu = 1, kActGelu = 2;
+constexpr float kGeluA = 0.7978845608028654f;  // sqrt(2 / pi)
+constexpr float kGeluB = 0.044715f;
+__device__ __forceinline__ float sigmoid_f(float z) { return __fdividef(1.f, 1.f + ex2(-kLog2e * z)); }
+__device__ __forceinline__ float act_fwd(int act, float z) {
+  if (act == kActNone) return z;
+  if (act == kActSilu) return z * sigmoid_f(z);
+  const float c = fminf(fmaxf(z, -16.f), 16.f);
+  return z * sigmoid_f(2.f * kGeluA * (c + kGeluB * c * c * c));
+}
+__device__ __forceinline__ float act_grad(int act, float z) {
+  if (act == kActNone) return 1.f;
+  const float c = fminf(fmaxf(z, -80.f), 80.f);
+  if (act == kActSilu) {
+    const float s = sigmoid_f(c);
+    return s * (1.f + c * (1.f - s));
+  }
+  const float g = fminf(fmaxf(z, -16.f), 16.f);
+  const float s = sigmoid_f(2.f * kGeluA * (g + kGeluB * g * g * g));
+  return s * (1.f + g * (1.f - s) * 2.f * kGeluA * (1.f + 3.f * kGeluB * g * g));
+}
+
+// fp32 as three bf16 pieces (8 + 8 + 8 bits). The first is cut towards zero
+// where rounding would overflow; a value that is not finite is its own first
+// piece.
+__device__ __forceinline__ void split3(float v, bf16& a, bf16& b, bf16& c) {
+  a = __float2bfloat16_rn(v);
+  const float f = __bfloat162float(a);
+  if (!isfinite(f)) {
+    if (isfinite(v)) a = __float2bfloat16_rz(v);
+    else {
+      b = c = __float2bfloat16_rn(0.f);
+      return;
+    }
+  }
+  const float r = v - __bfloat162float(a);
+  b = __float2bfloat16_rn(r);
+  c = __float2bfloat16_rn(r - __bfloat162float(b));
+}
+
+__device__ __forceinline__ float4 load4(const void* p, int f32, int64_t at) {
+  if (f32) return *reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+  const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const bf16*>(p) + at);
+  const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
+  const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
+  return make_float4(a.x, a.y, b.x, b.y);
+}
+__device__ __forceinline__ float load1(const void* p, int f32, int64_t at) {
+  return f32 ? static_cast<const float*>(p)[at] : __bfloat162float(static_cast<const bf16*>(p)[at]);
+}
+__device__ __forceinline__ void store4(void* p, int f32, int64_t at, float4 v) {
+  if (f32)
+    *reinterpret_cast<float4*>(static_cast<float*>(p) + at) = v;
+  else
+    *reinterpret_cast<uint2*>(static_cast<bf16*>(p) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+}
+__device__ __forceinline__ void store1(void* p, int f32, int64_t at, float v) {
+  if (f32) static_cast<float*>(p)[at] = v;
+  else static_cast<bf16*>(p)[at] = __float2bfloat16_rn(v);
+}
+
+// The output step of kEpiOut for up to four columns of one row.
+__device__ __forceinline__ void out4(const GemmParams& p, int64_t row, int col, float4 v, const float (&bias)[4],
+                                     bool split, int64_t out_off) {
+  const int64_t orow = p.row_map != nullptr ? p.row_map[row] : row;
+  const bool full = p.vec && col + 3 < p.n;
+  if (split) {
+    const int64_t at = out_off + orow * p.ld_out + col;
+    if (full) store4(p.out, 1, at, v);
+    else {
+      const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (col + j < p.n) store1(p.out, 1, at + j, e[j]);
+    }
+    return;
+  }
+  float e[4] = {v.x + bias[0], v.y + bias[1], v.z + bias[2], v.w + bias[3]};
+  if (p.pre != nullptr) {
+    const int64_t at = row * p.ld_pre + col;
+    if (full) store4(p.pre, p.pre_f32, at, make_float4(e[0], e[1], e[2], e[3]));
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (col + j < p.n) store1(p.pre, p.pre_f32, at + j, e[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) e[j] = act_fwd(p.act, e[j]);
+  if (p.res != nullptr) {
+    const int64_t at = row * p.ld_res + col;
+    if (full) {
+      const float4 r = load4(p.res, p.res_f32, at);
+      e[0] += r.x, e[1] += r.y, e[2] += r.z, e[3] += r.w;
+    } else
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (col + j < p.n) e[j] += load1(p.res, p.res_f32, at + j);
+  }
+  const int64_t at = orow * p.ld_out + col;
+  if (full) store4(p.out, p.out_f32, at, make_float4(e[0], e[1], e[2], e[3]));
+  else
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (col + j < p.n) store1(p.out, p.out_f32, at + j, e[j]);
+}
+__device__ __forceinline__ void bias4(const GemmParams& p, int col, float (&b)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) b[j] = p.bias != nullptr && col + j < p.n ? load1(p.bias, p.bias_f32, col + j) : 0.f;
+}
+
+// Extents of one call with the device's row count applied, and its tiles.
+template <int CG>
+struct Tiles {
+  int m, k, mt, nt, nk, total;
+  __device__ __forceinline__ explicit Tiles(const GemmParams& p) {
+    m = p.m;
+    k = p.k;
+    if (p.rows_axis == 1) m = min(m, *p.rows_dev);
+    if (p.rows_axis == 2) k = min(k, *p.rows_dev);
+    mt = (m + 128 * CG - 1) / (128 * CG);
+    nt = (p.n + p.bn - 1) / p.bn;
+    nk = (k + kBk - 1) / kBk;
+    total = mt * nt * p.splits;
+  }
+  // Tile t: groups of group_m row tiles, all column tiles of a group before the next.
+  __device__ __forceinline__ void at(const GemmParams& p, int t, int& tm, int& tn, int& k0, int& k1, int& sp) const {
+    sp = t / (mt * nt);
+    const int r = t - sp * (mt * nt), per = p.group_m * nt, g = r / per, q = r - g * per;
+    const int rows = min(p.group_m, mt - g * p.group_m);
+    tm = g * p.group_m + q % rows;
+    tn = q / rows;
+    k0 = (int)((int64_t)nk * sp / p.splits);
+    k1 = (int)((int64_t)nk * (sp + 1) / p.splits);
+  }
+};
+
+template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    k_gemm(const GemmParams p, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap) {
+  using S = GemmSmem<CG, BN, NP>;
+  constexpr int ST = S::kStages;
+  constexpr bool FLUSH = NP == 3;
+  constexpr uint32_t kCols = 2u * BN < 32u ? 32u : 2u * BN;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ uint64_t full[8], empty[8], accfull[2], accempty[2];
+  __shared__ uint32_t tslot;
+  unsigned char* sm = align1024(smem_raw);
+  const int t = threadIdx.x, w = t >> 5, lane = t & 31;
+  const uint32_t rank = CG == 2 ? cta_rank() : 0u;
+  const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
+  if (t == 0) {
+    for (int i = 0; i < ST; ++i) {
+      umma::bar_init(&full[i], 1);
+      umma::bar_init(&empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      umma::bar_init(&accfull[i], 1);
+      umma::bar_init(&accempty[i], kEpiWarps * CG);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  if (w == 2) gtmem_alloc<CG>(&tslot, kCols);
+  umma::fence_before_sync();
+  __syncthreads();
+  if constexpr (CG == 2) cluster_sync_all();
+  umma::fence_after_sync();
+  const uint32_t tm = tslot;
+  pdl_sync();
+  const Tiles<CG> T(p);
+  if (w == 0) {
+    // ---------------- producer ----------------
+    if (lane == 0) {
+      const uint32_t base = umma::smem_u32(sm);
+      bool ok = true;
+      int it = 0;
+      for (int tile = unit; tile < T.total && ok; tile += units) {
+        int tmi, tni, k0, k1, sp;
+        T.at(p, tile, tmi, tni, k0, k1, sp);
+        const int m0 = tmi * 128 * CG + (int)rank * 128;
+        const int n0 = tni * p.bn + (CG == 2 ? (int)rank * (p.bn / 2) : 0);
+        for (int kb = k0; kb < k1; ++kb, ++it) {
+          const int s = it % ST;
+          if (!(ok = gbar_wait<CG>(&empty[s], ((it / ST) & 1) ^ 1))) break;
+          if (rank == 0) bar_expect_tx(&full[s], S::kStage * CG);
+          const uint32_t bar = CG == 2 ? map_cta(umma::smem_u32(&full[s]), 0) : umma::smem_u32(&full[s]);
+          const uint32_t a = base + (uint32_t)s * S::kStage, b = a + NP * S::kA;
+#pragma unroll
+          for (int q = 0; q < NP; ++q) {
+            if constexpr (A_MN) {
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                gtma_load<CG>(a + q * S::kA + j * 8192u, &amap, m0 + 64 * j, kb * kBk, q, bar);
+            } else {
+              gtma_load<CG>(a + q * S::kA, &amap, kb * kBk, m0, q, bar);
+            }
+            if constexpr (B_MN) {
+#pragma unroll
+              for (int j = 0; j < BN / CG / 64; ++j)
+                gtma_load<CG>(b + q * S::kB + j * 8192u, &bmap, n0 + 64 * j, kb * kBk, q, bar);
+            } else {
+              gtma_load<CG>(b + q * S::kB, &bmap, kb * kBk, n0, q, bar);
+            }
+          }
+        }
+      }
+      // the stages in flight: consumed (their release has arrived in this CTA), or after a give-up at least landed
+      for (int i = max(0, it - ST); i < it; ++i) {
+        if (ok) ok = gbar_wait<CG>(&empty[i % ST], (i / ST) & 1);
+        if (!ok && rank == 0) gbar_wait<CG>(&full[i % ST], (i / ST) & 1);
+      }
+      if (!ok) atomicExch(p.flag, 1);
+    }
+  } else if (w == 1) {
+    // ---------------- MMA issue ----------------
+    if (lane == 0 && rank == 0) {
+      const uint32_t idesc = umma::idesc_bf16(128 * CG, (uint32_t)p.bn, A_MN, B_MN);
+      constexpr uint32_t astep = A_MN ? 2048u : 32u, bstep = B_MN ? 2048u : 32u;  // bytes per 16 elements of k
+      const uint32_t base = umma::smem_u32(sm);
+      bool ok = true;
+      int it = 0, job = 0;
+      for (int tile = unit; tile < T.total && ok; tile += units) {
+        int tmi, tni, k0, k1, sp;
+        T.at(p, tile, tmi, tni, k0, k1, sp);
+        for (int kb = k0; kb < k1; ++kb, ++it) {
+          const bool first = FLUSH || kb == k0, last = FLUSH || kb + 1 == k1;
+          if (first) {
+            if (!(ok = gbar_wait<CG>(&accempty[job & 1], ((job >> 1) & 1) ^ 1))) break;
+            umma::fence_after_sync();
+          }
+          const int s = it % ST;
+          if (!(ok = gbar_wait<CG>(&full[s], (it / ST) & 1))) break;
+          umma::fence_after_sync();
+          const uint32_t a = base + (uint32_t)s * S::kStage, b = a + NP * S::kA;
+          const uint32_t d = tm + (uint32_t)(job & 1) * BN;
+          const uint64_t da = umma::sdesc(a, A_MN ? 8192u : 16u, 1024u), db = umma::sdesc(b, B_MN ? 8192u : 16u, 1024u);
+          if constexpr (NP == 1) {
+#pragma unroll
+            for (int q = 0; q < kBk / 16; ++q)
+              gmma<CG>(d, umma::sdesc_adv(da, q * astep), umma::sdesc_adv(db, q * bstep), idesc, !first || q > 0);
+          } else {
+            constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};  // smallest terms first
+#pragma unroll
+            for (int c = 0; c < 6; ++c)
+#pragma unroll
+              for (int q = 0; q < kBk / 16; ++q)
+                gmma<CG>(d, umma::sdesc_adv(da, pa[c] * S::kA + q * astep),
+                         umma::sdesc_adv(db, pb[c] * S::kB + q * bstep), idesc, c > 0 || q > 0);
+          }
+          gcommit<CG>(&empty[s]);
+          if (last) {
+            gcommit<CG>(&accfull[job & 1]);
+            ++job;
+          }
+        }
+      }
+      if (!ok) atomicExch(p.flag, 1);
+    }
+  } else if (w >= 4) {
+    // ---------------- epilogue ----------------
+    const int ew = w - 4, half = ew >> 2;  // TMEM lanes 32 (w % 4) .. + 31, every second chunk of 32 columns
+    const uint32_t lanes = tm + ((uint32_t)(32 * (w & 3)) << 16);
+    float* stg = reinterpret_cast<float*>(sm + ST * S::kStage) + ew * 1024;
+    constexpr int NC = BN / 64;  // chunks of this warp
+    const int nchunks = (p.bn + 31) / 32;
+    bool ok = true;
+    int job = 0;
+    for (int tile = unit; tile < T.total; tile += units) {
+      int tmi, tni, k0, k1, sp;
+      T.at(p, tile, tmi, tni, k0, k1, sp);
+      const int jobs = FLUSH ? k1 - k0 : (k1 > k0 ? 1 : 0);
+      float acc[FLUSH ? NC * 32 : 1];
+      if constexpr (FLUSH) {
+#pragma unroll
+        for (int i = 0; i < NC * 32; ++i) acc[i] = 0.f;
+        for (int j = 0; j < jobs; ++j, ++job) {
+          if (!(ok = warp_wait<CG>(&accfull[job & 1], (job >> 1) & 1))) break;
+          umma::fence_after_sync();
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            float v[32];
+            umma::tmem_ld32(lanes + (uint32_t)(job & 1) * BN + 32u * (uint32_t)(2 * c + half), v);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[c * 32 + i] += v[i];
+          }
+          umma::fence_before_sync();
+          __syncwarp();
+          if (lane == 0) leader_arrive<CG>(&accempty[job & 1]);
+        }
+      } else if (jobs > 0) {
+        ok = warp_wait<CG>(&accfull[job & 1], (job >> 1) & 1);
+        umma::fence_after_sync();
+      }
+      if (!ok) break;
+      const int64_t row0 = (int64_t)tmi * 128 * CG + rank * 128 + 32 * (w & 3);
+      const int64_t row = row0 + lane;
+      const int nend = min(p.n, (tni + 1) * p.bn);
+      // per-row state of the loss epilogues
+      float rm = -INFINITY, rs = 0.f, rlse = 0.f, rg = 0.f;
+      int rt = -1;
+      if constexpr (EPI != kEpiOut) {
+        if (row < T.m) {
+          rt = p.target[row];
+          if constexpr (EPI == kEpiDz) {
+            rlse = p.lse[row];
+            rg = p.gscale[row];
+          }
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int ch = 2 * c + half;
+        const int col0 = tni * p.bn + 32 * ch;
+        const bool live = ch < nchunks && col0 < nend;  // uniform over the warp
+        float v[32];
+        if constexpr (FLUSH) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = acc[c * 32 + i];
+        } else if (jobs > 0 && live) {
+          umma::tmem_ld32(lanes + (uint32_t)(job & 1) * BN + 32u * (uint32_t)ch, v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = 0.f;
+        }
+        if constexpr (!FLUSH) {
+          if (c == NC - 1 && jobs > 0) {  // the accumulator may be overwritten
+            umma::fence_before_sync();
+            __syncwarp();
+            if (lane == 0) leader_arrive<CG>(&accempty[job & 1]);
+          }
+        }
+        if (!live) continue;
+        if constexpr (EPI == kEpiStats) {
+          const int vcol = p.v0 + col0;
+          const bool edge = col0 + 32 > nend || (unsigned)(p.excluded - vcol) < 32u;
+          if (edge) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (col0 + i >= nend || vcol + i == p.excluded) v[i] = -INFINITY;
+          }
+          if ((unsigned)(rt - vcol) < 32u && rt - vcol < nend - col0) {
+            float z = 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) z = rt - vcol == i ? v[i] : z;
+            p.at_target[row] = z;
+          }
+          float mx = v[0];
+#pragma unroll
+          for (int i = 1; i < 32; ++i) mx = fmaxf(mx, v[i]);
+          const float nm = fmaxf(rm, mx * kLog2e);
+          float add = 0.f;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) add += ex2(fmaf(v[i], kLog2e, -nm));
+          // a row with nothing so far (every entry excluded or past the end) stays at sum 0
+          // (or at NaN, which the maximum passes over)
+          if (nm != -INFINITY) {
+            rs = rs * ex2(rm - nm) + add;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) rs = isnan(v[i]) ? v[i] : rs;
+          }
+          rm = nm;
+        } else {
+          if constexpr (EPI == kEpiDz) {
+            const int vcol = p.v0 + col0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              float d = ex2((v[i] - rlse) * kLog2e);
+              d = vcol + i == rt ? d - 1.f : d;
+              v[i] = vcol + i == p.excluded ? 0.f : d * rg;
+            }
+            if (row >= T.m) {  // rows up to the next tile edge are read by the product over rows: exact zeros
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = 0.f;
+            }
+          }
+          // to memory through shared memory: 8 lanes per row, 4 columns each
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<float4*>(stg + lane * 32 + 4 * (j ^ (lane & 7))) =
+                make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          __syncwarp();
+          const int col = col0 + 4 * (lane & 7);
+          float b[4] = {0.f, 0.f, 0.f, 0.f};
+          if constexpr (EPI == kEpiOut) {
+            if (p.splits == 1) bias4(p, col, b);
+          }
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const int r = 4 * q + (lane >> 3);
+            const float4 u = *reinterpret_cast<const float4*>(stg + r * 32 + 4 * ((lane & 7) ^ (r & 7)));
+            if constexpr (EPI == kEpiOut) {
+              if (row0 + r < T.m && col < nend)
+                out4(p, row0 + r, col, u, b, p.splits > 1, (int64_t)sp * p.split_stride);
+            } else if (col < nend) {  // kEpiDz: the buffer holds whole tiles of rows and groups of 4 columns
+              const int64_t at = (row0 + r) * p.ld_out + col;
+              if constexpr (NP == 1) {
+                store4(p.out, 0, at, u);
+              } else {
+                const float e[4] = {u.x, u.y, u.z, u.w};
+                bf16 pc[3][4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) split3(e[j], pc[0][j], pc[1][j], pc[2][j]);
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                  *reinterpret_cast<uint2*>(static_cast<bf16*>(p.out) + k * p.plane + at) =
+                      *reinterpret_cast<const uint2*>(pc[k]);
+              }
+            }
+          }
+          __syncwarp();
+        }
+      }
+      if constexpr (EPI == kEpiStats) {
+        if (row < T.m) p.part[(int64_t)(2 * tni + half) * p.rows_ld + row] = make_float2(rm, rs);
+      }
+      if constexpr (!FLUSH) job += jobs;
+    }
+    if (!ok && lane == 0) atomicExch(p.flag, 1);
+  }
+  umma::fence_before_sync();
+  __syncthreads();
+  if constexpr (CG == 2) cluster_sync_all();
+  umma::fence_after_sync();
+  if (w == 2) gtmem_dealloc<CG>(tm, kCols);
+}
+
+// One CTA (or pair) per SM (or pair of SMs), at most one per tile.
+template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI>
+cudaError_t gemm_t(const GemmParams& p, const CUtensorMap& a, const CUtensorMap& b, cudaStream_t s) {
+  using S = GemmSmem<CG, BN, NP>;
+  auto kern = k_gemm<CG, BN, NP, A_MN, B_MN, EPI>;
+  cudaError_t e = set_smem_cached(reinterpret_cast<const void*>(kern), (int)S::kBytes, 100);
+  if (e != cudaSuccess) return e;
+  const int64_t mt = (p.m + 128 * CG - 1) / (128 * CG), nt = (p.n + p.bn - 1) / p.bn;
+  int64_t units = mt * nt * p.splits;
+  const int sms = sm_count_cached();
+  const int64_t most = (sms > 0 ? sms : 152) / CG;
+  if (units > most) units = most;
+  if (units <= 0) return cudaSuccess;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CG;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(units * CG));
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = S::kBytes;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = CG == 2 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, p, a, b);
+}
+
+}  // namespace
+}  // namespace bds

@@ -1,0 +1,19 @@
+// gemm_nt.cu -- instances of the matrix product of gemm.cuh: both operands with rows along m and n.
+#include "gemm.cuh"
+
+namespace bds {
+
+cudaError_t launch_gemm_nt(const GemmCfg& c, const GemmParams& p, const CUtensorMap& a, const CUtensorMap& b,
+                        cudaStream_t s) {
+  if (c.cg == 2 && c.bn == 256 && c.pieces == 1)
+    return gemm_t<2, 256, 1, false, false, kEpiOut>(p, a, b, s);
+  if (c.cg == 1 && c.bn == 128 && c.pieces == 1)
+    return gemm_t<1, 128, 1, false, false, kEpiOut>(p, a, b, s);
+  if (c.cg == 1 && c.bn == 64 && c.pieces == 1)
+    return gemm_t<1, 64, 1, false, false, kEpiOut>(p, a, b, s);
+  if (c.cg == 1 && c.bn == 128 && c.pieces == 3)
+    return gemm_t<1, 128, 3, false, false, kEpiOut>(p, a, b, s);
+  return cudaErrorInvalidValue;
+}
+
+}  // namespace bds
