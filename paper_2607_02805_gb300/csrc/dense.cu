@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(kThreads) k_split_reduce(const GemmParams p, c
   }
   float b[4];
   bias4(p, c, b);
-  out4(p, row, c, s, b, false, 0);
+  out4(p, row, c, s, b, 0);
 }
 
 // ---- a linear layer of a few rows ----

@@ -230,22 +230,13 @@ __device__ __forceinline__ void store1(void* p, int f32, int64_t at, float v) {
   else static_cast<bf16*>(p)[at] = __float2bfloat16_rn(v);
 }
 
-// The output step of kEpiOut for up to four columns of one row.
+// The output step of kEpiOut for up to four columns of one row: the general
+// form, for edge tiles, unaligned rows and mapped rows. (A split's partial sums
+// are an output without bias, activation and residual.)
 __device__ __forceinline__ void out4(const GemmParams& p, int64_t row, int col, float4 v, const float (&bias)[4],
-                                     bool split, int64_t out_off) {
+                                     int64_t out_off) {
   const int64_t orow = p.row_map != nullptr ? p.row_map[row] : row;
   const bool full = p.vec && col + 3 < p.n;
-  if (split) {
-    const int64_t at = out_off + orow * p.ld_out + col;
-    if (full) store4(p.out, 1, at, v);
-    else {
-      const float e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (col + j < p.n) store1(p.out, 1, at + j, e[j]);
-    }
-    return;
-  }
   float e[4] = {v.x + bias[0], v.y + bias[1], v.z + bias[2], v.w + bias[3]};
   if (p.pre != nullptr) {
     const int64_t at = row * p.ld_pre + col;
@@ -267,12 +258,61 @@ __device__ __forceinline__ void out4(const GemmParams& p, int64_t row, int col, 
       for (int j = 0; j < 4; ++j)
         if (col + j < p.n) e[j] += load1(p.res, p.res_f32, at + j);
   }
-  const int64_t at = orow * p.ld_out + col;
+  const int64_t at = out_off + orow * p.ld_out + col;
   if (full) store4(p.out, p.out_f32, at, make_float4(e[0], e[1], e[2], e[3]));
   else
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (col + j < p.n) store1(p.out, p.out_f32, at + j, e[j]);
+}
+
+// The same for rows row, row + 4, ... row + 28 of a whole 32 x 32 chunk: the
+// options are decided once per chunk and the loads of a chunk are issued
+// together. (With out4 unrolled over the chunks of a tile instead, the
+// instructions of one tile did not fit the instruction cache: 16384 x 832 x
+// 3328 took 346 us, most of it stalls on instruction fetch.)
+__device__ __forceinline__ void store_rows(void* p, int f32, int64_t at, int64_t ld, const float4 (&u)[8]) {
+  if (f32) {
+    float* d = static_cast<float*>(p) + at;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) *reinterpret_cast<float4*>(d + 4 * q * ld) = u[q];
+  } else {
+    bf16* d = static_cast<bf16*>(p) + at;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      *reinterpret_cast<uint2*>(d + 4 * q * ld) = make_uint2(pack_bf16(u[q].x, u[q].y), pack_bf16(u[q].z, u[q].w));
+  }
+}
+__device__ __forceinline__ void out_chunk(const GemmParams& p, int64_t row, int col, float4 (&u)[8],
+                                          const float (&bias)[4], int64_t out_off) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) u[q].x += bias[0], u[q].y += bias[1], u[q].z += bias[2], u[q].w += bias[3];
+  if (p.pre != nullptr) store_rows(p.pre, p.pre_f32, row * p.ld_pre + col, p.ld_pre, u);
+  if (p.act == kActSilu) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      u[q] = make_float4(act_fwd(kActSilu, u[q].x), act_fwd(kActSilu, u[q].y), act_fwd(kActSilu, u[q].z),
+                         act_fwd(kActSilu, u[q].w));
+  } else if (p.act == kActGelu) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      u[q] = make_float4(act_fwd(kActGelu, u[q].x), act_fwd(kActGelu, u[q].y), act_fwd(kActGelu, u[q].z),
+                         act_fwd(kActGelu, u[q].w));
+  }
+  if (p.res != nullptr) {
+    float4 r[8];
+    const int64_t at = row * p.ld_res + col;
+    if (p.res_f32) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) r[q] = load4(p.res, 1, at + 4 * q * p.ld_res);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) r[q] = load4(p.res, 0, at + 4 * q * p.ld_res);
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) u[q].x += r[q].x, u[q].y += r[q].y, u[q].z += r[q].z, u[q].w += r[q].w;
+  }
+  store_rows(p.out, p.out_f32, out_off + row * p.ld_out + col, p.ld_out, u);
 }
 __device__ __forceinline__ void bias4(const GemmParams& p, int col, float (&b)[4]) {
 #pragma unroll
@@ -477,7 +517,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           }
         }
       }
-#pragma unroll
+#pragma unroll(FLUSH ? NC : 1)
       for (int c = 0; c < NC; ++c) {
         const int ch = 2 * c + half;
         const int col0 = tni * p.bn + 32 * ch;
@@ -551,24 +591,36 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
           __syncwarp();
           const int col = col0 + 4 * (lane & 7);
-          float b[4] = {0.f, 0.f, 0.f, 0.f};
-          if constexpr (EPI == kEpiOut) {
-            if (p.splits == 1) bias4(p, col, b);
-          }
+          float4 u[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q) {
             const int r = 4 * q + (lane >> 3);
-            const float4 u = *reinterpret_cast<const float4*>(stg + r * 32 + 4 * ((lane & 7) ^ (r & 7)));
-            if constexpr (EPI == kEpiOut) {
-              if (row0 + r < T.m && col < nend)
-                out4(p, row0 + r, col, u, b, p.splits > 1, (int64_t)sp * p.split_stride);
-            } else if (col < nend) {  // kEpiDz: the buffer holds whole tiles of rows and groups of 4 columns
-              const int64_t at = (row0 + r) * p.ld_out + col;
+            u[q] = *reinterpret_cast<const float4*>(stg + r * 32 + 4 * ((lane & 7) ^ (r & 7)));
+          }
+          const int64_t r0 = row0 + (lane >> 3);  // rows r0, r0 + 4, ...
+          if constexpr (EPI == kEpiOut) {
+            float b[4] = {0.f, 0.f, 0.f, 0.f};
+            if (p.bias != nullptr) bias4(p, col, b);
+            if (p.vec && col0 + 32 <= nend && row0 + 32 <= T.m && p.row_map == nullptr)
+              out_chunk(p, r0, col, u, b, (int64_t)sp * p.split_stride);
+            else if (col < nend)
+#pragma unroll 1
+              for (int q = 0; q < 8; ++q)  // the chunk's row q is taken from shared memory again: u is indexed statically only
+                if (r0 + 4 * q < T.m) {
+                  const int r = 4 * q + (lane >> 3);
+                  out4(p, r0 + 4 * q, col,
+                       *reinterpret_cast<const float4*>(stg + r * 32 + 4 * ((lane & 7) ^ (r & 7))), b,
+                       (int64_t)sp * p.split_stride);
+                }
+          } else if (col < nend) {  // kEpiDz: the buffer holds whole tiles of rows and groups of 4 columns
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const int64_t at = (r0 + 4 * q) * p.ld_out + col;
               if constexpr (NP == 1) {
-                store4(p.out, 0, at, u);
+                store4(p.out, 0, at, u[q]);
               } else {
-                const float e[4] = {u.x, u.y, u.z, u.w};
-                bf16 pc[3][4];
+                const float e[4] = {u[q].x, u[q].y, u[q].z, u[q].w};
+                __align__(8) bf16 pc[3][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) split3(e[j], pc[0][j], pc[1][j], pc[2][j]);
 #pragma unroll
