@@ -136,9 +136,11 @@ __global__ void __launch_bounds__(kThreads) k_colsum(const float* part, int rang
 }
 
 // ---- the sums of a split product ----
+// A thread adds four columns of one row over the splits, in order, and ends
+// them as the product's own output step would.
 __global__ void __launch_bounds__(kThreads) k_split_reduce(const GemmParams p, const float* part, int64_t ld) {
   pdl_sync();
-  const int64_t groups = (p.n + 3) / 4;
+  const int64_t groups = ld / 4;
   const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   const int64_t row = idx / groups;
   const int c = (int)(idx - row * groups) * 4;
@@ -150,9 +152,24 @@ __global__ void __launch_bounds__(kThreads) k_split_reduce(const GemmParams p, c
     const float4 q = *reinterpret_cast<const float4*>(part + i * p.split_stride + row * ld + c);
     s.x += q.x, s.y += q.y, s.z += q.z, s.w += q.w;
   }
-  float b[4];
-  bias4(p, c, b);
-  out4(p, row, c, s, b, 0);
+  float e[4] = {s.x, s.y, s.z, s.w};
+  if (p.tma_out && p.vec && c + 3 < p.n && p.row_map == nullptr) {  // rows on 16-byte boundaries
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (p.bias != nullptr) e[j] += load1(p.bias, p.bias_f32, c + j);
+    if (p.pre != nullptr) store4(p.pre, p.pre_f32, row * p.ld_pre + c, make_float4(e[0], e[1], e[2], e[3]));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) e[j] = act_fwd(p.act, e[j]);
+    if (p.res != nullptr) {
+      const float4 r = load4(p.res, p.res_f32, row * p.ld_res + c);
+      e[0] += r.x, e[1] += r.y, e[2] += r.z, e[3] += r.w;
+    }
+    store4(p.out, p.out_f32, row * p.ld_out + c, make_float4(e[0], e[1], e[2], e[3]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (c + j < p.n) out1(p, row, c + j, e[j], p.bias != nullptr ? load1(p.bias, p.bias_f32, c + j) : 0.f, 0);
+  }
 }
 
 // ---- a linear layer of a few rows ----

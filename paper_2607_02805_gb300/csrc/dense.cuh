@@ -20,7 +20,7 @@ struct GemmParams {
   // Rows that count, known on the device only: limits m (1), k (2) or nothing (0).
   const int* rows_dev;
   int rows_axis;
-  int bn;         // columns of a tile (a multiple of 16 per CTA, at most the instance's BN)
+  int bn;         // columns of a tile (a multiple of 32, at most the instance's BN)
   int splits;     // ranges of k, each with its own partial sums
   int group_m;    // row tiles walked together
   // kEpiOut: out[row_map ? row_map[i] : i][j]
@@ -33,7 +33,8 @@ struct GemmParams {
   int64_t split_stride;  // elements between the partial sums of two splits
   int bias_f32, res_f32, out_f32, pre_f32;
   int act;
-  int vec;               // rows of res, out and pre start on 4-element boundaries
+  int tma_out;           // out and pre are written by TMA
+  int vec;               // rows of res start on 16-byte boundaries
   int64_t out_extent;    // elements of `out` (debug build)
   // kEpiStats / kEpiDz: rows i are the rows that count; column j is entry v0 + j
   int v0, excluded;
@@ -55,8 +56,10 @@ struct GemmCfg {
   int epi;
 };
 
-cudaError_t launch_gemm(const GemmCfg& c, const GemmParams& p, const CUtensorMap& a, const CUtensorMap& b,
-                        cudaStream_t s);
+// Tensor maps of a product; `out` and `pre` only with tma_out and for kEpiDz.
+struct GemmMaps {
+  CUtensorMap a, b, out, pre;
+};
 // Sums of the partial sums of p.splits splits, then the output step of kEpiOut.
 cudaError_t launch_split_reduce(const GemmParams& p, const float* part, cudaStream_t s);
 

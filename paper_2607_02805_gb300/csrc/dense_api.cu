@@ -14,10 +14,10 @@ namespace bds {
 
 PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder();  // ssd.cu
 
-cudaError_t launch_gemm_nt(const GemmCfg&, const GemmParams&, const CUtensorMap&, const CUtensorMap&, cudaStream_t);
-cudaError_t launch_gemm_nn(const GemmCfg&, const GemmParams&, const CUtensorMap&, const CUtensorMap&, cudaStream_t);
-cudaError_t launch_gemm_tn(const GemmCfg&, const GemmParams&, const CUtensorMap&, const CUtensorMap&, cudaStream_t);
-cudaError_t launch_gemm_loss(const GemmCfg&, const GemmParams&, const CUtensorMap&, const CUtensorMap&, cudaStream_t);
+cudaError_t launch_gemm_nt(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
+cudaError_t launch_gemm_nn(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
+cudaError_t launch_gemm_tn(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
+cudaError_t launch_gemm_loss(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
 
 namespace {
 
@@ -73,6 +73,22 @@ bool encode(CUtensorMap* m, const Operand& o, int box_rows) {
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The output [planes][rows][cols] as the epilogue stores it: boxes of 32 x 32.
+bool encode_out(CUtensorMap* m, const void* base, int f32, int64_t cols, int64_t rows, int64_t ld, int planes,
+                int64_t plane) {
+  const int64_t elt = f32 ? 4 : 2;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+  const cuuint64_t strides[2] = {(cuuint64_t)(ld * elt), (cuuint64_t)((planes > 1 ? plane : ld * 8) * elt)};
+  const cuuint32_t box[3] = {32u, 32u, 1u};
+  const cuuint32_t estr[3] = {1u, 1u, 1u};
+  return tensor_map_encoder()(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+                              const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Whether rows of `ld` elements start on 16-byte boundaries.
+bool rows16(int64_t ld, int f32) { return ld % (f32 ? 4 : 8) == 0; }
+
 // Whether rows of `ld` elements of `dtype` can be read by TMA where they lie.
 bool in_place(int dtype, int64_t ld) { return dtype == BDSCAN_BF16 && ld % 8 == 0; }
 size_t packed_bytes(int dtype, int64_t rows, int64_t cols) {
@@ -99,7 +115,7 @@ Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split) {
     q.cfg.bn = pieces == 3 || ((m + 127) / 128) * ((n + 127) / 128) >= kSms / 2 ? 128 : 64;
   }
   const int64_t nt = (n + q.cfg.bn - 1) / q.cfg.bn;
-  q.bn = (int)up((n + nt - 1) / nt, 16 * q.cfg.cg);
+  q.bn = (int)up((n + nt - 1) / nt, 32);
   const int64_t mt = (m + 128 * q.cfg.cg - 1) / (128 * q.cfg.cg);
   const int64_t tiles = mt * ((n + q.bn - 1) / q.bn), nk = (k + 63) / 64;
   q.group_m = q.cfg.cg == 2 ? 8 : 12;
@@ -131,26 +147,35 @@ GemmParams geometry(const Plan& q, int64_t m, int64_t n, int64_t k, int* flag) {
   return p;
 }
 
-cudaError_t run_product(const Plan& q, const GemmParams& p, const Operand& a, const Operand& b, cudaStream_t s) {
-  CUtensorMap am, bm;
-  const int b_rows = q.cfg.b_mn ? 64 : q.cfg.bn / q.cfg.cg;
-  if (!encode(&am, a, q.cfg.a_mn ? 64 : 128) || !encode(&bm, b, b_rows)) return cudaErrorInvalidValue;
+// `p.out` has `planes` planes (splits, or pieces of the logits' gradient) of
+// `out_rows` rows.
+cudaError_t run_product(const Plan& q, const GemmParams& p, const Operand& a, const Operand& b, int planes,
+                        int64_t plane, int64_t out_rows, cudaStream_t s) {
+  GemmMaps m;
+  memset(&m, 0, sizeof(m));
+  if (!encode(&m.a, a, q.cfg.a_mn ? 64 : 128) || !encode(&m.b, b, q.cfg.b_mn ? 64 : q.cfg.bn / q.cfg.cg))
+    return cudaErrorInvalidValue;
+  if (p.tma_out && (!encode_out(&m.out, p.out, p.out_f32, p.n, out_rows, p.ld_out, planes, plane) ||
+                    (p.pre != nullptr && !encode_out(&m.pre, p.pre, p.pre_f32, p.n, out_rows, p.ld_pre, 1, 0))))
+    return cudaErrorInvalidValue;
   cudaError_t e;
-  if (q.cfg.epi != kEpiOut) e = launch_gemm_loss(q.cfg, p, am, bm, s);
-  else if (q.cfg.a_mn) e = launch_gemm_tn(q.cfg, p, am, bm, s);
-  else if (q.cfg.b_mn) e = launch_gemm_nn(q.cfg, p, am, bm, s);
-  else e = launch_gemm_nt(q.cfg, p, am, bm, s);
+  if (q.cfg.epi != kEpiOut) e = launch_gemm_loss(q.cfg, p, m, s);
+  else if (q.cfg.a_mn) e = launch_gemm_tn(q.cfg, p, m, s);
+  else if (q.cfg.b_mn) e = launch_gemm_nn(q.cfg, p, m, s);
+  else e = launch_gemm_nt(q.cfg, p, m, s);
   return api_launched(e, s);
 }
 
 // A product with the output step of kEpiOut, split over k where the plan says
 // so: then the partial sums go to `part` and a second launch ends it.
-cudaError_t run_out(Plan q, bool a_mn, bool b_mn, const GemmParams& p, const Operand& a, const Operand& b, float* part,
+cudaError_t run_out(Plan q, bool a_mn, bool b_mn, GemmParams p, const Operand& a, const Operand& b, float* part,
                     cudaStream_t s) {
   q.cfg.a_mn = a_mn;
   q.cfg.b_mn = b_mn;
   q.cfg.epi = kEpiOut;
-  if (q.splits == 1) return run_product(q, p, a, b, s);
+  p.tma_out = p.row_map == nullptr && rows16(p.ld_out, p.out_f32) && (p.pre == nullptr || rows16(p.ld_pre, p.pre_f32));
+  p.vec = p.res == nullptr || rows16(p.ld_res, p.res_f32);
+  if (q.splits == 1) return run_product(q, p, a, b, 1, 0, p.m, s);
   GemmParams g = p;
   g.splits = q.splits;
   g.bias = g.res = nullptr;
@@ -159,16 +184,14 @@ cudaError_t run_out(Plan q, bool a_mn, bool b_mn, const GemmParams& p, const Ope
   g.out = part;
   g.ld_out = up(p.n, 4);
   g.split_stride = p.m * g.ld_out;
-  g.out_f32 = 1;
-  g.vec = 1;
+  g.out_f32 = g.tma_out = g.vec = 1;
   g.act = BDSCAN_ACT_NONE;
   g.out_extent = (int64_t)q.splits * g.split_stride;
-  cudaError_t e = run_product(q, g, a, b, s);
+  cudaError_t e = run_product(q, g, a, b, q.splits, g.split_stride, p.m, s);
   if (e != cudaSuccess) return e;
-  GemmParams r = p;
-  r.splits = q.splits;
-  r.split_stride = g.split_stride;
-  return api_launched(launch_split_reduce(r, part, s), s);
+  p.splits = q.splits;
+  p.split_stride = g.split_stride;
+  return api_launched(launch_split_reduce(p, part, s), s);
 }
 
 // The operand as the products read it: where it lies, or packed into `ws`.
@@ -492,7 +515,6 @@ int bdscan_linear_forward(const bdscan_linear_dims* dims, const void* x, const v
     p.bias_f32 = p.pre_f32 = l.dtype == BDSCAN_F32;
     p.res_f32 = p.out_f32 = l.out == BDSCAN_F32;
     p.act = l.act;
-    p.vec = l.ld_y % 4 == 0 && (residual == nullptr || l.ld_res % 4 == 0) && (pre == nullptr || l.N % 4 == 0);
     p.out_extent = (l.T - 1) * l.ld_y + l.N;
     e = run_out(ws.q, false, false, p, a, b, (float*)(base + ws.part), s);
   }
@@ -569,7 +591,6 @@ int bdscan_linear_backward(const bdscan_linear_dims* dims, const void* x, const 
       p.out = dx;
       p.ld_out = l.K;
       p.out_f32 = l.dtype == BDSCAN_F32;
-      p.vec = l.K % 4 == 0;
       p.out_extent = l.T * l.K;
       e = run_out(ws.qx, false, true, p, dz, b, part, s);
     }
@@ -582,7 +603,6 @@ int bdscan_linear_backward(const bdscan_linear_dims* dims, const void* x, const 
       p.out = dw;
       p.ld_out = l.K;
       p.out_f32 = l.dtype == BDSCAN_F32;
-      p.vec = l.K % 4 == 0;
       p.out_extent = l.N * l.K;
       e = run_out(ws.qw, true, true, p, dz, b, part, s);
     }
@@ -642,7 +662,7 @@ int bdscan_lm_loss_forward(const bdscan_lm_loss_dims* dims, const void* h, const
     p.part = (float2*)(base + ws.part);
     p.at_target = (float*)(base + ws.at);
     p.rows_ld = ws.r.rows;
-    e = run_product(q, p, a, b, s);
+    e = run_product(q, p, a, b, 1, 0, l.T, s);
   }
   if (e == cudaSuccess)
     e = api_launched(launch_loss_combine((const float2*)(base + ws.part), ws.parts, ws.r.rows,
@@ -727,7 +747,8 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
     p.ld_out = ld_dz;
     p.plane = ws.r.rows * ld_dz;
     p.out_extent = ws.r.rows * ld_dz;
-    e = run_product(q, p, a, bp, s);
+    p.tma_out = 1;
+    e = run_product(q, p, a, bp, l.pieces, p.plane, ws.r.rows, s);
     // this piece's rows of dw
     if (e == cudaSuccess) {
       GemmParams g = geometry(ws.qw, n, l.K, ws.r.rows, flag);
@@ -736,7 +757,6 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
       g.out = (char*)dw + (size_t)v0 * l.K * elt;
       g.ld_out = l.K;
       g.out_f32 = f32;
-      g.vec = l.K % 4 == 0;
       g.out_extent = n * l.K;
       e = run_out(ws.qw, true, true, g, dz, a, part, s);
     }
@@ -753,7 +773,6 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
       g.ld_out = last ? l.K : ld_acc;
       g.out_f32 = last ? f32 : 1;
       g.row_map = last ? rp.idx : nullptr;
-      g.vec = g.ld_out % 4 == 0;
       g.out_extent = last ? l.T * l.K : l.T * ld_acc;
       e = run_out(ws.qh, false, true, g, dz, bp, part, s);
     }

@@ -92,15 +92,17 @@ template <int CG>
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, gbar_wait<CG>(bar, parity));
 }
-// One arrival at the barrier at this offset in the tile's first CTA.
+// One arrival at the barrier at this offset in the tile's first CTA. What it
+// orders is this thread's TMEM loads, which have completed (wait::ld and the
+// tcgen05 fence before it); a release at cluster scope would also wait for the
+// global stores of the chunks before, which nobody in the cluster reads
+// (16384 x 832 x 3328: 80 us with it).
 template <int CG>
 __device__ __forceinline__ void leader_arrive(uint64_t* bar) {
   if constexpr (CG == 1)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(umma::smem_u32(bar)) : "memory");
   else
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(
-                     map_cta(umma::smem_u32(bar), 0))
-                 : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];\n" ::"r"(map_cta(umma::smem_u32(bar), 0)) : "memory");
 }
 template <int CG>
 __device__ __forceinline__ void gtma_load(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
@@ -166,29 +168,38 @@ __device__ __forceinline__ void gtmem_dealloc(uint32_t tm, uint32_t cols) {
 
 // ---- activations ----
 // GELU is its tanh form, z (1 + tanh u) / 2 = z sigmoid(2 u): one exponential
-// and one reciprocal on the MUFU unit instead of a polynomial per element. The
-// argument is clamped to +-16, where the sigmoid is 0 or 1 in fp32, so that the
-// cube cannot overflow.
+// and one reciprocal on the MUFU unit instead of a polynomial per element. An
+// overflow of the cube or of the exponential ends in the right limit, sigmoid
+// 0 or 1.
 constexpr int kActNone = 0, kActSilu = 1, kActGelu = 2;
 constexpr float kGeluA = 0.7978845608028654f;  // sqrt(2 / pi)
 constexpr float kGeluB = 0.044715f;
-__device__ __forceinline__ float sigmoid_f(float z) { return __fdividef(1.f, 1.f + ex2(-kLog2e * z)); }
-__device__ __forceinline__ float act_fwd(int act, float z) {
-  if (act == kActNone) return z;
-  if (act == kActSilu) return z * sigmoid_f(z);
-  const float c = fminf(fmaxf(z, -16.f), 16.f);
-  return z * sigmoid_f(2.f * kGeluA * (c + kGeluB * c * c * c));
+__device__ __forceinline__ float rcp_f(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
+__device__ __forceinline__ float silu_f(float z) { return z * rcp_f(1.f + ex2(-kLog2e * z)); }
+__device__ __forceinline__ float gelu_f(float z) {
+  constexpr float c1 = -2.f * kGeluA * kLog2e, c2 = c1 * kGeluB;
+  return z * rcp_f(1.f + ex2(z * fmaf(c2, z * z, c1)));
+}
+__device__ __forceinline__ float act_fwd(int act, float z) {
+  return act == kActNone ? z : act == kActSilu ? silu_f(z) : gelu_f(z);
+}
+// The derivative; the argument is clamped to where the sigmoid is 0 or 1 in
+// fp32, so that no infinity meets a zero.
 __device__ __forceinline__ float act_grad(int act, float z) {
   if (act == kActNone) return 1.f;
-  const float c = fminf(fmaxf(z, -80.f), 80.f);
   if (act == kActSilu) {
-    const float s = sigmoid_f(c);
+    const float c = fminf(fmaxf(z, -100.f), 100.f);
+    const float s = rcp_f(1.f + ex2(-kLog2e * c));
     return s * (1.f + c * (1.f - s));
   }
-  const float g = fminf(fmaxf(z, -16.f), 16.f);
-  const float s = sigmoid_f(2.f * kGeluA * (g + kGeluB * g * g * g));
-  return s * (1.f + g * (1.f - s) * 2.f * kGeluA * (1.f + 3.f * kGeluB * g * g));
+  const float c = fminf(fmaxf(z, -16.f), 16.f);
+  constexpr float c1 = -2.f * kGeluA * kLog2e, c2 = c1 * kGeluB;
+  const float s = rcp_f(1.f + ex2(c * fmaf(c2, c * c, c1)));
+  return s * (1.f + c * (1.f - s) * fmaf(6.f * kGeluA * kGeluB, c * c, 2.f * kGeluA));
 }
 
 // fp32 as three bf16 pieces (8 + 8 + 8 bits). The first is cut towards zero
@@ -207,6 +218,14 @@ __device__ __forceinline__ void split3(float v, bf16& a, bf16& b, bf16& c) {
   const float r = v - __bfloat162float(a);
   b = __float2bfloat16_rn(r);
   c = __float2bfloat16_rn(r - __bfloat162float(b));
+}
+
+// What split3 takes of a value: the nearest bf16, towards zero where that
+// would overflow, the value itself where it is not finite (the rest is then
+// NaN: nothing finite can be made of it).
+__device__ __forceinline__ float bf16_part(float v) {
+  const float f = __bfloat162float(__float2bfloat16_rn(v));
+  return isinf(f) && isfinite(v) ? __bfloat162float(__float2bfloat16_rz(v)) : f;
 }
 
 __device__ __forceinline__ float4 load4(const void* p, int f32, int64_t at) {
@@ -230,95 +249,94 @@ __device__ __forceinline__ void store1(void* p, int f32, int64_t at, float v) {
   else static_cast<bf16*>(p)[at] = __float2bfloat16_rn(v);
 }
 
-// The output step of kEpiOut for up to four columns of one row: the general
-// form, for edge tiles, unaligned rows and mapped rows. (A split's partial sums
-// are an output without bias, activation and residual.)
-__device__ __forceinline__ void out4(const GemmParams& p, int64_t row, int col, float4 v, const float (&bias)[4],
-                                     int64_t out_off) {
-  const int64_t orow = p.row_map != nullptr ? p.row_map[row] : row;
-  const bool full = p.vec && col + 3 < p.n;
-  float e[4] = {v.x + bias[0], v.y + bias[1], v.z + bias[2], v.w + bias[3]};
-  if (p.pre != nullptr) {
-    const int64_t at = row * p.ld_pre + col;
-    if (full) store4(p.pre, p.pre_f32, at, make_float4(e[0], e[1], e[2], e[3]));
-    else
+// ---- output ----
+// A warp's chunk is 32 rows x 32 columns, a thread holding one row (as TMEM
+// gives it). It leaves by TMA where rows start on 16-byte boundaries: the warp
+// writes the chunk to shared memory in the swizzle of the map's box and one lane
+// issues the store, which also cuts off what lies outside the matrix. Per
+// element that is a third of the instructions of a transposition through shared
+// memory with plain stores (16384 x 832 x 3328: @@).
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int c0, int c1, int c2, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];\n" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(c0), "r"(c1), "r"(c2), "r"(src)
+               : "memory");
+  asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
+}
+// At most N of this thread's stores still read shared memory.
+template <int N>
+__device__ __forceinline__ void tma_store_wait_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;\n" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory"); }
+
+// One chunk to the box at (col, row, z) of `map`. bf16: two buffers of 2 KB
+// (64-byte swizzle) in turn; fp32: one of 4 KB (128-byte swizzle). `mixed`: the
+// launch stores both types, so that the previous store may read either.
+__device__ __forceinline__ void chunk_store(const CUtensorMap* map, int f32, bool mixed, int col, int row, int z,
+                                            const float (&v)[32], unsigned char* stg, uint32_t& turn) {
+  const int lane = threadIdx.x & 31;
+  if (f32) {
+    if (lane == 0) tma_store_wait_read<0>();
+    __syncwarp();
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (col + j < p.n) store1(p.pre, p.pre_f32, at + j, e[j]);
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) e[j] = act_fwd(p.act, e[j]);
-  if (p.res != nullptr) {
-    const int64_t at = row * p.ld_res + col;
-    if (full) {
-      const float4 r = load4(p.res, p.res_f32, at);
-      e[0] += r.x, e[1] += r.y, e[2] += r.z, e[3] += r.w;
-    } else
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (col + j < p.n) e[j] += load1(p.res, p.res_f32, at + j);
-  }
-  const int64_t at = out_off + orow * p.ld_out + col;
-  if (full) store4(p.out, p.out_f32, at, make_float4(e[0], e[1], e[2], e[3]));
-  else
+    for (int j = 0; j < 8; ++j)
+      *reinterpret_cast<float4*>(stg + lane * 128 + 16 * (j ^ (lane & 7))) =
+          make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+  } else {
+    stg += 2048 * (turn & 1);
+    ++turn;
+    if (lane == 0) {
+      if (mixed) tma_store_wait_read<0>();
+      else tma_store_wait_read<1>();
+    }
+    __syncwarp();
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (col + j < p.n) store1(p.out, p.out_f32, at + j, e[j]);
+      *reinterpret_cast<uint4*>(stg + lane * 64 + 16 * (j ^ ((lane >> 1) & 3))) =
+          make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]),
+                     pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
+  }
+  umma::fence_async_smem();
+  __syncwarp();
+  if (lane == 0) tma_store_3d(map, col, row, z, umma::smem_u32(stg));
 }
 
-// The same for rows row, row + 4, ... row + 28 of a whole 32 x 32 chunk: the
-// options are decided once per chunk and the loads of a chunk are issued
-// together. (With out4 unrolled over the chunks of a tile instead, the
-// instructions of one tile did not fit the instruction cache: 16384 x 832 x
-// 3328 took 346 us, most of it stalls on instruction fetch.)
-__device__ __forceinline__ void store_rows(void* p, int f32, int64_t at, int64_t ld, const float4 (&u)[8]) {
+// 32 consecutive values at p[at], which lies on a 16-byte boundary.
+__device__ __forceinline__ void add32(float (&v)[32], const void* p, int f32, int64_t at) {
   if (f32) {
-    float* d = static_cast<float*>(p) + at;
+    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) *reinterpret_cast<float4*>(d + 4 * q * ld) = u[q];
-  } else {
-    bf16* d = static_cast<bf16*>(p) + at;
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-      *reinterpret_cast<uint2*>(d + 4 * q * ld) = make_uint2(pack_bf16(u[q].x, u[q].y), pack_bf16(u[q].z, u[q].w));
-  }
-}
-__device__ __forceinline__ void out_chunk(const GemmParams& p, int64_t row, int col, float4 (&u)[8],
-                                          const float (&bias)[4], int64_t out_off) {
-#pragma unroll
-  for (int q = 0; q < 8; ++q) u[q].x += bias[0], u[q].y += bias[1], u[q].z += bias[2], u[q].w += bias[3];
-  if (p.pre != nullptr) store_rows(p.pre, p.pre_f32, row * p.ld_pre + col, p.ld_pre, u);
-  if (p.act == kActSilu) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-      u[q] = make_float4(act_fwd(kActSilu, u[q].x), act_fwd(kActSilu, u[q].y), act_fwd(kActSilu, u[q].z),
-                         act_fwd(kActSilu, u[q].w));
-  } else if (p.act == kActGelu) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-      u[q] = make_float4(act_fwd(kActGelu, u[q].x), act_fwd(kActGelu, u[q].y), act_fwd(kActGelu, u[q].z),
-                         act_fwd(kActGelu, u[q].w));
-  }
-  if (p.res != nullptr) {
-    float4 r[8];
-    const int64_t at = row * p.ld_res + col;
-    if (p.res_f32) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) r[q] = load4(p.res, 1, at + 4 * q * p.ld_res);
-    } else {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) r[q] = load4(p.res, 0, at + 4 * q * p.ld_res);
+    for (int j = 0; j < 8; ++j) {
+      const float4 u = q[j];
+      v[4 * j] += u.x, v[4 * j + 1] += u.y, v[4 * j + 2] += u.z, v[4 * j + 3] += u.w;
     }
+  } else {
+    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const bf16*>(p) + at);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) u[q].x += r[q].x, u[q].y += r[q].y, u[q].z += r[q].z, u[q].w += r[q].w;
+    for (int j = 0; j < 4; ++j) {
+      const uint4 u = q[j];
+      const uint32_t e[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[8 * j + 2 * i] += __uint_as_float(e[i] << 16);
+        v[8 * j + 2 * i + 1] += __uint_as_float(e[i] & 0xffff0000u);
+      }
+    }
   }
-  store_rows(p.out, p.out_f32, out_off + row * p.ld_out + col, p.ld_out, u);
-}
-__device__ __forceinline__ void bias4(const GemmParams& p, int col, float (&b)[4]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) b[j] = p.bias != nullptr && col + j < p.n ? load1(p.bias, p.bias_f32, col + j) : 0.f;
 }
 
+// The output step of one element, for rows that TMA cannot write: unaligned
+// strides, mapped rows. (A split's partial sums are an output without bias,
+// activation and residual.)
+__device__ __forceinline__ void out1(const GemmParams& p, int64_t row, int col, float v, float bias, int64_t out_off) {
+  v += bias;
+  if (p.pre != nullptr) store1(p.pre, p.pre_f32, row * p.ld_pre + col, v);
+  v = act_fwd(p.act, v);
+  if (p.res != nullptr) v += load1(p.res, p.res_f32, row * p.ld_res + col);
+  const int64_t orow = p.row_map != nullptr ? p.row_map[row] : row;
+  store1(p.out, p.out_f32, out_off + orow * p.ld_out + col, v);
+}
 // Extents of one call with the device's row count applied, and its tiles.
 template <int CG>
 struct Tiles {
@@ -347,7 +365,8 @@ struct Tiles {
 
 template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-    k_gemm(const GemmParams p, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap) {
+    k_gemm(const GemmParams p, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
+           const __grid_constant__ CUtensorMap omap, const __grid_constant__ CUtensorMap pmap) {
   using S = GemmSmem<CG, BN, NP>;
   constexpr int ST = S::kStages;
   constexpr bool FLUSH = NP == 3;
@@ -470,7 +489,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     // ---------------- epilogue ----------------
     const int ew = w - 4, half = ew >> 2;  // TMEM lanes 32 (w % 4) .. + 31, every second chunk of 32 columns
     const uint32_t lanes = tm + ((uint32_t)(32 * (w & 3)) << 16);
-    float* stg = reinterpret_cast<float*>(sm + ST * S::kStage) + ew * 1024;
+    unsigned char* stg = sm + ST * S::kStage + ew * 4096;
+    uint32_t turn = 0;
+    const bool mixed = p.pre != nullptr && p.pre_f32 != p.out_f32;
     constexpr int NC = BN / 64;  // chunks of this warp
     const int nchunks = (p.bn + 31) / 32;
     bool ok = true;
@@ -517,29 +538,35 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           }
         }
       }
+      const uint32_t tacc = lanes + (uint32_t)(job & 1) * BN;
+      uint32_t nxt[32];  // the next chunk, on its way from TMEM while this one is worked on
+      if constexpr (!FLUSH) {
+        if (jobs > 0) umma::tmem_ld32_issue(tacc + 32u * (uint32_t)half, nxt);
+      }
 #pragma unroll(FLUSH ? NC : 1)
       for (int c = 0; c < NC; ++c) {
         const int ch = 2 * c + half;
         const int col0 = tni * p.bn + 32 * ch;
-        const bool live = ch < nchunks && col0 < nend;  // uniform over the warp
         float v[32];
         if constexpr (FLUSH) {
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = acc[c * 32 + i];
-        } else if (jobs > 0 && live) {
-          umma::tmem_ld32(lanes + (uint32_t)(job & 1) * BN + 32u * (uint32_t)ch, v);
-        } else {
+        } else if (jobs > 0) {
+          umma::tmem_ld_wait(nxt);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = 0.f;
-        }
-        if constexpr (!FLUSH) {
-          if (c == NC - 1 && jobs > 0) {  // the accumulator may be overwritten
+          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(nxt[i]);
+          if (c + 1 < NC) {
+            umma::tmem_ld32_issue(tacc + 32u * (uint32_t)(ch + 2), nxt);
+          } else {  // the accumulator may be overwritten
             umma::fence_before_sync();
             __syncwarp();
             if (lane == 0) leader_arrive<CG>(&accempty[job & 1]);
           }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = 0.f;
         }
-        if (!live) continue;
+        if (ch >= nchunks || col0 >= nend) continue;  // uniform over the warp
         if constexpr (EPI == kEpiStats) {
           const int vcol = p.v0 + col0;
           const bool edge = col0 + 32 > nend || (unsigned)(p.excluded - vcol) < 32u;
@@ -570,65 +597,77 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             for (int i = 0; i < 32; ++i) rs = isnan(v[i]) ? v[i] : rs;
           }
           rm = nm;
-        } else {
-          if constexpr (EPI == kEpiDz) {
-            const int vcol = p.v0 + col0;
+        } else if constexpr (EPI == kEpiDz) {
+          const int vcol = p.v0 + col0;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              float d = ex2((v[i] - rlse) * kLog2e);
-              d = vcol + i == rt ? d - 1.f : d;
-              v[i] = vcol + i == p.excluded ? 0.f : d * rg;
-            }
-            if (row >= T.m) {  // rows up to the next tile edge are read by the product over rows: exact zeros
+          for (int i = 0; i < 32; ++i) {
+            float d = ex2((v[i] - rlse) * kLog2e);
+            d = vcol + i == rt ? d - 1.f : d;
+            v[i] = vcol + i == p.excluded ? 0.f : d * rg;
+          }
+          if (row >= T.m) {  // rows up to the next tile edge are read by the product over rows: exact zeros
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = 0.f;
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+          }
+          if constexpr (NP == 1) {
+            chunk_store(&omap, 0, false, col0, (int)row0, 0, v, stg, turn);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {  // the largest piece of what is left of the value
+              float q[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                q[i] = bf16_part(v[i]);
+                v[i] -= q[i];
+              }
+              chunk_store(&omap, 0, false, col0, (int)row0, k, q, stg, turn);
             }
           }
-          // to memory through shared memory: 8 lanes per row, 4 columns each
+        } else if (p.tma_out) {
+          if (p.bias != nullptr) {
+            if (col0 + 32 <= p.n) {
+              add32(v, p.bias, p.bias_f32, col0);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (col0 + i < p.n) v[i] += load1(p.bias, p.bias_f32, col0 + i);
+            }
+          }
+          if (p.pre != nullptr) chunk_store(&pmap, p.pre_f32, mixed, col0, (int)row0, 0, v, stg, turn);
+          if (p.act == kActSilu) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = silu_f(v[i]);
+          } else if (p.act == kActGelu) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = gelu_f(v[i]);
+          }
+          if (p.res != nullptr && row < T.m) {
+            const int64_t at = row * p.ld_res + col0;
+            if (p.vec && col0 + 32 <= p.n) {
+              add32(v, p.res, p.res_f32, at);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (col0 + i < p.n) v[i] += load1(p.res, p.res_f32, at + i);
+            }
+          }
+          chunk_store(&omap, p.out_f32, mixed, col0, (int)row0, sp, v, stg, turn);
+        } else {
+          // through shared memory: lane = column, rows in turn
+          float* f = reinterpret_cast<float*>(stg);
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            *reinterpret_cast<float4*>(stg + lane * 32 + 4 * (j ^ (lane & 7))) =
+            *reinterpret_cast<float4*>(f + lane * 32 + 4 * (j ^ (lane & 7))) =
                 make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
           __syncwarp();
-          const int col = col0 + 4 * (lane & 7);
-          float4 u[8];
-#pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            const int r = 4 * q + (lane >> 3);
-            u[q] = *reinterpret_cast<const float4*>(stg + r * 32 + 4 * ((lane & 7) ^ (r & 7)));
-          }
-          const int64_t r0 = row0 + (lane >> 3);  // rows r0, r0 + 4, ...
-          if constexpr (EPI == kEpiOut) {
-            float b[4] = {0.f, 0.f, 0.f, 0.f};
-            if (p.bias != nullptr) bias4(p, col, b);
-            if (p.vec && col0 + 32 <= nend && row0 + 32 <= T.m && p.row_map == nullptr)
-              out_chunk(p, r0, col, u, b, (int64_t)sp * p.split_stride);
-            else if (col < nend)
-#pragma unroll 1
-              for (int q = 0; q < 8; ++q)  // the chunk's row q is taken from shared memory again: u is indexed statically only
-                if (r0 + 4 * q < T.m) {
-                  const int r = 4 * q + (lane >> 3);
-                  out4(p, r0 + 4 * q, col,
-                       *reinterpret_cast<const float4*>(stg + r * 32 + 4 * ((lane & 7) ^ (r & 7))), b,
-                       (int64_t)sp * p.split_stride);
-                }
-          } else if (col < nend) {  // kEpiDz: the buffer holds whole tiles of rows and groups of 4 columns
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              const int64_t at = (r0 + 4 * q) * p.ld_out + col;
-              if constexpr (NP == 1) {
-                store4(p.out, 0, at, u[q]);
-              } else {
-                const float e[4] = {u[q].x, u[q].y, u[q].z, u[q].w};
-                __align__(8) bf16 pc[3][4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) split3(e[j], pc[0][j], pc[1][j], pc[2][j]);
-#pragma unroll
-                for (int k = 0; k < 3; ++k)
-                  *reinterpret_cast<uint2*>(static_cast<bf16*>(p.out) + k * p.plane + at) =
-                      *reinterpret_cast<const uint2*>(pc[k]);
-              }
-            }
+          const int col = col0 + lane;
+          if (col < nend) {
+            const float b = p.bias != nullptr ? load1(p.bias, p.bias_f32, col) : 0.f;
+            const int rows = (int)min((int64_t)32, T.m - row0);
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r)
+              out1(p, row0 + r, col, f[r * 32 + 4 * ((lane >> 2) ^ (r & 7)) + (lane & 3)], b,
+                   (int64_t)sp * p.split_stride);
           }
           __syncwarp();
         }
@@ -638,6 +677,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       if constexpr (!FLUSH) job += jobs;
     }
+    if (lane == 0) tma_store_wait();
     if (!ok && lane == 0) atomicExch(p.flag, 1);
   }
   umma::fence_before_sync();
@@ -649,7 +689,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 
 // One CTA (or pair) per SM (or pair of SMs), at most one per tile.
 template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI>
-cudaError_t gemm_t(const GemmParams& p, const CUtensorMap& a, const CUtensorMap& b, cudaStream_t s) {
+cudaError_t gemm_t(const GemmParams& p, const GemmMaps& m, cudaStream_t s) {
   using S = GemmSmem<CG, BN, NP>;
   auto kern = k_gemm<CG, BN, NP, A_MN, B_MN, EPI>;
   cudaError_t e = set_smem_cached(reinterpret_cast<const void*>(kern), (int)S::kBytes, 100);
@@ -674,7 +714,7 @@ cudaError_t gemm_t(const GemmParams& p, const CUtensorMap& a, const CUtensorMap&
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = CG == 2 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, p, a, b);
+  return cudaLaunchKernelEx(&cfg, kern, p, m.a, m.b, m.out, m.pre);
 }
 
 }  // namespace

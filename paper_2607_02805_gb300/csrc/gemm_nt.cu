@@ -3,16 +3,15 @@
 
 namespace bds {
 
-cudaError_t launch_gemm_nt(const GemmCfg& c, const GemmParams& p, const CUtensorMap& a, const CUtensorMap& b,
-                        cudaStream_t s) {
+cudaError_t launch_gemm_nt(const GemmCfg& c, const GemmParams& p, const GemmMaps& m, cudaStream_t s) {
   if (c.cg == 2 && c.bn == 256 && c.pieces == 1)
-    return gemm_t<2, 256, 1, false, false, kEpiOut>(p, a, b, s);
+    return gemm_t<2, 256, 1, false, false, kEpiOut>(p, m, s);
   if (c.cg == 1 && c.bn == 128 && c.pieces == 1)
-    return gemm_t<1, 128, 1, false, false, kEpiOut>(p, a, b, s);
+    return gemm_t<1, 128, 1, false, false, kEpiOut>(p, m, s);
   if (c.cg == 1 && c.bn == 64 && c.pieces == 1)
-    return gemm_t<1, 64, 1, false, false, kEpiOut>(p, a, b, s);
+    return gemm_t<1, 64, 1, false, false, kEpiOut>(p, m, s);
   if (c.cg == 1 && c.bn == 128 && c.pieces == 3)
-    return gemm_t<1, 128, 3, false, false, kEpiOut>(p, a, b, s);
+    return gemm_t<1, 128, 3, false, false, kEpiOut>(p, m, s);
   return cudaErrorInvalidValue;
 }
 
