@@ -314,22 +314,13 @@ __global__ void __launch_bounds__(kThreads) k_loss_combine(const float2* part, i
   if ((int64_t)blockIdx.x * 32 >= *count) return;
   const bool live = i < *count;
   float m = -INFINITY, s = 0.f;
-  auto join = [&](float2 q) {
-    const float nm = fmaxf(m, q.x);
-    if (nm == -INFINITY) {  // nothing but excluded entries so far, or NaN
-      s += q.y;
-      return;
-    }
-    s = s * ex2(m - nm) + q.y * ex2(q.x - nm);
-    m = nm;
-  };
   if (live)
-    for (int k = w; k < parts; k += 8) join(part[(int64_t)k * rows_ld + i]);
+    for (int k = w; k < parts; k += 8) stats_join(m, s, part[(int64_t)k * rows_ld + i]);
   red[w][lane] = make_float2(m, s);
   __syncthreads();
   if (w == 0 && live) {
 #pragma unroll
-    for (int k = 1; k < 8; ++k) join(red[k][lane]);
+    for (int k = 1; k < 8; ++k) stats_join(m, s, red[k][lane]);
     const float l = (m + log2f(s)) * kLn2;
     const int row = idx[i];
     const float zt = at_target[i];

@@ -39,7 +39,7 @@ struct GemmParams {
   // kEpiStats / kEpiDz: rows i are the rows that count; column j is entry v0 + j
   int v0, excluded;
   const int* target;     // [rows] of the rows that count
-  float2* part;          // [2 * column tiles][rows] (maximum, sum of exponentials), base 2
+  float2* part;          // [column tiles][rows] (maximum, sum of exponentials), base 2
   float* at_target;      // [rows]
   int64_t rows_ld;       // rows of `part`
   const float* lse;      // [rows] of the rows that count

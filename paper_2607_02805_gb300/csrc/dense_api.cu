@@ -73,17 +73,18 @@ bool encode(CUtensorMap* m, const Operand& o, int box_rows) {
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The output [planes][rows][cols] as the epilogue stores it: boxes of 32 x 32.
+// The output [planes][rows][cols] as the epilogue stores it: boxes of 32
+// rows x 64 bytes.
 bool encode_out(CUtensorMap* m, const void* base, int f32, int64_t cols, int64_t rows, int64_t ld, int planes,
                 int64_t plane) {
   const int64_t elt = f32 ? 4 : 2;
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
   const cuuint64_t strides[2] = {(cuuint64_t)(ld * elt), (cuuint64_t)((planes > 1 ? plane : ld * 8) * elt)};
-  const cuuint32_t box[3] = {32u, 32u, 1u};
+  const cuuint32_t box[3] = {f32 ? 16u : 32u, 32u, 1u};
   const cuuint32_t estr[3] = {1u, 1u, 1u};
   return tensor_map_encoder()(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
                               const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                              CU_TENSOR_MAP_SWIZZLE_64B,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // Whether rows of `ld` elements start on 16-byte boundaries.
@@ -379,7 +380,7 @@ LossFwdWs loss_fwd_ws(const Loss& l) {
   size_t o = w.r.end;
   w.w = o;
   if (!in_place(l.dtype, l.K)) o += packed_bytes(l.dtype, l.V, l.K);
-  w.parts = (int)(2 * ((l.V + w.q.bn - 1) / w.q.bn));
+  w.parts = (int)((l.V + w.q.bn - 1) / w.q.bn);
   w.part = o;
   o += al256((size_t)w.parts * w.r.rows * 8);
   w.at = o;

@@ -9,8 +9,10 @@
 // than an SM's share of the L2; the pair takes 32 KB.
 //
 // Persistent CTAs, roles by warp: 0 issues the TMA loads of a ring of stages,
-// 1 the MMAs, 2 owns the TMEM allocation, 4 to 11 run the epilogue of one
-// accumulator while the MMAs fill the other. A stage holds 64 elements of k of
+// 1 the MMAs, 2 owns the TMEM allocation, 4 to 19 run the epilogue of one
+// accumulator while the MMAs fill the other (four warps per scheduler: the
+// epilogue is chains of latencies, and with two the GELU of a 16384 x 832 x
+// 3328 product took longer than its MMAs). A stage holds 64 elements of k of
 // both operands in the 128-byte swizzled layout of umma.cuh, rows along m or n
 // (K-major) or along k (MN-major), as the operand lies in memory: no operand
 // is transposed by a pass of its own.
@@ -37,8 +39,8 @@
 namespace bds {
 namespace {
 
-constexpr int kGemmThreads = 384;
-constexpr int kEpiWarps = 8;
+constexpr int kEpiWarps = 16;
+constexpr int kGemmThreads = 128 + 32 * kEpiWarps;
 constexpr int kBk = 64;  // elements of k per stage: one 128-byte swizzled row
 
 template <int CG, int BN, int NP>
@@ -46,7 +48,7 @@ struct GemmSmem {
   static constexpr uint32_t kA = 128u * 128u;                // one piece of A
   static constexpr uint32_t kB = (uint32_t)(BN / CG) * 128u;  // one piece of B
   static constexpr uint32_t kStage = NP * (kA + kB);
-  static constexpr uint32_t kEpi = kEpiWarps * 4096u;
+  static constexpr uint32_t kEpi = kEpiWarps * 2048u;
   static constexpr int kStages = (int)((232448u - 1024u - 512u - kEpi) / kStage) > 8
                                      ? 8
                                      : (int)((232448u - 1024u - 512u - kEpi) / kStage);
@@ -65,32 +67,18 @@ __device__ __forceinline__ uint32_t map_cta(uint32_t saddr, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(r) : "r"(saddr), "r"(rank));
   return r;
 }
+// One lane of a warp that executes this together.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+  return p != 0;
+}
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
 }
-template <int CG>
-__device__ __forceinline__ bool gbar_wait(uint64_t* bar, uint32_t parity) {
-  if constexpr (CG == 1) {
-    return umma::bar_wait(bar, parity);
-  } else {
-    const uint32_t a = umma::smem_u32(bar);
-    for (uint32_t i = 0; i < (1u << 22); ++i) {
-      uint32_t done;
-      asm volatile(
-          "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-          " selp.u32 %0, 1, 0, p;\n}\n"
-          : "=r"(done)
-          : "r"(a), "r"(parity)
-          : "memory");
-      if (done) return true;
-    }
-    return false;
-  }
-}
-// The same by every lane of a warp, which leaves together.
-template <int CG>
+// A wait by every lane of a warp, which leaves together.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
-  return __all_sync(0xffffffffu, gbar_wait<CG>(bar, parity));
+  return __all_sync(0xffffffffu, umma::bar_wait(bar, parity));
 }
 // One arrival at the barrier at this offset in the tile's first CTA. What it
 // orders is this thread's TMEM loads, which have completed (wait::ld and the
@@ -179,10 +167,24 @@ __device__ __forceinline__ float rcp_f(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float silu_f(float z) { return z * rcp_f(1.f + ex2(-kLog2e * z)); }
-__device__ __forceinline__ float gelu_f(float z) {
+// exp(-x) of the sigmoid's argument x, as the base-2 exponent that ex2 takes.
+__device__ __forceinline__ float silu_arg(float z) { return -kLog2e * z; }
+__device__ __forceinline__ float gelu_arg(float z) {
   constexpr float c1 = -2.f * kGeluA * kLog2e, c2 = c1 * kGeluB;
-  return z * rcp_f(1.f + ex2(z * fmaf(c2, z * z, c1)));
+  return z * fmaf(c2, z * z, c1);
+}
+__device__ __forceinline__ float silu_f(float z) { return z * rcp_f(1.f + ex2(silu_arg(z))); }
+__device__ __forceinline__ float gelu_f(float z) { return z * rcp_f(1.f + ex2(gelu_arg(z))); }
+// Two at a time with one reciprocal, 1/a = b (1/ab): the MUFU unit gives half
+// as many reciprocals per clock as exponentials. Exponentials above 2^60 count
+// as that, so that the product stays finite; the sigmoid is below 1e-18 there.
+// A NaN stays its own element's through the last product.
+template <float (*ARG)(float)>
+__device__ __forceinline__ void sigmoid_mul2(float& z0, float& z1) {
+  const float a = 1.f + fminf(ex2(ARG(z0)), 0x1p60f), b = 1.f + fminf(ex2(ARG(z1)), 0x1p60f);
+  const float r = rcp_f(a * b);
+  z0 *= r * b;
+  z1 *= r * a;
 }
 __device__ __forceinline__ float act_fwd(int act, float z) {
   return act == kActNone ? z : act == kActSilu ? silu_f(z) : gelu_f(z);
@@ -253,9 +255,9 @@ __device__ __forceinline__ void store1(void* p, int f32, int64_t at, float v) {
 // A warp's chunk is 32 rows x 32 columns, a thread holding one row (as TMEM
 // gives it). It leaves by TMA where rows start on 16-byte boundaries: the warp
 // writes the chunk to shared memory in the swizzle of the map's box and one lane
-// issues the store, which also cuts off what lies outside the matrix. Per
-// element that is a third of the instructions of a transposition through shared
-// memory with plain stores (16384 x 832 x 3328: @@).
+// issues the store, which also cuts off what lies outside the matrix. A
+// transposition through shared memory with plain stores, as unaligned rows need
+// it, took three times the instructions.
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int c0, int c1, int c2, uint32_t src) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];\n" ::"l"(
                    reinterpret_cast<uint64_t>(map)),
@@ -270,39 +272,63 @@ __device__ __forceinline__ void tma_store_wait_read() {
 }
 __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory"); }
 
-// One chunk to the box at (col, row, z) of `map`. bf16: two buffers of 2 KB
-// (64-byte swizzle) in turn; fp32: one of 4 KB (128-byte swizzle). `mixed`: the
-// launch stores both types, so that the previous store may read either.
-__device__ __forceinline__ void chunk_store(const CUtensorMap* map, int f32, bool mixed, int col, int row, int z,
-                                            const float (&v)[32], unsigned char* stg, uint32_t& turn) {
+// One chunk to (col, row, z) of `map` through the warp's 2 KB: at once (bf16) or
+// as two halves of 16 columns (fp32), 64-byte rows and swizzle either way.
+__device__ __forceinline__ void chunk_store(const CUtensorMap* map, int f32, int col, int row, int z, int ncols,
+                                            const float (&v)[32], unsigned char* stg) {
   const int lane = threadIdx.x & 31;
-  if (f32) {
-    if (lane == 0) tma_store_wait_read<0>();
-    __syncwarp();
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      *reinterpret_cast<float4*>(stg + lane * 128 + 16 * (j ^ (lane & 7))) =
-          make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-  } else {
-    stg += 2048 * (turn & 1);
-    ++turn;
-    if (lane == 0) {
-      if (mixed) tma_store_wait_read<0>();
-      else tma_store_wait_read<1>();
-    }
-    __syncwarp();
+  unsigned char* mine = stg + lane * 64;
+  const int sw = (lane >> 1) & 3;
+  if (lane == 0) tma_store_wait_read<0>();
+  __syncwarp();
+  if (!f32) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<uint4*>(stg + lane * 64 + 16 * (j ^ ((lane >> 1) & 3))) =
+      *reinterpret_cast<uint4*>(mine + 16 * (j ^ sw)) =
           make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]),
                      pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
+    umma::fence_async_smem();
+    __syncwarp();
+    if (lane == 0) tma_store_3d(map, col, row, z, umma::smem_u32(stg));
+    return;
   }
-  umma::fence_async_smem();
-  __syncwarp();
-  if (lane == 0) tma_store_3d(map, col, row, z, umma::smem_u32(stg));
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (h == 1) {
+      if (col + 16 >= ncols) return;
+      if (lane == 0) tma_store_wait_read<0>();
+      __syncwarp();
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<float4*>(mine + 16 * (j ^ sw)) =
+          make_float4(v[16 * h + 4 * j], v[16 * h + 4 * j + 1], v[16 * h + 4 * j + 2], v[16 * h + 4 * j + 3]);
+    umma::fence_async_smem();
+    __syncwarp();
+    if (lane == 0) tma_store_3d(map, col + 16 * h, row, z, umma::smem_u32(stg));
+  }
 }
 
-// 32 consecutive values at p[at], which lies on a 16-byte boundary.
+// 32 consecutive bf16 values at p[at], which lies on a 16-byte boundary, in two
+// steps: the loads, and the sums once they are there.
+__device__ __forceinline__ void load32(uint4 (&r)[4], const void* p, int64_t at) {
+  const uint4* q = reinterpret_cast<const uint4*>(static_cast<const bf16*>(p) + at);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) r[j] = q[j];
+}
+__device__ __forceinline__ void add32(float (&v)[32], const uint4 (&r)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t e[4] = {r[j].x, r[j].y, r[j].z, r[j].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[8 * j + 2 * i] += __uint_as_float(e[i] << 16);
+      v[8 * j + 2 * i + 1] += __uint_as_float(e[i] & 0xffff0000u);
+    }
+  }
+}
+
+// Both steps, for either type.
 __device__ __forceinline__ void add32(float (&v)[32], const void* p, int f32, int64_t at) {
   if (f32) {
     const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
@@ -313,16 +339,8 @@ __device__ __forceinline__ void add32(float (&v)[32], const void* p, int f32, in
     }
   } else {
     const uint4* q = reinterpret_cast<const uint4*>(static_cast<const bf16*>(p) + at);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint4 u = q[j];
-      const uint32_t e[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[8 * j + 2 * i] += __uint_as_float(e[i] << 16);
-        v[8 * j + 2 * i + 1] += __uint_as_float(e[i] & 0xffff0000u);
-      }
-    }
+    const uint4 r[4] = {q[0], q[1], q[2], q[3]};
+    add32(v, r);
   }
 }
 
@@ -337,6 +355,18 @@ __device__ __forceinline__ void out1(const GemmParams& p, int64_t row, int col, 
   const int64_t orow = p.row_map != nullptr ? p.row_map[row] : row;
   store1(p.out, p.out_f32, out_off + orow * p.ld_out + col, v);
 }
+// Joins two partial (maximum, sum of exponentials) of a row, base 2. A part
+// without a maximum (every entry excluded) adds its sum, 0 or NaN.
+__device__ __forceinline__ void stats_join(float& m, float& s, float2 q) {
+  const float nm = fmaxf(m, q.x);
+  if (nm == -INFINITY) {
+    s += q.y;
+    return;
+  }
+  s = s * ex2(m - nm) + q.y * ex2(q.x - nm);
+  m = nm;
+}
+
 // Extents of one call with the device's row count applied, and its tiles.
 template <int CG>
 struct Tiles {
@@ -375,7 +405,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   __shared__ uint64_t full[8], empty[8], accfull[2], accempty[2];
   __shared__ uint32_t tslot;
   unsigned char* sm = align1024(smem_raw);
-  const int t = threadIdx.x, w = t >> 5, lane = t & 31;
+  const int t = threadIdx.x, lane = t & 31;
+  const int w = __shfl_sync(0xffffffffu, t >> 5, 0);  // uniform over the warp, also to the compiler
   const uint32_t rank = CG == 2 ? cta_rank() : 0u;
   const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
   if (t == 0) {
@@ -399,20 +430,26 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   const Tiles<CG> T(p);
   if (w == 0) {
     // ---------------- producer ----------------
-    if (lane == 0) {
-      const uint32_t base = umma::smem_u32(sm);
-      bool ok = true;
-      int it = 0;
-      for (int tile = unit; tile < T.total && ok; tile += units) {
-        int tmi, tni, k0, k1, sp;
-        T.at(p, tile, tmi, tni, k0, k1, sp);
-        const int m0 = tmi * 128 * CG + (int)rank * 128;
-        const int n0 = tni * p.bn + (CG == 2 ? (int)rank * (p.bn / 2) : 0);
-        for (int kb = k0; kb < k1; ++kb, ++it) {
-          const int s = it % ST;
-          if (!(ok = gbar_wait<CG>(&empty[s], ((it / ST) & 1) ^ 1))) break;
+    // Producer and issuer run their loops as whole warps, one elected lane
+    // issuing: addresses and descriptors then stay in uniform registers, where
+    // the instructions want them. (As loops of lane 0 alone: 722 clocks per 64
+    // of k instead of 512, 4864 x 16384 x 1024.)
+    const bool leader = elect_one();
+    const uint32_t base = umma::smem_u32(sm);
+    const uint32_t full0 = CG == 2 ? map_cta(umma::smem_u32(&full[0]), 0) : umma::smem_u32(&full[0]);
+    bool ok = true;
+    int it = 0, s = 0;
+    uint32_t ph = 0;  // stage and its phase
+    for (int tile = unit; tile < T.total && ok; tile += units) {
+      int tmi, tni, k0, k1, sp;
+      T.at(p, tile, tmi, tni, k0, k1, sp);
+      const int m0 = tmi * 128 * CG + (int)rank * 128;
+      const int n0 = tni * p.bn + (CG == 2 ? (int)rank * (p.bn / 2) : 0);
+      for (int kb = k0; kb < k1; ++kb, ++it) {
+        if (!(ok = warp_wait(&empty[s], ph ^ 1))) break;
+        if (leader) {
           if (rank == 0) bar_expect_tx(&full[s], S::kStage * CG);
-          const uint32_t bar = CG == 2 ? map_cta(umma::smem_u32(&full[s]), 0) : umma::smem_u32(&full[s]);
+          const uint32_t bar = full0 + 8u * (uint32_t)s;
           const uint32_t a = base + (uint32_t)s * S::kStage, b = a + NP * S::kA;
 #pragma unroll
           for (int q = 0; q < NP; ++q) {
@@ -432,67 +469,69 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             }
           }
         }
+        if (++s == ST) s = 0, ph ^= 1;
       }
-      // the stages in flight: consumed (their release has arrived in this CTA), or after a give-up at least landed
-      for (int i = max(0, it - ST); i < it; ++i) {
-        if (ok) ok = gbar_wait<CG>(&empty[i % ST], (i / ST) & 1);
-        if (!ok && rank == 0) gbar_wait<CG>(&full[i % ST], (i / ST) & 1);
-      }
-      if (!ok) atomicExch(p.flag, 1);
     }
+    // the stages in flight: consumed (their release has arrived in this CTA), or after a give-up at least landed
+    for (int i = max(0, it - ST); i < it; ++i) {
+      if (ok) ok = warp_wait(&empty[i % ST], (i / ST) & 1);
+      if (!ok && rank == 0) warp_wait(&full[i % ST], (i / ST) & 1);
+    }
+    if (!ok && leader) atomicExch(p.flag, 1);
   } else if (w == 1) {
     // ---------------- MMA issue ----------------
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
+      const bool leader = elect_one();
       const uint32_t idesc = umma::idesc_bf16(128 * CG, (uint32_t)p.bn, A_MN, B_MN);
       constexpr uint32_t astep = A_MN ? 2048u : 32u, bstep = B_MN ? 2048u : 32u;  // bytes per 16 elements of k
       const uint32_t base = umma::smem_u32(sm);
+      const uint64_t da0 = umma::sdesc(base, A_MN ? 8192u : 16u, 1024u),
+                     db0 = umma::sdesc(base + NP * S::kA, B_MN ? 8192u : 16u, 1024u);
       bool ok = true;
-      int it = 0, job = 0;
+      int job = 0, s = 0;
+      uint32_t ph = 0;
       for (int tile = unit; tile < T.total && ok; tile += units) {
         int tmi, tni, k0, k1, sp;
         T.at(p, tile, tmi, tni, k0, k1, sp);
-        for (int kb = k0; kb < k1; ++kb, ++it) {
+        for (int kb = k0; kb < k1; ++kb) {
           const bool first = FLUSH || kb == k0, last = FLUSH || kb + 1 == k1;
           if (first) {
-            if (!(ok = gbar_wait<CG>(&accempty[job & 1], ((job >> 1) & 1) ^ 1))) break;
+            if (!(ok = warp_wait(&accempty[job & 1], ((job >> 1) & 1) ^ 1))) break;
             umma::fence_after_sync();
           }
-          const int s = it % ST;
-          if (!(ok = gbar_wait<CG>(&full[s], (it / ST) & 1))) break;
-          umma::fence_after_sync();
-          const uint32_t a = base + (uint32_t)s * S::kStage, b = a + NP * S::kA;
+          if (!(ok = warp_wait(&full[s], ph))) break;
           const uint32_t d = tm + (uint32_t)(job & 1) * BN;
-          const uint64_t da = umma::sdesc(a, A_MN ? 8192u : 16u, 1024u), db = umma::sdesc(b, B_MN ? 8192u : 16u, 1024u);
-          if constexpr (NP == 1) {
-#pragma unroll
-            for (int q = 0; q < kBk / 16; ++q)
-              gmma<CG>(d, umma::sdesc_adv(da, q * astep), umma::sdesc_adv(db, q * bstep), idesc, !first || q > 0);
-          } else {
-            constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};  // smallest terms first
-#pragma unroll
-            for (int c = 0; c < 6; ++c)
+          const uint64_t da = umma::sdesc_adv(da0, (uint32_t)s * S::kStage), db = umma::sdesc_adv(db0, (uint32_t)s * S::kStage);
+          if (leader) {
+            if constexpr (NP == 1) {
 #pragma unroll
               for (int q = 0; q < kBk / 16; ++q)
-                gmma<CG>(d, umma::sdesc_adv(da, pa[c] * S::kA + q * astep),
-                         umma::sdesc_adv(db, pb[c] * S::kB + q * bstep), idesc, c > 0 || q > 0);
+                gmma<CG>(d, umma::sdesc_adv(da, q * astep), umma::sdesc_adv(db, q * bstep), idesc, !first || q > 0);
+            } else {
+              constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};  // smallest terms first
+#pragma unroll
+              for (int c = 0; c < 6; ++c)
+#pragma unroll
+                for (int q = 0; q < kBk / 16; ++q)
+                  gmma<CG>(d, umma::sdesc_adv(da, pa[c] * S::kA + q * astep),
+                           umma::sdesc_adv(db, pb[c] * S::kB + q * bstep), idesc, c > 0 || q > 0);
+            }
+            gcommit<CG>(&empty[s]);
+            if (last) gcommit<CG>(&accfull[job & 1]);
           }
-          gcommit<CG>(&empty[s]);
-          if (last) {
-            gcommit<CG>(&accfull[job & 1]);
-            ++job;
-          }
+          if (++s == ST) s = 0, ph ^= 1;
+          if (last) ++job;
         }
       }
-      if (!ok) atomicExch(p.flag, 1);
+      if (!ok && leader) atomicExch(p.flag, 1);
     }
   } else if (w >= 4) {
     // ---------------- epilogue ----------------
-    const int ew = w - 4, half = ew >> 2;  // TMEM lanes 32 (w % 4) .. + 31, every second chunk of 32 columns
+    const int ew = w - 4, quarter = ew >> 2;  // TMEM lanes 32 (w % 4) .. + 31, every fourth chunk of 32 columns
     const uint32_t lanes = tm + ((uint32_t)(32 * (w & 3)) << 16);
-    unsigned char* stg = sm + ST * S::kStage + ew * 4096;
+    unsigned char* stg = sm + ST * S::kStage + ew * 2048;
     uint32_t turn = 0;
-    const bool mixed = p.pre != nullptr && p.pre_f32 != p.out_f32;
-    constexpr int NC = BN / 64;  // chunks of this warp
+    constexpr int NC = BN < 128 ? 1 : BN / 128;  // chunks of this warp at most
     const int nchunks = (p.bn + 31) / 32;
     bool ok = true;
     int job = 0;
@@ -505,12 +544,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 #pragma unroll
         for (int i = 0; i < NC * 32; ++i) acc[i] = 0.f;
         for (int j = 0; j < jobs; ++j, ++job) {
-          if (!(ok = warp_wait<CG>(&accfull[job & 1], (job >> 1) & 1))) break;
+          if (!(ok = warp_wait(&accfull[job & 1], (job >> 1) & 1))) break;
           umma::fence_after_sync();
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
             float v[32];
-            umma::tmem_ld32(lanes + (uint32_t)(job & 1) * BN + 32u * (uint32_t)(2 * c + half), v);
+            umma::tmem_ld32(lanes + (uint32_t)(job & 1) * BN + 32u * (uint32_t)(4 * c + quarter), v);
 #pragma unroll
             for (int i = 0; i < 32; ++i) acc[c * 32 + i] += v[i];
           }
@@ -518,9 +557,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           __syncwarp();
           if (lane == 0) leader_arrive<CG>(&accempty[job & 1]);
         }
-      } else if (jobs > 0) {
-        ok = warp_wait<CG>(&accfull[job & 1], (job >> 1) & 1);
-        umma::fence_after_sync();
       }
       if (!ok) break;
       const int64_t row0 = (int64_t)tmi * 128 * CG + rank * 128 + 32 * (w & 3);
@@ -538,35 +574,48 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           }
         }
       }
-      const uint32_t tacc = lanes + (uint32_t)(job & 1) * BN;
-      uint32_t nxt[32];  // the next chunk, on its way from TMEM while this one is worked on
+      // bias and residual of a chunk are loaded while the chunk before is worked on (bf16, whole chunks)
+      uint4 braw[4], rraw[4];
+      auto early_b = [&](int col) { return EPI == kEpiOut && p.tma_out && p.bias != nullptr && !p.bias_f32 && col + 32 <= p.n; };
+      auto early_r = [&](int col) {
+        return EPI == kEpiOut && p.tma_out && p.res != nullptr && !p.res_f32 && p.vec && col + 32 <= p.n && row < T.m;
+      };
+      auto early = [&](int col) {
+        if (early_b(col)) load32(braw, p.bias, col);
+        if (early_r(col)) load32(rraw, p.res, row * p.ld_res + col);
+      };
+      if constexpr (EPI == kEpiOut) early(tni * p.bn + 32 * quarter);
       if constexpr (!FLUSH) {
-        if (jobs > 0) umma::tmem_ld32_issue(tacc + 32u * (uint32_t)half, nxt);
+        if (jobs > 0) {
+          ok = warp_wait(&accfull[job & 1], (job >> 1) & 1);
+          umma::fence_after_sync();
+        }
+        if (!ok) break;
       }
+      const uint32_t tacc = lanes + (uint32_t)(job & 1) * BN;
 #pragma unroll(FLUSH ? NC : 1)
       for (int c = 0; c < NC; ++c) {
-        const int ch = 2 * c + half;
+        const int ch = 4 * c + quarter;
         const int col0 = tni * p.bn + 32 * ch;
+        const bool live = ch < nchunks && col0 < nend;  // uniform over the warp
         float v[32];
         if constexpr (FLUSH) {
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = acc[c * 32 + i];
-        } else if (jobs > 0) {
-          umma::tmem_ld_wait(nxt);
+        } else {
+          if (jobs > 0 && live) {
+            umma::tmem_ld32(tacc + 32u * (uint32_t)ch, v);
+          } else {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(nxt[i]);
-          if (c + 1 < NC) {
-            umma::tmem_ld32_issue(tacc + 32u * (uint32_t)(ch + 2), nxt);
-          } else {  // the accumulator may be overwritten
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+          }
+          if (c == NC - 1 && jobs > 0) {  // the accumulator may be overwritten
             umma::fence_before_sync();
             __syncwarp();
             if (lane == 0) leader_arrive<CG>(&accempty[job & 1]);
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = 0.f;
         }
-        if (ch >= nchunks || col0 >= nend) continue;  // uniform over the warp
+        if (!live) continue;
         if constexpr (EPI == kEpiStats) {
           const int vcol = p.v0 + col0;
           const bool edge = col0 + 32 > nend || (unsigned)(p.excluded - vcol) < 32u;
@@ -610,7 +659,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             for (int i = 0; i < 32; ++i) v[i] = 0.f;
           }
           if constexpr (NP == 1) {
-            chunk_store(&omap, 0, false, col0, (int)row0, 0, v, stg, turn);
+            chunk_store(&omap, 0, col0, (int)row0, 0, p.n, v, stg);
           } else {
 #pragma unroll
             for (int k = 0; k < 3; ++k) {  // the largest piece of what is left of the value
@@ -620,12 +669,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 q[i] = bf16_part(v[i]);
                 v[i] -= q[i];
               }
-              chunk_store(&omap, 0, false, col0, (int)row0, k, q, stg, turn);
+              chunk_store(&omap, 0, col0, (int)row0, k, p.n, q, stg);
             }
           }
         } else if (p.tma_out) {
           if (p.bias != nullptr) {
-            if (col0 + 32 <= p.n) {
+            if (early_b(col0)) {
+              add32(v, braw);
+            } else if (col0 + 32 <= p.n) {
               add32(v, p.bias, p.bias_f32, col0);
             } else {
 #pragma unroll
@@ -633,17 +684,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 if (col0 + i < p.n) v[i] += load1(p.bias, p.bias_f32, col0 + i);
             }
           }
-          if (p.pre != nullptr) chunk_store(&pmap, p.pre_f32, mixed, col0, (int)row0, 0, v, stg, turn);
+          if (p.pre != nullptr) chunk_store(&pmap, p.pre_f32, col0, (int)row0, 0, p.n, v, stg);
           if (p.act == kActSilu) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = silu_f(v[i]);
+            for (int i = 0; i < 32; i += 2) sigmoid_mul2<silu_arg>(v[i], v[i + 1]);
           } else if (p.act == kActGelu) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = gelu_f(v[i]);
+            for (int i = 0; i < 32; i += 2) sigmoid_mul2<gelu_arg>(v[i], v[i + 1]);
           }
           if (p.res != nullptr && row < T.m) {
             const int64_t at = row * p.ld_res + col0;
-            if (p.vec && col0 + 32 <= p.n) {
+            if (early_r(col0)) {
+              add32(v, rraw);
+            } else if (p.vec && col0 + 32 <= p.n) {
               add32(v, p.res, p.res_f32, at);
             } else {
 #pragma unroll
@@ -651,29 +704,42 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 if (col0 + i < p.n) v[i] += load1(p.res, p.res_f32, at + i);
             }
           }
-          chunk_store(&omap, p.out_f32, mixed, col0, (int)row0, sp, v, stg, turn);
+          if (c + 1 < NC) early(col0 + 128);
+          chunk_store(&omap, p.out_f32, col0, (int)row0, sp, p.n, v, stg);
         } else {
-          // through shared memory: lane = column, rows in turn
+          // through shared memory, 16 columns at a time: 16 lanes per row, a row per half warp
           float* f = reinterpret_cast<float*>(stg);
+          const int rows = (int)min((int64_t)32, T.m - row0);
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            *reinterpret_cast<float4*>(f + lane * 32 + 4 * (j ^ (lane & 7))) =
-                make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-          __syncwarp();
-          const int col = col0 + lane;
-          if (col < nend) {
-            const float b = p.bias != nullptr ? load1(p.bias, p.bias_f32, col) : 0.f;
-            const int rows = (int)min((int64_t)32, T.m - row0);
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              *reinterpret_cast<float4*>(f + lane * 16 + 4 * (j ^ ((lane >> 1) & 3))) =
+                  make_float4(v[16 * h + 4 * j], v[16 * h + 4 * j + 1], v[16 * h + 4 * j + 2], v[16 * h + 4 * j + 3]);
+            __syncwarp();
+            const int cl = lane & 15, col = col0 + 16 * h + cl;
+            if (col < nend) {
+              const float b = p.bias != nullptr ? load1(p.bias, p.bias_f32, col) : 0.f;
 #pragma unroll 4
-            for (int r = 0; r < rows; ++r)
-              out1(p, row0 + r, col, f[r * 32 + 4 * ((lane >> 2) ^ (r & 7)) + (lane & 3)], b,
-                   (int64_t)sp * p.split_stride);
+              for (int r = lane >> 4; r < rows; r += 2)
+                out1(p, row0 + r, col, f[r * 16 + 4 * ((cl >> 2) ^ ((r >> 1) & 3)) + (cl & 3)], b,
+                     (int64_t)sp * p.split_stride);
+            }
+            __syncwarp();
           }
-          __syncwarp();
         }
       }
       if constexpr (EPI == kEpiStats) {
-        if (row < T.m) p.part[(int64_t)(2 * tni + half) * p.rows_ld + row] = make_float2(rm, rs);
+        // the row's four quarters meet in shared memory (two buffers in turn:
+        // a warp is at most one tile ahead of the one that joins)
+        float2* q = reinterpret_cast<float2*>(sm + ST * S::kStage) + 512 * (turn++ & 1);
+        q[128 * quarter + 32 * (w & 3) + lane] = make_float2(rm, rs);
+        asm volatile("bar.sync 1, %0;\n" ::"n"(32 * kEpiWarps) : "memory");
+        if (quarter == 0 && row < T.m) {
+#pragma unroll
+          for (int k = 1; k < 4; ++k) stats_join(rm, rs, q[128 * k + 32 * w + lane - 128]);
+          p.part[(int64_t)tni * p.rows_ld + row] = make_float2(rm, rs);
+        }
       }
       if constexpr (!FLUSH) job += jobs;
     }
