@@ -11,108 +11,187 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// ---- operand packing ----
-// A thread converts four columns of one row. Operands whose rows start on
-// 16-byte boundaries are read in place and never come here; the others, fp32
-// operands and the loss's gathered rows cost one read and one write.
-__global__ void __launch_bounds__(kThreads) k_pack(const PackParams p) {
-  pdl_sync();
-  const int64_t groups = p.ld_dst / 4;
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t row = idx / groups;
-  const int c = (int)(idx - row * groups) * 4;
-  if (row >= p.rows) return;
-  int64_t src_row = row;
-  bool zero = false;
-  if (p.idx != nullptr) {
-    const int n = *p.count;
-    if (row >= ((n + 255) & ~255)) return;
-    zero = row >= n;
-    if (!zero) src_row = p.idx[row];
-  }
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  if (!zero) {
-    const int64_t at = src_row * p.ld + c;
-    if (p.ld % 4 == 0 && c + 3 < p.cols) {
-      const float4 q = load4(p.src, p.src_f32, at);
-      v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
-    } else {
+// Eight consecutive values at p[at], which lies on a 16-byte boundary.
+__device__ __forceinline__ void load8(float (&v)[8], const void* p, int f32, int64_t at) {
+  if (f32) {
+    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+    const float4 a = q[0], b = q[1];
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  } else {
+    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const bf16*>(p) + at);
+    const uint32_t e[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (c + j < p.cols) v[j] = load1(p.src, p.src_f32, at + j);
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(e[i] << 16);
+      v[2 * i + 1] = __uint_as_float(e[i] & 0xffff0000u);
     }
   }
-  bf16* d = p.dst + row * p.ld_dst + c;
-  if (p.pieces == 1) {
-    *reinterpret_cast<uint2*>(d) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+}
+
+// ---- operand packing ----
+// A thread converts eight columns of one row. Operands whose rows start on
+// 16-byte boundaries are read in place and never come here; the others, fp32
+// operands and the loss's rows cost one read and one write.
+__device__ __forceinline__ void pack_store(bf16* d, int64_t plane, int pieces, const float (&v)[8]) {
+  if (pieces == 1) {
+    *reinterpret_cast<uint4*>(d) =
+        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
     return;
   }
-  __align__(8) bf16 q[3][4];
+  __align__(16) bf16 q[3][8];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) split3(v[j], q[0][j], q[1][j], q[2][j]);
+  for (int j = 0; j < 8; ++j) split3(v[j], q[0][j], q[1][j], q[2][j]);
 #pragma unroll
-  for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(d + k * p.plane) = *reinterpret_cast<const uint2*>(q[k]);
+  for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(d + k * plane) = *reinterpret_cast<const uint4*>(q[k]);
+}
+__device__ __forceinline__ void pack_load(float (&v)[8], const PackParams& p, int64_t row, int c) {
+  const int64_t at = row * p.ld + c;
+  if (p.ld % (p.src_f32 ? 4 : 8) == 0 && c + 8 <= p.cols) {
+    load8(v, p.src, p.src_f32, at);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < p.cols ? load1(p.src, p.src_f32, at + j) : 0.f;
+  }
+}
+__global__ void __launch_bounds__(kThreads) k_pack(const PackParams p) {
+  pdl_sync();
+  const int groups = (int)(p.ld_dst / 8);
+  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t row = idx / groups;
+  const int c = (int)(idx - row * groups) * 8;
+  if (row >= p.rows) return;
+  float v[8];
+  pack_load(v, p, row, c);
+  pack_store(p.dst + row * p.ld_dst + c, p.plane, p.pieces, v);
+}
+// The rows of the loss that count, each to its slot (pos), and zeros behind
+// them up to a whole tile of rows; in the backward a second copy scaled by the
+// row's weight, and zeros in the gradient of the rows that do not count.
+__global__ void __launch_bounds__(kThreads) k_pack_rows(const PackParams p) {
+  pdl_sync();
+  const int groups = (int)(p.ld_dst / 8);
+  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t row = idx / groups;
+  const int c = (int)(idx - row * groups) * 8;
+  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  int64_t to;
+  float g = 0.f;
+  if (row >= p.rows) {
+    const int n = *p.count;
+    to = n + (row - p.rows);
+    if (to >= ((n + 255) & ~255)) return;
+  } else {
+    to = p.pos[row];
+    if (to < 0) {
+      if (p.zero != nullptr) {
+        const int64_t at = row * p.cols + c;
+        const int f32 = p.src_f32;
+        if (p.cols % (f32 ? 4 : 8) == 0) {
+          if (c < p.cols) {  // cols is a multiple of 4 (fp32) or 8: whole halves
+            uint4* z = f32 ? reinterpret_cast<uint4*>(static_cast<float*>(p.zero) + at)
+                           : reinterpret_cast<uint4*>(static_cast<bf16*>(p.zero) + at);
+            z[0] = make_uint4(0, 0, 0, 0);
+            if (f32 && c + 4 < p.cols) z[1] = make_uint4(0, 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (c + j < p.cols) store1(p.zero, f32, at + j, 0.f);
+        }
+      }
+      return;
+    }
+    pack_load(v, p, row, c);
+    if (p.gscale != nullptr) g = p.gscale[to];
+  }
+  pack_store(p.dst + to * p.ld_dst + c, p.plane, p.pieces, v);
+  if (p.scaled != nullptr) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= g;
+    pack_store(p.scaled + to * p.ld_dst + c, p.plane, p.pieces, v);
+  }
 }
 
 // ---- dz = dy act'(pre), and the column sums for the bias ----
-// CTA: 128 columns (a warp's lanes hold 4 each) x one range of rows; its eight
-// warps take every eighth row. The sums are of the unrounded products, added
-// in a fixed order: rows of a warp, then warps, then ranges.
-__global__ void __launch_bounds__(kThreads) k_dact(const DactParams p) {
+// CTA: 256 columns (a lane holds 8) x one range of rows; its eight warps take
+// every eighth row, two of them in flight. One read of dy and pre and one
+// write of dz (16384 x 3328 bf16: 327 MB). The sums are of the unrounded
+// products, added in a fixed order: rows of a warp, then warps, then ranges.
+constexpr int kDactCols = 256, kDactFlight = 2;
+template <bool DYF32, bool PREF32>
+__global__ void __launch_bounds__(kThreads, 3) k_dact(const DactParams p) {
   pdl_sync();
-  __shared__ float4 red[8][32];
+  __shared__ float red[8][kDactCols];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int c = blockIdx.x * 128 + lane * 4;
+  const int c = blockIdx.x * kDactCols + lane * 8;
   const int64_t r0 = p.rows * blockIdx.y / p.ranges, r1 = p.rows * (blockIdx.y + 1) / p.ranges;
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  const bool full = c + 3 < p.cols && p.ld_dy % 4 == 0 && (p.act == kActNone || p.ld_pre % 4 == 0);
-  for (int64_t r = r0 + w; r < r1; r += 8) {
-    if (c >= p.cols) break;
-    float e[4] = {0.f, 0.f, 0.f, 0.f};
-    if (full) {
-      const float4 g = load4(p.dy, p.dy_f32, r * p.ld_dy + c);
-      e[0] = g.x, e[1] = g.y, e[2] = g.z, e[3] = g.w;
-      if (p.act != kActNone) {
-        const float4 z = load4(p.pre, p.pre_f32, r * p.ld_pre + c);
-        e[0] *= act_grad(p.act, z.x), e[1] *= act_grad(p.act, z.y);
-        e[2] *= act_grad(p.act, z.z), e[3] *= act_grad(p.act, z.w);
-      }
-    } else {
+  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  // 16-byte boundaries, eight whole columns
+  const bool full = c + 8 <= p.cols && p.ld_dy % (DYF32 ? 4 : 8) == 0 &&
+                    (p.act == kActNone || p.ld_pre % (PREF32 ? 4 : 8) == 0);
+  auto finish = [&](int64_t r, float (&e)[8], const float (&z)[8]) {
+    if (p.act == kActSilu) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (c + j < p.cols) {
-          e[j] = load1(p.dy, p.dy_f32, r * p.ld_dy + c + j);
-          if (p.act != kActNone) e[j] *= act_grad(p.act, load1(p.pre, p.pre_f32, r * p.ld_pre + c + j));
-        }
+      for (int j = 0; j < 8; ++j) e[j] *= act_grad(kActSilu, z[j]);
+    } else if (p.act == kActGelu) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) e[j] *= act_grad(kActGelu, z[j]);
     }
-    sum.x += e[0], sum.y += e[1], sum.z += e[2], sum.w += e[3];
-    if (p.dz != nullptr) {
-      bf16* d = p.dz + r * p.ld_dz + c;
-      if (p.pieces == 1) {
-        *reinterpret_cast<uint2*>(d) = make_uint2(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]));
-      } else {
-        __align__(8) bf16 q[3][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) split3(e[j], q[0][j], q[1][j], q[2][j]);
+    for (int j = 0; j < 8; ++j) sum[j] += e[j];
+    if (p.dz == nullptr) return;
+    bf16* d = p.dz + r * p.ld_dz + c;  // rows of whole groups of 8
+    if (p.pieces == 1) {
+      *reinterpret_cast<uint4*>(d) =
+          make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+      return;
+    }
+    __align__(16) bf16 q[3][8];
 #pragma unroll
-        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(d + k * p.plane) = *reinterpret_cast<const uint2*>(q[k]);
+    for (int j = 0; j < 8; ++j) split3(e[j], q[0][j], q[1][j], q[2][j]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(d + k * p.plane) = *reinterpret_cast<const uint4*>(q[k]);
+  };
+  if (full) {
+    int64_t r = r0 + w;
+    for (; r + 8 * (kDactFlight - 1) < r1; r += 8 * kDactFlight) {
+      float e[kDactFlight][8], z[kDactFlight][8];
+#pragma unroll
+      for (int i = 0; i < kDactFlight; ++i) {
+        load8(e[i], p.dy, DYF32, (r + 8 * i) * p.ld_dy + c);
+        if (p.act != kActNone) load8(z[i], p.pre, PREF32, (r + 8 * i) * p.ld_pre + c);
       }
+#pragma unroll
+      for (int i = 0; i < kDactFlight; ++i) finish(r + 8 * i, e[i], z[i]);
+    }
+    for (; r < r1; r += 8) {
+      float e[8], z[8];
+      load8(e, p.dy, DYF32, r * p.ld_dy + c);
+      if (p.act != kActNone) load8(z, p.pre, PREF32, r * p.ld_pre + c);
+      finish(r, e, z);
+    }
+  } else if (c < p.cols) {
+#pragma unroll 2
+    for (int64_t r = r0 + w; r < r1; r += 8) {
+      float e[8], z[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        e[j] = c + j < p.cols ? load1(p.dy, DYF32, r * p.ld_dy + c + j) : 0.f;
+        z[j] = p.act != kActNone && c + j < p.cols ? load1(p.pre, PREF32, r * p.ld_pre + c + j) : 0.f;
+      }
+      finish(r, e, z);
     }
   }
   if (p.part == nullptr) return;
-  red[w][lane] = sum;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) red[w][j * 32 + lane] = sum[j];
   __syncthreads();
-  if (w == 0 && c < p.cols) {
-    float4 s = red[0][lane];
+  const int lc = threadIdx.x, col = blockIdx.x * kDactCols + (lc & 31) * 8 + (lc >> 5);
+  if (col < p.cols) {
+    float s = red[0][lc];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) {
-      const float4 q = red[i][lane];
-      s.x += q.x, s.y += q.y, s.z += q.z, s.w += q.w;
-    }
-    const float e[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (c + j < p.cols) p.part[(int64_t)blockIdx.y * p.cols + c + j] = e[j];
+    for (int i = 1; i < 8; ++i) s += red[i][lc];
+    p.part[(int64_t)blockIdx.y * p.cols + col] = s;
   }
 }
 
@@ -124,8 +203,10 @@ __global__ void __launch_bounds__(kThreads) k_colsum(const float* part, int rang
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int64_t c = (int64_t)blockIdx.x * 32 + lane;
   float s = 0.f;
-  if (c < cols)
+  if (c < cols) {
+#pragma unroll 8
     for (int r = w; r < ranges; r += 8) s += part[(int64_t)r * cols + c];
+  }
   red[w][lane] = s;
   __syncthreads();
   if (w == 0 && c < cols) {
@@ -147,10 +228,16 @@ __global__ void __launch_bounds__(kThreads) k_split_reduce(const GemmParams p, c
   int m = p.m;
   if (p.rows_axis == 1) m = min(m, *p.rows_dev);
   if (row >= m) return;
-  float4 s = *reinterpret_cast<const float4*>(part + row * ld + c);
-  for (int i = 1; i < p.splits; ++i) {
-    const float4 q = *reinterpret_cast<const float4*>(part + i * p.split_stride + row * ld + c);
-    s.x += q.x, s.y += q.y, s.z += q.z, s.w += q.w;
+  const float* at = part + row * ld + c;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < p.splits; i += 8) {
+    float4 q[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i + j < p.splits) q[j] = *reinterpret_cast<const float4*>(at + (i + j) * p.split_stride);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i + j < p.splits) s.x += q[j].x, s.y += q[j].y, s.z += q[j].z, s.w += q[j].w;
   }
   float e[4] = {s.x, s.y, s.z, s.w};
   if (p.tma_out && p.vec && c + 3 < p.n && p.row_map == nullptr) {  // rows on 16-byte boundaries
@@ -168,7 +255,7 @@ __global__ void __launch_bounds__(kThreads) k_split_reduce(const GemmParams p, c
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (c + j < p.n) out1(p, row, c + j, e[j], p.bias != nullptr ? load1(p.bias, p.bias_f32, c + j) : 0.f, 0);
+      if (c + j < p.n) out1(p, row, c + j, e[j], p.bias != nullptr ? load1(p.bias, p.bias_f32, c + j) : 0.f);
   }
 }
 
@@ -249,78 +336,108 @@ __global__ void __launch_bounds__(128) k_linear_vec(const VecParams p) {
 }
 
 // ---- rows of the loss ----
-__device__ __forceinline__ bool row_counts(const int64_t* target, const float* weight, const float* dloss,
-                                           int64_t vocab, int64_t i) {
-  const int64_t t = target[i];
-  return t >= 0 && t < vocab && (weight == nullptr || weight[i] != 0.f) && (dloss == nullptr || dloss[i] != 0.f);
-}
-
-// One CTA: each thread counts a run of rows, a scan over the threads gives the
-// run's first slot, and the thread fills it in order.
-__global__ void __launch_bounds__(1024) k_loss_rows(const LossRowsParams p) {
+// A CTA takes `per` rows (a multiple of 1024). It counts the rows before its
+// own, all of them, rather than waiting for another CTA's count: up to 64 CTAs
+// re-read at most the 16 bytes per row that the launch reads anyway, from L2.
+// Then it numbers its own rows, 1024 at a time. (One CTA for all rows, which
+// reads them twice: 21 us at 16384 rows; this 10, from DRAM.)
+constexpr int kRowsCtas = 64;
+__global__ void __launch_bounds__(1024) k_loss_rows(const LossRowsParams p, int64_t per) {
   pdl_sync();
+  constexpr int F = 4;
   __shared__ int wsum[32];
   const int t = threadIdx.x, lane = t & 31, w = t >> 5;
-  const int64_t per = (p.rows + 1023) / 1024;
-  const int64_t r0 = min(p.rows, t * per), r1 = min(p.rows, r0 + per);
+  // weight (times dloss) of row i, and its target: -1 where the row does not count
+  auto load = [&](int64_t i, float& wt, int64_t& tg) {
+    const bool in = i < p.rows;
+    tg = in ? p.target[i] : -1;
+    wt = in && p.weight != nullptr ? p.weight[i] : 1.f;
+    const float dl = in && p.dloss != nullptr ? p.dloss[i] : 1.f;
+    if (wt == 0.f || dl == 0.f || tg >= p.vocab || tg < 0) tg = -1;
+    wt *= dl;
+  };
+  const int64_t begin = blockIdx.x * per, end = min(begin + per, p.rows);
   int n = 0;
-  for (int64_t i = r0; i < r1; ++i) n += row_counts(p.target, p.weight, p.dloss, p.vocab, i) ? 1 : 0;
-  int inc = n;
+  for (int64_t i = t; i < begin; i += 1024 * F) {
+    float wt[F];
+    int64_t tg[F];
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += v;
-  }
-  if (lane == 31) wsum[w] = inc;
-  __syncthreads();
-  if (w == 0) {
-    int v = wsum[lane];
+    for (int j = 0; j < F; ++j) load(i + 1024 * j < begin ? i + 1024 * j : p.rows, wt[j], tg[j]);
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, v, o);
-      if (lane >= o) v += u;
-    }
-    wsum[lane] = v;
+    for (int j = 0; j < F; ++j) n += tg[j] >= 0 ? 1 : 0;
   }
+  n = __reduce_add_sync(0xffffffffu, n);
+  if (lane == 0) wsum[w] = n;
   __syncthreads();
-  int at = inc - n + (w > 0 ? wsum[w - 1] : 0);
-  for (int64_t i = r0; i < r1; ++i) {
-    if (row_counts(p.target, p.weight, p.dloss, p.vocab, i)) {
-      p.idx[at] = (int)i;
-      p.tgt[at] = (int)p.target[i];
+  int at = __reduce_add_sync(0xffffffffu, wsum[lane]);  // rows before this CTA's
+  for (int64_t i0 = begin; i0 < end; i0 += 1024) {
+    const int64_t i = i0 + t;
+    float wt;
+    int64_t tg;
+    load(i, wt, tg);
+    const float ls = p.lse_in != nullptr && i < p.rows ? p.lse_in[i] : 0.f;
+    const bool c = tg >= 0;
+    const uint32_t m = __ballot_sync(0xffffffffu, c);
+    __syncthreads();  // wsum has been read
+    if (lane == 0) wsum[w] = __popc(m);
+    __syncthreads();
+    const int mine = wsum[lane];
+    const int before = __reduce_add_sync(0xffffffffu, lane < w ? mine : 0);
+    const int to = at + before + __popc(m & ((1u << lane) - 1u));
+    at += __reduce_add_sync(0xffffffffu, mine);
+    if (i >= p.rows) continue;  // no barrier is skipped: the loop ends for the whole CTA with this round
+    p.pos[i] = c ? to : -1;
+    if (c) {
+      p.idx[to] = (int)i;
+      p.tgt[to] = (int)tg;
       if (p.gscale != nullptr) {
-        const float wt = p.weight != nullptr ? p.weight[i] : 1.f;
-        p.gscale[at] = p.dloss != nullptr ? wt * p.dloss[i] : wt;
-        p.lse_c[at] = p.lse_in[i];
+        p.gscale[to] = wt;
+        p.lse_c[to] = ls;
       }
-      ++at;
     } else if (p.loss != nullptr) {
       p.loss[i] = 0.f;
       p.lse[i] = 0.f;
     }
   }
-  if (t == 1023) *p.count = at;
+  if (end == p.rows && t == 0) *p.count = at;
 }
 
-// Joins a row's partial maxima and sums: 32 rows per CTA, eight warps over the
-// partials in strides, then the warps in order.
-__global__ void __launch_bounds__(kThreads) k_loss_combine(const float2* part, int parts, int64_t rows_ld,
-                                                           const float* at_target, const int* count, const int* idx,
-                                                           const float* weight, float* loss, float* lse) {
+// Joins a row's partial maxima and sums: 32 rows per CTA, 32 warps over the
+// partials in strides with eight loads in flight, then the warps in order.
+__global__ void __launch_bounds__(1024) k_loss_combine(const float2* part, int parts, int64_t rows_ld,
+                                                       const float* at_target, const int* count, const int* idx,
+                                                       const float* weight, float* loss, float* lse) {
   pdl_sync();
-  __shared__ float2 red[8][32];
+  __shared__ float2 red[32][33];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int64_t i = (int64_t)blockIdx.x * 32 + lane;
-  if ((int64_t)blockIdx.x * 32 >= *count) return;
-  const bool live = i < *count;
+  const int n = *count;
+  const int i0 = blockIdx.x * 32;
+  if (i0 >= n) return;
+  const bool live = i0 + lane < n;
   float m = -INFINITY, s = 0.f;
-  if (live)
-    for (int k = w; k < parts; k += 8) stats_join(m, s, part[(int64_t)k * rows_ld + i]);
-  red[w][lane] = make_float2(m, s);
-  __syncthreads();
-  if (w == 0 && live) {
+  if (live) {
+    const float2* q = part + i0 + lane;
+    for (int k = w; k < parts; k += 256) {
+      float2 v[8];
 #pragma unroll
-    for (int k = 1; k < 8; ++k) stats_join(m, s, red[k][lane]);
+      for (int j = 0; j < 8; ++j)
+        v[j] = k + 32 * j < parts ? q[(int64_t)(k + 32 * j) * rows_ld] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) stats_join(m, s, v[j]);
+    }
+  }
+  red[lane][w] = make_float2(m, s);
+  __syncthreads();
+  // warp w joins the 32 parts of row w: a butterfly (each step joins the same two on both sides)
+  const float2 mine = red[w][lane];
+  m = mine.x, s = mine.y;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const float2 q = make_float2(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o));
+    stats_join(m, s, q);
+  }
+  const int i = i0 + w;
+  if (lane == 0 && i < n) {
     const float l = (m + log2f(s)) * kLn2;
     const int row = idx[i];
     const float zt = at_target[i];
@@ -328,21 +445,6 @@ __global__ void __launch_bounds__(kThreads) k_loss_combine(const float2* part, i
     const float d = zt == -INFINITY ? INFINITY : l - zt;
     lse[row] = l;
     loss[row] = weight != nullptr ? weight[row] * d : d;
-  }
-}
-
-__global__ void __launch_bounds__(kThreads) k_zero_rows(const int64_t* target, const float* weight,
-                                                        const float* dloss, int64_t rows, int64_t vocab,
-                                                        unsigned char* dst, int64_t row_bytes) {
-  pdl_sync();
-  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (row >= rows || row_counts(target, weight, dloss, vocab, row)) return;
-  unsigned char* d = dst + row * row_bytes;
-  const int lane = threadIdx.x & 31;
-  if (row_bytes % 16 == 0) {
-    for (int64_t b = lane * 16; b < row_bytes; b += 512) *reinterpret_cast<uint4*>(d + b) = make_uint4(0, 0, 0, 0);
-  } else {
-    for (int64_t b = lane * 2; b < row_bytes; b += 64) *reinterpret_cast<unsigned short*>(d + b) = 0;
   }
 }
 
@@ -364,13 +466,21 @@ void vec_rows(const VecParams& p, bool vec, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_pack(const PackParams& p, cudaStream_t s) {
-  const int64_t n = p.rows * (p.ld_dst / 4);
+  const int64_t n = p.rows * (p.ld_dst / 8);
   if (n == 0) return cudaSuccess;
   launch_pdl(k_pack, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, p);
   return cudaGetLastError();
 }
+cudaError_t launch_pack_rows(const PackParams& p, cudaStream_t s) {
+  const int64_t n = (p.rows + 256) * (p.ld_dst / 8);
+  launch_pdl(k_pack_rows, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, p);
+  return cudaGetLastError();
+}
 cudaError_t launch_dact(const DactParams& p, cudaStream_t s) {
-  launch_pdl(k_dact, dim3((unsigned)((p.cols + 127) / 128), (unsigned)p.ranges), dim3(kThreads), 0, s, p);
+  const dim3 grid((unsigned)((p.cols + kDactCols - 1) / kDactCols), (unsigned)p.ranges);
+  if (p.pre_f32) launch_pdl(k_dact<true, true>, grid, dim3(kThreads), 0, s, p);
+  else if (p.dy_f32) launch_pdl(k_dact<true, false>, grid, dim3(kThreads), 0, s, p);
+  else launch_pdl(k_dact<false, false>, grid, dim3(kThreads), 0, s, p);
   return cudaGetLastError();
 }
 cudaError_t launch_colsum(const float* part, int ranges, int64_t cols, void* out, int out_f32, cudaStream_t s) {
@@ -390,20 +500,16 @@ cudaError_t launch_linear_vec(const VecParams& p, cudaStream_t s) {
   return cudaGetLastError();
 }
 cudaError_t launch_loss_rows(const LossRowsParams& p, cudaStream_t s) {
-  launch_pdl(k_loss_rows, dim3(1), dim3(1024), 0, s, p);
+  int64_t per = (p.rows + kRowsCtas - 1) / kRowsCtas;
+  per = (per + 1023) / 1024 * 1024;
+  launch_pdl(k_loss_rows, dim3((unsigned)((p.rows + per - 1) / per)), dim3(1024), 0, s, p, per);
   return cudaGetLastError();
 }
 cudaError_t launch_loss_combine(const float2* part, int parts, int64_t rows_ld, const float* at_target,
                                 const int* count, const int* idx, const float* weight, float* loss, float* lse,
                                 int64_t rows, cudaStream_t s) {
-  launch_pdl(k_loss_combine, dim3((unsigned)((rows + 31) / 32)), dim3(kThreads), 0, s, part, parts, rows_ld, at_target,
+  launch_pdl(k_loss_combine, dim3((unsigned)((rows + 31) / 32)), dim3(1024), 0, s, part, parts, rows_ld, at_target,
              count, idx, weight, loss, lse);
-  return cudaGetLastError();
-}
-cudaError_t launch_zero_rows(const int64_t* target, const float* weight, const float* dloss, int64_t rows,
-                             int64_t vocab, void* dst, int64_t row_bytes, cudaStream_t s) {
-  launch_pdl(k_zero_rows, dim3((unsigned)((rows + 7) / 8)), dim3(kThreads), 0, s, target, weight, dloss, rows, vocab,
-             static_cast<unsigned char*>(dst), row_bytes);
   return cudaGetLastError();
 }
 

@@ -29,6 +29,7 @@ struct GemmParams {
   void* out;
   void* pre;
   const int* row_map;
+  const float* row_scale;  // with row_map: row i is scaled by row_scale[i]
   int64_t ld_res, ld_out, ld_pre;
   int64_t split_stride;  // elements between the partial sums of two splits
   int bias_f32, res_f32, out_f32, pre_f32;
@@ -43,8 +44,6 @@ struct GemmParams {
   float* at_target;      // [rows]
   int64_t rows_ld;       // rows of `part`
   const float* lse;      // [rows] of the rows that count
-  const float* gscale;   // [rows]
-  int64_t plane;         // kEpiDz with three pieces: elements between two of them
   int* flag;             // set by a bounded wait that gave up
 };
 
@@ -64,19 +63,23 @@ struct GemmMaps {
 cudaError_t launch_split_reduce(const GemmParams& p, const float* part, cudaStream_t s);
 
 // rows x cols of src (row stride ld) into `pieces` bf16 planes with row stride
-// ld_dst: the values themselves (bf16), or three pieces whose sum they are
-// (fp32). With `idx`, row i is source row idx[i] for i < *count and zero up to
-// the next multiple of 256 rows.
+// ld_dst (a multiple of 8): the values themselves (bf16), or three pieces whose
+// sum they are (fp32).
 struct PackParams {
   const void* src;
   int64_t ld, rows, cols;
   __nv_bfloat16* dst;
   int64_t ld_dst, plane;
   int src_f32, pieces;
-  const int* idx;
-  const int* count;
+  // launch_pack_rows only: slot of each row or -1, the number of slots, and in
+  // the backward the slots' scales, the scaled copy and the gradient to zero
+  const int *pos, *count;
+  const float* gscale;
+  __nv_bfloat16* scaled;
+  void* zero;
 };
 cudaError_t launch_pack(const PackParams& p, cudaStream_t s);
+cudaError_t launch_pack_rows(const PackParams& p, cudaStream_t s);
 
 // dz = dy * act'(pre) in `pieces` bf16 planes, and partial column sums of the
 // unrounded values per row range.
@@ -110,7 +113,7 @@ struct LossRowsParams {
   const int64_t* target;
   const float *weight, *dloss, *lse_in;
   int64_t rows, vocab;
-  int *count, *idx, *tgt;
+  int *count, *idx, *tgt, *pos;  // pos [rows]: slot, or -1
   float *gscale, *lse_c;
   float *loss, *lse;
 };
@@ -118,10 +121,6 @@ cudaError_t launch_loss_rows(const LossRowsParams& p, cudaStream_t s);
 cudaError_t launch_loss_combine(const float2* part, int parts, int64_t rows_ld, const float* at_target,
                                 const int* count, const int* idx, const float* weight, float* loss, float* lse,
                                 int64_t rows, cudaStream_t s);
-// Zeroes the rows of dst that do not count.
-cudaError_t launch_zero_rows(const int64_t* target, const float* weight, const float* dloss, int64_t rows,
-                             int64_t vocab, void* dst, int64_t row_bytes, cudaStream_t s);
-
 int* ssd_wait_flag_ptr();  // ssd.cu
 
 }  // namespace bds

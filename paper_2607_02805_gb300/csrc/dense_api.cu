@@ -281,10 +281,10 @@ LinFwdWs lin_fwd_ws(const Lin& l) {
   return w;
 }
 
-// Row ranges of the pass over dy: about four CTAs per SM, 32 rows at least.
+// Row ranges of the pass over dy: about six CTAs per SM, 32 rows at least.
 int dact_ranges(int64_t rows, int64_t cols) {
-  const int64_t strips = (cols + 127) / 128;
-  int64_t r = (4 * kSms + strips - 1) / strips;
+  const int64_t strips = (cols + 255) / 256;
+  int64_t r = 6 * kSms / strips;
   if (r > (rows + 31) / 32) r = (rows + 31) / 32;
   return (int)(r < 1 ? 1 : r);
 }
@@ -347,22 +347,29 @@ int check_loss(const bdscan_lm_loss_dims* d, Loss* l, const char* fn) {
 }
 
 // The rows that count, gathered: their h (whole tiles of rows), indices,
-// targets, and in the backward their gradient scales and log sums.
+// targets; in the backward also their gradient scales and log sums and a copy
+// of h with the scales applied. The gradient at the logits is kept without the
+// scale, as p - 1 at the target and p elsewhere: dh is scaled in fp32 by the
+// output step and dw by that copy. (With the scale inside, the entry that
+// dominates a row was rounded with its scale, the same way for the whole row.)
 struct LossRows {
-  size_t count, idx, tgt, gscale, lse, h, end;
+  size_t count, idx, tgt, pos, gscale, lse, h, scaled, end;
   int64_t rows;  // T rounded up to whole tiles
 };
-LossRows loss_rows_ws(const Loss& l, size_t o) {
+LossRows loss_rows_ws(const Loss& l, bool backward) {
+  size_t o = 0;
   LossRows r;
   r.rows = up(l.T, 256);
   const size_t v = al256((size_t)r.rows * 4);
   r.count = o;
   r.idx = o + 256;
   r.tgt = r.idx + v;
-  r.gscale = r.tgt + v;
+  r.pos = r.tgt + v;
+  r.gscale = r.pos + v;
   r.lse = r.gscale + v;
   r.h = r.lse + v;
-  r.end = r.h + packed_bytes(l.dtype, r.rows, l.K);
+  r.scaled = r.h + packed_bytes(l.dtype, r.rows, l.K);
+  r.end = backward ? r.scaled + packed_bytes(l.dtype, r.rows, l.K) : r.scaled;
   return r;
 }
 struct LossFwdWs {
@@ -376,7 +383,7 @@ LossFwdWs loss_fwd_ws(const Loss& l) {
   memset(&w, 0, sizeof(w));
   w.q = plan(l.T, l.V, l.K, l.pieces, false);
   if (w.q.cfg.bn == 64) w.q = plan(1 << 20, l.V, l.K, 3, false), w.q.cfg.pieces = l.pieces;
-  w.r = loss_rows_ws(l, 0);
+  w.r = loss_rows_ws(l, false);
   size_t o = w.r.end;
   w.w = o;
   if (!in_place(l.dtype, l.K)) o += packed_bytes(l.dtype, l.V, l.K);
@@ -401,7 +408,7 @@ struct LossBwdWs {
 LossBwdWs loss_bwd_ws(const Loss& l) {
   LossBwdWs w;
   memset(&w, 0, sizeof(w));
-  w.r = loss_rows_ws(l, 0);
+  w.r = loss_rows_ws(l, true);
   int64_t most = kPieceBytes / (w.r.rows * 2 * l.pieces) / 256 * 256;
   if (most < 256) most = 256;
   w.pieces = (int)((l.V + most - 1) / most);
@@ -424,22 +431,31 @@ LossBwdWs loss_bwd_ws(const Loss& l) {
   return w;
 }
 
-cudaError_t gather_h(const Loss& l, const LossRows& r, const void* h, char* ws, Operand* o, cudaStream_t s) {
+// h of the rows that count as an operand; in the backward (dh given) also the
+// scaled copy, and zeros in dh where a row does not count.
+cudaError_t gather_h(const Loss& l, const LossRows& r, const void* h, char* ws, void* dh, Operand* o, Operand* scaled,
+                     cudaStream_t s) {
   PackParams p;
   memset(&p, 0, sizeof(p));
   p.src = h;
   p.ld = l.ld_h;
-  p.rows = r.rows;
+  p.rows = l.T;
   p.cols = l.K;
   p.dst = (__nv_bfloat16*)(ws + r.h);
   p.ld_dst = up(l.K, 8);
   p.plane = r.rows * p.ld_dst;
   p.src_f32 = l.dtype == BDSCAN_F32;
   p.pieces = l.pieces;
-  p.idx = (const int*)(ws + r.idx);
+  p.pos = (const int*)(ws + r.pos);
   p.count = (const int*)(ws + r.count);
+  if (dh != nullptr) {
+    p.gscale = (const float*)(ws + r.gscale);
+    p.scaled = (__nv_bfloat16*)(ws + r.scaled);
+    p.zero = dh;
+    *scaled = Operand{p.scaled, l.K, r.rows, p.ld_dst, p.pieces, p.plane};
+  }
   *o = Operand{p.dst, l.K, r.rows, p.ld_dst, p.pieces, p.plane};
-  return api_launched(launch_pack(p, s), s);
+  return api_launched(launch_pack_rows(p, s), s);
 }
 
 int check_workspace(const void* ws, size_t have, size_t need, const char* fn) {
@@ -646,11 +662,12 @@ int bdscan_lm_loss_forward(const bdscan_lm_loss_dims* dims, const void* h, const
   rp.count = (int*)(base + ws.r.count);
   rp.idx = (int*)(base + ws.r.idx);
   rp.tgt = (int*)(base + ws.r.tgt);
+  rp.pos = (int*)(base + ws.r.pos);
   rp.loss = loss;
   rp.lse = lse;
   cudaError_t e = api_launched(launch_loss_rows(rp, s), s);
   Operand a, b;
-  if (e == cudaSuccess) e = gather_h(l, ws.r, h, base, &a, s);
+  if (e == cudaSuccess) e = gather_h(l, ws.r, h, base, nullptr, &a, nullptr, s);
   if (e == cudaSuccess) e = operand(&b, l.dtype, w, l.V, l.K, l.K, base + ws.w, s);
   if (e == cudaSuccess) {
     Plan q = ws.q;
@@ -715,13 +732,12 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
   rp.count = (int*)(base + ws.r.count);
   rp.idx = (int*)(base + ws.r.idx);
   rp.tgt = (int*)(base + ws.r.tgt);
+  rp.pos = (int*)(base + ws.r.pos);
   rp.gscale = (float*)(base + ws.r.gscale);
   rp.lse_c = (float*)(base + ws.r.lse);
   cudaError_t e = api_launched(launch_loss_rows(rp, s), s);
-  if (e == cudaSuccess)
-    e = api_launched(launch_zero_rows(target, weight, dloss, l.T, l.V, dh, (int64_t)(l.K * elt), s), s);
-  Operand a, b;
-  if (e == cudaSuccess) e = gather_h(l, ws.r, h, base, &a, s);
+  Operand a, b, scaled;
+  if (e == cudaSuccess) e = gather_h(l, ws.r, h, base, dh, &a, &scaled, s);
   if (e == cudaSuccess) e = operand(&b, l.dtype, w, l.V, l.K, l.K, base + ws.w, s);
   const int64_t ld_dz = up(ws.piece, 8), ld_acc = up(l.K, 4);
   const int f32 = l.dtype == BDSCAN_F32;
@@ -743,13 +759,11 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
     p.v0 = (int)v0;
     p.excluded = (int)l.excluded;
     p.lse = rp.lse_c;
-    p.gscale = rp.gscale;
     p.out = base + ws.dz;
     p.ld_out = ld_dz;
-    p.plane = ws.r.rows * ld_dz;
     p.out_extent = ws.r.rows * ld_dz;
     p.tma_out = 1;
-    e = run_product(q, p, a, bp, l.pieces, p.plane, ws.r.rows, s);
+    e = run_product(q, p, a, bp, l.pieces, ws.r.rows * ld_dz, ws.r.rows, s);
     // this piece's rows of dw
     if (e == cudaSuccess) {
       GemmParams g = geometry(ws.qw, n, l.K, ws.r.rows, flag);
@@ -759,7 +773,7 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
       g.ld_out = l.K;
       g.out_f32 = f32;
       g.out_extent = n * l.K;
-      e = run_out(ws.qw, true, true, g, dz, a, part, s);
+      e = run_out(ws.qw, true, true, g, dz, scaled, part, s);
     }
     // its part of dh: fp32 sums over the pieces, the last one writes dh
     if (e == cudaSuccess) {
@@ -774,6 +788,7 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
       g.ld_out = last ? l.K : ld_acc;
       g.out_f32 = last ? f32 : 1;
       g.row_map = last ? rp.idx : nullptr;
+      g.row_scale = rp.gscale;
       g.out_extent = last ? l.T * l.K : l.T * ld_acc;
       e = run_out(ws.qh, false, true, g, dz, bp, part, s);
     }

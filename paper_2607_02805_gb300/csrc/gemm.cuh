@@ -344,16 +344,61 @@ __device__ __forceinline__ void add32(float (&v)[32], const void* p, int f32, in
   }
 }
 
-// The output step of one element, for rows that TMA cannot write: unaligned
-// strides, mapped rows. (A split's partial sums are an output without bias,
-// activation and residual.)
-__device__ __forceinline__ void out1(const GemmParams& p, int64_t row, int col, float v, float bias, int64_t out_off) {
+// The output step of rows row, row + 2, ... (those below row + left) of one
+// column, for rows that TMA cannot write: unaligned strides, mapped rows. (A
+// split's partial sums are an output without bias, activation and residual.)
+__device__ __forceinline__ void out_rows(const GemmParams& p, int64_t row, int left, int col, float (&x)[16],
+                                         int64_t out_off) {
+  if (p.bias != nullptr) {
+    const float b = load1(p.bias, p.bias_f32, col);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] += b;
+  }
+  if (p.pre != nullptr) {
+    const int64_t at = row * p.ld_pre + col;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (2 * i < left) store1(p.pre, p.pre_f32, at + 2 * i * p.ld_pre, x[i]);
+  }
+  if (p.act == kActSilu) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) sigmoid_mul2<silu_arg>(x[i], x[i + 1]);
+  } else if (p.act == kActGelu) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) sigmoid_mul2<gelu_arg>(x[i], x[i + 1]);
+  }
+  if (p.res != nullptr) {
+    float r[16];
+    const int64_t at = row * p.ld_res + col;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = 2 * i < left ? load1(p.res, p.res_f32, at + 2 * i * p.ld_res) : 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] += r[i];
+  }
+  if (p.row_map != nullptr) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (2 * i < left)
+        store1(p.out, p.out_f32, p.row_map[row + 2 * i] * p.ld_out + col, x[i] * p.row_scale[row + 2 * i]);
+    return;
+  }
+  const int64_t at = out_off + row * p.ld_out + col;
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (2 * i < left) store1(p.out, p.out_f32, at + 2 * i * p.ld_out, x[i]);
+}
+// The same for one element.
+__device__ __forceinline__ void out1(const GemmParams& p, int64_t row, int col, float v, float bias) {
   v += bias;
   if (p.pre != nullptr) store1(p.pre, p.pre_f32, row * p.ld_pre + col, v);
   v = act_fwd(p.act, v);
   if (p.res != nullptr) v += load1(p.res, p.res_f32, row * p.ld_res + col);
-  const int64_t orow = p.row_map != nullptr ? p.row_map[row] : row;
-  store1(p.out, p.out_f32, out_off + orow * p.ld_out + col, v);
+  int64_t orow = row;
+  if (p.row_map != nullptr) {
+    orow = p.row_map[row];
+    v *= p.row_scale[row];
+  }
+  store1(p.out, p.out_f32, orow * p.ld_out + col, v);
 }
 // Joins two partial (maximum, sum of exponentials) of a row, base 2. A part
 // without a maximum (every entry excluded) adds its sum, 0 or NaN.
@@ -563,15 +608,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       const int64_t row = row0 + lane;
       const int nend = min(p.n, (tni + 1) * p.bn);
       // per-row state of the loss epilogues
-      float rm = -INFINITY, rs = 0.f, rlse = 0.f, rg = 0.f;
+      float rm = -INFINITY, rs = 0.f, rlse = 0.f;
       int rt = -1;
       if constexpr (EPI != kEpiOut) {
         if (row < T.m) {
           rt = p.target[row];
-          if constexpr (EPI == kEpiDz) {
-            rlse = p.lse[row];
-            rg = p.gscale[row];
-          }
+          if constexpr (EPI == kEpiDz) rlse = p.lse[row];
         }
       }
       // bias and residual of a chunk are loaded while the chunk before is worked on (bf16, whole chunks)
@@ -652,7 +694,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           for (int i = 0; i < 32; ++i) {
             float d = ex2((v[i] - rlse) * kLog2e);
             d = vcol + i == rt ? d - 1.f : d;
-            v[i] = vcol + i == p.excluded ? 0.f : d * rg;
+            v[i] = vcol + i == p.excluded ? 0.f : d;
           }
           if (row >= T.m) {  // rows up to the next tile edge are read by the product over rows: exact zeros
 #pragma unroll
@@ -709,21 +751,24 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         } else {
           // through shared memory, 16 columns at a time: 16 lanes per row, a row per half warp
           float* f = reinterpret_cast<float*>(stg);
-          const int rows = (int)min((int64_t)32, T.m - row0);
-#pragma unroll
+#pragma unroll 1
           for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               *reinterpret_cast<float4*>(f + lane * 16 + 4 * (j ^ ((lane >> 1) & 3))) =
-                  make_float4(v[16 * h + 4 * j], v[16 * h + 4 * j + 1], v[16 * h + 4 * j + 2], v[16 * h + 4 * j + 3]);
+                  h == 0 ? make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3])
+                         : make_float4(v[16 + 4 * j], v[17 + 4 * j], v[18 + 4 * j], v[19 + 4 * j]);
             __syncwarp();
             const int cl = lane & 15, col = col0 + 16 * h + cl;
             if (col < nend) {
-              const float b = p.bias != nullptr ? load1(p.bias, p.bias_f32, col) : 0.f;
-#pragma unroll 4
-              for (int r = lane >> 4; r < rows; r += 2)
-                out1(p, row0 + r, col, f[r * 16 + 4 * ((cl >> 2) ^ ((r >> 1) & 3)) + (cl & 3)], b,
-                     (int64_t)sp * p.split_stride);
+              float x[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int r = 2 * i + (lane >> 4);
+                x[i] = f[r * 16 + 4 * ((cl >> 2) ^ ((r >> 1) & 3)) + (cl & 3)];
+              }
+              out_rows(p, row0 + (lane >> 4), (int)min((int64_t)32, T.m - row0) - (lane >> 4), col, x,
+                       (int64_t)sp * p.split_stride);
             }
             __syncwarp();
           }

@@ -10,6 +10,8 @@ buffers, valid until its next call; a holder serves one stream at a time.
 
 from __future__ import annotations
 
+import ctypes
+
 import torch
 
 from . import binding
@@ -24,15 +26,35 @@ def _code(dtype):
     return CODES[dtype]
 
 
-def _check(name, t, shape, dtype, device):
-    if t is None:
-        return
-    if tuple(t.shape) != shape:
+def _refuse(name, t, shape, dtype, device):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {shape}")
     if t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, not {dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
+    raise ValueError(f"{name} is not contiguous")
+
+
+def _whole(name, t, shape, dtype, device):
+    """Address of a contiguous tensor (None stays None). torch.Size compares with a tuple, dtypes are singletons."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
+        _refuse(name, t, shape, dtype, device)
+    return t.data_ptr()
+
+
+def _rows(name, t, shape, dtype, device):
+    """Address and row stride of a 2-D tensor with contiguous rows."""
+    if t is None:
+        return None, 0
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        _refuse(name, t, shape, dtype, device)
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
+        raise ValueError(f"the rows of {name} are not contiguous")
+    return t.data_ptr(), ld if shape[0] > 1 else shape[1]
 
 
 class _Holder:
@@ -40,7 +62,7 @@ class _Holder:
         self.device = torch.device(device)
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
-        self._dims = {}  # row strides -> (dims, forward workspace, backward workspace)
+        self._plans = {}  # (kind, row strides) -> (dims, workspace bytes)
         self._buf = {}
 
     def _buffer(self, name, shape, dtype):
@@ -49,13 +71,20 @@ class _Holder:
             t = self._buf[name] = torch.empty(shape, dtype=dtype, device=self.device)
         return t
 
-    def _workspace(self, name, size, dims):
-        """One workspace for all calls of a kind, of the largest size that its dims have asked for."""
-        need = size(dims)
-        t = self._buf.get(name)
-        if need and (t is None or t.numel() < need):
-            t = self._buf[name] = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return t
+    def _plan(self, key, size):
+        """What a kind of call passes for its row strides, asked for once: the dims, and address and size of the
+        workspace. One workspace serves all calls of the holder, which run one after another."""
+        plan = self._plans.get(key)
+        if plan is None:
+            dims = self._make_dims(*key[1:])
+            need = size(dims)
+            ws = self._buf.get("workspace")
+            if need and (ws is None or ws.numel() < need):
+                ws = self._buf["workspace"] = torch.empty(need, dtype=torch.uint8, device=self.device)
+                self._plans = {k: v[:2] + (ws.data_ptr(), ws.numel()) for k, v in self._plans.items()}
+            plan = (dims, ctypes.byref(dims)) + ((None, 0) if ws is None else (ws.data_ptr(), ws.numel()))
+            self._plans[key] = plan
+        return plan
 
 
 class Linear(_Holder):
@@ -69,46 +98,47 @@ class Linear(_Holder):
         self.dtype, self.out_dtype = dtype, dtype if out_dtype is None else out_dtype
         _code(self.dtype), _code(self.out_dtype)
         self.pre = None
+        self._x, self._w, self._y = (self.rows, self.d_in), (self.d_out, self.d_in), (self.rows, self.d_out)
+        self._b = (self.d_out,)
 
-    def _get(self, x, residual, y):
-        key = (binding.row_stride(x), 0 if residual is None else binding.row_stride(residual), binding.row_stride(y))
-        d = self._dims.get(key)
-        if d is None:
-            d = self._dims[key] = binding.make_linear_dims(self.rows, self.d_in, self.d_out, ACTS[self.act],
-                                                           _code(self.dtype), _code(self.out_dtype), *key)
-        return d
+    def _make_dims(self, ld_x, ld_res, ld_y):
+        return binding.make_linear_dims(self.rows, self.d_in, self.d_out, ACTS[self.act], _code(self.dtype),
+                                        _code(self.out_dtype), ld_x, ld_res, ld_y)
 
     def forward(self, x, w, bias=None, residual=None, save_pre=False, out=None, stream=None):
         """y (the holder's buffer, or `out`); with save_pre the pre-activations
         are kept for backward(). Without an activation there is none to keep."""
-        _check("x", x, (self.rows, self.d_in), self.dtype, self.device)
-        _check("w", w, (self.d_out, self.d_in), self.dtype, self.device)
-        _check("bias", bias, (self.d_out,), self.dtype, self.device)
-        _check("residual", residual, (self.rows, self.d_out), self.out_dtype, self.device)
-        _check("out", out, (self.rows, self.d_out), self.out_dtype, self.device)
-        y = self._buffer("y", (self.rows, self.d_out), self.out_dtype) if out is None else out
-        self.pre = None
+        dt, od, dev = self.dtype, self.out_dtype, self.device
+        px, ld_x = _rows("x", x, self._x, dt, dev)
+        pr, ld_r = _rows("residual", residual, self._y, od, dev)
+        y = self._buffer("y", self._y, od) if out is None else out
+        py, ld_y = _rows("out", y, self._y, od, dev)
+        pw = _whole("w", w, self._w, dt, dev)
+        pb = _whole("bias", bias, self._b, dt, dev)
+        self.pre = pp = None
         if save_pre and self.act != "none":
-            self.pre = self._buffer("pre", (self.rows, self.d_out), self.dtype)
-        d = self._get(x, residual, y)
-        ws = self._workspace("ws_f", binding.bdscan_linear_forward_workspace_size, d)
-        binding.linear_forward(d, x, w, bias, residual, self.pre, y, ws, stream)
+            self.pre = self._buffer("pre", self._y, dt)
+            pp = self.pre.data_ptr()
+        _, d, ws, size = self._plan(("forward", ld_x, ld_r, ld_y), binding.bdscan_linear_forward_workspace_size)
+        binding._call("bdscan_linear_forward", d, px, pw, pb, pr, pp, py, ws, size, binding._stream(stream))
         return y
 
     def backward(self, x, w, dy, bias=True, need_dx=True, need_dw=True, stream=None):
         """(dx, dw, dbias) of <dy, y>; dbias None without `bias`. The
         residual's gradient is dy."""
-        _check("x", x, (self.rows, self.d_in), self.dtype, self.device)
-        _check("w", w, (self.d_out, self.d_in), self.dtype, self.device)
-        _check("dy", dy, (self.rows, self.d_out), self.out_dtype, self.device)
+        dt, dev = self.dtype, self.device
+        px, ld_x = _rows("x", x, self._x, dt, dev)
+        py, ld_y = _rows("dy", dy, self._y, self.out_dtype, dev)
+        pw = _whole("w", w, self._w, dt, dev)
         if self.act != "none" and self.pre is None:
             raise ValueError("backward needs a forward with save_pre=True")
-        dx = self._buffer("dx", (self.rows, self.d_in), self.dtype) if need_dx else None
-        dw = self._buffer("dw", (self.d_out, self.d_in), self.dtype) if need_dw else None
-        db = self._buffer("dbias", (self.d_out,), self.dtype) if bias else None
-        d = self._get(x, None, dy)
-        ws = self._workspace("ws_b", binding.bdscan_linear_backward_workspace_size, d)
-        binding.linear_backward(d, x, w, self.pre, dy, dx, dw, db, ws, stream)
+        dx = self._buffer("dx", self._x, dt) if need_dx else None
+        dw = self._buffer("dw", self._w, dt) if need_dw else None
+        db = self._buffer("dbias", self._b, dt) if bias else None
+        p = binding._ptr
+        _, d, ws, size = self._plan(("backward", ld_x, 0, ld_y), binding.bdscan_linear_backward_workspace_size)
+        binding._call("bdscan_linear_backward", d, px, pw, p(self.pre), py, p(dx), p(dw), p(db), ws, size,
+                      binding._stream(stream))
         return dx, dw, db
 
 
@@ -121,43 +151,39 @@ class LmLoss(_Holder):
         self.rows, self.d_model, self.vocab, self.dtype = int(rows), int(d_model), int(vocab), dtype
         self.excluded = int(excluded)
         _code(dtype)
+        self._h, self._w, self._t = (self.rows, self.d_model), (self.vocab, self.d_model), (self.rows,)
 
-    def _get(self, h):
-        key = binding.row_stride(h)
-        d = self._dims.get(key)
-        if d is None:
-            d = self._dims[key] = binding.make_lm_loss_dims(self.rows, self.d_model, self.vocab, _code(self.dtype),
-                                                            self.excluded, key)
-        return d
+    def _make_dims(self, ld_h):
+        return binding.make_lm_loss_dims(self.rows, self.d_model, self.vocab, _code(self.dtype), self.excluded, ld_h)
 
-    def _check_inputs(self, h, w, target, weight):
-        _check("h", h, (self.rows, self.d_model), self.dtype, self.device)
-        _check("w", w, (self.vocab, self.d_model), self.dtype, self.device)
-        _check("target", target, (self.rows,), torch.int64, self.device)
-        _check("weight", weight, (self.rows,), torch.float32, self.device)
+    def _inputs(self, h, w, target, weight):
+        ph, ld_h = _rows("h", h, self._h, self.dtype, self.device)
+        return ld_h, (ph, _whole("w", w, self._w, self.dtype, self.device),
+                      _whole("target", target, self._t, torch.int64, self.device),
+                      _whole("weight", weight, self._t, torch.float32, self.device))
 
     def forward(self, h, w, target, weight=None, stream=None):
         """(loss, lse), fp32 per row; zero at the rows that do not count."""
-        self._check_inputs(h, w, target, weight)
-        loss = self._buffer("loss", (self.rows,), torch.float32)
-        lse = self._buffer("lse", (self.rows,), torch.float32)
-        d = self._get(h)
-        ws = self._workspace("ws_f", binding.bdscan_lm_loss_forward_workspace_size, d)
-        binding.lm_loss_forward(d, h, w, target, weight, loss, lse, ws, stream)
+        ld_h, inputs = self._inputs(h, w, target, weight)
+        loss = self._buffer("loss", self._t, torch.float32)
+        lse = self._buffer("lse", self._t, torch.float32)
+        _, d, ws, size = self._plan(("forward", ld_h), binding.bdscan_lm_loss_forward_workspace_size)
+        binding._call("bdscan_lm_loss_forward", d, *inputs, loss.data_ptr(), lse.data_ptr(), ws, size,
+                      binding._stream(stream))
         return loss, lse
 
     def backward(self, h, w, target, weight=None, dloss=None, lse=None, stream=None):
         """(dh, dw) of <dloss, loss>, from the last forward's lse or the one given."""
-        self._check_inputs(h, w, target, weight)
-        _check("dloss", dloss, (self.rows,), torch.float32, self.device)
-        _check("lse", lse, (self.rows,), torch.float32, self.device)
+        ld_h, inputs = self._inputs(h, w, target, weight)
+        pd = _whole("dloss", dloss, self._t, torch.float32, self.device)
         if lse is None:
             lse = self._buf.get("lse")
             if lse is None:
                 raise ValueError("backward needs a forward or its lse")
-        dh = self._buffer("dh", (self.rows, self.d_model), self.dtype)
-        dw = self._buffer("dw", (self.vocab, self.d_model), self.dtype)
-        d = self._get(h)
-        ws = self._workspace("ws_b", binding.bdscan_lm_loss_backward_workspace_size, d)
-        binding.lm_loss_backward(d, h, w, target, weight, lse, dloss, dh, dw, ws, stream)
+        pl = _whole("lse", lse, self._t, torch.float32, self.device)
+        dh = self._buffer("dh", self._h, self.dtype)
+        dw = self._buffer("dw", self._w, self.dtype)
+        _, d, ws, size = self._plan(("backward", ld_h), binding.bdscan_lm_loss_backward_workspace_size)
+        binding._call("bdscan_lm_loss_backward", d, *inputs, pl, pd, dh.data_ptr(), dw.data_ptr(), ws, size,
+                      binding._stream(stream))
         return dh, dw
