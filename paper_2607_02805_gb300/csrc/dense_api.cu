@@ -60,16 +60,17 @@ struct Operand {
   int64_t plane;
 };
 
-// Boxes of 64 elements x `box_rows` rows, 128-byte swizzle; elements outside
-// the operand read as zero.
-bool encode(CUtensorMap* m, const Operand& o, int box_rows) {
+// Boxes of `box_inner` elements (a swizzled row of 128 or 64 bytes) x
+// `box_rows` rows; elements outside the operand read as zero.
+bool encode(CUtensorMap* m, const Operand& o, int box_inner, int box_rows) {
   const cuuint64_t dims[3] = {(cuuint64_t)o.inner, (cuuint64_t)o.rows, (cuuint64_t)o.pieces};
   const int64_t plane = o.pieces > 1 ? o.plane : up(o.ld * 8, 8);  // one piece: never stepped over
   const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)plane * 2};
-  const cuuint32_t box[3] = {64u, (cuuint32_t)box_rows, 1u};
+  const cuuint32_t box[3] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows, 1u};
   const cuuint32_t estr[3] = {1u, 1u, 1u};
   return tensor_map_encoder()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.base), dims, strides, box,
-                              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              box_inner == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -103,31 +104,57 @@ struct Plan {
   int bn, splits, group_m;
 };
 constexpr int64_t kSms = 152;
-Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split) {
-  Plan q;
-  memset(&q, 0, sizeof(q));
-  q.cfg.pieces = pieces;
-  const int64_t pairs = ((m + 255) / 256) * ((n + 255) / 256);
-  if (pieces == 1 && m > 128 && pairs >= kSms / 4) {
-    q.cfg.cg = 2;
-    q.cfg.bn = 256;
-  } else {
-    q.cfg.cg = 1;
-    q.cfg.bn = pieces == 3 || ((m + 127) / 128) * ((n + 127) / 128) >= kSms / 2 ? 128 : 64;
+// The choice minimises a model of the product's time in clocks. A tile's step
+// of 64 k takes the larger of its MMAs (128 x 256 x 16 in 128 clocks per SM)
+// and its operands' way from L2 (64 bytes per clock and SM); a tile adds about
+// 400 clocks, and the epilogue of the last one 8 per column; the sums of a split
+// add a launch and their way to memory and back. Measured against the first
+// rule (256 x 256 tiles by pairs from a quarter of the pairs on, else 128 x 128
+// or 64, up to 16 splits): @@
+struct Instance {
+  int cg, bn;
+};
+Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split, bool loss) {
+  static const Instance bf16_out[] = {{2, 256}, {1, 128}, {1, 64}}, bf16_loss[] = {{2, 256}, {1, 128}};
+  static const Instance f32_any[] = {{2, 128}, {1, 128}};
+  const Instance* inst = pieces == 3 ? f32_any : loss ? bf16_loss : bf16_out;
+  const int count = pieces == 3 || loss ? 2 : 3;
+  const int64_t products = pieces == 3 ? 6 : 1, nk = (k + 63) / 64;
+  Plan best;
+  memset(&best, 0, sizeof(best));
+  double best_cost = -1;
+  for (int i = 0; i < count; ++i) {
+    const int cg = inst[i].cg;
+    if (cg == 2 && m <= 128) continue;
+    const int64_t units = kSms / cg, mt = (m + 128 * cg - 1) / (128 * cg);
+    for (int bn = inst[i].bn; bn >= 32; bn -= 32) {
+      if (bn - 32 >= n) continue;
+      const int64_t nt = (n + bn - 1) / bn, tiles = mt * nt;
+      const double a_rows = m < 128 ? (double)m : 128.0;
+      const double mma = 2.0 * bn * products, load = 2.0 * pieces * (a_rows + bn / cg);
+      const double step = mma > load ? mma : load;
+      for (int waves = 1; waves <= 4; ++waves) {
+        int64_t s = waves == 1 && !may_split ? 1 : units * waves / tiles;
+        if (s < 1 || !may_split) s = 1;
+        if (s > nk / 2) s = nk / 2 > 0 ? nk / 2 : 1;
+        if (s > 64) s = 64;
+        const int64_t w = (tiles * s + units - 1) / units;
+        double cost = 1500 + w * ((nk + s - 1) / s * step + 400) + 8.0 * bn;
+        if (s > 1) cost += 5000 + 8.0 * s * m * n / 3000;
+        if (best_cost < 0 || cost < best_cost) {
+          best_cost = cost;
+          best.cfg.cg = cg;
+          best.cfg.bn = inst[i].bn;
+          best.bn = bn;
+          best.splits = (int)s;
+        }
+        if (!may_split) break;
+      }
+    }
   }
-  const int64_t nt = (n + q.cfg.bn - 1) / q.cfg.bn;
-  q.bn = (int)up((n + nt - 1) / nt, 32);
-  const int64_t mt = (m + 128 * q.cfg.cg - 1) / (128 * q.cfg.cg);
-  const int64_t tiles = mt * ((n + q.bn - 1) / q.bn), nk = (k + 63) / 64;
-  q.group_m = q.cfg.cg == 2 ? 8 : 12;
-  q.splits = 1;
-  if (may_split && tiles > 0) {
-    int64_t s = (kSms / q.cfg.cg) / tiles;
-    if (s > nk / 4) s = nk / 4;
-    if (s > 16) s = 16;
-    if (s > 1) q.splits = (int)s;
-  }
-  return q;
+  best.cfg.pieces = pieces;
+  best.group_m = best.cfg.cg == 2 ? 8 : 12;
+  return best;
 }
 size_t split_bytes(const Plan& q, int64_t m, int64_t n) {
   return q.splits > 1 ? al256((size_t)q.splits * m * up(n, 4) * 4) : 0;
@@ -154,7 +181,9 @@ cudaError_t run_product(const Plan& q, const GemmParams& p, const Operand& a, co
                         int64_t plane, int64_t out_rows, cudaStream_t s) {
   GemmMaps m;
   memset(&m, 0, sizeof(m));
-  if (!encode(&m.a, a, q.cfg.a_mn ? 64 : 128) || !encode(&m.b, b, q.cfg.b_mn ? 64 : q.cfg.bn / q.cfg.cg))
+  const int bk = gemm_bk(q.cfg.pieces);
+  if (!(q.cfg.a_mn ? encode(&m.a, a, 64, bk) : encode(&m.a, a, bk, 128)) ||
+      !(q.cfg.b_mn ? encode(&m.b, b, 64, bk) : encode(&m.b, b, bk, q.bn / q.cfg.cg)))
     return cudaErrorInvalidValue;
   if (p.tma_out && (!encode_out(&m.out, p.out, p.out_f32, p.n, out_rows, p.ld_out, planes, plane) ||
                     (p.pre != nullptr && !encode_out(&m.pre, p.pre, p.pre_f32, p.n, out_rows, p.ld_pre, 1, 0))))
@@ -270,7 +299,7 @@ LinFwdWs lin_fwd_ws(const Lin& l) {
   LinFwdWs w;
   memset(&w, 0, sizeof(w));
   if (l.T <= kVecRows) return w;
-  w.q = plan(l.T, l.N, l.K, l.pieces, true);
+  w.q = plan(l.T, l.N, l.K, l.pieces, true, false);
   size_t o = 0;
   w.x = o;
   if (!in_place(l.dtype, l.ld_x)) o += packed_bytes(l.dtype, l.T, l.K);
@@ -297,8 +326,8 @@ struct LinBwdWs {
 LinBwdWs lin_bwd_ws(const Lin& l) {
   LinBwdWs w;
   memset(&w, 0, sizeof(w));
-  w.qx = plan(l.T, l.K, l.N, l.pieces, true);
-  w.qw = plan(l.N, l.K, l.T, l.pieces, true);
+  w.qx = plan(l.T, l.K, l.N, l.pieces, true, false);
+  w.qw = plan(l.N, l.K, l.T, l.pieces, true, false);
   w.make_dz = l.act != BDSCAN_ACT_NONE || l.out != BDSCAN_BF16 || !in_place(l.out, l.ld_y);
   size_t o = 0;
   w.x = o;
@@ -381,8 +410,7 @@ struct LossFwdWs {
 LossFwdWs loss_fwd_ws(const Loss& l) {
   LossFwdWs w;
   memset(&w, 0, sizeof(w));
-  w.q = plan(l.T, l.V, l.K, l.pieces, false);
-  if (w.q.cfg.bn == 64) w.q = plan(1 << 20, l.V, l.K, 3, false), w.q.cfg.pieces = l.pieces;
+  w.q = plan(l.T, l.V, l.K, l.pieces, false, true);
   w.r = loss_rows_ws(l, false);
   size_t o = w.r.end;
   w.w = o;
@@ -414,10 +442,9 @@ LossBwdWs loss_bwd_ws(const Loss& l) {
   w.pieces = (int)((l.V + most - 1) / most);
   w.piece = w.pieces == 1 ? l.V : up((l.V + w.pieces - 1) / w.pieces, 256);
   w.pieces = (int)((l.V + w.piece - 1) / w.piece);
-  w.qz = plan(l.T, w.piece, l.K, l.pieces, false);
-  if (w.qz.cfg.bn == 64) w.qz = plan(1 << 20, w.piece, l.K, 3, false), w.qz.cfg.pieces = l.pieces;
-  w.qh = plan(l.T, l.K, w.piece, l.pieces, true);
-  w.qw = plan(w.piece, l.K, l.T, l.pieces, true);
+  w.qz = plan(l.T, w.piece, l.K, l.pieces, false, true);
+  w.qh = plan(l.T, l.K, w.piece, l.pieces, true, false);
+  w.qw = plan(w.piece, l.K, l.T, l.pieces, true, false);
   size_t o = w.r.end;
   w.w = o;
   if (!in_place(l.dtype, l.K)) o += packed_bytes(l.dtype, l.V, l.K);

@@ -12,15 +12,15 @@
 // 1 the MMAs, 2 owns the TMEM allocation, 4 to 19 run the epilogue of one
 // accumulator while the MMAs fill the other (four warps per scheduler: the
 // epilogue is chains of latencies, and with two the GELU of a 16384 x 832 x
-// 3328 product took longer than its MMAs). A stage holds 64 elements of k of
-// both operands in the 128-byte swizzled layout of umma.cuh, rows along m or n
-// (K-major) or along k (MN-major), as the operand lies in memory: no operand
+// 3328 product took longer than its MMAs). A stage holds 64 elements of k
+// (fp32: 32) of both operands in the swizzled layouts of umma.cuh, rows along m
+// or n (K-major) or along k (MN-major), as the operand lies in memory: no operand
 // is transposed by a pass of its own.
 //
 // fp32 operands come as three bf16 pieces each (value = p0 + p1 + p2 to 24
 // bits); the six products with the largest terms are accumulated, smallest
-// first, and after every 64 elements of k the epilogue warps add the
-// accumulator to fp32 registers: the tensor core's own accumulation truncates,
+// first, and after every 64 elements of k (two stages of 32: with stages of 64
+// only two fit) the epilogue warps add the accumulator to fp32 registers: the tensor core's own accumulation truncates,
 // and over a long k that error would grow with k.
 //
 // Every wait has a poll limit. A role that gives up sets the wait flag and
@@ -41,12 +41,14 @@ namespace {
 
 constexpr int kEpiWarps = 16;
 constexpr int kGemmThreads = 128 + 32 * kEpiWarps;
-constexpr int kBk = 64;  // elements of k per stage: one 128-byte swizzled row
 
 template <int CG, int BN, int NP>
 struct GemmSmem {
-  static constexpr uint32_t kA = 128u * 128u;                // one piece of A
-  static constexpr uint32_t kB = (uint32_t)(BN / CG) * 128u;  // one piece of B
+  static constexpr int kBk = gemm_bk(NP);                              // elements of k per stage
+  static constexpr uint32_t kRow = kBk * 2u;                           // bytes of a K-major row
+  static constexpr uint32_t kA = 128u * kRow;                          // one piece of A
+  static constexpr uint32_t kB = (uint32_t)(BN / CG) * kRow;           // one piece of B
+  static constexpr uint32_t kCol = kBk * 128u;                         // 64 columns of an MN-major operand
   static constexpr uint32_t kStage = NP * (kA + kB);
   static constexpr uint32_t kEpi = kEpiWarps * 2048u;
   static constexpr int kStages = (int)((232448u - 1024u - 512u - kEpi) / kStage) > 8
@@ -416,14 +418,14 @@ __device__ __forceinline__ void stats_join(float& m, float& s, float2 q) {
 template <int CG>
 struct Tiles {
   int m, k, mt, nt, nk, total;
-  __device__ __forceinline__ explicit Tiles(const GemmParams& p) {
+  __device__ __forceinline__ Tiles(const GemmParams& p, int bk) {
     m = p.m;
     k = p.k;
     if (p.rows_axis == 1) m = min(m, *p.rows_dev);
     if (p.rows_axis == 2) k = min(k, *p.rows_dev);
     mt = (m + 128 * CG - 1) / (128 * CG);
     nt = (p.n + p.bn - 1) / p.bn;
-    nk = (k + kBk - 1) / kBk;
+    nk = (k + bk - 1) / bk;
     total = mt * nt * p.splits;
   }
   // Tile t: groups of group_m row tiles, all column tiles of a group before the next.
@@ -443,7 +445,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     k_gemm(const GemmParams p, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
            const __grid_constant__ CUtensorMap omap, const __grid_constant__ CUtensorMap pmap) {
   using S = GemmSmem<CG, BN, NP>;
-  constexpr int ST = S::kStages;
+  constexpr int ST = S::kStages, BK = S::kBk;
   constexpr bool FLUSH = NP == 3;
   constexpr uint32_t kCols = 2u * BN < 32u ? 32u : 2u * BN;
   extern __shared__ unsigned char smem_raw[];
@@ -472,7 +474,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   umma::fence_after_sync();
   const uint32_t tm = tslot;
   pdl_sync();
-  const Tiles<CG> T(p);
+  const Tiles<CG> T(p, BK);
   if (w == 0) {
     // ---------------- producer ----------------
     // Producer and issuer run their loops as whole warps, one elected lane
@@ -481,6 +483,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     // of k instead of 512, 4864 x 16384 x 1024.)
     const bool leader = elect_one();
     const uint32_t base = umma::smem_u32(sm);
+    // columns of B that a CTA loads: its share of the tile, MN-major in whole groups of 64
+    const int bcols = B_MN ? (p.bn / CG + 63) / 64 : p.bn / CG;
+    const uint32_t stage_tx = CG * NP * (S::kA + (uint32_t)bcols * (B_MN ? S::kCol : S::kRow));
     const uint32_t full0 = CG == 2 ? map_cta(umma::smem_u32(&full[0]), 0) : umma::smem_u32(&full[0]);
     bool ok = true;
     int it = 0, s = 0;
@@ -493,7 +498,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       for (int kb = k0; kb < k1; ++kb, ++it) {
         if (!(ok = warp_wait(&empty[s], ph ^ 1))) break;
         if (leader) {
-          if (rank == 0) bar_expect_tx(&full[s], S::kStage * CG);
+          if (rank == 0) bar_expect_tx(&full[s], stage_tx);
           const uint32_t bar = full0 + 8u * (uint32_t)s;
           const uint32_t a = base + (uint32_t)s * S::kStage, b = a + NP * S::kA;
 #pragma unroll
@@ -501,16 +506,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             if constexpr (A_MN) {
 #pragma unroll
               for (int j = 0; j < 2; ++j)
-                gtma_load<CG>(a + q * S::kA + j * 8192u, &amap, m0 + 64 * j, kb * kBk, q, bar);
+                gtma_load<CG>(a + q * S::kA + j * S::kCol, &amap, m0 + 64 * j, kb * BK, q, bar);
             } else {
-              gtma_load<CG>(a + q * S::kA, &amap, kb * kBk, m0, q, bar);
+              gtma_load<CG>(a + q * S::kA, &amap, kb * BK, m0, q, bar);
             }
             if constexpr (B_MN) {
 #pragma unroll
-              for (int j = 0; j < BN / CG / 64; ++j)
-                gtma_load<CG>(b + q * S::kB + j * 8192u, &bmap, n0 + 64 * j, kb * kBk, q, bar);
+              for (int j = 0; j < (BN / CG + 63) / 64; ++j)
+                if (j < bcols) gtma_load<CG>(b + q * S::kB + j * S::kCol, &bmap, n0 + 64 * j, kb * BK, q, bar);
             } else {
-              gtma_load<CG>(b + q * S::kB, &bmap, kb * kBk, n0, q, bar);
+              gtma_load<CG>(b + q * S::kB, &bmap, kb * BK, n0, q, bar);
             }
           }
         }
@@ -530,8 +535,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       const uint32_t idesc = umma::idesc_bf16(128 * CG, (uint32_t)p.bn, A_MN, B_MN);
       constexpr uint32_t astep = A_MN ? 2048u : 32u, bstep = B_MN ? 2048u : 32u;  // bytes per 16 elements of k
       const uint32_t base = umma::smem_u32(sm);
-      const uint64_t da0 = umma::sdesc(base, A_MN ? 8192u : 16u, 1024u),
-                     db0 = umma::sdesc(base + NP * S::kA, B_MN ? 8192u : 16u, 1024u);
+      auto desc = [](uint32_t at, bool mn) {
+        if (mn) return umma::sdesc(at, S::kCol, 1024u);
+        return BK == 64 ? umma::sdesc(at, 16u, 1024u) : umma::sdesc64(at, 16u, 512u);
+      };
+      const uint64_t da0 = desc(base, A_MN), db0 = desc(base + NP * S::kA, B_MN);
       bool ok = true;
       int job = 0, s = 0;
       uint32_t ph = 0;
@@ -539,7 +547,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         int tmi, tni, k0, k1, sp;
         T.at(p, tile, tmi, tni, k0, k1, sp);
         for (int kb = k0; kb < k1; ++kb) {
-          const bool first = FLUSH || kb == k0, last = FLUSH || kb + 1 == k1;
+          const bool first = kb == k0 || (FLUSH && ((kb - k0) & 1) == 0);
+          const bool last = kb + 1 == k1 || (FLUSH && ((kb - k0) & 1) == 1);
           if (first) {
             if (!(ok = warp_wait(&accempty[job & 1], ((job >> 1) & 1) ^ 1))) break;
             umma::fence_after_sync();
@@ -550,16 +559,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           if (leader) {
             if constexpr (NP == 1) {
 #pragma unroll
-              for (int q = 0; q < kBk / 16; ++q)
+              for (int q = 0; q < BK / 16; ++q)
                 gmma<CG>(d, umma::sdesc_adv(da, q * astep), umma::sdesc_adv(db, q * bstep), idesc, !first || q > 0);
             } else {
               constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};  // smallest terms first
 #pragma unroll
               for (int c = 0; c < 6; ++c)
 #pragma unroll
-                for (int q = 0; q < kBk / 16; ++q)
+                for (int q = 0; q < BK / 16; ++q)
                   gmma<CG>(d, umma::sdesc_adv(da, pa[c] * S::kA + q * astep),
-                           umma::sdesc_adv(db, pb[c] * S::kB + q * bstep), idesc, c > 0 || q > 0);
+                           umma::sdesc_adv(db, pb[c] * S::kB + q * bstep), idesc, !first || c > 0 || q > 0);
             }
             gcommit<CG>(&empty[s]);
             if (last) gcommit<CG>(&accfull[job & 1]);
@@ -583,7 +592,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     for (int tile = unit; tile < T.total; tile += units) {
       int tmi, tni, k0, k1, sp;
       T.at(p, tile, tmi, tni, k0, k1, sp);
-      const int jobs = FLUSH ? k1 - k0 : (k1 > k0 ? 1 : 0);
+      const int jobs = FLUSH ? (k1 - k0 + 1) / 2 : (k1 > k0 ? 1 : 0);
       float acc[FLUSH ? NC * 32 : 1];
       if constexpr (FLUSH) {
 #pragma unroll
