@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kThreads) k_split_reduce(const GemmParams p, c
       if (i + j < p.splits) s.x += q[j].x, s.y += q[j].y, s.z += q[j].z, s.w += q[j].w;
   }
   float e[4] = {s.x, s.y, s.z, s.w};
-  if (p.tma_out && p.vec && c + 3 < p.n && p.row_map == nullptr) {  // rows on 16-byte boundaries
+  if (p.vec && c + 3 < p.n) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (p.bias != nullptr) e[j] += load1(p.bias, p.bias_f32, c + j);

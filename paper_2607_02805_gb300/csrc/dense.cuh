@@ -10,7 +10,8 @@
 namespace bds {
 
 // What a product does with its accumulators.
-constexpr int kEpiOut = 0;    // residual + act(acc + bias), or a split's partial sums
+constexpr int kEpiOut = 0;    // residual + act(acc + bias), or a split's partial sums, by TMA
+constexpr int kEpiRows = 3;   // the same by plain stores: unaligned or mapped rows
 constexpr int kEpiStats = 1;  // running maximum and sum of a row's logits, and the target's logit
 constexpr int kEpiDz = 2;     // the loss's gradient at the logits
 
@@ -23,7 +24,7 @@ struct GemmParams {
   int bn;         // columns of a tile (a multiple of 32, at most the instance's BN)
   int splits;     // ranges of k, each with its own partial sums
   int group_m;    // row tiles walked together
-  // kEpiOut: out[row_map ? row_map[i] : i][j]
+  // kEpiOut, kEpiRows: out[row_map ? row_map[i] : i][j]; kEpiOut has res of out's type
   const void* bias;
   const void* res;
   void* out;
@@ -34,8 +35,7 @@ struct GemmParams {
   int64_t split_stride;  // elements between the partial sums of two splits
   int bias_f32, res_f32, out_f32, pre_f32;
   int act;
-  int tma_out;           // out and pre are written by TMA
-  int vec;               // rows of res start on 16-byte boundaries
+  int vec;               // rows of out, pre and res start on 16-byte boundaries, none is mapped
   int64_t out_extent;    // elements of `out` (debug build)
   // kEpiStats / kEpiDz: rows i are the rows that count; column j is entry v0 + j
   int v0, excluded;
@@ -56,9 +56,10 @@ struct GemmCfg {
   int cg, bn, pieces;
   bool a_mn, b_mn;  // operand rows along k (true) or along m / n (false)
   int epi;
+  bool out_f32;     // kEpiOut, kEpiRows
 };
 
-// Tensor maps of a product; `out` and `pre` only with tma_out and for kEpiDz.
+// Tensor maps of a product; `out` and `pre` for kEpiOut, `out` for kEpiDz.
 struct GemmMaps {
   CUtensorMap a, b, out, pre;
 };

@@ -17,6 +17,9 @@ PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder();  // ssd.cu
 cudaError_t launch_gemm_nt(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
 cudaError_t launch_gemm_nn(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
 cudaError_t launch_gemm_tn(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
+cudaError_t launch_gemm_nt3(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
+cudaError_t launch_gemm_nn3(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
+cudaError_t launch_gemm_tn3(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
 cudaError_t launch_gemm_loss(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
 
 namespace {
@@ -114,11 +117,10 @@ constexpr int64_t kSms = 152;
 struct Instance {
   int cg, bn;
 };
-Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split, bool loss) {
-  static const Instance bf16_out[] = {{2, 256}, {1, 128}, {1, 64}}, bf16_loss[] = {{2, 256}, {1, 128}};
-  static const Instance f32_any[] = {{2, 128}, {1, 128}};
-  const Instance* inst = pieces == 3 ? f32_any : loss ? bf16_loss : bf16_out;
-  const int count = pieces == 3 || loss ? 2 : 3;
+Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split) {
+  static const Instance bf16_any[] = {{2, 256}, {1, 128}}, f32_any[] = {{2, 128}, {1, 128}};
+  const Instance* inst = pieces == 3 ? f32_any : bf16_any;
+  const int count = 2;
   const int64_t products = pieces == 3 ? 6 : 1, nk = (k + 63) / 64;
   Plan best;
   memset(&best, 0, sizeof(best));
@@ -185,14 +187,17 @@ cudaError_t run_product(const Plan& q, const GemmParams& p, const Operand& a, co
   if (!(q.cfg.a_mn ? encode(&m.a, a, 64, bk) : encode(&m.a, a, bk, 128)) ||
       !(q.cfg.b_mn ? encode(&m.b, b, 64, bk) : encode(&m.b, b, bk, q.bn / q.cfg.cg)))
     return cudaErrorInvalidValue;
-  if (p.tma_out && (!encode_out(&m.out, p.out, p.out_f32, p.n, out_rows, p.ld_out, planes, plane) ||
-                    (p.pre != nullptr && !encode_out(&m.pre, p.pre, p.pre_f32, p.n, out_rows, p.ld_pre, 1, 0))))
+  const int epi = q.cfg.epi;
+  if ((epi == kEpiOut || epi == kEpiDz) && !encode_out(&m.out, p.out, p.out_f32, p.n, out_rows, p.ld_out, planes, plane))
     return cudaErrorInvalidValue;
+  if (epi == kEpiOut && p.pre != nullptr && !encode_out(&m.pre, p.pre, p.pre_f32, p.n, out_rows, p.ld_pre, 1, 0))
+    return cudaErrorInvalidValue;
+  const bool f32 = q.cfg.pieces == 3;
   cudaError_t e;
-  if (q.cfg.epi != kEpiOut) e = launch_gemm_loss(q.cfg, p, m, s);
-  else if (q.cfg.a_mn) e = launch_gemm_tn(q.cfg, p, m, s);
-  else if (q.cfg.b_mn) e = launch_gemm_nn(q.cfg, p, m, s);
-  else e = launch_gemm_nt(q.cfg, p, m, s);
+  if (epi == kEpiStats || epi == kEpiDz) e = launch_gemm_loss(q.cfg, p, m, s);
+  else if (q.cfg.a_mn) e = f32 ? launch_gemm_tn3(q.cfg, p, m, s) : launch_gemm_tn(q.cfg, p, m, s);
+  else if (q.cfg.b_mn) e = f32 ? launch_gemm_nn3(q.cfg, p, m, s) : launch_gemm_nn(q.cfg, p, m, s);
+  else e = f32 ? launch_gemm_nt3(q.cfg, p, m, s) : launch_gemm_nt(q.cfg, p, m, s);
   return api_launched(e, s);
 }
 
@@ -202,9 +207,10 @@ cudaError_t run_out(Plan q, bool a_mn, bool b_mn, GemmParams p, const Operand& a
                     cudaStream_t s) {
   q.cfg.a_mn = a_mn;
   q.cfg.b_mn = b_mn;
-  q.cfg.epi = kEpiOut;
-  p.tma_out = p.row_map == nullptr && rows16(p.ld_out, p.out_f32) && (p.pre == nullptr || rows16(p.ld_pre, p.pre_f32));
-  p.vec = p.res == nullptr || rows16(p.ld_res, p.res_f32);
+  p.vec = p.row_map == nullptr && rows16(p.ld_out, p.out_f32) && (p.pre == nullptr || rows16(p.ld_pre, p.pre_f32)) &&
+          (p.res == nullptr || (p.res_f32 == p.out_f32 && rows16(p.ld_res, p.res_f32)));
+  q.cfg.epi = p.vec ? kEpiOut : kEpiRows;
+  q.cfg.out_f32 = p.out_f32 != 0;
   if (q.splits == 1) return run_product(q, p, a, b, 1, 0, p.m, s);
   GemmParams g = p;
   g.splits = q.splits;
@@ -214,7 +220,9 @@ cudaError_t run_out(Plan q, bool a_mn, bool b_mn, GemmParams p, const Operand& a
   g.out = part;
   g.ld_out = up(p.n, 4);
   g.split_stride = p.m * g.ld_out;
-  g.out_f32 = g.tma_out = g.vec = 1;
+  g.out_f32 = 1;
+  q.cfg.epi = kEpiOut;
+  q.cfg.out_f32 = true;
   g.act = BDSCAN_ACT_NONE;
   g.out_extent = (int64_t)q.splits * g.split_stride;
   cudaError_t e = run_product(q, g, a, b, q.splits, g.split_stride, p.m, s);
@@ -299,7 +307,7 @@ LinFwdWs lin_fwd_ws(const Lin& l) {
   LinFwdWs w;
   memset(&w, 0, sizeof(w));
   if (l.T <= kVecRows) return w;
-  w.q = plan(l.T, l.N, l.K, l.pieces, true, false);
+  w.q = plan(l.T, l.N, l.K, l.pieces, true);
   size_t o = 0;
   w.x = o;
   if (!in_place(l.dtype, l.ld_x)) o += packed_bytes(l.dtype, l.T, l.K);
@@ -326,8 +334,8 @@ struct LinBwdWs {
 LinBwdWs lin_bwd_ws(const Lin& l) {
   LinBwdWs w;
   memset(&w, 0, sizeof(w));
-  w.qx = plan(l.T, l.K, l.N, l.pieces, true, false);
-  w.qw = plan(l.N, l.K, l.T, l.pieces, true, false);
+  w.qx = plan(l.T, l.K, l.N, l.pieces, true);
+  w.qw = plan(l.N, l.K, l.T, l.pieces, true);
   w.make_dz = l.act != BDSCAN_ACT_NONE || l.out != BDSCAN_BF16 || !in_place(l.out, l.ld_y);
   size_t o = 0;
   w.x = o;
@@ -410,7 +418,7 @@ struct LossFwdWs {
 LossFwdWs loss_fwd_ws(const Loss& l) {
   LossFwdWs w;
   memset(&w, 0, sizeof(w));
-  w.q = plan(l.T, l.V, l.K, l.pieces, false, true);
+  w.q = plan(l.T, l.V, l.K, l.pieces, false);
   w.r = loss_rows_ws(l, false);
   size_t o = w.r.end;
   w.w = o;
@@ -442,9 +450,9 @@ LossBwdWs loss_bwd_ws(const Loss& l) {
   w.pieces = (int)((l.V + most - 1) / most);
   w.piece = w.pieces == 1 ? l.V : up((l.V + w.pieces - 1) / w.pieces, 256);
   w.pieces = (int)((l.V + w.piece - 1) / w.piece);
-  w.qz = plan(l.T, w.piece, l.K, l.pieces, false, true);
-  w.qh = plan(l.T, l.K, w.piece, l.pieces, true, false);
-  w.qw = plan(w.piece, l.K, l.T, l.pieces, true, false);
+  w.qz = plan(l.T, w.piece, l.K, l.pieces, false);
+  w.qh = plan(l.T, l.K, w.piece, l.pieces, true);
+  w.qw = plan(w.piece, l.K, l.T, l.pieces, true);
   size_t o = w.r.end;
   w.w = o;
   if (!in_place(l.dtype, l.K)) o += packed_bytes(l.dtype, l.V, l.K);
@@ -789,7 +797,6 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
     p.out = base + ws.dz;
     p.ld_out = ld_dz;
     p.out_extent = ws.r.rows * ld_dz;
-    p.tma_out = 1;
     e = run_product(q, p, a, bp, l.pieces, ws.r.rows * ld_dz, ws.r.rows, s);
     // this piece's rows of dw
     if (e == cudaSuccess) {

@@ -109,6 +109,9 @@ __device__ __forceinline__ void gtma_load(uint32_t dst, const CUtensorMap* map, 
         "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
         : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
 template <int CG>
 __device__ __forceinline__ void gmma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
   if constexpr (CG == 1)
@@ -239,6 +242,15 @@ __device__ __forceinline__ float4 load4(const void* p, int f32, int64_t at) {
   const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
   return make_float4(a.x, a.y, b.x, b.y);
 }
+// e += the eight bf16 of u.
+__device__ __forceinline__ void add8(float (&e)[8], const uint4& u) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    e[2 * i] += __uint_as_float(w[i] << 16);
+    e[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
 __device__ __forceinline__ float load1(const void* p, int f32, int64_t at) {
   return f32 ? static_cast<const float*>(p)[at] : __bfloat162float(static_cast<const bf16*>(p)[at]);
 }
@@ -255,11 +267,13 @@ __device__ __forceinline__ void store1(void* p, int f32, int64_t at, float v) {
 
 // ---- output ----
 // A warp's chunk is 32 rows x 32 columns, a thread holding one row (as TMEM
-// gives it). It leaves by TMA where rows start on 16-byte boundaries: the warp
-// writes the chunk to shared memory in the swizzle of the map's box and one lane
-// issues the store, which also cuts off what lies outside the matrix. A
-// transposition through shared memory with plain stores, as unaligned rows need
-// it, took three times the instructions.
+// gives it). Where rows start on 16-byte boundaries it leaves by TMA (kEpiOut,
+// kEpiDz), in units of 32 rows x 64 bytes (32 bf16 or 16 fp32 columns): the warp
+// writes a unit to its 2 KB of shared memory in the swizzle of the map's box and
+// one lane issues the store, which also cuts off what lies outside the matrix.
+// A residual comes through the same 2 KB: it is loaded with whole 64-byte rows
+// (four lanes each) a unit ahead. Other rows (kEpiRows: unaligned strides,
+// mapped rows) go through shared memory to plain stores with 16 lanes per row.
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int c0, int c1, int c2, uint32_t src) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];\n" ::"l"(
                    reinterpret_cast<uint64_t>(map)),
@@ -267,100 +281,123 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int c0, int
                : "memory");
   asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
 }
-// At most N of this thread's stores still read shared memory.
-template <int N>
-__device__ __forceinline__ void tma_store_wait_read() {
-  asm volatile("cp.async.bulk.wait_group.read %0;\n" ::"n"(N) : "memory");
-}
+// This thread's stores have read shared memory; are complete.
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory"); }
 __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory"); }
 
-// One chunk to (col, row, z) of `map` through the warp's 2 KB: at once (bf16) or
-// as two halves of 16 columns (fp32), 64-byte rows and swizzle either way.
-__device__ __forceinline__ void chunk_store(const CUtensorMap* map, int f32, int col, int row, int z, int ncols,
-                                            const float (&v)[32], unsigned char* stg) {
+// Columns H * 16 .. + 15 (fp32) or all 32 (bf16) of the chunk v to (col, row, z)
+// of `map`, plus the residual unit `raw` where `res`. `next` runs once raw has
+// been put away: it loads what the next unit needs.
+template <bool F32, int H, typename NEXT>
+__device__ __forceinline__ void unit_store(const CUtensorMap* map, int col, int row, int z, const float (&v)[32],
+                                           bool res, const uint4 (&raw)[4], unsigned char* stg, NEXT next) {
   const int lane = threadIdx.x & 31;
+  if (lane == 0) tma_store_wait_read();
+  __syncwarp();
+  if (res) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = 8 * j + (lane >> 2);
+      *reinterpret_cast<uint4*>(stg + r * 64 + 16 * ((lane & 3) ^ ((r >> 1) & 3))) = raw[j];
+    }
+    __syncwarp();
+  }
+  next();
   unsigned char* mine = stg + lane * 64;
   const int sw = (lane >> 1) & 3;
-  if (lane == 0) tma_store_wait_read<0>();
-  __syncwarp();
-  if (!f32) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<uint4*>(mine + 16 * (j ^ sw)) =
-          make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]),
-                     pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
-    umma::fence_async_smem();
-    __syncwarp();
-    if (lane == 0) tma_store_3d(map, col, row, z, umma::smem_u32(stg));
-    return;
-  }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (h == 1) {
-      if (col + 16 >= ncols) return;
-      if (lane == 0) tma_store_wait_read<0>();
-      __syncwarp();
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<float4*>(mine + 16 * (j ^ sw)) =
-          make_float4(v[16 * h + 4 * j], v[16 * h + 4 * j + 1], v[16 * h + 4 * j + 2], v[16 * h + 4 * j + 3]);
-    umma::fence_async_smem();
-    __syncwarp();
-    if (lane == 0) tma_store_3d(map, col + 16 * h, row, z, umma::smem_u32(stg));
-  }
-}
-
-// 32 consecutive bf16 values at p[at], which lies on a 16-byte boundary, in two
-// steps: the loads, and the sums once they are there.
-__device__ __forceinline__ void load32(uint4 (&r)[4], const void* p, int64_t at) {
-  const uint4* q = reinterpret_cast<const uint4*>(static_cast<const bf16*>(p) + at);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) r[j] = q[j];
-}
-__device__ __forceinline__ void add32(float (&v)[32], const uint4 (&r)[4]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const uint32_t e[4] = {r[j].x, r[j].y, r[j].z, r[j].w};
+    uint4* slot = reinterpret_cast<uint4*>(mine + 16 * (j ^ sw));
+    if constexpr (F32) {
+      float4 e = make_float4(v[16 * H + 4 * j], v[16 * H + 4 * j + 1], v[16 * H + 4 * j + 2], v[16 * H + 4 * j + 3]);
+      if (res) {
+        const uint4 u = *slot;
+        e.x += __uint_as_float(u.x), e.y += __uint_as_float(u.y), e.z += __uint_as_float(u.z), e.w += __uint_as_float(u.w);
+      }
+      *reinterpret_cast<float4*>(slot) = e;
+    } else {
+      float e[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[8 * j + 2 * i] += __uint_as_float(e[i] << 16);
-      v[8 * j + 2 * i + 1] += __uint_as_float(e[i] & 0xffff0000u);
+      for (int i = 0; i < 8; ++i) e[i] = v[8 * j + i];
+      if (res) add8(e, *slot);
+      *slot = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+    }
+  }
+  umma::fence_async_smem();
+  __syncwarp();
+  if (lane == 0) tma_store_3d(map, col, row, z, umma::smem_u32(stg));
+}
+// The residual of a unit at (row0, col): lane l holds 16 bytes of rows l / 4 + 8 j.
+// A piece may reach past column n (never read, and inside the row's stride) but
+// not past the last row's end.
+template <bool F32>
+__device__ __forceinline__ void load_res(uint4 (&raw)[4], const GemmParams& p, int64_t row0, int col) {
+  constexpr int PE = F32 ? 4 : 8;
+  const int lane = threadIdx.x & 31, c = col + PE * (lane & 3);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t r = row0 + 8 * j + (lane >> 2);
+    raw[j] = make_uint4(0, 0, 0, 0);
+    if (r >= p.m || c >= p.n) continue;
+    const int64_t at = r * p.ld_res + c;
+    if (c + PE <= p.n || r + 1 < p.m) {
+      raw[j] = *reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(p.res) + at * (F32 ? 4 : 2));
+    } else if constexpr (F32) {
+      const uint32_t* q = static_cast<const uint32_t*>(p.res) + at;
+      raw[j] = make_uint4(q[0], c + 1 < p.n ? q[1] : 0u, c + 2 < p.n ? q[2] : 0u, 0u);
+    } else {
+      const unsigned short* q = static_cast<const unsigned short*>(p.res) + at;
+      auto two = [&](int i) {
+        return (c + i < p.n ? (uint32_t)q[i] : 0u) | (c + i + 1 < p.n ? (uint32_t)q[i + 1] << 16 : 0u);
+      };
+      raw[j] = make_uint4(two(0), two(2), two(4), two(6));
     }
   }
 }
-
-// Both steps, for either type.
-__device__ __forceinline__ void add32(float (&v)[32], const void* p, int f32, int64_t at) {
-  if (f32) {
-    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+// bf16 bias of 32 columns, the same for every lane, in two steps.
+__device__ __forceinline__ void load_bias(uint4 (&r)[4], const GemmParams& p, int col) {
+  const uint4* q = reinterpret_cast<const uint4*>(static_cast<const bf16*>(p.bias) + col);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float4 u = q[j];
-      v[4 * j] += u.x, v[4 * j + 1] += u.y, v[4 * j + 2] += u.z, v[4 * j + 3] += u.w;
-    }
-  } else {
-    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const bf16*>(p) + at);
-    const uint4 r[4] = {q[0], q[1], q[2], q[3]};
-    add32(v, r);
+  for (int j = 0; j < 4; ++j)  // whole pieces; the last one of an odd width is added from memory
+    r[j] = col + 8 * j + 8 <= p.n ? q[j] : make_uint4(0, 0, 0, 0);
+}
+__device__ __forceinline__ void add_bias(float (&v)[32], const uint4 (&r)[4], const GemmParams& p, int col) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = v[8 * j + i];
+    add8(e, r[j]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[8 * j + i] = e[i];
+  }
+  if (col + 32 > p.n && (p.n & 7) != 0) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (col + i >= (p.n & ~7) && col + i < p.n) v[i] += load1(p.bias, 0, col + i);
   }
 }
 
 // The output step of rows row, row + 2, ... (those below row + left) of one
-// column, for rows that TMA cannot write: unaligned strides, mapped rows. (A
-// split's partial sums are an output without bias, activation and residual.)
-__device__ __forceinline__ void out_rows(const GemmParams& p, int64_t row, int left, int col, float (&x)[16],
-                                         int64_t out_off) {
+// column, by plain stores. IN32: bias and pre are fp32; OF32: the output is.
+template <bool IN32, bool OF32>
+__device__ __forceinline__ void out_rows(const GemmParams& p, int64_t row, int left, int col, float (&x)[16]) {
   if (p.bias != nullptr) {
-    const float b = load1(p.bias, p.bias_f32, col);
+    const float b = load1(p.bias, IN32, col);
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] += b;
+  }
+  float r[16];
+  if (p.res != nullptr) {
+    const int64_t at = row * p.ld_res + col;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = 2 * i < left ? load1(p.res, p.res_f32, at + 2 * i * p.ld_res) : 0.f;
   }
   if (p.pre != nullptr) {
     const int64_t at = row * p.ld_pre + col;
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      if (2 * i < left) store1(p.pre, p.pre_f32, at + 2 * i * p.ld_pre, x[i]);
+      if (2 * i < left) store1(p.pre, IN32, at + 2 * i * p.ld_pre, x[i]);
   }
   if (p.act == kActSilu) {
 #pragma unroll
@@ -370,10 +407,6 @@ __device__ __forceinline__ void out_rows(const GemmParams& p, int64_t row, int l
     for (int i = 0; i < 16; i += 2) sigmoid_mul2<gelu_arg>(x[i], x[i + 1]);
   }
   if (p.res != nullptr) {
-    float r[16];
-    const int64_t at = row * p.ld_res + col;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = 2 * i < left ? load1(p.res, p.res_f32, at + 2 * i * p.ld_res) : 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] += r[i];
   }
@@ -381,15 +414,15 @@ __device__ __forceinline__ void out_rows(const GemmParams& p, int64_t row, int l
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (2 * i < left)
-        store1(p.out, p.out_f32, p.row_map[row + 2 * i] * p.ld_out + col, x[i] * p.row_scale[row + 2 * i]);
+        store1(p.out, OF32, p.row_map[row + 2 * i] * p.ld_out + col, x[i] * p.row_scale[row + 2 * i]);
     return;
   }
-  const int64_t at = out_off + row * p.ld_out + col;
+  const int64_t at = row * p.ld_out + col;
 #pragma unroll
   for (int i = 0; i < 16; ++i)
-    if (2 * i < left) store1(p.out, p.out_f32, at + 2 * i * p.ld_out, x[i]);
+    if (2 * i < left) store1(p.out, OF32, at + 2 * i * p.ld_out, x[i]);
 }
-// The same for one element.
+// The same for one element (the last step of a split product).
 __device__ __forceinline__ void out1(const GemmParams& p, int64_t row, int col, float v, float bias) {
   v += bias;
   if (p.pre != nullptr) store1(p.pre, p.pre_f32, row * p.ld_pre + col, v);
@@ -414,7 +447,20 @@ __device__ __forceinline__ void stats_join(float& m, float& s, float2 q) {
   m = nm;
 }
 
+// a / b for 0 <= a, 0 < b: by a float reciprocal where that is off by one at
+// most (every role divides several times per tile).
+__device__ __forceinline__ int fast_div(int a, int b) {
+  if (a >= (1 << 20)) return a / b;
+  int q = (int)((float)a * rcp_f((float)b));
+  const int r = a - q * b;
+  if (r < 0) --q;
+  else if (r >= b) ++q;
+  return q;
+}
 // Extents of one call with the device's row count applied, and its tiles.
+struct Tile {
+  int tm, tn, k0, k1, sp;
+};
 template <int CG>
 struct Tiles {
   int m, k, mt, nt, nk, total;
@@ -429,18 +475,20 @@ struct Tiles {
     total = mt * nt * p.splits;
   }
   // Tile t: groups of group_m row tiles, all column tiles of a group before the next.
-  __device__ __forceinline__ void at(const GemmParams& p, int t, int& tm, int& tn, int& k0, int& k1, int& sp) const {
-    sp = t / (mt * nt);
-    const int r = t - sp * (mt * nt), per = p.group_m * nt, g = r / per, q = r - g * per;
+  __device__ __forceinline__ Tile at(const GemmParams& p, int t) const {
+    Tile x;
+    x.sp = p.splits == 1 ? 0 : fast_div(t, mt * nt);
+    const int r = t - x.sp * (mt * nt), per = p.group_m * nt, g = fast_div(r, per), q = r - g * per;
     const int rows = min(p.group_m, mt - g * p.group_m);
-    tm = g * p.group_m + q % rows;
-    tn = q / rows;
-    k0 = (int)((int64_t)nk * sp / p.splits);
-    k1 = (int)((int64_t)nk * (sp + 1) / p.splits);
+    x.tn = fast_div(q, rows);
+    x.tm = g * p.group_m + q - x.tn * rows;
+    x.k0 = p.splits == 1 ? 0 : (int)((int64_t)nk * x.sp / p.splits);
+    x.k1 = p.splits == 1 ? nk : (int)((int64_t)nk * (x.sp + 1) / p.splits);
+    return x;
   }
 };
 
-template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI>
+template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI, bool OF32>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_gemm(const GemmParams p, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
            const __grid_constant__ CUtensorMap omap, const __grid_constant__ CUtensorMap pmap) {
@@ -456,6 +504,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   const int w = __shfl_sync(0xffffffffu, t >> 5, 0);  // uniform over the warp, also to the compiler
   const uint32_t rank = CG == 2 ? cta_rank() : 0u;
   const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
+  if (t == 96) {  // the maps are on their way while the barriers and TMEM are set up
+    prefetch_map(&amap);
+    prefetch_map(&bmap);
+    if (EPI == kEpiOut || EPI == kEpiDz) prefetch_map(&omap);
+  }
   if (t == 0) {
     for (int i = 0; i < ST; ++i) {
       umma::bar_init(&full[i], 1);
@@ -491,11 +544,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     int it = 0, s = 0;
     uint32_t ph = 0;  // stage and its phase
     for (int tile = unit; tile < T.total && ok; tile += units) {
-      int tmi, tni, k0, k1, sp;
-      T.at(p, tile, tmi, tni, k0, k1, sp);
-      const int m0 = tmi * 128 * CG + (int)rank * 128;
-      const int n0 = tni * p.bn + (CG == 2 ? (int)rank * (p.bn / 2) : 0);
-      for (int kb = k0; kb < k1; ++kb, ++it) {
+      const Tile x = T.at(p, tile);
+      const int m0 = x.tm * 128 * CG + (int)rank * 128;
+      const int n0 = x.tn * p.bn + (CG == 2 ? (int)rank * (p.bn / 2) : 0);
+      for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
         if (!(ok = warp_wait(&empty[s], ph ^ 1))) break;
         if (leader) {
           if (rank == 0) bar_expect_tx(&full[s], stage_tx);
@@ -544,8 +596,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       int job = 0, s = 0;
       uint32_t ph = 0;
       for (int tile = unit; tile < T.total && ok; tile += units) {
-        int tmi, tni, k0, k1, sp;
-        T.at(p, tile, tmi, tni, k0, k1, sp);
+        const Tile x = T.at(p, tile);
+        const int k0 = x.k0, k1 = x.k1;
         for (int kb = k0; kb < k1; ++kb) {
           const bool first = kb == k0 || (FLUSH && ((kb - k0) & 1) == 0);
           const bool last = kb + 1 == k1 || (FLUSH && ((kb - k0) & 1) == 1);
@@ -586,17 +638,51 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     unsigned char* stg = sm + ST * S::kStage + ew * 2048;
     uint32_t turn = 0;
     constexpr int NC = BN < 128 ? 1 : BN / 128;  // chunks of this warp at most
-    const int nchunks = (p.bn + 31) / 32;
+    constexpr bool IN32 = NP == 3;               // type of bias and pre
+    const bool has_bias = EPI == kEpiOut && p.bias != nullptr, has_res = EPI == kEpiOut && p.res != nullptr;
+    // what a unit needs besides its accumulators is loaded while the unit before is worked on, across tiles too
+    uint4 braw[4], rraw[4];
+    auto ahead_of = [&](int64_t row0, int col) {
+      if constexpr (EPI == kEpiOut) {
+        if (!IN32 && has_bias) load_bias(braw, p, col);
+        if (has_res) load_res<OF32>(rraw, p, row0, col);
+      }
+    };
+    auto first_row = [&](const Tile& x) { return (int64_t)x.tm * 128 * CG + rank * 128 + 32 * (w & 3); };
     bool ok = true;
     int job = 0;
+    Tile x, nx;
+    if (unit < T.total) {
+      nx = T.at(p, unit);
+      ahead_of(first_row(nx), nx.tn * p.bn + 32 * quarter);
+    }
     for (int tile = unit; tile < T.total; tile += units) {
-      int tmi, tni, k0, k1, sp;
-      T.at(p, tile, tmi, tni, k0, k1, sp);
-      const int jobs = FLUSH ? (k1 - k0 + 1) / 2 : (k1 > k0 ? 1 : 0);
+      x = nx;
+      if (tile + units < T.total) nx = T.at(p, tile + units);
+      const int jobs = FLUSH ? (x.k1 - x.k0 + 1) / 2 : (x.k1 > x.k0 ? 1 : 0);
+      const int nend = min(p.n, (x.tn + 1) * p.bn);
       float acc[FLUSH ? NC * 32 : 1];
       if constexpr (FLUSH) {
 #pragma unroll
         for (int i = 0; i < NC * 32; ++i) acc[i] = 0.f;
+        if (EPI == kEpiOut && has_bias) {  // the sums start from the bias
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            const int col = x.tn * p.bn + 32 * (4 * c + quarter);
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              const float* b = static_cast<const float*>(p.bias) + col + i;
+              if (col + i + 4 <= p.n) {
+                const float4 u = *reinterpret_cast<const float4*>(b);
+                acc[c * 32 + i] = u.x, acc[c * 32 + i + 1] = u.y, acc[c * 32 + i + 2] = u.z, acc[c * 32 + i + 3] = u.w;
+              } else {
+#pragma unroll
+                for (int j = 0; j < 3; ++j)
+                  if (col + i + j < p.n) acc[c * 32 + i + j] = b[j];
+              }
+            }
+          }
+        }
         for (int j = 0; j < jobs; ++j, ++job) {
           if (!(ok = warp_wait(&accfull[job & 1], (job >> 1) & 1))) break;
           umma::fence_after_sync();
@@ -612,43 +698,29 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           if (lane == 0) leader_arrive<CG>(&accempty[job & 1]);
         }
       }
-      if (!ok) break;
-      const int64_t row0 = (int64_t)tmi * 128 * CG + rank * 128 + 32 * (w & 3);
-      const int64_t row = row0 + lane;
-      const int nend = min(p.n, (tni + 1) * p.bn);
+      const int64_t row0 = first_row(x), row = row0 + lane;
       // per-row state of the loss epilogues
       float rm = -INFINITY, rs = 0.f, rlse = 0.f;
       int rt = -1;
-      if constexpr (EPI != kEpiOut) {
+      if constexpr (EPI == kEpiStats || EPI == kEpiDz) {
         if (row < T.m) {
           rt = p.target[row];
           if constexpr (EPI == kEpiDz) rlse = p.lse[row];
         }
       }
-      // bias and residual of a chunk are loaded while the chunk before is worked on (bf16, whole chunks)
-      uint4 braw[4], rraw[4];
-      auto early_b = [&](int col) { return EPI == kEpiOut && p.tma_out && p.bias != nullptr && !p.bias_f32 && col + 32 <= p.n; };
-      auto early_r = [&](int col) {
-        return EPI == kEpiOut && p.tma_out && p.res != nullptr && !p.res_f32 && p.vec && col + 32 <= p.n && row < T.m;
-      };
-      auto early = [&](int col) {
-        if (early_b(col)) load32(braw, p.bias, col);
-        if (early_r(col)) load32(rraw, p.res, row * p.ld_res + col);
-      };
-      if constexpr (EPI == kEpiOut) early(tni * p.bn + 32 * quarter);
       if constexpr (!FLUSH) {
         if (jobs > 0) {
           ok = warp_wait(&accfull[job & 1], (job >> 1) & 1);
           umma::fence_after_sync();
         }
-        if (!ok) break;
       }
+      if (!ok) break;
       const uint32_t tacc = lanes + (uint32_t)(job & 1) * BN;
 #pragma unroll(FLUSH ? NC : 1)
       for (int c = 0; c < NC; ++c) {
         const int ch = 4 * c + quarter;
-        const int col0 = tni * p.bn + 32 * ch;
-        const bool live = ch < nchunks && col0 < nend;  // uniform over the warp
+        const int col0 = x.tn * p.bn + 32 * ch;
+        const bool live = 32 * ch < p.bn && col0 < nend;  // uniform over the warp
         float v[32];
         if constexpr (FLUSH) {
 #pragma unroll
@@ -666,7 +738,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             if (lane == 0) leader_arrive<CG>(&accempty[job & 1]);
           }
         }
-        if (!live) continue;
+        // the unit after this chunk's last: the next chunk if that is live, else the next tile's first
+        const bool more = c + 1 < NC && 32 * (ch + 4) < p.bn && col0 + 128 < nend;
+        auto next = [&]() {
+          if (more) ahead_of(row0, col0 + 128);
+          else if (tile + units < T.total) ahead_of(first_row(nx), nx.tn * p.bn + 32 * quarter);
+        };
+        if (!live) {
+          if (c == 0) next();
+          continue;
+        }
         if constexpr (EPI == kEpiStats) {
           const int vcol = p.v0 + col0;
           const bool edge = col0 + 32 > nend || (unsigned)(p.excluded - vcol) < 32u;
@@ -709,8 +790,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = 0.f;
           }
+          auto none = [] {};
           if constexpr (NP == 1) {
-            chunk_store(&omap, 0, col0, (int)row0, 0, p.n, v, stg);
+            unit_store<false, 0>(&omap, col0, (int)row0, 0, v, false, rraw, stg, none);
           } else {
 #pragma unroll
             for (int k = 0; k < 3; ++k) {  // the largest piece of what is left of the value
@@ -720,22 +802,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 q[i] = bf16_part(v[i]);
                 v[i] -= q[i];
               }
-              chunk_store(&omap, 0, col0, (int)row0, k, p.n, q, stg);
+              unit_store<false, 0>(&omap, col0, (int)row0, k, q, false, rraw, stg, none);
             }
           }
-        } else if (p.tma_out) {
-          if (p.bias != nullptr) {
-            if (early_b(col0)) {
-              add32(v, braw);
-            } else if (col0 + 32 <= p.n) {
-              add32(v, p.bias, p.bias_f32, col0);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (col0 + i < p.n) v[i] += load1(p.bias, p.bias_f32, col0 + i);
-            }
+        } else if constexpr (EPI == kEpiOut) {
+          auto none = [] {};
+          if (!IN32 && has_bias) add_bias(v, braw, p, col0);
+          if (p.pre != nullptr) {
+            unit_store<IN32, 0>(&pmap, col0, (int)row0, 0, v, false, rraw, stg, none);
+            if (IN32 && col0 + 16 < p.n) unit_store<IN32, 1>(&pmap, col0 + 16, (int)row0, 0, v, false, rraw, stg, none);
           }
-          if (p.pre != nullptr) chunk_store(&pmap, p.pre_f32, col0, (int)row0, 0, p.n, v, stg);
           if (p.act == kActSilu) {
 #pragma unroll
             for (int i = 0; i < 32; i += 2) sigmoid_mul2<silu_arg>(v[i], v[i + 1]);
@@ -743,20 +819,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 #pragma unroll
             for (int i = 0; i < 32; i += 2) sigmoid_mul2<gelu_arg>(v[i], v[i + 1]);
           }
-          if (p.res != nullptr && row < T.m) {
-            const int64_t at = row * p.ld_res + col0;
-            if (early_r(col0)) {
-              add32(v, rraw);
-            } else if (p.vec && col0 + 32 <= p.n) {
-              add32(v, p.res, p.res_f32, at);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (col0 + i < p.n) v[i] += load1(p.res, p.res_f32, at + i);
-            }
+          if constexpr (OF32) {
+            const bool two = col0 + 16 < p.n;
+            unit_store<true, 0>(&omap, col0, (int)row0, x.sp, v, has_res, rraw, stg, [&]() {
+              if (!two) next();
+              else if (has_res) load_res<true>(rraw, p, row0, col0 + 16);
+            });
+            if (two) unit_store<true, 1>(&omap, col0 + 16, (int)row0, x.sp, v, has_res, rraw, stg, next);
+          } else {
+            unit_store<false, 0>(&omap, col0, (int)row0, x.sp, v, has_res, rraw, stg, next);
           }
-          if (c + 1 < NC) early(col0 + 128);
-          chunk_store(&omap, p.out_f32, col0, (int)row0, sp, p.n, v, stg);
         } else {
           // through shared memory, 16 columns at a time: 16 lanes per row, a row per half warp
           float* f = reinterpret_cast<float*>(stg);
@@ -770,14 +842,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             __syncwarp();
             const int cl = lane & 15, col = col0 + 16 * h + cl;
             if (col < nend) {
-              float x[16];
+              float y[16];
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
                 const int r = 2 * i + (lane >> 4);
-                x[i] = f[r * 16 + 4 * ((cl >> 2) ^ ((r >> 1) & 3)) + (cl & 3)];
+                y[i] = f[r * 16 + 4 * ((cl >> 2) ^ ((r >> 1) & 3)) + (cl & 3)];
               }
-              out_rows(p, row0 + (lane >> 4), (int)min((int64_t)32, T.m - row0) - (lane >> 4), col, x,
-                       (int64_t)sp * p.split_stride);
+              out_rows<IN32, OF32>(p, row0 + (lane >> 4), (int)min((int64_t)32, T.m - row0) - (lane >> 4), col, y);
             }
             __syncwarp();
           }
@@ -792,12 +863,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         if (quarter == 0 && row < T.m) {
 #pragma unroll
           for (int k = 1; k < 4; ++k) stats_join(rm, rs, q[128 * k + 32 * w + lane - 128]);
-          p.part[(int64_t)tni * p.rows_ld + row] = make_float2(rm, rs);
+          p.part[(int64_t)x.tn * p.rows_ld + row] = make_float2(rm, rs);
         }
       }
       if constexpr (!FLUSH) job += jobs;
     }
-    if (lane == 0) tma_store_wait();
+    if ((EPI == kEpiOut || EPI == kEpiDz) && lane == 0) tma_store_wait();
     if (!ok && lane == 0) atomicExch(p.flag, 1);
   }
   umma::fence_before_sync();
@@ -808,10 +879,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 }
 
 // One CTA (or pair) per SM (or pair of SMs), at most one per tile.
-template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI>
+template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI, bool OF32>
 cudaError_t gemm_t(const GemmParams& p, const GemmMaps& m, cudaStream_t s) {
   using S = GemmSmem<CG, BN, NP>;
-  auto kern = k_gemm<CG, BN, NP, A_MN, B_MN, EPI>;
+  auto kern = k_gemm<CG, BN, NP, A_MN, B_MN, EPI, OF32>;
   cudaError_t e = set_smem_cached(reinterpret_cast<const void*>(kern), (int)S::kBytes, 100);
   if (e != cudaSuccess) return e;
   const int64_t mt = (p.m + 128 * CG - 1) / (128 * CG), nt = (p.n + p.bn - 1) / p.bn;

@@ -1,19 +1,25 @@
-// gemm_nt.cu -- instances of the matrix product of gemm.cuh: both operands with rows along m and n.
+// gemm_nt.cu -- instances of the matrix product of gemm.cuh: both operands with rows along m and n, bf16.
 #include "gemm.cuh"
 
 namespace bds {
 
 cudaError_t launch_gemm_nt(const GemmCfg& c, const GemmParams& p, const GemmMaps& m, cudaStream_t s) {
-  if (c.cg == 2 && c.bn == 256 && c.pieces == 1)
-    return gemm_t<2, 256, 1, false, false, kEpiOut>(p, m, s);
-  if (c.cg == 1 && c.bn == 128 && c.pieces == 1)
-    return gemm_t<1, 128, 1, false, false, kEpiOut>(p, m, s);
-  if (c.cg == 1 && c.bn == 64 && c.pieces == 1)
-    return gemm_t<1, 64, 1, false, false, kEpiOut>(p, m, s);
-  if (c.cg == 2 && c.bn == 128 && c.pieces == 3)
-    return gemm_t<2, 128, 3, false, false, kEpiOut>(p, m, s);
-  if (c.cg == 1 && c.bn == 128 && c.pieces == 3)
-    return gemm_t<1, 128, 3, false, false, kEpiOut>(p, m, s);
+  if (c.epi == kEpiOut && c.cg == 2 && c.bn == 256 && c.pieces == 1 && c.out_f32 == false)
+    return gemm_t<2, 256, 1, false, false, kEpiOut, false>(p, m, s);
+  if (c.epi == kEpiOut && c.cg == 2 && c.bn == 256 && c.pieces == 1 && c.out_f32 == true)
+    return gemm_t<2, 256, 1, false, false, kEpiOut, true>(p, m, s);
+  if (c.epi == kEpiOut && c.cg == 1 && c.bn == 128 && c.pieces == 1 && c.out_f32 == false)
+    return gemm_t<1, 128, 1, false, false, kEpiOut, false>(p, m, s);
+  if (c.epi == kEpiOut && c.cg == 1 && c.bn == 128 && c.pieces == 1 && c.out_f32 == true)
+    return gemm_t<1, 128, 1, false, false, kEpiOut, true>(p, m, s);
+  if (c.epi == kEpiRows && c.cg == 2 && c.bn == 256 && c.pieces == 1 && c.out_f32 == false)
+    return gemm_t<2, 256, 1, false, false, kEpiRows, false>(p, m, s);
+  if (c.epi == kEpiRows && c.cg == 2 && c.bn == 256 && c.pieces == 1 && c.out_f32 == true)
+    return gemm_t<2, 256, 1, false, false, kEpiRows, true>(p, m, s);
+  if (c.epi == kEpiRows && c.cg == 1 && c.bn == 128 && c.pieces == 1 && c.out_f32 == false)
+    return gemm_t<1, 128, 1, false, false, kEpiRows, false>(p, m, s);
+  if (c.epi == kEpiRows && c.cg == 1 && c.bn == 128 && c.pieces == 1 && c.out_f32 == true)
+    return gemm_t<1, 128, 1, false, false, kEpiRows, true>(p, m, s);
   return cudaErrorInvalidValue;
 }
 
