@@ -29,9 +29,11 @@ __device__ __forceinline__ void load8(float (&v)[8], const void* p, int f32, int
 }
 
 // ---- operand packing ----
-// A thread converts eight columns of one row. Operands whose rows start on
-// 16-byte boundaries are read in place and never come here; the others, fp32
-// operands and the loss's rows cost one read and one write.
+// A warp converts 256 columns of one row: a lane eight consecutive ones where
+// rows start on 16-byte boundaries, else every 32nd column, so that its loads
+// and stores stay contiguous over the warp. Operands that TMA can read where
+// they lie never come here; the others, fp32 operands and the loss's rows cost
+// one read and one write.
 __device__ __forceinline__ void pack_store(bf16* d, int64_t plane, int pieces, const float (&v)[8]) {
   if (pieces == 1) {
     *reinterpret_cast<uint4*>(d) =
@@ -44,6 +46,51 @@ __device__ __forceinline__ void pack_store(bf16* d, int64_t plane, int pieces, c
 #pragma unroll
   for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(d + k * plane) = *reinterpret_cast<const uint4*>(q[k]);
 }
+// The same for column c, c + 32, ... below `cols`.
+__device__ __forceinline__ void pack_store_strided(bf16* d, int64_t plane, int pieces, const float (&v)[8], int c,
+                                                   int cols) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if (c + 32 * j >= cols) break;
+    if (pieces == 1) {
+      d[32 * j] = __float2bfloat16_rn(v[j]);
+    } else {
+      bf16 q0, q1, q2;
+      split3(v[j], q0, q1, q2);
+      d[32 * j] = q0;
+      d[plane + 32 * j] = q1;
+      d[2 * plane + 32 * j] = q2;
+    }
+  }
+}
+__device__ __forceinline__ void pack_block(const PackParams& p, int64_t block) {
+  const int lane = threadIdx.x & 31;
+  const int groups = (int)((p.ld_dst + 255) / 256);
+  const int64_t idx = block * (kThreads / 32) + (threadIdx.x >> 5);
+  const int64_t row = idx / groups;
+  const int c0 = (int)(idx - row * groups) * 256;
+  if (row >= p.rows) return;
+  float v[8];
+  if (p.ld % (p.src_f32 ? 4 : 8) == 0) {
+    const int c = c0 + 8 * lane;
+    if (c >= p.ld_dst) return;
+    if (c + 8 <= p.cols) {
+      load8(v, p.src, p.src_f32, row * p.ld + c);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = c + j < p.cols ? load1(p.src, p.src_f32, row * p.ld + c + j) : 0.f;
+    }
+    pack_store(p.dst + row * p.ld_dst + c, p.plane, p.pieces, v);
+  } else {  // columns past `cols` are outside the operand's map: never read
+    const int c = c0 + lane;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + 32 * j < p.cols ? load1(p.src, p.src_f32, row * p.ld + c + 32 * j) : 0.f;
+    pack_store_strided(p.dst + row * p.ld_dst + c, p.plane, p.pieces, v, c, (int)p.cols);
+  }
+}
+int64_t pack_blocks(const PackParams& p) {
+  return p.dst == nullptr ? 0 : (p.rows * ((p.ld_dst + 255) / 256) + kThreads / 32 - 1) / (kThreads / 32);
+}
 __device__ __forceinline__ void pack_load(float (&v)[8], const PackParams& p, int64_t row, int c) {
   const int64_t at = row * p.ld + c;
   if (p.ld % (p.src_f32 ? 4 : 8) == 0 && c + 8 <= p.cols) {
@@ -52,17 +99,6 @@ __device__ __forceinline__ void pack_load(float (&v)[8], const PackParams& p, in
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = c + j < p.cols ? load1(p.src, p.src_f32, at + j) : 0.f;
   }
-}
-__global__ void __launch_bounds__(kThreads) k_pack(const PackParams p) {
-  pdl_sync();
-  const int groups = (int)(p.ld_dst / 8);
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t row = idx / groups;
-  const int c = (int)(idx - row * groups) * 8;
-  if (row >= p.rows) return;
-  float v[8];
-  pack_load(v, p, row, c);
-  pack_store(p.dst + row * p.ld_dst + c, p.plane, p.pieces, v);
 }
 // The rows of the loss that count, each to its slot (pos), and zeros behind
 // them up to a whole tile of rows; in the backward a second copy scaled by the
@@ -119,17 +155,15 @@ __global__ void __launch_bounds__(kThreads) k_pack_rows(const PackParams p) {
 // products, added in a fixed order: rows of a warp, then warps, then ranges.
 constexpr int kDactCols = 256, kDactFlight = 2;
 template <bool DYF32, bool PREF32>
-__global__ void __launch_bounds__(kThreads, 3) k_dact(const DactParams p) {
-  pdl_sync();
+__device__ __forceinline__ void dact_block(const DactParams& p, int strip, int range) {
   __shared__ float red[8][kDactCols];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int c = blockIdx.x * kDactCols + lane * 8;
-  const int64_t r0 = p.rows * blockIdx.y / p.ranges, r1 = p.rows * (blockIdx.y + 1) / p.ranges;
+  const int64_t r0 = p.rows * range / p.ranges, r1 = p.rows * (range + 1) / p.ranges;
   float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  // 16-byte boundaries, eight whole columns
-  const bool full = c + 8 <= p.cols && p.ld_dy % (DYF32 ? 4 : 8) == 0 &&
-                    (p.act == kActNone || p.ld_pre % (PREF32 ? 4 : 8) == 0);
-  auto finish = [&](int64_t r, float (&e)[8], const float (&z)[8]) {
+  // a lane's eight columns: consecutive ones where rows start on 16-byte boundaries, else every 32nd
+  const bool aligned = p.ld_dy % (DYF32 ? 4 : 8) == 0 && (p.act == kActNone || p.ld_pre % (PREF32 ? 4 : 8) == 0);
+  const int c0 = strip * kDactCols, c = c0 + (aligned ? lane * 8 : lane), step = aligned ? 1 : 32;
+  auto grad = [&](float (&e)[8], const float (&z)[8]) {
     if (p.act == kActSilu) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) e[j] *= act_grad(kActSilu, z[j]);
@@ -139,20 +173,12 @@ __global__ void __launch_bounds__(kThreads, 3) k_dact(const DactParams p) {
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] += e[j];
-    if (p.dz == nullptr) return;
-    bf16* d = p.dz + r * p.ld_dz + c;  // rows of whole groups of 8
-    if (p.pieces == 1) {
-      *reinterpret_cast<uint4*>(d) =
-          make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
-      return;
-    }
-    __align__(16) bf16 q[3][8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) split3(e[j], q[0][j], q[1][j], q[2][j]);
-#pragma unroll
-    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(d + k * p.plane) = *reinterpret_cast<const uint4*>(q[k]);
   };
-  if (full) {
+  if (aligned && c + 8 <= p.cols) {
+    auto finish = [&](int64_t r, float (&e)[8], const float (&z)[8]) {
+      grad(e, z);
+      if (p.dz != nullptr) pack_store(p.dz + r * p.ld_dz + c, p.plane, p.pieces, e);
+    };
     int64_t r = r0 + w;
     for (; r + 8 * (kDactFlight - 1) < r1; r += 8 * kDactFlight) {
       float e[kDactFlight][8], z[kDactFlight][8];
@@ -171,28 +197,55 @@ __global__ void __launch_bounds__(kThreads, 3) k_dact(const DactParams p) {
       finish(r, e, z);
     }
   } else if (c < p.cols) {
-#pragma unroll 2
     for (int64_t r = r0 + w; r < r1; r += 8) {
       float e[8], z[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        e[j] = c + j < p.cols ? load1(p.dy, DYF32, r * p.ld_dy + c + j) : 0.f;
-        z[j] = p.act != kActNone && c + j < p.cols ? load1(p.pre, PREF32, r * p.ld_pre + c + j) : 0.f;
+        const bool in = c + step * j < p.cols;
+        e[j] = in ? load1(p.dy, DYF32, r * p.ld_dy + c + step * j) : 0.f;
+        z[j] = in && p.act != kActNone ? load1(p.pre, PREF32, r * p.ld_pre + c + step * j) : 0.f;
       }
-      finish(r, e, z);
+      grad(e, z);
+      if (p.dz == nullptr) continue;
+      bf16* d = p.dz + r * p.ld_dz + c;
+      if (aligned) pack_store(d, p.plane, p.pieces, e);  // rows of whole groups of 8
+      else pack_store_strided(d, p.plane, p.pieces, e, c, (int)p.cols);
     }
   }
   if (p.part == nullptr) return;
 #pragma unroll
   for (int j = 0; j < 8; ++j) red[w][j * 32 + lane] = sum[j];
   __syncthreads();
-  const int lc = threadIdx.x, col = blockIdx.x * kDactCols + (lc & 31) * 8 + (lc >> 5);
+  const int lc = threadIdx.x, col = c0 + (aligned ? (lc & 31) * 8 + (lc >> 5) : lc);
   if (col < p.cols) {
     float s = red[0][lc];
 #pragma unroll
     for (int i = 1; i < 8; ++i) s += red[i][lc];
-    p.part[(int64_t)blockIdx.y * p.cols + col] = s;
+    p.part[(int64_t)range * p.cols + col] = s;
   }
+}
+
+// The passes over a call's inputs in one launch: dz first (the longest), then
+// the operands that have to be packed.
+template <bool DYF32, bool PREF32>
+__global__ void __launch_bounds__(kThreads, 3) k_prep(const DactParams d, const PackParams a, const PackParams b,
+                                                      int64_t nd, int64_t na) {
+  pdl_sync();
+  const int64_t block = blockIdx.x;
+  if (block < nd) {
+    const int strips = (int)((d.cols + kDactCols - 1) / kDactCols);
+    dact_block<DYF32, PREF32>(d, (int)(block % strips), (int)(block / strips));
+  } else if (block < nd + na) {
+    pack_block(a, block - nd);
+  } else {
+    pack_block(b, block - nd - na);
+  }
+}
+__global__ void __launch_bounds__(kThreads) k_pack(const PackParams a, const PackParams b, int64_t na) {
+  pdl_sync();
+  const int64_t block = blockIdx.x;
+  if (block < na) pack_block(a, block);
+  else pack_block(b, block - na);
 }
 
 // Sum over row ranges, 32 columns per CTA, eight warps in strides, fixed order.
@@ -465,10 +518,10 @@ void vec_rows(const VecParams& p, bool vec, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_pack(const PackParams& p, cudaStream_t s) {
-  const int64_t n = p.rows * (p.ld_dst / 8);
-  if (n == 0) return cudaSuccess;
-  launch_pdl(k_pack, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, p);
+cudaError_t launch_pack(const PackParams& a, const PackParams& b, cudaStream_t s) {
+  const int64_t na = pack_blocks(a), nb = pack_blocks(b);
+  if (na + nb == 0) return cudaSuccess;
+  launch_pdl(k_pack, dim3((unsigned)(na + nb)), dim3(kThreads), 0, s, a, b, na);
   return cudaGetLastError();
 }
 cudaError_t launch_pack_rows(const PackParams& p, cudaStream_t s) {
@@ -476,11 +529,12 @@ cudaError_t launch_pack_rows(const PackParams& p, cudaStream_t s) {
   launch_pdl(k_pack_rows, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, p);
   return cudaGetLastError();
 }
-cudaError_t launch_dact(const DactParams& p, cudaStream_t s) {
-  const dim3 grid((unsigned)((p.cols + kDactCols - 1) / kDactCols), (unsigned)p.ranges);
-  if (p.pre_f32) launch_pdl(k_dact<true, true>, grid, dim3(kThreads), 0, s, p);
-  else if (p.dy_f32) launch_pdl(k_dact<true, false>, grid, dim3(kThreads), 0, s, p);
-  else launch_pdl(k_dact<false, false>, grid, dim3(kThreads), 0, s, p);
+cudaError_t launch_prep(const DactParams& p, const PackParams& a, const PackParams& b, cudaStream_t s) {
+  const int64_t nd = (p.cols + kDactCols - 1) / kDactCols * p.ranges, na = pack_blocks(a), nb = pack_blocks(b);
+  const dim3 grid((unsigned)(nd + na + nb));
+  if (p.pre_f32) launch_pdl(k_prep<true, true>, grid, dim3(kThreads), 0, s, p, a, b, nd, na);
+  else if (p.dy_f32) launch_pdl(k_prep<true, false>, grid, dim3(kThreads), 0, s, p, a, b, nd, na);
+  else launch_pdl(k_prep<false, false>, grid, dim3(kThreads), 0, s, p, a, b, nd, na);
   return cudaGetLastError();
 }
 cudaError_t launch_colsum(const float* part, int ranges, int64_t cols, void* out, int out_f32, cudaStream_t s) {

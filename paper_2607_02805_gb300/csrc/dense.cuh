@@ -44,6 +44,13 @@ struct GemmParams {
   float* at_target;      // [rows]
   int64_t rows_ld;       // rows of `part`
   const float* lse;      // [rows] of the rows that count
+  // Column sums that a warp without another role finishes on the side (the bias
+  // gradient, from launch_prep's partial sums): sum_out[c] = sum of
+  // sum_part[0 .. sum_ranges - 1][c]; null: none.
+  const float* sum_part;
+  void* sum_out;
+  int64_t sum_cols;
+  int sum_ranges, sum_f32;
   int* flag;             // set by a bounded wait that gave up
 };
 
@@ -82,7 +89,8 @@ struct PackParams {
   __nv_bfloat16* scaled;
   void* zero;
 };
-cudaError_t launch_pack(const PackParams& p, cudaStream_t s);
+// One launch for two operands; dst null: nothing to pack.
+cudaError_t launch_pack(const PackParams& a, const PackParams& b, cudaStream_t s);
 cudaError_t launch_pack_rows(const PackParams& p, cudaStream_t s);
 
 // dz = dy * act'(pre) in `pieces` bf16 planes, and partial column sums of the
@@ -97,7 +105,8 @@ struct DactParams {
   float* part;  // [ranges][cols], null: no sums
   int ranges;
 };
-cudaError_t launch_dact(const DactParams& p, cudaStream_t s);
+// That and up to two operands to pack, in one launch.
+cudaError_t launch_prep(const DactParams& p, const PackParams& a, const PackParams& b, cudaStream_t s);
 cudaError_t launch_colsum(const float* part, int ranges, int64_t cols, void* out, int out_f32, cudaStream_t s);
 
 // y = res + act(x w^T + bias) for a few rows, without the tensor cores.

@@ -232,27 +232,23 @@ cudaError_t run_out(Plan q, bool a_mn, bool b_mn, GemmParams p, const Operand& a
   return api_launched(launch_split_reduce(p, part, s), s);
 }
 
-// The operand as the products read it: where it lies, or packed into `ws`.
-cudaError_t operand(Operand* o, int dtype, const void* src, int64_t rows, int64_t cols, int64_t ld, char* ws,
-                    cudaStream_t s) {
-  if (in_place(dtype, ld)) {
-    *o = Operand{src, cols, rows, ld, 1, 0};
-    return cudaSuccess;
-  }
-  PackParams p;
-  memset(&p, 0, sizeof(p));
-  p.src = src;
-  p.ld = ld;
-  p.rows = rows;
-  p.cols = cols;
-  p.dst = (__nv_bfloat16*)ws;
-  p.ld_dst = up(cols, 8);
-  p.plane = rows * p.ld_dst;
-  p.src_f32 = dtype == BDSCAN_F32;
-  p.pieces = p.src_f32 ? 3 : 1;
-  *o = Operand{ws, cols, rows, p.ld_dst, p.pieces, p.plane};
-  return api_launched(launch_pack(p, s), s);
+// The operand as the products read it: where it lies, or packed into `ws` by
+// the launch that gets `p` (dst null: nothing to pack).
+Operand operand(PackParams* p, int dtype, const void* src, int64_t rows, int64_t cols, int64_t ld, char* ws) {
+  memset(p, 0, sizeof(*p));
+  if (in_place(dtype, ld)) return Operand{src, cols, rows, ld, 1, 0};
+  p->src = src;
+  p->ld = ld;
+  p->rows = rows;
+  p->cols = cols;
+  p->dst = (__nv_bfloat16*)ws;
+  p->ld_dst = up(cols, 8);
+  p->plane = rows * p->ld_dst;
+  p->src_f32 = dtype == BDSCAN_F32;
+  p->pieces = p->src_f32 ? 3 : 1;
+  return Operand{ws, cols, rows, p->ld_dst, p->pieces, p->plane};
 }
+const PackParams kNoPack{};
 
 int check_types(int dtype, int out_dtype, const char* fn) {
   if (dtype != BDSCAN_F32 && dtype != BDSCAN_BF16) return fail_msg(BDSCAN_ERR_ARG, fn, "bad dtype");
@@ -552,9 +548,11 @@ int bdscan_linear_forward(const bdscan_linear_dims* dims, const void* x, const v
   int* flag;
   if ((rc = check_device(fn, &flag))) return rc;
   char* base = (char*)workspace;
-  Operand a, b;
-  cudaError_t e = operand(&a, l.dtype, x, l.T, l.K, l.ld_x, base + ws.x, s);
-  if (e == cudaSuccess) e = operand(&b, l.dtype, w, l.N, l.K, l.K, base + ws.w, s);
+  PackParams px, pw;
+  const Operand a = operand(&px, l.dtype, x, l.T, l.K, l.ld_x, base + ws.x);
+  const Operand b = operand(&pw, l.dtype, w, l.N, l.K, l.K, base + ws.w);
+  cudaError_t e = cudaSuccess;
+  if (px.dst != nullptr || pw.dst != nullptr) e = api_launched(launch_pack(px, pw, s), s);
   if (e == cudaSuccess) {
     GemmParams p = geometry(ws.q, l.T, l.N, l.K, flag);
     p.bias = bias;
@@ -609,7 +607,11 @@ int bdscan_linear_backward(const bdscan_linear_dims* dims, const void* x, const 
   float* part = (float*)(base + ws.part);
   cudaError_t e = cudaSuccess;
   const bool products = dx != nullptr || dw != nullptr;
-  Operand dz{dy, l.N, l.T, l.ld_y, 1, 0};
+  Operand dz{dy, l.N, l.T, l.ld_y, 1, 0}, ox{}, ow{};
+  PackParams px = kNoPack, pw = kNoPack;
+  if (dx != nullptr) ow = operand(&pw, l.dtype, w, l.N, l.K, l.K, base + ws.w);
+  if (dw != nullptr) ox = operand(&px, l.dtype, x, l.T, l.K, l.ld_x, base + ws.x);
+  float* sums = dbias != nullptr ? (float*)(base + ws.sums) : nullptr;
   if ((products && ws.make_dz) || dbias != nullptr) {
     DactParams p;
     memset(&p, 0, sizeof(p));
@@ -630,34 +632,40 @@ int bdscan_linear_backward(const bdscan_linear_dims* dims, const void* x, const 
       p.plane = l.T * p.ld_dz;
       dz = Operand{p.dz, l.N, l.T, p.ld_dz, l.pieces, p.plane};
     }
-    p.part = dbias != nullptr ? (float*)(base + ws.sums) : nullptr;
-    e = api_launched(launch_dact(p, s), s);
-    if (e == cudaSuccess && dbias != nullptr)
-      e = api_launched(launch_colsum(p.part, p.ranges, l.N, dbias, l.dtype == BDSCAN_F32, s), s);
+    p.part = sums;
+    e = api_launched(launch_prep(p, px, pw, s), s);
+    if (e == cudaSuccess && dbias != nullptr && !products)
+      e = api_launched(launch_colsum(sums, ws.ranges, l.N, dbias, l.dtype == BDSCAN_F32, s), s);
+  } else if (px.dst != nullptr || pw.dst != nullptr) {
+    e = api_launched(launch_pack(px, pw, s), s);
   }
+  // the first of the products also ends the bias gradient
+  auto add_sums = [&](GemmParams* p) {
+    if (sums == nullptr) return;
+    p->sum_part = sums;
+    p->sum_out = dbias;
+    p->sum_cols = l.N;
+    p->sum_ranges = ws.ranges;
+    p->sum_f32 = l.dtype == BDSCAN_F32;
+    sums = nullptr;
+  };
   if (e == cudaSuccess && dx != nullptr) {
-    Operand b;
-    e = operand(&b, l.dtype, w, l.N, l.K, l.K, base + ws.w, s);
-    if (e == cudaSuccess) {
-      GemmParams p = geometry(ws.qx, l.T, l.K, l.N, flag);
-      p.out = dx;
-      p.ld_out = l.K;
-      p.out_f32 = l.dtype == BDSCAN_F32;
-      p.out_extent = l.T * l.K;
-      e = run_out(ws.qx, false, true, p, dz, b, part, s);
-    }
+    GemmParams p = geometry(ws.qx, l.T, l.K, l.N, flag);
+    p.out = dx;
+    p.ld_out = l.K;
+    p.out_f32 = l.dtype == BDSCAN_F32;
+    p.out_extent = l.T * l.K;
+    add_sums(&p);
+    e = run_out(ws.qx, false, true, p, dz, ow, part, s);
   }
   if (e == cudaSuccess && dw != nullptr) {
-    Operand b;
-    e = operand(&b, l.dtype, x, l.T, l.K, l.ld_x, base + ws.x, s);
-    if (e == cudaSuccess) {
-      GemmParams p = geometry(ws.qw, l.N, l.K, l.T, flag);
-      p.out = dw;
-      p.ld_out = l.K;
-      p.out_f32 = l.dtype == BDSCAN_F32;
-      p.out_extent = l.N * l.K;
-      e = run_out(ws.qw, true, true, p, dz, b, part, s);
-    }
+    GemmParams p = geometry(ws.qw, l.N, l.K, l.T, flag);
+    p.out = dw;
+    p.ld_out = l.K;
+    p.out_f32 = l.dtype == BDSCAN_F32;
+    p.out_extent = l.N * l.K;
+    add_sums(&p);
+    e = run_out(ws.qw, true, true, p, dz, ox, part, s);
   }
   return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
 }
@@ -701,9 +709,11 @@ int bdscan_lm_loss_forward(const bdscan_lm_loss_dims* dims, const void* h, const
   rp.loss = loss;
   rp.lse = lse;
   cudaError_t e = api_launched(launch_loss_rows(rp, s), s);
-  Operand a, b;
+  Operand a;
+  PackParams pw;
+  const Operand b = operand(&pw, l.dtype, w, l.V, l.K, l.K, base + ws.w);
   if (e == cudaSuccess) e = gather_h(l, ws.r, h, base, nullptr, &a, nullptr, s);
-  if (e == cudaSuccess) e = operand(&b, l.dtype, w, l.V, l.K, l.K, base + ws.w, s);
+  if (e == cudaSuccess && pw.dst != nullptr) e = api_launched(launch_pack(pw, kNoPack, s), s);
   if (e == cudaSuccess) {
     Plan q = ws.q;
     q.cfg.epi = kEpiStats;
@@ -771,9 +781,11 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
   rp.gscale = (float*)(base + ws.r.gscale);
   rp.lse_c = (float*)(base + ws.r.lse);
   cudaError_t e = api_launched(launch_loss_rows(rp, s), s);
-  Operand a, b, scaled;
+  Operand a, scaled;
+  PackParams pw;
+  const Operand b = operand(&pw, l.dtype, w, l.V, l.K, l.K, base + ws.w);
   if (e == cudaSuccess) e = gather_h(l, ws.r, h, base, dh, &a, &scaled, s);
-  if (e == cudaSuccess) e = operand(&b, l.dtype, w, l.V, l.K, l.K, base + ws.w, s);
+  if (e == cudaSuccess && pw.dst != nullptr) e = api_launched(launch_pack(pw, kNoPack, s), s);
   const int64_t ld_dz = up(ws.piece, 8), ld_acc = up(l.K, 4);
   const int f32 = l.dtype == BDSCAN_F32;
   float* part = (float*)(base + ws.part);

@@ -378,20 +378,39 @@ __device__ __forceinline__ void add_bias(float (&v)[32], const uint4 (&r)[4], co
   }
 }
 
+// What a chunk's output by plain stores needs besides its accumulators, loaded
+// ahead: columns col0 + lane % 16 and 16 further, rows row0 + lane / 16 + 2 i.
+// Bits as they lie in memory, so that nothing waits for them yet.
+struct RowsAhead {
+  uint32_t res[2][16];
+  float bias[2];
+};
+template <bool IN32>
+__device__ __forceinline__ void load_rows_ahead(RowsAhead& a, const GemmParams& p, int64_t row0, int col0) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int col = col0 + 16 * h + (lane & 15);
+    if (p.bias != nullptr) a.bias[h] = col < p.n ? load1(p.bias, IN32, col) : 0.f;
+    if (p.res == nullptr) continue;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int64_t r = row0 + (lane >> 4) + 2 * i;
+      if (r >= p.m || col >= p.n) continue;
+      const int64_t at = r * p.ld_res + col;
+      a.res[h][i] = p.res_f32 ? static_cast<const uint32_t*>(p.res)[at]
+                              : (uint32_t)static_cast<const unsigned short*>(p.res)[at];
+    }
+  }
+}
 // The output step of rows row, row + 2, ... (those below row + left) of one
 // column, by plain stores. IN32: bias and pre are fp32; OF32: the output is.
 template <bool IN32, bool OF32>
-__device__ __forceinline__ void out_rows(const GemmParams& p, int64_t row, int left, int col, float (&x)[16]) {
+__device__ __forceinline__ void out_rows(const GemmParams& p, int64_t row, int left, int col, float (&x)[16],
+                                         const uint32_t (&res)[16], float bias) {
   if (p.bias != nullptr) {
-    const float b = load1(p.bias, IN32, col);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] += b;
-  }
-  float r[16];
-  if (p.res != nullptr) {
-    const int64_t at = row * p.ld_res + col;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = 2 * i < left ? load1(p.res, p.res_f32, at + 2 * i * p.ld_res) : 0.f;
+    for (int i = 0; i < 16; ++i) x[i] += bias;
   }
   if (p.pre != nullptr) {
     const int64_t at = row * p.ld_pre + col;
@@ -407,8 +426,9 @@ __device__ __forceinline__ void out_rows(const GemmParams& p, int64_t row, int l
     for (int i = 0; i < 16; i += 2) sigmoid_mul2<gelu_arg>(x[i], x[i + 1]);
   }
   if (p.res != nullptr) {
+    const int sh = p.res_f32 ? 0 : 16;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] += r[i];
+    for (int i = 0; i < 16; ++i) x[i] += 2 * i < left ? __uint_as_float(res[i] << sh) : 0.f;
   }
   if (p.row_map != nullptr) {
 #pragma unroll
@@ -631,6 +651,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       if (!ok && leader) atomicExch(p.flag, 1);
     }
+  } else if (w == 3) {
+    // ---------------- column sums on the side ----------------
+    if (p.sum_part != nullptr) {
+      for (int64_t c = (int64_t)blockIdx.x * 32 + lane; c < p.sum_cols; c += (int64_t)gridDim.x * 32) {
+        float sum = 0.f;
+#pragma unroll 8
+        for (int r = 0; r < p.sum_ranges; ++r) sum += p.sum_part[(int64_t)r * p.sum_cols + c];
+        store1(p.sum_out, p.sum_f32, c, sum);
+      }
+    }
   } else if (w >= 4) {
     // ---------------- epilogue ----------------
     const int ew = w - 4, quarter = ew >> 2;  // TMEM lanes 32 (w % 4) .. + 31, every fourth chunk of 32 columns
@@ -642,11 +672,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     const bool has_bias = EPI == kEpiOut && p.bias != nullptr, has_res = EPI == kEpiOut && p.res != nullptr;
     // what a unit needs besides its accumulators is loaded while the unit before is worked on, across tiles too
     uint4 braw[4], rraw[4];
+    RowsAhead rahead;
     auto ahead_of = [&](int64_t row0, int col) {
       if constexpr (EPI == kEpiOut) {
         if (!IN32 && has_bias) load_bias(braw, p, col);
         if (has_res) load_res<OF32>(rraw, p, row0, col);
       }
+      if constexpr (EPI == kEpiRows) load_rows_ahead<IN32>(rahead, p, row0, col);
     };
     auto first_row = [&](const Tile& x) { return (int64_t)x.tm * 128 * CG + rank * 128 + 32 * (w & 3); };
     bool ok = true;
@@ -832,13 +864,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         } else {
           // through shared memory, 16 columns at a time: 16 lanes per row, a row per half warp
           float* f = reinterpret_cast<float*>(stg);
-#pragma unroll 1
+#pragma unroll
           for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               *reinterpret_cast<float4*>(f + lane * 16 + 4 * (j ^ ((lane >> 1) & 3))) =
-                  h == 0 ? make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3])
-                         : make_float4(v[16 + 4 * j], v[17 + 4 * j], v[18 + 4 * j], v[19 + 4 * j]);
+                  make_float4(v[16 * h + 4 * j], v[16 * h + 4 * j + 1], v[16 * h + 4 * j + 2], v[16 * h + 4 * j + 3]);
             __syncwarp();
             const int cl = lane & 15, col = col0 + 16 * h + cl;
             if (col < nend) {
@@ -848,10 +879,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 const int r = 2 * i + (lane >> 4);
                 y[i] = f[r * 16 + 4 * ((cl >> 2) ^ ((r >> 1) & 3)) + (cl & 3)];
               }
-              out_rows<IN32, OF32>(p, row0 + (lane >> 4), (int)min((int64_t)32, T.m - row0) - (lane >> 4), col, y);
+              out_rows<IN32, OF32>(p, row0 + (lane >> 4), (int)min((int64_t)32, T.m - row0) - (lane >> 4), col, y,
+                                   rahead.res[h], rahead.bias[h]);
             }
             __syncwarp();
           }
+          next();
         }
       }
       if constexpr (EPI == kEpiStats) {
