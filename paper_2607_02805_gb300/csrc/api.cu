@@ -55,7 +55,7 @@ const char* site_name(int site) {
   static const char* names[] = {"?", "k_chunk_local", "k_chunk_carry", "k_block_scan", "k_active_block",
                                 "k_bwd_noisy", "k_bwd_carry", "k_bwd_clean", "k_reduce_tok", "k_reduce_par",
                                 "k_ssd_block_state", "k_ssd_state_pass", "k_ssd_block_scan", "k_ssd_bwd_tile",
-                                "k_ssd_bwd_state"};
+                                "k_ssd_bwd_state", "k_gemm", "k_split_reduce", "k_linear_vec", "k_pack"};
   static_assert(sizeof(names) / sizeof(names[0]) == bds::kSiteCount, "one name per debug site");
   return site > 0 && site < bds::kSiteCount ? names[site] : names[0];
 }

@@ -40,6 +40,10 @@ enum DebugSite : int {
   kSiteSsdBlockScan,
   kSiteSsdBwdTile,
   kSiteSsdBwdState,
+  kSiteGemm,
+  kSiteSplitReduce,
+  kSiteLinearVec,
+  kSitePack,
   kSiteCount
 };
 

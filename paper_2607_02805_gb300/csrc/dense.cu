@@ -70,6 +70,8 @@ __device__ __forceinline__ void pack_block(const PackParams& p, int64_t block) {
   const int64_t row = idx / groups;
   const int c0 = (int)(idx - row * groups) * 256;
   if (row >= p.rows) return;
+  // debug build: the last element of the warp's row (no barrier follows)
+  if (!dguard(kSitePack, (p.pieces - 1) * p.plane + row * p.ld_dst + p.ld_dst - 1, p.dst_extent)) return;
   float v[8];
   if (p.ld % (p.src_f32 ? 4 : 8) == 0) {
     const int c = c0 + 8 * lane;
@@ -281,6 +283,7 @@ __global__ void __launch_bounds__(kThreads) k_split_reduce(const GemmParams p, c
   int m = p.m;
   if (p.rows_axis == 1) m = min(m, *p.rows_dev);
   if (row >= m) return;
+  if (!dguard(kSiteSplitReduce, p.out_last, p.out_extent)) return;
   const float* at = part + row * ld + c;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i = 0; i < p.splits; i += 8) {
@@ -324,6 +327,7 @@ __global__ void __launch_bounds__(128) k_linear_vec(const VecParams p) {
   const int lane = threadIdx.x & 31;
   const int64_t n0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 5)) * NC;
   if (n0 >= p.n) return;
+  if (!dguard(kSiteLinearVec, (p.rows - 1) * p.ld_y + p.n - 1, p.out_extent)) return;
   const T* x = static_cast<const T*>(p.x);
   const T* w = static_cast<const T*>(p.w);
   float acc[ROWS][NC];

@@ -36,7 +36,7 @@ struct GemmParams {
   int bias_f32, res_f32, out_f32, pre_f32;
   int act;
   int vec;               // rows of out, pre and res start on 16-byte boundaries, none is mapped
-  int64_t out_extent;    // elements of `out` (debug build)
+  int64_t out_last, out_extent;  // last element written and elements of `out` or `part` (debug build)
   // kEpiStats / kEpiDz: rows i are the rows that count; column j is entry v0 + j
   int v0, excluded;
   const int* target;     // [rows] of the rows that count
@@ -82,6 +82,7 @@ struct PackParams {
   __nv_bfloat16* dst;
   int64_t ld_dst, plane;
   int src_f32, pieces;
+  int64_t dst_extent;  // elements of dst (debug build)
   // launch_pack_rows only: slot of each row or -1, the number of slots, and in
   // the backward the slots' scales, the scaled copy and the gradient to zero
   const int *pos, *count;
@@ -116,6 +117,7 @@ struct VecParams {
   void *y, *pre;
   int64_t ld_x, ld_res, ld_y;
   int rows, k, n, act, f32, out_f32;
+  int64_t out_extent;  // elements of y (debug build)
 };
 cudaError_t launch_linear_vec(const VecParams& p, cudaStream_t s);
 

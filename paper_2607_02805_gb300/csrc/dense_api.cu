@@ -202,15 +202,21 @@ cudaError_t run_product(const Plan& q, const GemmParams& p, const Operand& a, co
 }
 
 // A product with the output step of kEpiOut, split over k where the plan says
-// so: then the partial sums go to `part` and a second launch ends it.
+// so: then the partial sums go to `part` and a second launch ends it. `padded`:
+// the output is fp32 in the workspace, its rows padded to 16 bytes.
 cudaError_t run_out(Plan q, bool a_mn, bool b_mn, GemmParams p, const Operand& a, const Operand& b, float* part,
-                    cudaStream_t s) {
+                    cudaStream_t s, bool padded = false) {
   q.cfg.a_mn = a_mn;
   q.cfg.b_mn = b_mn;
-  p.vec = p.row_map == nullptr && rows16(p.ld_out, p.out_f32) && (p.pre == nullptr || rows16(p.ld_pre, p.pre_f32)) &&
+  // TMA stores whole groups of 16 bytes: a row has to end on such a boundary as
+  // well, unless what follows is padding of the workspace
+  const int64_t width = padded ? up(p.n, 4) : p.n;
+  p.vec = p.row_map == nullptr && rows16(p.ld_out, p.out_f32) && rows16(width, p.out_f32) &&
+          (p.pre == nullptr || (rows16(p.ld_pre, p.pre_f32) && rows16(width, p.pre_f32))) &&
           (p.res == nullptr || (p.res_f32 == p.out_f32 && rows16(p.ld_res, p.res_f32)));
   q.cfg.epi = p.vec ? kEpiOut : kEpiRows;
   q.cfg.out_f32 = p.out_f32 != 0;
+  p.out_last = p.row_map != nullptr ? p.out_extent - 1 : (p.m - 1) * p.ld_out + p.n - 1;
   if (q.splits == 1) return run_product(q, p, a, b, 1, 0, p.m, s);
   GemmParams g = p;
   g.splits = q.splits;
@@ -225,6 +231,7 @@ cudaError_t run_out(Plan q, bool a_mn, bool b_mn, GemmParams p, const Operand& a
   q.cfg.out_f32 = true;
   g.act = BDSCAN_ACT_NONE;
   g.out_extent = (int64_t)q.splits * g.split_stride;
+  g.out_last = (q.splits - 1) * g.split_stride + (p.m - 1) * g.ld_out + p.n - 1;
   cudaError_t e = run_product(q, g, a, b, q.splits, g.split_stride, p.m, s);
   if (e != cudaSuccess) return e;
   p.splits = q.splits;
@@ -246,6 +253,7 @@ Operand operand(PackParams* p, int dtype, const void* src, int64_t rows, int64_t
   p->plane = rows * p->ld_dst;
   p->src_f32 = dtype == BDSCAN_F32;
   p->pieces = p->src_f32 ? 3 : 1;
+  p->dst_extent = p->pieces * p->plane;
   return Operand{ws, cols, rows, p->ld_dst, p->pieces, p->plane};
 }
 const PackParams kNoPack{};
@@ -540,6 +548,7 @@ int bdscan_linear_forward(const bdscan_linear_dims* dims, const void* x, const v
     v.ld_x = l.ld_x, v.ld_res = l.ld_res, v.ld_y = l.ld_y;
     v.rows = (int)l.T, v.k = (int)l.K, v.n = (int)l.N, v.act = l.act;
     v.f32 = l.dtype == BDSCAN_F32, v.out_f32 = l.out == BDSCAN_F32;
+    v.out_extent = (l.T - 1) * l.ld_y + l.N;
     const cudaError_t e = api_launched(launch_linear_vec(v, s), s);
     return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
   }
@@ -725,6 +734,8 @@ int bdscan_lm_loss_forward(const bdscan_lm_loss_dims* dims, const void* h, const
     p.part = (float2*)(base + ws.part);
     p.at_target = (float*)(base + ws.at);
     p.rows_ld = ws.r.rows;
+    p.out_last = (ws.parts - 1) * p.rows_ld + l.T - 1;
+    p.out_extent = ws.parts * p.rows_ld;
     e = run_product(q, p, a, b, 1, 0, l.T, s);
   }
   if (e == cudaSuccess)
@@ -808,7 +819,8 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
     p.lse = rp.lse_c;
     p.out = base + ws.dz;
     p.ld_out = ld_dz;
-    p.out_extent = ws.r.rows * ld_dz;
+    p.out_last = (l.pieces - 1) * ws.r.rows * ld_dz + (ws.r.rows - 1) * ld_dz + n - 1;
+    p.out_extent = l.pieces * ws.r.rows * ld_dz;
     e = run_product(q, p, a, bp, l.pieces, ws.r.rows * ld_dz, ws.r.rows, s);
     // this piece's rows of dw
     if (e == cudaSuccess) {
@@ -836,7 +848,7 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
       g.row_map = last ? rp.idx : nullptr;
       g.row_scale = rp.gscale;
       g.out_extent = last ? l.T * l.K : l.T * ld_acc;
-      e = run_out(ws.qh, false, true, g, dz, bp, part, s);
+      e = run_out(ws.qh, false, true, g, dz, bp, part, s, !last);
     }
   }
   return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);

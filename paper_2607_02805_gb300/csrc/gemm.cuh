@@ -30,6 +30,7 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 
+#include "debug.cuh"
 #include "dense.cuh"
 #include "device.cuh"
 #include "params.h"
@@ -516,6 +517,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   constexpr int ST = S::kStages, BK = S::kBk;
   constexpr bool FLUSH = NP == 3;
   constexpr uint32_t kCols = 2u * BN < 32u ? 32u : 2u * BN;
+  // debug build: the last output element of the launch (uniform over the grid)
+  if (!dguard(kSiteGemm, p.out_last, p.out_extent)) return;
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t full[8], empty[8], accfull[2], accempty[2];
   __shared__ uint32_t tslot;

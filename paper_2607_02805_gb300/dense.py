@@ -91,12 +91,12 @@ class Linear(_Holder):
     """y = residual + act(x w^T + bias) for x [rows, d_in], w [d_out, d_in]."""
 
     def __init__(self, rows, d_in, d_out, act="none", dtype=torch.bfloat16, out_dtype=None, device="cuda"):
-        super().__init__(device)
         if act not in ACTS:
             raise ValueError(f"unknown activation {act!r}")
+        _code(dtype), _code(dtype if out_dtype is None else out_dtype)
+        super().__init__(device)
         self.rows, self.d_in, self.d_out, self.act = int(rows), int(d_in), int(d_out), act
         self.dtype, self.out_dtype = dtype, dtype if out_dtype is None else out_dtype
-        _code(self.dtype), _code(self.out_dtype)
         self.pre = None
         self._x, self._w, self._y = (self.rows, self.d_in), (self.d_out, self.d_in), (self.rows, self.d_out)
         self._b = (self.d_out,)
@@ -147,10 +147,10 @@ class LmLoss(_Holder):
     h [rows, d_model], w [vocab, d_model]; include/bdscan_dense.h has the rules."""
 
     def __init__(self, rows, d_model, vocab, dtype=torch.bfloat16, excluded=-1, device="cuda"):
+        _code(dtype)
         super().__init__(device)
         self.rows, self.d_model, self.vocab, self.dtype = int(rows), int(d_model), int(vocab), dtype
         self.excluded = int(excluded)
-        _code(dtype)
         self._h, self._w, self._t = (self.rows, self.d_model), (self.vocab, self.d_model), (self.rows,)
 
     def _make_dims(self, ld_h):
