@@ -295,24 +295,7 @@ __global__ void __launch_bounds__(kThreads) k_split_reduce(const GemmParams p, c
     for (int j = 0; j < 8; ++j)
       if (i + j < p.splits) s.x += q[j].x, s.y += q[j].y, s.z += q[j].z, s.w += q[j].w;
   }
-  float e[4] = {s.x, s.y, s.z, s.w};
-  if (p.vec && c + 3 < p.n) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (p.bias != nullptr) e[j] += load1(p.bias, p.bias_f32, c + j);
-    if (p.pre != nullptr) store4(p.pre, p.pre_f32, row * p.ld_pre + c, make_float4(e[0], e[1], e[2], e[3]));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) e[j] = act_fwd(p.act, e[j]);
-    if (p.res != nullptr) {
-      const float4 r = load4(p.res, p.res_f32, row * p.ld_res + c);
-      e[0] += r.x, e[1] += r.y, e[2] += r.z, e[3] += r.w;
-    }
-    store4(p.out, p.out_f32, row * p.ld_out + c, make_float4(e[0], e[1], e[2], e[3]));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (c + j < p.n) out1(p, row, c + j, e[j], p.bias != nullptr ? load1(p.bias, p.bias_f32, c + j) : 0.f);
-  }
+  out4(p, row, c, s);
 }
 
 // ---- a linear layer of a few rows ----

@@ -12,6 +12,7 @@ namespace bds {
 // What a product does with its accumulators.
 constexpr int kEpiOut = 0;    // residual + act(acc + bias), or a split's partial sums, by TMA
 constexpr int kEpiRows = 3;   // the same by plain stores: unaligned or mapped rows
+constexpr int kEpiJoin = 4;   // the same, the ranges of k of a tile joined by a cluster
 constexpr int kEpiStats = 1;  // running maximum and sum of a row's logits, and the target's logit
 constexpr int kEpiDz = 2;     // the loss's gradient at the logits
 
@@ -23,6 +24,7 @@ struct GemmParams {
   int rows_axis;
   int bn;         // columns of a tile (a multiple of 32, at most the instance's BN)
   int splits;     // ranges of k, each with its own partial sums
+  int join;       // kEpiJoin: CTAs of a tile's cluster, each with a range of k
   int group_m;    // row tiles walked together
   // kEpiOut, kEpiRows: out[row_map ? row_map[i] : i][j]; kEpiOut has res of out's type
   const void* bias;

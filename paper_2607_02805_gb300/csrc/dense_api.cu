@@ -104,14 +104,15 @@ size_t packed_bytes(int dtype, int64_t rows, int64_t cols) {
 // for 152 SMs, so that workspace sizes do not depend on the device.
 struct Plan {
   GemmCfg cfg;
-  int bn, splits, group_m;
+  int bn, splits, join, group_m;  // splits > 1: through memory; join > 1: in clusters
 };
 constexpr int64_t kSms = 152;
 // The choice minimises a model of the product's time in clocks. A tile's step
 // of 64 k takes the larger of its MMAs (128 x 256 x 16 in 128 clocks per SM)
 // and its operands' way from L2 (64 bytes per clock and SM); a tile adds about
 // 400 clocks, and the epilogue of the last one 8 per column; the sums of a split
-// add a launch and their way to memory and back. Measured against the first
+// add a launch and their way to memory and back, a cluster that joins 2500 clocks.
+// Measured against the first
 // rule (256 x 256 tiles by pairs from a quarter of the pairs on, else 128 x 128
 // or 64, up to 16 splits): @@
 struct Instance {
@@ -134,7 +135,8 @@ Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split) {
       const int64_t nt = (n + bn - 1) / bn, tiles = mt * nt;
       const double a_rows = m < 128 ? (double)m : 128.0;
       const double mma = 2.0 * bn * products, load = 2.0 * pieces * (a_rows + bn / cg);
-      const double step = mma > load ? mma : load;
+      double step = mma > load ? mma : load;
+      if (step < 300) step = 300;  // six stages in flight at a latency of about 1800 clocks
       for (int waves = 1; waves <= 4; ++waves) {
         int64_t s = waves == 1 && !may_split ? 1 : units * waves / tiles;
         if (s < 1 || !may_split) s = 1;
@@ -149,8 +151,23 @@ Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split) {
           best.cfg.bn = inst[i].bn;
           best.bn = bn;
           best.splits = (int)s;
+          best.join = 1;
         }
         if (!may_split) break;
+      }
+      // a cluster per tile, as many as are resident together (fp32 by twos was slower than pairs without a
+      // split: 2048 x 448 x 1792 training step 86 us against 82)
+      for (int j = pieces == 3 ? 4 : 2; cg == 1 && may_split && j <= 8; j *= 2) {
+        if (tiles > (j == 2 ? 76 : j == 4 ? 36 : 15) || nk < 2 * j) break;
+        const double cost = 1500 + (nk + j - 1) / j * step + 8.0 * bn + 2500;
+        if (cost < best_cost) {
+          best_cost = cost;
+          best.cfg.cg = cg;
+          best.cfg.bn = inst[i].bn;
+          best.bn = bn;
+          best.splits = 1;
+          best.join = j;
+        }
       }
     }
   }
@@ -216,6 +233,10 @@ cudaError_t run_out(Plan q, bool a_mn, bool b_mn, GemmParams p, const Operand& a
           (p.res == nullptr || (p.res_f32 == p.out_f32 && rows16(p.ld_res, p.res_f32)));
   q.cfg.epi = p.vec ? kEpiOut : kEpiRows;
   q.cfg.out_f32 = p.out_f32 != 0;
+  if (q.join > 1) {
+    q.cfg.epi = kEpiJoin;
+    p.join = q.join;
+  }
   p.out_last = p.row_map != nullptr ? p.out_extent - 1 : (p.m - 1) * p.ld_out + p.n - 1;
   if (q.splits == 1) return run_product(q, p, a, b, 1, 0, p.m, s);
   GemmParams g = p;

@@ -23,6 +23,12 @@
 // only two fit) the epilogue warps add the accumulator to fp32 registers: the tensor core's own accumulation truncates,
 // and over a long k that error would grow with k.
 //
+// kEpiJoin splits a long k over a cluster: each of its CTAs sums a range of k of
+// the same tile, leaves its accumulators in shared memory, and ends a share of
+// the tile's elements from all of them through distributed shared memory, in
+// the order of the ranges. One launch instead of two and no way through memory
+// (32 x 3328 x 832: @@).
+//
 // Every wait has a poll limit. A role that gives up sets the wait flag and
 // leaves its loop; the producer then waits for its copies in flight, and TMEM
 // is freed.
@@ -64,6 +70,19 @@ __device__ __forceinline__ uint32_t cta_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(r));
   return r;
+}
+__device__ __forceinline__ int cluster_size() {
+  int n;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;\n" : "=r"(n));
+  return n;
+}
+__device__ __forceinline__ float4 load_cluster4(uint32_t saddr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(saddr)
+               : "memory");
+  return v;
 }
 __device__ __forceinline__ uint32_t map_cta(uint32_t saddr, uint32_t rank) {
   uint32_t r;
@@ -456,6 +475,29 @@ __device__ __forceinline__ void out1(const GemmParams& p, int64_t row, int col, 
   }
   store1(p.out, p.out_f32, orow * p.ld_out + col, v);
 }
+// Four columns of a row whose sums are complete, from the sums of a split.
+__device__ __forceinline__ void out4(const GemmParams& p, int64_t row, int c, float4 s) {
+  float e[4] = {s.x, s.y, s.z, s.w};
+  if (p.vec && c + 3 < p.n) {
+    if (p.bias != nullptr) {
+      const float4 b = load4(p.bias, p.bias_f32, c);
+      e[0] += b.x, e[1] += b.y, e[2] += b.z, e[3] += b.w;
+    }
+    if (p.pre != nullptr) store4(p.pre, p.pre_f32, row * p.ld_pre + c, make_float4(e[0], e[1], e[2], e[3]));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) e[j] = act_fwd(p.act, e[j]);
+    if (p.res != nullptr) {
+      const float4 r = load4(p.res, p.res_f32, row * p.ld_res + c);
+      e[0] += r.x, e[1] += r.y, e[2] += r.z, e[3] += r.w;
+    }
+    store4(p.out, p.out_f32, row * p.ld_out + c, make_float4(e[0], e[1], e[2], e[3]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (c + j < p.n) out1(p, row, c + j, e[j], p.bias != nullptr ? load1(p.bias, p.bias_f32, c + j) : 0.f);
+  }
+}
+
 // Joins two partial (maximum, sum of exponentials) of a row, base 2. A part
 // without a maximum (every entry excluded) adds its sum, 0 or NaN.
 __device__ __forceinline__ void stats_join(float& m, float& s, float2 q) {
@@ -495,16 +537,18 @@ struct Tiles {
     nk = (k + bk - 1) / bk;
     total = mt * nt * p.splits;
   }
-  // Tile t: groups of group_m row tiles, all column tiles of a group before the next.
-  __device__ __forceinline__ Tile at(const GemmParams& p, int t) const {
+  // Tile t: groups of group_m row tiles, all column tiles of a group before the
+  // next. Its range of k: the split's, or in a cluster that joins, part `part`.
+  __device__ __forceinline__ Tile at(const GemmParams& p, int t, int part, int parts) const {
     Tile x;
     x.sp = p.splits == 1 ? 0 : fast_div(t, mt * nt);
     const int r = t - x.sp * (mt * nt), per = p.group_m * nt, g = fast_div(r, per), q = r - g * per;
     const int rows = min(p.group_m, mt - g * p.group_m);
     x.tn = fast_div(q, rows);
     x.tm = g * p.group_m + q - x.tn * rows;
-    x.k0 = p.splits == 1 ? 0 : (int)((int64_t)nk * x.sp / p.splits);
-    x.k1 = p.splits == 1 ? nk : (int)((int64_t)nk * (x.sp + 1) / p.splits);
+    const int of = p.splits == 1 ? parts : p.splits, at = p.splits == 1 ? part : x.sp;
+    x.k0 = of == 1 ? 0 : (int)((int64_t)nk * at / of);
+    x.k1 = of == 1 ? nk : (int)((int64_t)nk * (at + 1) / of);
     return x;
   }
 };
@@ -526,7 +570,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   const int t = threadIdx.x, lane = t & 31;
   const int w = __shfl_sync(0xffffffffu, t >> 5, 0);  // uniform over the warp, also to the compiler
   const uint32_t rank = CG == 2 ? cta_rank() : 0u;
-  const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
+  constexpr bool JOIN = EPI == kEpiJoin;
+  const int parts = JOIN ? cluster_size() : 1, part = JOIN ? (int)cta_rank() : 0;  // ranges of k of a tile
+  const int unit = (int)blockIdx.x / (JOIN ? parts : CG);
+  const int units = JOIN ? 1 << 30 : (int)gridDim.x / CG;  // one tile per cluster
   if (t == 96) {  // the maps are on their way while the barriers and TMEM are set up
     prefetch_map(&amap);
     prefetch_map(&bmap);
@@ -566,8 +613,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     bool ok = true;
     int it = 0, s = 0;
     uint32_t ph = 0;  // stage and its phase
-    for (int tile = unit; tile < T.total && ok; tile += units) {
-      const Tile x = T.at(p, tile);
+    for (int tile = unit; tile < T.total && ok; tile = JOIN ? T.total : tile + units) {
+      const Tile x = T.at(p, tile, part, parts);
       const int m0 = x.tm * 128 * CG + (int)rank * 128;
       const int n0 = x.tn * p.bn + (CG == 2 ? (int)rank * (p.bn / 2) : 0);
       for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
@@ -618,8 +665,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       bool ok = true;
       int job = 0, s = 0;
       uint32_t ph = 0;
-      for (int tile = unit; tile < T.total && ok; tile += units) {
-        const Tile x = T.at(p, tile);
+      for (int tile = unit; tile < T.total && ok; tile = JOIN ? T.total : tile + units) {
+        const Tile x = T.at(p, tile, part, parts);
         const int k0 = x.k0, k1 = x.k1;
         for (int kb = k0; kb < k1; ++kb) {
           const bool first = kb == k0 || (FLUSH && ((kb - k0) & 1) == 0);
@@ -688,12 +735,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     int job = 0;
     Tile x, nx;
     if (unit < T.total) {
-      nx = T.at(p, unit);
+      nx = T.at(p, unit, part, parts);
       ahead_of(first_row(nx), nx.tn * p.bn + 32 * quarter);
     }
-    for (int tile = unit; tile < T.total; tile += units) {
+    for (int tile = unit; tile < T.total; tile = JOIN ? T.total : tile + units) {
       x = nx;
-      if (tile + units < T.total) nx = T.at(p, tile + units);
+      if (tile < T.total - units) nx = T.at(p, tile + units, part, parts);
       const int jobs = FLUSH ? (x.k1 - x.k0 + 1) / 2 : (x.k1 > x.k0 ? 1 : 0);
       const int nend = min(p.n, (x.tn + 1) * p.bn);
       float acc[FLUSH ? NC * 32 : 1];
@@ -777,7 +824,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         const bool more = c + 1 < NC && 32 * (ch + 4) < p.bn && col0 + 128 < nend;
         auto next = [&]() {
           if (more) ahead_of(row0, col0 + 128);
-          else if (tile + units < T.total) ahead_of(first_row(nx), nx.tn * p.bn + 32 * quarter);
+          else if (tile < T.total - units) ahead_of(first_row(nx), nx.tn * p.bn + 32 * quarter);
         };
         if (!live) {
           if (c == 0) next();
@@ -864,6 +911,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           } else {
             unit_store<false, 0>(&omap, col0, (int)row0, x.sp, v, has_res, rraw, stg, next);
           }
+        } else if constexpr (JOIN) {
+          float* mine = reinterpret_cast<float*>(sm) + (32 * (w & 3) + lane) * p.bn;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<float4*>(mine + 4 * ((8 * ch + j) ^ (lane & 7))) =
+                make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
         } else {
           // through shared memory, 16 columns at a time: 16 lanes per row, a row per half warp
           float* f = reinterpret_cast<float*>(stg);
@@ -909,12 +962,33 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   }
   umma::fence_before_sync();
   __syncthreads();
-  if constexpr (CG == 2) cluster_sync_all();
+  if constexpr (CG == 2 || JOIN) cluster_sync_all();
+  if constexpr (JOIN) {
+    // the stages, where the accumulators are now, have all been consumed
+    if (unit < T.total) {
+      const Tile x = T.at(p, unit, 0, 1);
+      const int row0 = x.tm * 128, rows = min(128, T.m - row0), groups = p.bn / 4;
+      const uint32_t base = umma::smem_u32(sm);
+      for (int i = part * kGemmThreads + t; i < rows * groups; i += parts * kGemmThreads) {
+        const int r = fast_div(i, groups), g = i - r * groups;
+        const int col = x.tn * p.bn + 4 * g;
+        if (col >= p.n) continue;
+        const uint32_t at = base + 16u * (uint32_t)(r * groups + (g ^ (r & 7)));
+        float4 sum = load_cluster4(map_cta(at, 0));
+        for (int k = 1; k < parts; ++k) {
+          const float4 q = load_cluster4(map_cta(at, k));
+          sum.x += q.x, sum.y += q.y, sum.z += q.z, sum.w += q.w;
+        }
+        out4(p, row0 + r, col, sum);
+      }
+    }
+    cluster_sync_all();  // nobody leaves while its shared memory is read
+  }
   umma::fence_after_sync();
   if (w == 2) gtmem_dealloc<CG>(tm, kCols);
 }
 
-// One CTA (or pair) per SM (or pair of SMs), at most one per tile.
+// One CTA (or pair) per SM (or pair of SMs), at most one per tile; one cluster per tile where they join.
 template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI, bool OF32>
 cudaError_t gemm_t(const GemmParams& p, const GemmMaps& m, cudaStream_t s) {
   using S = GemmSmem<CG, BN, NP>;
@@ -923,24 +997,27 @@ cudaError_t gemm_t(const GemmParams& p, const GemmMaps& m, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   const int64_t mt = (p.m + 128 * CG - 1) / (128 * CG), nt = (p.n + p.bn - 1) / p.bn;
   int64_t units = mt * nt * p.splits;
-  const int sms = sm_count_cached();
-  const int64_t most = (sms > 0 ? sms : 152) / CG;
-  if (units > most) units = most;
+  const int cluster = EPI == kEpiJoin ? p.join : CG;
+  if (EPI != kEpiJoin) {
+    const int sms = sm_count_cached();
+    const int64_t most = (sms > 0 ? sms : 152) / CG;
+    if (units > most) units = most;
+  }
   if (units <= 0) return cudaSuccess;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = CG;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(units * CG));
+  cfg.gridDim = dim3((unsigned)(units * cluster));
   cfg.blockDim = dim3(kGemmThreads);
   cfg.dynamicSmemBytes = S::kBytes;
   cfg.stream = s;
   cfg.attrs = attr;
-  cfg.numAttrs = CG == 2 ? 2 : 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, p, m.a, m.b, m.out, m.pre);
 }
 

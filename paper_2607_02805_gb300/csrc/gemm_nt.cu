@@ -20,6 +20,8 @@ cudaError_t launch_gemm_nt(const GemmCfg& c, const GemmParams& p, const GemmMaps
     return gemm_t<1, 128, 1, false, false, kEpiRows, false>(p, m, s);
   if (c.epi == kEpiRows && c.cg == 1 && c.bn == 128 && c.pieces == 1 && c.out_f32 == true)
     return gemm_t<1, 128, 1, false, false, kEpiRows, true>(p, m, s);
+  if (c.epi == kEpiJoin && c.cg == 1 && c.bn == 128 && c.pieces == 1)
+    return gemm_t<1, 128, 1, false, false, kEpiJoin, false>(p, m, s);
   return cudaErrorInvalidValue;
 }
 

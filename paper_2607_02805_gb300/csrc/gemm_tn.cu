@@ -16,6 +16,8 @@ cudaError_t launch_gemm_tn(const GemmCfg& c, const GemmParams& p, const GemmMaps
     return gemm_t<2, 256, 1, true, true, kEpiRows, false>(p, m, s);
   if (c.epi == kEpiRows && c.cg == 1 && c.bn == 128 && c.pieces == 1 && c.out_f32 == false)
     return gemm_t<1, 128, 1, true, true, kEpiRows, false>(p, m, s);
+  if (c.epi == kEpiJoin && c.cg == 1 && c.bn == 128 && c.pieces == 1)
+    return gemm_t<1, 128, 1, true, true, kEpiJoin, false>(p, m, s);
   return cudaErrorInvalidValue;
 }
 
