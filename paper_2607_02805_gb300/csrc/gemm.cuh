@@ -475,27 +475,28 @@ __device__ __forceinline__ void out1(const GemmParams& p, int64_t row, int col, 
   }
   store1(p.out, p.out_f32, orow * p.ld_out + col, v);
 }
-// Four columns of a row whose sums are complete, from the sums of a split.
+// Four columns of a row whose sums are complete (a split product), where rows
+// lie on 16-byte boundaries and all four are inside: with bias and residual
+// loaded before, or by itself and for the other rows too.
+__device__ __forceinline__ void finish4(const GemmParams& p, int64_t row, int c, float4 s, float4 b, float4 r) {
+  float e[4] = {s.x + b.x, s.y + b.y, s.z + b.z, s.w + b.w};
+  if (p.pre != nullptr) store4(p.pre, p.pre_f32, row * p.ld_pre + c, make_float4(e[0], e[1], e[2], e[3]));
+#pragma unroll
+  for (int j = 0; j < 4; ++j) e[j] = act_fwd(p.act, e[j]);
+  store4(p.out, p.out_f32, row * p.ld_out + c, make_float4(e[0] + r.x, e[1] + r.y, e[2] + r.z, e[3] + r.w));
+}
 __device__ __forceinline__ void out4(const GemmParams& p, int64_t row, int c, float4 s) {
-  float e[4] = {s.x, s.y, s.z, s.w};
   if (p.vec && c + 3 < p.n) {
-    if (p.bias != nullptr) {
-      const float4 b = load4(p.bias, p.bias_f32, c);
-      e[0] += b.x, e[1] += b.y, e[2] += b.z, e[3] += b.w;
-    }
-    if (p.pre != nullptr) store4(p.pre, p.pre_f32, row * p.ld_pre + c, make_float4(e[0], e[1], e[2], e[3]));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) e[j] = act_fwd(p.act, e[j]);
-    if (p.res != nullptr) {
-      const float4 r = load4(p.res, p.res_f32, row * p.ld_res + c);
-      e[0] += r.x, e[1] += r.y, e[2] += r.z, e[3] += r.w;
-    }
-    store4(p.out, p.out_f32, row * p.ld_out + c, make_float4(e[0], e[1], e[2], e[3]));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (c + j < p.n) out1(p, row, c + j, e[j], p.bias != nullptr ? load1(p.bias, p.bias_f32, c + j) : 0.f);
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 b = p.bias != nullptr ? load4(p.bias, p.bias_f32, c) : zero;
+    const float4 r = p.res != nullptr ? load4(p.res, p.res_f32, row * p.ld_res + c) : zero;
+    finish4(p, row, c, s, b, r);
+    return;
   }
+  const float e[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (c + j < p.n) out1(p, row, c + j, e[j], p.bias != nullptr ? load1(p.bias, p.bias_f32, c + j) : 0.f);
 }
 
 // Joins two partial (maximum, sum of exponentials) of a row, base 2. A part
@@ -962,27 +963,40 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   }
   umma::fence_before_sync();
   __syncthreads();
-  if constexpr (CG == 2 || JOIN) cluster_sync_all();
   if constexpr (JOIN) {
-    // the stages, where the accumulators are now, have all been consumed
-    if (unit < T.total) {
-      const Tile x = T.at(p, unit, 0, 1);
-      const int row0 = x.tm * 128, rows = min(128, T.m - row0), groups = p.bn / 4;
-      const uint32_t base = umma::smem_u32(sm);
-      for (int i = part * kGemmThreads + t; i < rows * groups; i += parts * kGemmThreads) {
-        const int r = fast_div(i, groups), g = i - r * groups;
-        const int col = x.tn * p.bn + 4 * g;
-        if (col >= p.n) continue;
-        const uint32_t at = base + 16u * (uint32_t)(r * groups + (g ^ (r & 7)));
-        float4 sum = load_cluster4(map_cta(at, 0));
-        for (int k = 1; k < parts; ++k) {
-          const float4 q = load_cluster4(map_cta(at, k));
-          sum.x += q.x, sum.y += q.y, sum.z += q.z, sum.w += q.w;
-        }
-        out4(p, row0 + r, col, sum);
+    // this thread's share of the tile; what its first four columns need besides the sums is loaded before the
+    // barrier
+    const bool any = unit < T.total;
+    const Tile x = any ? T.at(p, unit, 0, 1) : Tile{0, 0, 0, 0, 0};
+    const int row0 = x.tm * 128, rows = any ? min(128, T.m - row0) : 0, groups = p.bn / 4;
+    const uint32_t base = umma::smem_u32(sm);
+    const int first = part * kGemmThreads + t;
+    float4 b0 = make_float4(0.f, 0.f, 0.f, 0.f), r0 = b0;
+    const int fr = fast_div(first, groups), fcol = x.tn * p.bn + 4 * (first - fr * groups);
+    const bool early = p.vec && first < rows * groups && fcol + 3 < p.n;
+    if (early) {
+      if (p.bias != nullptr) b0 = load4(p.bias, p.bias_f32, fcol);
+      if (p.res != nullptr) r0 = load4(p.res, p.res_f32, (row0 + fr) * p.ld_res + fcol);
+    }
+    cluster_sync_all();
+    for (int i = first; i < rows * groups; i += parts * kGemmThreads) {
+      const int r = fast_div(i, groups), g = i - r * groups;
+      const int col = x.tn * p.bn + 4 * g;
+      if (col >= p.n) continue;
+      const uint32_t at = base + 16u * (uint32_t)(r * groups + (g ^ (r & 7)));
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (k >= parts) break;
+        const float4 q = load_cluster4(map_cta(at, k));
+        sum.x += q.x, sum.y += q.y, sum.z += q.z, sum.w += q.w;
       }
+      if (i == first && early) finish4(p, row0 + r, col, sum, b0, r0);
+      else out4(p, row0 + r, col, sum);
     }
     cluster_sync_all();  // nobody leaves while its shared memory is read
+  } else if constexpr (CG == 2) {
+    cluster_sync_all();
   }
   umma::fence_after_sync();
   if (w == 2) gtmem_dealloc<CG>(tm, kCols);
