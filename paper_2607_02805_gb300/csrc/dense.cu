@@ -93,60 +93,165 @@ __device__ __forceinline__ void pack_block(const PackParams& p, int64_t block) {
 int64_t pack_blocks(const PackParams& p) {
   return p.dst == nullptr ? 0 : (p.rows * ((p.ld_dst + 255) / 256) + kThreads / 32 - 1) / (kThreads / 32);
 }
-__device__ __forceinline__ void pack_load(float (&v)[8], const PackParams& p, int64_t row, int c) {
-  const int64_t at = row * p.ld + c;
-  if (p.ld % (p.src_f32 ? 4 : 8) == 0 && c + 8 <= p.cols) {
-    load8(v, p.src, p.src_f32, at);
-  } else {
+// One row's 256 columns from c0 on, to slot `to`: h, and in the backward h times
+// the row's scale g.
+__device__ __forceinline__ void pack_row(const PackParams& p, int64_t row, int64_t to, float g, int c0) {
+  const int lane = threadIdx.x & 31;
+  float v[8];
+  if (p.ld % (p.src_f32 ? 4 : 8) == 0) {
+    const int c = c0 + 8 * lane;
+    if (c >= p.ld_dst) return;
+    if (c + 8 <= p.cols) {
+      load8(v, p.src, p.src_f32, row * p.ld + c);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < p.cols ? load1(p.src, p.src_f32, at + j) : 0.f;
-  }
-}
-// The rows of the loss that count, each to its slot (pos), and zeros behind
-// them up to a whole tile of rows; in the backward a second copy scaled by the
-// row's weight, and zeros in the gradient of the rows that do not count.
-__global__ void __launch_bounds__(kThreads) k_pack_rows(const PackParams p) {
-  pdl_sync();
-  const int groups = (int)(p.ld_dst / 8);
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t row = idx / groups;
-  const int c = (int)(idx - row * groups) * 8;
-  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  int64_t to;
-  float g = 0.f;
-  if (row >= p.rows) {
-    const int n = *p.count;
-    to = n + (row - p.rows);
-    if (to >= ((n + 255) & ~255)) return;
-  } else {
-    to = p.pos[row];
-    if (to < 0) {
-      if (p.zero != nullptr) {
-        const int64_t at = row * p.cols + c;
-        const int f32 = p.src_f32;
-        if (p.cols % (f32 ? 4 : 8) == 0) {
-          if (c < p.cols) {  // cols is a multiple of 4 (fp32) or 8: whole halves
-            uint4* z = f32 ? reinterpret_cast<uint4*>(static_cast<float*>(p.zero) + at)
-                           : reinterpret_cast<uint4*>(static_cast<bf16*>(p.zero) + at);
-            z[0] = make_uint4(0, 0, 0, 0);
-            if (f32 && c + 4 < p.cols) z[1] = make_uint4(0, 0, 0, 0);
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (c + j < p.cols) store1(p.zero, f32, at + j, 0.f);
-        }
-      }
-      return;
+      for (int j = 0; j < 8; ++j) v[j] = c + j < p.cols ? load1(p.src, p.src_f32, row * p.ld + c + j) : 0.f;
     }
-    pack_load(v, p, row, c);
-    if (p.gscale != nullptr) g = p.gscale[to];
-  }
-  pack_store(p.dst + to * p.ld_dst + c, p.plane, p.pieces, v);
-  if (p.scaled != nullptr) {
+    pack_store(p.dst + to * p.ld_dst + c, p.plane, p.pieces, v);
+    if (p.scaled == nullptr) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] *= g;
     pack_store(p.scaled + to * p.ld_dst + c, p.plane, p.pieces, v);
+  } else {  // columns past `cols` are outside the operand's map: never read
+    const int c = c0 + lane;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + 32 * j < p.cols ? load1(p.src, p.src_f32, row * p.ld + c + 32 * j) : 0.f;
+    pack_store_strided(p.dst + to * p.ld_dst + c, p.plane, p.pieces, v, c, (int)p.cols);
+    if (p.scaled == nullptr) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= g;
+    pack_store_strided(p.scaled + to * p.ld_dst + c, p.plane, p.pieces, v, c, (int)p.cols);
+  }
+}
+// Zeros in a slot behind the last row that counts, and in the gradient of a row that does not.
+__device__ __forceinline__ void pack_zero_slot(const PackParams& p, int64_t to, int c0) {
+  const int c = c0 + 8 * (threadIdx.x & 31);
+  if (c >= p.ld_dst) return;
+  const float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  pack_store(p.dst + to * p.ld_dst + c, p.plane, p.pieces, v);
+  if (p.scaled != nullptr) pack_store(p.scaled + to * p.ld_dst + c, p.plane, p.pieces, v);
+}
+__device__ __forceinline__ void zero_gradient(const PackParams& p, int64_t row, int c0) {
+  const int lane = threadIdx.x & 31, f32 = p.src_f32;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int c = c0 + 32 * j + lane;
+    if (c < p.cols) store1(p.zero, f32, row * p.cols + c, 0.f);
+  }
+}
+
+// The rows of the loss that count, each to its slot (pos), and zeros behind
+// them up to a whole tile of rows; in the backward a second copy scaled by the
+// row's weight, and zeros in the gradient of the rows that do not count. A warp
+// per 256 columns of a row. Behind them the blocks of an operand to pack.
+__global__ void __launch_bounds__(kThreads) k_pack_rows(const PackParams p, const PackParams b, int64_t na) {
+  pdl_sync();
+  if (blockIdx.x >= na) {
+    pack_block(b, blockIdx.x - na);
+    return;
+  }
+  const int groups = (int)((p.ld_dst + 255) / 256);
+  const int64_t idx = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  const int64_t row = idx / groups;
+  const int c0 = (int)(idx - row * groups) * 256;
+  if (row >= p.rows) {
+    const int n = *p.count;
+    const int64_t to = n + (row - p.rows);
+    if (to < ((n + 255) & ~255)) pack_zero_slot(p, to, c0);
+    return;
+  }
+  const int to = p.pos[row];
+  if (to >= 0) pack_row(p, row, to, p.gscale != nullptr ? p.gscale[to] : 0.f, c0);
+  else if (p.zero != nullptr) zero_gradient(p, row, c0);
+}
+
+// Weight (times dloss) of row i of the loss, and its target: -1 where the row
+// does not count.
+__device__ __forceinline__ void loss_row(const LossRowsParams& p, int64_t i, float& wt, int64_t& tg) {
+  const bool in = i < p.rows;
+  tg = in ? p.target[i] : -1;
+  wt = in && p.weight != nullptr ? p.weight[i] : 1.f;
+  const float dl = in && p.dloss != nullptr ? p.dloss[i] : 1.f;
+  if (wt == 0.f || dl == 0.f || tg >= p.vocab || tg < 0) tg = -1;
+  wt *= dl;
+}
+// The slot's bookkeeping of a row that counts, the outputs of one that does not.
+__device__ __forceinline__ void loss_row_out(const LossRowsParams& p, int64_t i, int to, float wt, int64_t tg) {
+  if (tg >= 0) {
+    p.idx[to] = (int)i;
+    p.tgt[to] = (int)tg;
+    if (p.gscale != nullptr) {
+      p.gscale[to] = wt;
+      p.lse_c[to] = p.lse_in[i];
+    }
+  } else if (p.loss != nullptr) {
+    p.loss[i] = 0.f;
+    p.lse[i] = 0.f;
+  }
+}
+
+// Numbering and packing in one launch for up to kSmallRows rows: a CTA takes
+// eight rows and counts all rows before them by itself (at most eight loads per
+// thread, one latency), instead of waiting for a launch of its own.
+constexpr int kSmallRows = 2048;
+__global__ void __launch_bounds__(kThreads) k_loss_prep(const LossRowsParams l, const PackParams p, const PackParams b,
+                                                        int64_t na) {
+  pdl_sync();
+  if (blockIdx.x >= na) {
+    pack_block(b, blockIdx.x - na);
+    return;
+  }
+  __shared__ int wsum[kThreads / 32];
+  __shared__ int slot[8];
+  __shared__ float scale[8];
+  const int t = threadIdx.x, lane = t & 31, w = t >> 5;
+  const int rows = (int)l.rows, r0 = blockIdx.x * 8, before = min(r0, rows);
+  int n = 0;
+#pragma unroll
+  for (int j = 0; j < kSmallRows / kThreads; ++j) {
+    const int i = t + j * kThreads;
+    if (i < before) {
+      float wt;
+      int64_t tg;
+      loss_row(l, i, wt, tg);
+      n += tg >= 0 ? 1 : 0;
+    }
+  }
+  n = __reduce_add_sync(0xffffffffu, n);
+  if (lane == 0) wsum[w] = n;
+  __syncthreads();
+  int at = 0;  // rows that count before this CTA's
+#pragma unroll
+  for (int k = 0; k < kThreads / 32; ++k) at += wsum[k];
+  if (w == 0) {
+    float wt = 0.f;
+    int64_t tg = -1;
+    if (lane < 8) loss_row(l, r0 + lane, wt, tg);
+    const uint32_t m = __ballot_sync(0xffffffffu, tg >= 0);
+    const int to = at + __popc(m & ((1u << lane) - 1u));
+    if (lane < 8) {
+      slot[lane] = tg >= 0 ? to : -1;
+      scale[lane] = wt;
+      if (r0 + lane < rows) loss_row_out(l, r0 + lane, to, wt, tg);
+    }
+    if (lane == 0 && r0 < rows && r0 + 8 >= rows) {
+      l.count[0] = at + __popc(m);
+      l.count[1] = 0;  // the ticket of the forward's product
+    }
+  }
+  __syncthreads();
+  const int row = r0 + w;
+  for (int c0 = 0; c0 < p.ld_dst; c0 += 256) {
+    if (row >= rows) {  // these CTAs have counted every row; the first of them may also hold the last rows
+      int total = at;
+      for (int k = 0; k < 8; ++k) total += slot[k] >= 0 ? 1 : 0;
+      const int to = total + (row - rows);
+      if (to < ((total + 255) & ~255)) pack_zero_slot(p, to, c0);
+    } else if (slot[w] >= 0) {
+      pack_row(p, row, slot[w], scale[w], c0);
+    } else if (p.zero != nullptr) {
+      zero_gradient(p, row, c0);
+    }
   }
 }
 
@@ -387,22 +492,13 @@ __global__ void __launch_bounds__(1024) k_loss_rows(const LossRowsParams p, int6
   constexpr int F = 4;
   __shared__ int wsum[32];
   const int t = threadIdx.x, lane = t & 31, w = t >> 5;
-  // weight (times dloss) of row i, and its target: -1 where the row does not count
-  auto load = [&](int64_t i, float& wt, int64_t& tg) {
-    const bool in = i < p.rows;
-    tg = in ? p.target[i] : -1;
-    wt = in && p.weight != nullptr ? p.weight[i] : 1.f;
-    const float dl = in && p.dloss != nullptr ? p.dloss[i] : 1.f;
-    if (wt == 0.f || dl == 0.f || tg >= p.vocab || tg < 0) tg = -1;
-    wt *= dl;
-  };
   const int64_t begin = blockIdx.x * per, end = min(begin + per, p.rows);
   int n = 0;
   for (int64_t i = t; i < begin; i += 1024 * F) {
     float wt[F];
     int64_t tg[F];
 #pragma unroll
-    for (int j = 0; j < F; ++j) load(i + 1024 * j < begin ? i + 1024 * j : p.rows, wt[j], tg[j]);
+    for (int j = 0; j < F; ++j) loss_row(p, i + 1024 * j < begin ? i + 1024 * j : p.rows, wt[j], tg[j]);
 #pragma unroll
     for (int j = 0; j < F; ++j) n += tg[j] >= 0 ? 1 : 0;
   }
@@ -414,8 +510,7 @@ __global__ void __launch_bounds__(1024) k_loss_rows(const LossRowsParams p, int6
     const int64_t i = i0 + t;
     float wt;
     int64_t tg;
-    load(i, wt, tg);
-    const float ls = p.lse_in != nullptr && i < p.rows ? p.lse_in[i] : 0.f;
+    loss_row(p, i, wt, tg);
     const bool c = tg >= 0;
     const uint32_t m = __ballot_sync(0xffffffffu, c);
     __syncthreads();  // wsum has been read
@@ -427,65 +522,22 @@ __global__ void __launch_bounds__(1024) k_loss_rows(const LossRowsParams p, int6
     at += __reduce_add_sync(0xffffffffu, mine);
     if (i >= p.rows) continue;  // no barrier is skipped: the loop ends for the whole CTA with this round
     p.pos[i] = c ? to : -1;
-    if (c) {
-      p.idx[to] = (int)i;
-      p.tgt[to] = (int)tg;
-      if (p.gscale != nullptr) {
-        p.gscale[to] = wt;
-        p.lse_c[to] = ls;
-      }
-    } else if (p.loss != nullptr) {
-      p.loss[i] = 0.f;
-      p.lse[i] = 0.f;
-    }
+    loss_row_out(p, i, to, wt, tg);
   }
-  if (end == p.rows && t == 0) *p.count = at;
+  if (end == p.rows && t == 0) {
+    p.count[0] = at;
+    p.count[1] = 0;  // the ticket of the forward's product
+  }
 }
 
-// Joins a row's partial maxima and sums: 32 rows per CTA, 32 warps over the
-// partials in strides with eight loads in flight, then the warps in order.
+// The rows' partial maxima and sums joined, 32 rows per CTA.
 __global__ void __launch_bounds__(1024) k_loss_combine(const float2* part, int parts, int64_t rows_ld,
                                                        const float* at_target, const int* count, const int* idx,
                                                        const float* weight, float* loss, float* lse) {
   pdl_sync();
   __shared__ float2 red[32][33];
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int n = *count;
-  const int i0 = blockIdx.x * 32;
-  if (i0 >= n) return;
-  const bool live = i0 + lane < n;
-  float m = -INFINITY, s = 0.f;
-  if (live) {
-    const float2* q = part + i0 + lane;
-    for (int k = w; k < parts; k += 256) {
-      float2 v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        v[j] = k + 32 * j < parts ? q[(int64_t)(k + 32 * j) * rows_ld] : make_float2(-INFINITY, 0.f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) stats_join(m, s, v[j]);
-    }
-  }
-  red[lane][w] = make_float2(m, s);
-  __syncthreads();
-  // warp w joins the 32 parts of row w: a butterfly (each step joins the same two on both sides)
-  const float2 mine = red[w][lane];
-  m = mine.x, s = mine.y;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const float2 q = make_float2(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o));
-    stats_join(m, s, q);
-  }
-  const int i = i0 + w;
-  if (lane == 0 && i < n) {
-    const float l = (m + log2f(s)) * kLn2;
-    const int row = idx[i];
-    const float zt = at_target[i];
-    // a target that is the excluded entry has probability zero, also where no entry is left
-    const float d = zt == -INFINITY ? INFINITY : l - zt;
-    lse[row] = l;
-    loss[row] = weight != nullptr ? weight[row] * d : d;
-  }
+  const int n = *count, i0 = blockIdx.x * 32;
+  if (i0 < n) join_rows<32>(part, parts, rows_ld, at_target, n, i0, idx, weight, loss, lse, red);
 }
 
 template <typename T, int ROWS, int NC>
@@ -505,15 +557,21 @@ void vec_rows(const VecParams& p, bool vec, cudaStream_t s) {
 
 }  // namespace
 
+int64_t small_loss_rows() { return kSmallRows; }
 cudaError_t launch_pack(const PackParams& a, const PackParams& b, cudaStream_t s) {
   const int64_t na = pack_blocks(a), nb = pack_blocks(b);
   if (na + nb == 0) return cudaSuccess;
   launch_pdl(k_pack, dim3((unsigned)(na + nb)), dim3(kThreads), 0, s, a, b, na);
   return cudaGetLastError();
 }
-cudaError_t launch_pack_rows(const PackParams& p, cudaStream_t s) {
-  const int64_t n = (p.rows + 256) * (p.ld_dst / 8);
-  launch_pdl(k_pack_rows, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, p);
+cudaError_t launch_loss_prep(const LossRowsParams& l, const PackParams& p, const PackParams& b, cudaStream_t s) {
+  const int64_t na = (l.rows + 256 + 7) / 8;
+  launch_pdl(k_loss_prep, dim3((unsigned)(na + pack_blocks(b))), dim3(kThreads), 0, s, l, p, b, na);
+  return cudaGetLastError();
+}
+cudaError_t launch_pack_rows(const PackParams& p, const PackParams& b, cudaStream_t s) {
+  const int64_t n = (p.rows + 256) * ((p.ld_dst + 255) / 256), na = (n + kThreads / 32 - 1) / (kThreads / 32);
+  launch_pdl(k_pack_rows, dim3((unsigned)(na + pack_blocks(b))), dim3(kThreads), 0, s, p, b, na);
   return cudaGetLastError();
 }
 cudaError_t launch_prep(const DactParams& p, const PackParams& a, const PackParams& b, cudaStream_t s) {

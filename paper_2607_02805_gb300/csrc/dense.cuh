@@ -46,6 +46,12 @@ struct GemmParams {
   float* at_target;      // [rows]
   int64_t rows_ld;       // rows of `part`
   const float* lse;      // [rows] of the rows that count
+  // kEpiStats with few rows: the last CTA to end (by `ticket`, zero before)
+  // joins the partial statistics into the outputs; null: launch_loss_combine does
+  int* ticket;
+  const int* row_idx;
+  const float* row_weight;
+  float *loss_out, *lse_out;
   // Column sums that a warp without another role finishes on the side (the bias
   // gradient, from launch_prep's partial sums): sum_out[c] = sum of
   // sum_part[0 .. sum_ranges - 1][c]; null: none.
@@ -94,7 +100,7 @@ struct PackParams {
 };
 // One launch for two operands; dst null: nothing to pack.
 cudaError_t launch_pack(const PackParams& a, const PackParams& b, cudaStream_t s);
-cudaError_t launch_pack_rows(const PackParams& p, cudaStream_t s);
+cudaError_t launch_pack_rows(const PackParams& p, const PackParams& b, cudaStream_t s);  // b: one more operand
 
 // dz = dy * act'(pre) in `pieces` bf16 planes, and partial column sums of the
 // unrounded values per row range.
@@ -130,11 +136,14 @@ struct LossRowsParams {
   const int64_t* target;
   const float *weight, *dloss, *lse_in;
   int64_t rows, vocab;
-  int *count, *idx, *tgt, *pos;  // pos [rows]: slot, or -1
+  int *count, *idx, *tgt, *pos;  // count [2]: rows that count, and a zero; pos [rows]: slot, or -1
   float *gscale, *lse_c;
   float *loss, *lse;
 };
 cudaError_t launch_loss_rows(const LossRowsParams& p, cudaStream_t s);
+// launch_loss_rows and launch_pack_rows in one, for up to small_loss_rows() rows.
+int64_t small_loss_rows();
+cudaError_t launch_loss_prep(const LossRowsParams& l, const PackParams& p, const PackParams& b, cudaStream_t s);
 cudaError_t launch_loss_combine(const float2* part, int parts, int64_t rows_ld, const float* at_target,
                                 const int* count, const int* idx, const float* weight, float* loss, float* lse,
                                 int64_t rows, cudaStream_t s);

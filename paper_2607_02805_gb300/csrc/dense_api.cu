@@ -434,6 +434,9 @@ LossRows loss_rows_ws(const Loss& l, bool backward) {
   r.end = backward ? r.scaled + packed_bytes(l.dtype, r.rows, l.K) : r.scaled;
   return r;
 }
+// Up to this many rows the product's last CTA joins their statistics, 32 at a
+// time in about 2 us each; more rows get a launch of their own, a CTA per 32.
+constexpr int64_t kJoinRows = 64;
 struct LossFwdWs {
   Plan q;
   LossRows r;
@@ -491,10 +494,11 @@ LossBwdWs loss_bwd_ws(const Loss& l) {
   return w;
 }
 
-// h of the rows that count as an operand; in the backward (dh given) also the
-// scaled copy, and zeros in dh where a row does not count.
-cudaError_t gather_h(const Loss& l, const LossRows& r, const void* h, char* ws, void* dh, Operand* o, Operand* scaled,
-                     cudaStream_t s) {
+// Numbers the rows that count and gathers their h as an operand; in the
+// backward (dh given) also the scaled copy, and zeros in dh where a row does not
+// count. `pw`: w, if it has to be packed.
+cudaError_t prepare_rows(const Loss& l, const LossRows& r, const LossRowsParams& rp, const void* h, char* ws, void* dh,
+                         const PackParams& pw, Operand* o, Operand* scaled, cudaStream_t s) {
   PackParams p;
   memset(&p, 0, sizeof(p));
   p.src = h;
@@ -515,7 +519,9 @@ cudaError_t gather_h(const Loss& l, const LossRows& r, const void* h, char* ws, 
     *scaled = Operand{p.scaled, l.K, r.rows, p.ld_dst, p.pieces, p.plane};
   }
   *o = Operand{p.dst, l.K, r.rows, p.ld_dst, p.pieces, p.plane};
-  return api_launched(launch_pack_rows(p, s), s);
+  if (l.T <= small_loss_rows()) return api_launched(launch_loss_prep(rp, p, pw, s), s);
+  const cudaError_t e = api_launched(launch_loss_rows(rp, s), s);
+  return e != cudaSuccess ? e : api_launched(launch_pack_rows(p, pw, s), s);
 }
 
 int check_workspace(const void* ws, size_t have, size_t need, const char* fn) {
@@ -738,12 +744,11 @@ int bdscan_lm_loss_forward(const bdscan_lm_loss_dims* dims, const void* h, const
   rp.pos = (int*)(base + ws.r.pos);
   rp.loss = loss;
   rp.lse = lse;
-  cudaError_t e = api_launched(launch_loss_rows(rp, s), s);
   Operand a;
   PackParams pw;
   const Operand b = operand(&pw, l.dtype, w, l.V, l.K, l.K, base + ws.w);
-  if (e == cudaSuccess) e = gather_h(l, ws.r, h, base, nullptr, &a, nullptr, s);
-  if (e == cudaSuccess && pw.dst != nullptr) e = api_launched(launch_pack(pw, kNoPack, s), s);
+  cudaError_t e = prepare_rows(l, ws.r, rp, h, base, nullptr, pw, &a, nullptr, s);
+  const bool last_joins = l.T <= kJoinRows && ws.q.cfg.cg == 1;
   if (e == cudaSuccess) {
     Plan q = ws.q;
     q.cfg.epi = kEpiStats;
@@ -757,9 +762,16 @@ int bdscan_lm_loss_forward(const bdscan_lm_loss_dims* dims, const void* h, const
     p.rows_ld = ws.r.rows;
     p.out_last = (ws.parts - 1) * p.rows_ld + l.T - 1;
     p.out_extent = ws.parts * p.rows_ld;
+    if (last_joins) {
+      p.ticket = rp.count + 1;
+      p.row_idx = rp.idx;
+      p.row_weight = weight;
+      p.loss_out = loss;
+      p.lse_out = lse;
+    }
     e = run_product(q, p, a, b, 1, 0, l.T, s);
   }
-  if (e == cudaSuccess)
+  if (e == cudaSuccess && !last_joins)
     e = api_launched(launch_loss_combine((const float2*)(base + ws.part), ws.parts, ws.r.rows,
                                          (const float*)(base + ws.at), rp.count, rp.idx, weight, loss, lse, l.T, s),
                      s);
@@ -812,12 +824,10 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
   rp.pos = (int*)(base + ws.r.pos);
   rp.gscale = (float*)(base + ws.r.gscale);
   rp.lse_c = (float*)(base + ws.r.lse);
-  cudaError_t e = api_launched(launch_loss_rows(rp, s), s);
   Operand a, scaled;
   PackParams pw;
   const Operand b = operand(&pw, l.dtype, w, l.V, l.K, l.K, base + ws.w);
-  if (e == cudaSuccess) e = gather_h(l, ws.r, h, base, dh, &a, &scaled, s);
-  if (e == cudaSuccess && pw.dst != nullptr) e = api_launched(launch_pack(pw, kNoPack, s), s);
+  cudaError_t e = prepare_rows(l, ws.r, rp, h, base, dh, pw, &a, &scaled, s);
   const int64_t ld_dz = up(ws.piece, 8), ld_acc = up(l.K, 4);
   const int f32 = l.dtype == BDSCAN_F32;
   float* part = (float*)(base + ws.part);

@@ -511,6 +511,49 @@ __device__ __forceinline__ void stats_join(float& m, float& s, float2 q) {
   m = nm;
 }
 
+// Loss and log sum of up to 32 rows that count, from row i0 on, by a CTA of
+// WARPS warps: the partials in strides over the warps with eight loads in
+// flight, then the warps in order.
+template <int WARPS>
+__device__ __forceinline__ void join_rows(const float2* part, int parts, int64_t rows_ld, const float* at_target,
+                                          int n, int i0, const int* idx, const float* weight, float* loss, float* lse,
+                                          float2 (*red)[WARPS + 1]) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  float m = -INFINITY, s = 0.f;
+  if (i0 + lane < n) {
+    const float2* q = part + i0 + lane;
+    for (int k = w; k < parts; k += 8 * WARPS) {
+      float2 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        v[j] = k + WARPS * j < parts ? __ldcg(q + (int64_t)(k + WARPS * j) * rows_ld) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) stats_join(m, s, v[j]);
+    }
+  }
+  red[lane][w] = make_float2(m, s);
+  __syncthreads();
+  // a warp joins the parts of a row: a butterfly (each step joins the same two on both sides)
+  for (int r = w; r < 32 && i0 + r < n; r += WARPS) {
+    const float2 mine = lane < WARPS ? red[r][lane] : make_float2(-INFINITY, 0.f);
+    m = mine.x, s = mine.y;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const float2 q = make_float2(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o));
+      stats_join(m, s, q);
+    }
+    if (lane == 0) {
+      const int i = i0 + r, row = idx[i];
+      const float l = (m + log2f(s)) * kLn2;
+      const float zt = __ldcg(at_target + i);
+      // a target that is the excluded entry has probability zero, also where no entry is left
+      const float d = zt == -INFINITY ? INFINITY : l - zt;
+      lse[row] = l;
+      loss[row] = weight != nullptr ? weight[row] * d : d;
+    }
+  }
+}
+
 // a / b for 0 <= a, 0 < b: by a float reciprocal where that is off by one at
 // most (every role divides several times per tile).
 __device__ __forceinline__ int fast_div(int a, int b) {
@@ -1000,6 +1043,27 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   }
   umma::fence_after_sync();
   if (w == 2) gtmem_dealloc<CG>(tm, kCols);
+  if constexpr (EPI == kEpiStats && CG == 1) {
+    if (p.ticket != nullptr) {
+      // every CTA's partials are out (the epilogue warps' writes, then the barrier above, then the fence)
+      int* last = reinterpret_cast<int*>(&tslot);
+      __syncthreads();  // tslot has been read by all
+      if (t == 0) {
+        __threadfence();
+        *last = atomicAdd(p.ticket, 1) == (int)gridDim.x - 1;
+      }
+      __syncthreads();
+      if (*last) {
+        __threadfence();
+        auto red = reinterpret_cast<float2 (*)[kGemmThreads / 32 + 1]>(sm);  // the stages have been consumed
+        for (int i0 = 0; i0 < T.m; i0 += 32) {
+          join_rows<kGemmThreads / 32>(p.part, T.nt, p.rows_ld, p.at_target, T.m, i0, p.row_idx, p.row_weight,
+                                       p.loss_out, p.lse_out, red);
+          __syncthreads();
+        }
+      }
+    }
+  }
 }
 
 // One CTA (or pair) per SM (or pair of SMs), at most one per tile; one cluster per tile where they join.
