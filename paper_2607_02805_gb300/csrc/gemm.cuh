@@ -301,9 +301,8 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int c0, int
                : "memory");
   asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
 }
-// This thread's stores have read shared memory; are complete.
+// This thread's stores have read shared memory.
 __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory"); }
-__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory"); }
 
 // Columns H * 16 .. + 15 (fp32) or all 32 (bf16) of the chunk v to (col, row, z)
 // of `map`, plus the residual unit `raw` where `res`. `next` runs once raw has
@@ -634,12 +633,22 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     }
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
-  if (w == 2) gtmem_alloc<CG>(&tslot, kCols);
-  umma::fence_before_sync();
-  __syncthreads();
-  if constexpr (CG == 2) cluster_sync_all();
-  umma::fence_after_sync();
-  const uint32_t tm = tslot;
+  // The producer starts as soon as the barriers are there; the others also wait
+  // for TMEM.
+  if constexpr (CG == 2) {
+    __syncthreads();
+    cluster_sync_all();
+  } else {
+    __syncthreads();
+  }
+  uint32_t tm = 0;
+  if (w != 0) {
+    if (w == 2) gtmem_alloc<CG>(&tslot, kCols);
+    umma::fence_before_sync();
+    asm volatile("bar.sync 2, %0;\n" ::"n"(kGemmThreads - 32) : "memory");
+    umma::fence_after_sync();
+    tm = tslot;
+  }
   pdl_sync();
   const Tiles<CG> T(p, BK);
   if (w == 0) {
@@ -1001,7 +1010,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       if constexpr (!FLUSH) job += jobs;
     }
-    if ((EPI == kEpiOut || EPI == kEpiDz) && lane == 0) tma_store_wait();
+    // shared memory has been read; the stores themselves end with the grid
+    if ((EPI == kEpiOut || EPI == kEpiDz) && lane == 0) tma_store_wait_read();
     if (!ok && lane == 0) atomicExch(p.flag, 1);
   }
   umma::fence_before_sync();
