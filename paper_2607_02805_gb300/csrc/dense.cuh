@@ -13,6 +13,7 @@ namespace bds {
 constexpr int kEpiOut = 0;    // residual + act(acc + bias), or a split's partial sums, by TMA
 constexpr int kEpiRows = 3;   // the same by plain stores: unaligned or mapped rows
 constexpr int kEpiJoin = 4;   // the same, the ranges of k of a tile joined by a cluster
+constexpr int kEpiPair = 5;   // two products in one launch, each kEpiOut or kEpiRows without bias, activation and residual
 constexpr int kEpiStats = 1;  // running maximum and sum of a row's logits, and the target's logit
 constexpr int kEpiDz = 2;     // the loss's gradient at the logits
 
@@ -26,6 +27,8 @@ struct GemmParams {
   int splits;     // ranges of k, each with its own partial sums
   int join;       // kEpiJoin: CTAs of a tile's cluster, each with a range of k
   int group_m;    // row tiles walked together
+  int epi, a_mn;  // kEpiPair: kEpiOut or kEpiRows, and how A lies
+  int pair_extra; // kEpiPair, problem 0: tiles of problem 1 that take as long as one of its own
   // kEpiOut, kEpiRows: out[row_map ? row_map[i] : i][j]; kEpiOut has res of out's type
   const void* bias;
   const void* res;
@@ -77,6 +80,11 @@ struct GemmCfg {
 // Tensor maps of a product; `out` and `pre` for kEpiOut, `out` for kEpiDz.
 struct GemmMaps {
   CUtensorMap a, b, out, pre;
+};
+template <int N>
+struct GemmCall {
+  GemmMaps m[N];
+  GemmParams p[N];
 };
 // Sums of the partial sums of p.splits splits, then the output step of kEpiOut.
 cudaError_t launch_split_reduce(const GemmParams& p, const float* part, cudaStream_t s);

@@ -20,6 +20,7 @@ cudaError_t launch_gemm_tn(const GemmCfg&, const GemmParams&, const GemmMaps&, c
 cudaError_t launch_gemm_nt3(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
 cudaError_t launch_gemm_nn3(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
 cudaError_t launch_gemm_tn3(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
+cudaError_t launch_gemm_pair(const GemmCfg&, const GemmCall<2>&, cudaStream_t);
 cudaError_t launch_gemm_loss(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
 
 namespace {
@@ -105,13 +106,15 @@ size_t packed_bytes(int dtype, int64_t rows, int64_t cols) {
 struct Plan {
   GemmCfg cfg;
   int bn, splits, join, group_m;  // splits > 1: through memory; join > 1: in clusters
+  double cost;
 };
 constexpr int64_t kSms = 152;
 // The choice minimises a model of the product's time in clocks. A tile's step
 // of 64 k takes the larger of its MMAs (128 x 256 x 16 in 128 clocks per SM)
 // and its operands' way from L2 (64 bytes per clock and SM); a tile adds about
 // 400 clocks, and the epilogue of the last one 8 per column; the sums of a split
-// add a launch and their way to memory and back, a cluster that joins 2500 clocks.
+// add a launch and their way to memory and back, a cluster that joins 5000
+// clocks; a launch of pairs of CTAs starts 1500 clocks later.
 // Measured against the first
 // rule (256 x 256 tiles by pairs from a quarter of the pairs on, else 128 x 128
 // or 64, up to 16 splits): @@
@@ -143,7 +146,7 @@ Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split) {
         if (s > nk / 2) s = nk / 2 > 0 ? nk / 2 : 1;
         if (s > 64) s = 64;
         const int64_t w = (tiles * s + units - 1) / units;
-        double cost = 1500 + w * ((nk + s - 1) / s * step + 400) + 8.0 * bn;
+        double cost = (cg == 2 ? 3000 : 1500) + w * ((nk + s - 1) / s * step + 400) + 8.0 * bn;
         if (s > 1) cost += 5000 + 8.0 * s * m * n / 3000;
         if (best_cost < 0 || cost < best_cost) {
           best_cost = cost;
@@ -157,9 +160,9 @@ Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split) {
       }
       // a cluster per tile, as many as are resident together (fp32 by twos was slower than pairs without a
       // split: 2048 x 448 x 1792 training step 86 us against 82)
-      for (int j = pieces == 3 ? 4 : 2; cg == 1 && may_split && j <= 8; j *= 2) {
+      for (int j = 2; cg == 1 && pieces == 1 && may_split && j <= 8; j *= 2) {
         if (tiles > (j == 2 ? 76 : j == 4 ? 36 : 15) || nk < 2 * j) break;
-        const double cost = 1500 + (nk + j - 1) / j * step + 8.0 * bn + 2500;
+        const double cost = 1500 + (nk + j - 1) / j * step + 8.0 * bn + 5000;
         if (cost < best_cost) {
           best_cost = cost;
           best.cfg.cg = cg;
@@ -172,8 +175,82 @@ Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split) {
     }
   }
   best.cfg.pieces = pieces;
+  best.cost = best_cost;
   best.group_m = best.cfg.cg == 2 ? 8 : 12;
   return best;
+}
+// Two products in one launch (the gradients of a linear layer or of the head),
+// neither of them split: instead of a launch (about 6000 clocks with its start
+// and end) and two last waves. Problem 0 is the one with the longer tiles.
+struct PairPlan {
+  Plan q[2];
+  int extra;
+  double cost;
+};
+PairPlan plan_pair(const int64_t (&m)[2], const int64_t (&n)[2], const int64_t (&k)[2], int pieces) {
+  static const Instance bf16_any[] = {{2, 256}, {1, 128}}, f32_any[] = {{2, 128}, {1, 128}};
+  const Instance* inst = pieces == 3 ? f32_any : bf16_any;
+  PairPlan best;
+  memset(&best, 0, sizeof(best));
+  best.cost = -1;
+  for (int i = 0; i < 2; ++i) {
+    const int cg = inst[i].cg;
+    if (cg == 2 && m[0] <= 128 && m[1] <= 128) continue;
+    const double units = (double)(kSms / cg);
+    double tile[2][8], count[2][8];
+    for (int j = 0; j < 2; ++j)
+      for (int c = 0; c < 8; ++c) {
+        const int bn = 32 * (c + 1);
+        count[j][c] = 0;
+        if (bn > inst[i].bn || bn - 32 >= n[j]) continue;
+        const double mma = 2.0 * bn * (pieces == 3 ? 6 : 1), rows = m[j] < 128 ? (double)m[j] : 128.0;
+        const double load = 2.0 * pieces * (rows + bn / cg);
+        double step = mma > load ? mma : load;
+        if (step < 300) step = 300;
+        tile[j][c] = (k[j] + 63) / 64 * step + 400;
+        count[j][c] = (double)((m[j] + 128 * cg - 1) / (128 * cg)) * ((n[j] + bn - 1) / bn);
+      }
+    for (int c = 7; c >= 0; --c)
+      for (int d = 7; d >= 0; --d) {
+        if (count[0][c] == 0 || count[1][d] == 0 || tile[0][c] < tile[1][d]) continue;
+        const double first = (double)(int64_t)((count[0][c] + units - 1) / units) * tile[0][c];
+        const double all = (count[0][c] * tile[0][c] + count[1][d] * tile[1][d]) / units + 0.5 * tile[1][d];
+        const double one = count[0][c] + count[1][d] <= units ? tile[0][c] : all;
+        const double cost = (cg == 2 ? 3000 : 1500) + (first > one ? first : one) + 8.0 * 32 * (c > d ? c + 1 : d + 1);
+        if (best.cost >= 0 && cost >= best.cost) continue;
+        best.cost = cost;
+        const int bn[2] = {32 * (c + 1), 32 * (d + 1)};
+        for (int j = 0; j < 2; ++j) {
+          best.q[j].cfg.cg = cg;
+          best.q[j].cfg.bn = inst[i].bn;
+          best.q[j].cfg.pieces = pieces;
+          best.q[j].cfg.b_mn = true;
+          best.q[j].bn = bn[j];
+          best.q[j].splits = best.q[j].join = 1;
+          best.q[j].group_m = cg == 2 ? 8 : 12;
+        }
+        best.extra = (int)(tile[0][c] / tile[1][d] + 0.5);
+      }
+  }
+  return best;
+}
+// The gradient's products as the calls make them: dx = dz w and dw = dz^T x, one
+// launch where that is estimated to be faster.
+struct GradPlan {
+  Plan x, w;
+  PairPlan pair;
+  bool one, w_first;
+};
+GradPlan plan_grad(int64_t rows, int64_t in, int64_t out, int pieces) {
+  GradPlan g;
+  g.x = plan(rows, in, out, pieces, true);
+  g.w = plan(out, in, rows, pieces, true);
+  const PairPlan wx = plan_pair({out, rows}, {in, in}, {rows, out}, pieces);
+  const PairPlan xw = plan_pair({rows, out}, {in, in}, {out, rows}, pieces);
+  g.w_first = xw.cost < 0 || (wx.cost >= 0 && wx.cost < xw.cost);
+  g.pair = g.w_first ? wx : xw;
+  g.one = g.pair.cost >= 0 && g.pair.cost < g.x.cost + g.w.cost + 3000;
+  return g;
 }
 size_t split_bytes(const Plan& q, int64_t m, int64_t n) {
   return q.splits > 1 ? al256((size_t)q.splits * m * up(n, 4) * 4) : 0;
@@ -258,6 +335,31 @@ cudaError_t run_out(Plan q, bool a_mn, bool b_mn, GemmParams p, const Operand& a
   p.splits = q.splits;
   p.split_stride = g.split_stride;
   return api_launched(launch_split_reduce(p, part, s), s);
+}
+
+// Both products of a gradient in one launch: out (with dz [rows][out] as A) and w.
+cudaError_t run_pair(const GradPlan& g, GemmParams px, GemmParams pw, const Operand& dz, const Operand& bx,
+                     const Operand& bw, cudaStream_t s) {
+  GemmCall<2> call;
+  memset(&call, 0, sizeof(call));
+  const int bk = gemm_bk(g.x.cfg.pieces);
+  for (int j = 0; j < 2; ++j) {
+    const bool w = (j == 0) == g.w_first;
+    const Plan& q = g.pair.q[j];
+    GemmParams& p = call.p[j];
+    p = w ? pw : px;
+    p.bn = q.bn;
+    p.group_m = q.group_m;
+    p.a_mn = w;
+    p.pair_extra = g.pair.extra;
+    p.epi = p.row_map == nullptr && rows16(p.ld_out, p.out_f32) && rows16(p.n, p.out_f32) ? kEpiOut : kEpiRows;
+    p.out_last = p.row_map != nullptr ? p.out_extent - 1 : (p.m - 1) * p.ld_out + p.n - 1;
+    GemmMaps& m = call.m[j];
+    if (!(w ? encode(&m.a, dz, 64, bk) : encode(&m.a, dz, bk, 128)) || !encode(&m.b, w ? bw : bx, 64, bk))
+      return cudaErrorInvalidValue;
+    if (p.epi == kEpiOut && !encode_out(&m.out, p.out, p.out_f32, p.n, p.m, p.ld_out, 1, 0)) return cudaErrorInvalidValue;
+  }
+  return api_launched(launch_gemm_pair(g.pair.q[0].cfg, call, s), s);
 }
 
 // The operand as the products read it: where it lies, or packed into `ws` by
@@ -351,7 +453,7 @@ int dact_ranges(int64_t rows, int64_t cols) {
   return (int)(r < 1 ? 1 : r);
 }
 struct LinBwdWs {
-  Plan qx, qw;
+  GradPlan g;
   bool make_dz;  // dz differs from dy, or dy cannot be read by TMA
   size_t x, w, dz, sums, part, total;
   int ranges;
@@ -359,8 +461,7 @@ struct LinBwdWs {
 LinBwdWs lin_bwd_ws(const Lin& l) {
   LinBwdWs w;
   memset(&w, 0, sizeof(w));
-  w.qx = plan(l.T, l.K, l.N, l.pieces, true);
-  w.qw = plan(l.N, l.K, l.T, l.pieces, true);
+  w.g = plan_grad(l.T, l.K, l.N, l.pieces);
   w.make_dz = l.act != BDSCAN_ACT_NONE || l.out != BDSCAN_BF16 || !in_place(l.out, l.ld_y);
   size_t o = 0;
   w.x = o;
@@ -373,7 +474,7 @@ LinBwdWs lin_bwd_ws(const Lin& l) {
   w.ranges = dact_ranges(l.T, l.N);
   o += al256((size_t)w.ranges * l.N * 4);
   w.part = o;
-  const size_t a = split_bytes(w.qx, l.T, l.K), b = split_bytes(w.qw, l.N, l.K);
+  const size_t a = split_bytes(w.g.x, l.T, l.K), b = split_bytes(w.g.w, l.N, l.K);
   w.total = o + (a > b ? a : b);
   return w;
 }
@@ -463,7 +564,8 @@ LossFwdWs loss_fwd_ws(const Loss& l) {
 // the logits' gradient, in pieces of equal size.
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;
 struct LossBwdWs {
-  Plan qz, qh, qw;
+  Plan qz;
+  GradPlan g;
   LossRows r;
   size_t w, dz, acc, part, total;
   int64_t piece;  // entries, a multiple of 256 unless there is one piece
@@ -479,8 +581,7 @@ LossBwdWs loss_bwd_ws(const Loss& l) {
   w.piece = w.pieces == 1 ? l.V : up((l.V + w.pieces - 1) / w.pieces, 256);
   w.pieces = (int)((l.V + w.piece - 1) / w.piece);
   w.qz = plan(l.T, w.piece, l.K, l.pieces, false);
-  w.qh = plan(l.T, l.K, w.piece, l.pieces, true);
-  w.qw = plan(w.piece, l.K, l.T, l.pieces, true);
+  w.g = plan_grad(l.T, l.K, w.piece, l.pieces);
   size_t o = w.r.end;
   w.w = o;
   if (!in_place(l.dtype, l.K)) o += packed_bytes(l.dtype, l.V, l.K);
@@ -489,7 +590,7 @@ LossBwdWs loss_bwd_ws(const Loss& l) {
   w.acc = o;
   if (w.pieces > 1) o += al256((size_t)l.T * up(l.K, 4) * 4);
   w.part = o;
-  const size_t a = split_bytes(w.qh, l.T, l.K), b = split_bytes(w.qw, w.piece, l.K);
+  const size_t a = split_bytes(w.g.x, l.T, l.K), b = split_bytes(w.g.w, w.piece, l.K);
   w.total = o + (a > b ? a : b);
   return w;
 }
@@ -685,23 +786,25 @@ int bdscan_linear_backward(const bdscan_linear_dims* dims, const void* x, const 
     p->sum_f32 = l.dtype == BDSCAN_F32;
     sums = nullptr;
   };
+  GemmParams gx = geometry(ws.g.x, l.T, l.K, l.N, flag), gw = geometry(ws.g.w, l.N, l.K, l.T, flag);
+  gx.out = dx;
+  gw.out = dw;
+  gx.ld_out = gw.ld_out = l.K;
+  gx.out_f32 = gw.out_f32 = l.dtype == BDSCAN_F32;
+  gx.out_extent = l.T * l.K;
+  gw.out_extent = l.N * l.K;
+  if (e == cudaSuccess && dx != nullptr && dw != nullptr && ws.g.one) {
+    add_sums(ws.g.w_first ? &gw : &gx);
+    e = run_pair(ws.g, gx, gw, dz, ow, ox, s);
+    return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+  }
   if (e == cudaSuccess && dx != nullptr) {
-    GemmParams p = geometry(ws.qx, l.T, l.K, l.N, flag);
-    p.out = dx;
-    p.ld_out = l.K;
-    p.out_f32 = l.dtype == BDSCAN_F32;
-    p.out_extent = l.T * l.K;
-    add_sums(&p);
-    e = run_out(ws.qx, false, true, p, dz, ow, part, s);
+    add_sums(&gx);
+    e = run_out(ws.g.x, false, true, gx, dz, ow, part, s);
   }
   if (e == cudaSuccess && dw != nullptr) {
-    GemmParams p = geometry(ws.qw, l.N, l.K, l.T, flag);
-    p.out = dw;
-    p.ld_out = l.K;
-    p.out_f32 = l.dtype == BDSCAN_F32;
-    p.out_extent = l.N * l.K;
-    add_sums(&p);
-    e = run_out(ws.qw, true, true, p, dz, ox, part, s);
+    add_sums(&gw);
+    e = run_out(ws.g.w, true, true, gw, dz, ox, part, s);
   }
   return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
 }
@@ -853,33 +956,30 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
     p.out_last = (l.pieces - 1) * ws.r.rows * ld_dz + (ws.r.rows - 1) * ld_dz + n - 1;
     p.out_extent = l.pieces * ws.r.rows * ld_dz;
     e = run_product(q, p, a, bp, l.pieces, ws.r.rows * ld_dz, ws.r.rows, s);
-    // this piece's rows of dw
-    if (e == cudaSuccess) {
-      GemmParams g = geometry(ws.qw, n, l.K, ws.r.rows, flag);
-      g.rows_dev = rp.count;
-      g.rows_axis = 2;
-      g.out = (char*)dw + (size_t)v0 * l.K * elt;
-      g.ld_out = l.K;
-      g.out_f32 = f32;
-      g.out_extent = n * l.K;
-      e = run_out(ws.qw, true, true, g, dz, scaled, part, s);
-    }
-    // its part of dh: fp32 sums over the pieces, the last one writes dh
-    if (e == cudaSuccess) {
-      const bool last = i + 1 == ws.pieces;
-      GemmParams g = geometry(ws.qh, l.T, l.K, n, flag);
-      g.rows_dev = rp.count;
-      g.rows_axis = 1;
-      g.res = i > 0 ? acc : nullptr;
-      g.ld_res = ld_acc;
-      g.res_f32 = 1;
-      g.out = last ? dh : acc;
-      g.ld_out = last ? l.K : ld_acc;
-      g.out_f32 = last ? f32 : 1;
-      g.row_map = last ? rp.idx : nullptr;
-      g.row_scale = rp.gscale;
-      g.out_extent = last ? l.T * l.K : l.T * ld_acc;
-      e = run_out(ws.qh, false, true, g, dz, bp, part, s, !last);
+    // this piece's rows of dw, and its part of dh: fp32 sums over the pieces, the last one writes dh
+    const bool last = i + 1 == ws.pieces;
+    GemmParams gw = geometry(ws.g.w, n, l.K, ws.r.rows, flag), gh = geometry(ws.g.x, l.T, l.K, n, flag);
+    gw.rows_dev = gh.rows_dev = rp.count;
+    gw.rows_axis = 2;
+    gw.out = (char*)dw + (size_t)v0 * l.K * elt;
+    gw.ld_out = l.K;
+    gw.out_f32 = f32;
+    gw.out_extent = n * l.K;
+    gh.rows_axis = 1;
+    gh.res = i > 0 ? acc : nullptr;
+    gh.ld_res = ld_acc;
+    gh.res_f32 = 1;
+    gh.out = last ? dh : acc;
+    gh.ld_out = last ? l.K : ld_acc;
+    gh.out_f32 = last ? f32 : 1;
+    gh.row_map = last ? rp.idx : nullptr;
+    gh.row_scale = rp.gscale;
+    gh.out_extent = last ? l.T * l.K : l.T * ld_acc;
+    if (e == cudaSuccess && ws.pieces == 1 && ws.g.one) {
+      e = run_pair(ws.g, gh, gw, dz, bp, scaled, s);
+    } else {
+      if (e == cudaSuccess) e = run_out(ws.g.w, true, true, gw, dz, scaled, part, s);
+      if (e == cudaSuccess) e = run_out(ws.g.x, false, true, gh, dz, bp, part, s, !last);
     }
   }
   return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);

@@ -423,28 +423,29 @@ __device__ __forceinline__ void load_rows_ahead(RowsAhead& a, const GemmParams& 
   }
 }
 // The output step of rows row, row + 2, ... (those below row + left) of one
-// column, by plain stores. IN32: bias and pre are fp32; OF32: the output is.
-template <bool IN32, bool OF32>
+// column, by plain stores. IN32: bias and pre are fp32; OF32: the output is;
+// PLAIN: there is neither bias, pre, activation nor residual.
+template <bool IN32, bool OF32, bool PLAIN>
 __device__ __forceinline__ void out_rows(const GemmParams& p, int64_t row, int left, int col, float (&x)[16],
                                          const uint32_t (&res)[16], float bias) {
-  if (p.bias != nullptr) {
+  if (!PLAIN && p.bias != nullptr) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] += bias;
   }
-  if (p.pre != nullptr) {
+  if (!PLAIN && p.pre != nullptr) {
     const int64_t at = row * p.ld_pre + col;
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (2 * i < left) store1(p.pre, IN32, at + 2 * i * p.ld_pre, x[i]);
   }
-  if (p.act == kActSilu) {
+  if (!PLAIN && p.act == kActSilu) {
 #pragma unroll
     for (int i = 0; i < 16; i += 2) sigmoid_mul2<silu_arg>(x[i], x[i + 1]);
-  } else if (p.act == kActGelu) {
+  } else if (!PLAIN && p.act == kActGelu) {
 #pragma unroll
     for (int i = 0; i < 16; i += 2) sigmoid_mul2<gelu_arg>(x[i], x[i + 1]);
   }
-  if (p.res != nullptr) {
+  if (!PLAIN && p.res != nullptr) {
     const int sh = p.res_f32 ? 0 : 16;
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] += 2 * i < left ? __uint_as_float(res[i] << sh) : 0.f;
@@ -565,7 +566,7 @@ __device__ __forceinline__ int fast_div(int a, int b) {
 }
 // Extents of one call with the device's row count applied, and its tiles.
 struct Tile {
-  int tm, tn, k0, k1, sp;
+  int tm, tn, k0, k1, sp, q;  // q: problem of a paired launch
 };
 template <int CG>
 struct Tiles {
@@ -584,6 +585,7 @@ struct Tiles {
   // next. Its range of k: the split's, or in a cluster that joins, part `part`.
   __device__ __forceinline__ Tile at(const GemmParams& p, int t, int part, int parts) const {
     Tile x;
+    x.q = 0;
     x.sp = p.splits == 1 ? 0 : fast_div(t, mt * nt);
     const int r = t - x.sp * (mt * nt), per = p.group_m * nt, g = fast_div(r, per), q = r - g * per;
     const int rows = min(p.group_m, mt - g * p.group_m);
@@ -596,16 +598,62 @@ struct Tiles {
   }
 };
 
+// Which tiles a unit (a CTA or a pair) works on: every units-th; one in a cluster
+// that joins. A paired launch has two products: problem 0, whose tiles take
+// longer, is dealt first; where that leaves units with a tile less, those get
+// `pair_extra` tiles of problem 1 more (as many as fit beside one of problem 0)
+// before the rest is dealt to all.
+template <int CG, bool PAIR, bool JOIN>
+struct Sched {
+  Tiles<CG> T0, T1;
+  int unit, units, part, parts;
+  int own0, extra, rest, step;  // pair: tiles of problem 0, extra ones of 1, where the rest of 1 begins
+  __device__ __forceinline__ Sched(const GemmParams& p0, const GemmParams& p1, int bk, int unit_, int units_, int part_,
+                                   int parts_)
+      : T0(p0, bk), T1(PAIR ? Tiles<CG>(p1, bk) : T0), unit(unit_), units(units_), part(part_), parts(parts_) {
+    if constexpr (PAIR) {
+      const int n0 = T0.total, n1 = T1.total, full = n0 / units, r = n0 - full * units;
+      own0 = full + (unit < r ? 1 : 0);
+      step = units - r;
+      rest = r == 0 ? 0 : min(n1, p0.pair_extra * step);
+      extra = unit >= r && rest > unit - r ? (rest - (unit - r) + step - 1) / step : 0;
+    }
+  }
+  __device__ __forceinline__ const Tiles<CG>& of(const Tile& x) const { return PAIR && x.q ? T1 : T0; }
+  // The unit's i-th tile.
+  __device__ __forceinline__ bool get(const GemmParams& p0, const GemmParams& p1, int i, Tile& x) const {
+    if constexpr (!PAIR) {
+      if (JOIN && i > 0) return false;
+      const int t = unit + i * units;
+      if (t >= T0.total) return false;
+      x = T0.at(p0, t, part, parts);
+      return true;
+    } else {
+      if (i < own0) {
+        x = T0.at(p0, unit + i * units, 0, 1);
+        return true;
+      }
+      i -= own0;
+      const int t = i < extra ? unit - (units - step) + i * step : rest + unit + (i - extra) * units;
+      if (t >= T1.total) return false;
+      x = T1.at(p1, t, 0, 1);
+      x.q = 1;
+      return true;
+    }
+  }
+};
+
 template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI, bool OF32>
-__global__ void __launch_bounds__(kGemmThreads, 1)
-    k_gemm(const GemmParams p, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
-           const __grid_constant__ CUtensorMap omap, const __grid_constant__ CUtensorMap pmap) {
+__global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant__ GemmCall<EPI == kEpiPair ? 2 : 1> call) {
+  constexpr bool PAIR = EPI == kEpiPair;
+  const GemmParams &p = call.p[0], &p1 = call.p[PAIR ? 1 : 0];
   using S = GemmSmem<CG, BN, NP>;
   constexpr int ST = S::kStages, BK = S::kBk;
   constexpr bool FLUSH = NP == 3;
   constexpr uint32_t kCols = 2u * BN < 32u ? 32u : 2u * BN;
   // debug build: the last output element of the launch (uniform over the grid)
   if (!dguard(kSiteGemm, p.out_last, p.out_extent)) return;
+  if (PAIR && !dguard(kSiteGemm, p1.out_last, p1.out_extent)) return;
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t full[8], empty[8], accfull[2], accempty[2];
   __shared__ uint32_t tslot;
@@ -616,11 +664,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   constexpr bool JOIN = EPI == kEpiJoin;
   const int parts = JOIN ? cluster_size() : 1, part = JOIN ? (int)cta_rank() : 0;  // ranges of k of a tile
   const int unit = (int)blockIdx.x / (JOIN ? parts : CG);
-  const int units = JOIN ? 1 << 30 : (int)gridDim.x / CG;  // one tile per cluster
+  const int units = (int)gridDim.x / (JOIN ? parts : CG);
   if (t == 96) {  // the maps are on their way while the barriers and TMEM are set up
-    prefetch_map(&amap);
-    prefetch_map(&bmap);
-    if (EPI == kEpiOut || EPI == kEpiDz) prefetch_map(&omap);
+#pragma unroll
+    for (int q = 0; q < (PAIR ? 2 : 1); ++q) {
+      prefetch_map(&call.m[q].a);
+      prefetch_map(&call.m[q].b);
+    }
+    if (EPI == kEpiOut || EPI == kEpiDz) prefetch_map(&call.m[0].out);
   }
   if (t == 0) {
     for (int i = 0; i < ST; ++i) {
@@ -650,7 +701,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     tm = tslot;
   }
   pdl_sync();
-  const Tiles<CG> T(p, BK);
+  const Sched<CG, PAIR, JOIN> sched(p, p1, BK, unit, units, part, parts);
+  const Tiles<CG>& T = sched.T0;
   if (w == 0) {
     // ---------------- producer ----------------
     // Producer and issuer run their loops as whole warps, one elected lane
@@ -659,17 +711,20 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     // of k instead of 512, 4864 x 16384 x 1024.)
     const bool leader = elect_one();
     const uint32_t base = umma::smem_u32(sm);
-    // columns of B that a CTA loads: its share of the tile, MN-major in whole groups of 64
-    const int bcols = B_MN ? (p.bn / CG + 63) / 64 : p.bn / CG;
-    const uint32_t stage_tx = CG * NP * (S::kA + (uint32_t)bcols * (B_MN ? S::kCol : S::kRow));
     const uint32_t full0 = CG == 2 ? map_cta(umma::smem_u32(&full[0]), 0) : umma::smem_u32(&full[0]);
     bool ok = true;
     int it = 0, s = 0;
     uint32_t ph = 0;  // stage and its phase
-    for (int tile = unit; tile < T.total && ok; tile = JOIN ? T.total : tile + units) {
-      const Tile x = T.at(p, tile, part, parts);
+    Tile x;
+    for (int i = 0; ok && sched.get(p, p1, i, x); ++i) {
+      const GemmParams& pq = PAIR && x.q ? p1 : p;
+      const CUtensorMap *amap = &call.m[PAIR ? x.q : 0].a, *bmap = &call.m[PAIR ? x.q : 0].b;
+      const bool a_mn = PAIR ? pq.a_mn != 0 : A_MN;
+      // columns of B that a CTA loads: its share of the tile, MN-major in whole groups of 64
+      const int bcols = B_MN ? (pq.bn / CG + 63) / 64 : pq.bn / CG;
+      const uint32_t stage_tx = CG * NP * (S::kA + (uint32_t)bcols * (B_MN ? S::kCol : S::kRow));
       const int m0 = x.tm * 128 * CG + (int)rank * 128;
-      const int n0 = x.tn * p.bn + (CG == 2 ? (int)rank * (p.bn / 2) : 0);
+      const int n0 = x.tn * pq.bn + (CG == 2 ? (int)rank * (pq.bn / 2) : 0);
       for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
         if (!(ok = warp_wait(&empty[s], ph ^ 1))) break;
         if (leader) {
@@ -678,19 +733,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           const uint32_t a = base + (uint32_t)s * S::kStage, b = a + NP * S::kA;
 #pragma unroll
           for (int q = 0; q < NP; ++q) {
-            if constexpr (A_MN) {
+            if (a_mn) {
 #pragma unroll
               for (int j = 0; j < 2; ++j)
-                gtma_load<CG>(a + q * S::kA + j * S::kCol, &amap, m0 + 64 * j, kb * BK, q, bar);
+                gtma_load<CG>(a + q * S::kA + j * S::kCol, amap, m0 + 64 * j, kb * BK, q, bar);
             } else {
-              gtma_load<CG>(a + q * S::kA, &amap, kb * BK, m0, q, bar);
+              gtma_load<CG>(a + q * S::kA, amap, kb * BK, m0, q, bar);
             }
             if constexpr (B_MN) {
 #pragma unroll
               for (int j = 0; j < (BN / CG + 63) / 64; ++j)
-                if (j < bcols) gtma_load<CG>(b + q * S::kB + j * S::kCol, &bmap, n0 + 64 * j, kb * BK, q, bar);
+                if (j < bcols) gtma_load<CG>(b + q * S::kB + j * S::kCol, bmap, n0 + 64 * j, kb * BK, q, bar);
             } else {
-              gtma_load<CG>(b + q * S::kB, &bmap, kb * BK, n0, q, bar);
+              gtma_load<CG>(b + q * S::kB, bmap, kb * BK, n0, q, bar);
             }
           }
         }
@@ -707,19 +762,22 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     // ---------------- MMA issue ----------------
     if (rank == 0) {
       const bool leader = elect_one();
-      const uint32_t idesc = umma::idesc_bf16(128 * CG, (uint32_t)p.bn, A_MN, B_MN);
-      constexpr uint32_t astep = A_MN ? 2048u : 32u, bstep = B_MN ? 2048u : 32u;  // bytes per 16 elements of k
       const uint32_t base = umma::smem_u32(sm);
       auto desc = [](uint32_t at, bool mn) {
         if (mn) return umma::sdesc(at, S::kCol, 1024u);
         return BK == 64 ? umma::sdesc(at, 16u, 1024u) : umma::sdesc64(at, 16u, 512u);
       };
-      const uint64_t da0 = desc(base, A_MN), db0 = desc(base + NP * S::kA, B_MN);
+      const uint64_t db0 = desc(base + NP * S::kA, B_MN);
       bool ok = true;
       int job = 0, s = 0;
       uint32_t ph = 0;
-      for (int tile = unit; tile < T.total && ok; tile = JOIN ? T.total : tile + units) {
-        const Tile x = T.at(p, tile, part, parts);
+      Tile x;
+      for (int i = 0; ok && sched.get(p, p1, i, x); ++i) {
+        const GemmParams& pq = PAIR && x.q ? p1 : p;
+        const bool a_mn = PAIR ? pq.a_mn != 0 : A_MN;
+        const uint32_t idesc = umma::idesc_bf16(128 * CG, (uint32_t)pq.bn, a_mn, B_MN);
+        const uint32_t astep = a_mn ? 2048u : 32u, bstep = B_MN ? 2048u : 32u;  // bytes per 16 elements of k
+        const uint64_t da0 = desc(base, a_mn);
         const int k0 = x.k0, k1 = x.k1;
         for (int kb = k0; kb < k1; ++kb) {
           const bool first = kb == k0 || (FLUSH && ((kb - k0) & 1) == 0);
@@ -787,15 +845,15 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     bool ok = true;
     int job = 0;
     Tile x, nx;
-    if (unit < T.total) {
-      nx = T.at(p, unit, part, parts);
-      ahead_of(first_row(nx), nx.tn * p.bn + 32 * quarter);
-    }
-    for (int tile = unit; tile < T.total; tile = JOIN ? T.total : tile + units) {
+    bool another = sched.get(p, p1, 0, nx);
+    if (another) ahead_of(first_row(nx), nx.tn * p.bn + 32 * quarter);
+    for (int i = 0; another;) {
       x = nx;
-      if (tile < T.total - units) nx = T.at(p, tile + units, part, parts);
+      another = sched.get(p, p1, ++i, nx);
+      const GemmParams& pq = PAIR && x.q ? p1 : p;
+      const int rows_m = sched.of(x).m;
       const int jobs = FLUSH ? (x.k1 - x.k0 + 1) / 2 : (x.k1 > x.k0 ? 1 : 0);
-      const int nend = min(p.n, (x.tn + 1) * p.bn);
+      const int nend = min(pq.n, (x.tn + 1) * pq.bn);
       float acc[FLUSH ? NC * 32 : 1];
       if constexpr (FLUSH) {
 #pragma unroll
@@ -854,8 +912,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 #pragma unroll(FLUSH ? NC : 1)
       for (int c = 0; c < NC; ++c) {
         const int ch = 4 * c + quarter;
-        const int col0 = x.tn * p.bn + 32 * ch;
-        const bool live = 32 * ch < p.bn && col0 < nend;  // uniform over the warp
+        const int col0 = x.tn * pq.bn + 32 * ch;
+        const bool live = 32 * ch < pq.bn && col0 < nend;  // uniform over the warp
         float v[32];
         if constexpr (FLUSH) {
 #pragma unroll
@@ -877,7 +935,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         const bool more = c + 1 < NC && 32 * (ch + 4) < p.bn && col0 + 128 < nend;
         auto next = [&]() {
           if (more) ahead_of(row0, col0 + 128);
-          else if (tile < T.total - units) ahead_of(first_row(nx), nx.tn * p.bn + 32 * quarter);
+          else if (another) ahead_of(first_row(nx), nx.tn * p.bn + 32 * quarter);
         };
         if (!live) {
           if (c == 0) next();
@@ -927,7 +985,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           }
           auto none = [] {};
           if constexpr (NP == 1) {
-            unit_store<false, 0>(&omap, col0, (int)row0, 0, v, false, rraw, stg, none);
+            unit_store<false, 0>(&call.m[0].out, col0, (int)row0, 0, v, false, rraw, stg, none);
           } else {
 #pragma unroll
             for (int k = 0; k < 3; ++k) {  // the largest piece of what is left of the value
@@ -937,15 +995,15 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 q[i] = bf16_part(v[i]);
                 v[i] -= q[i];
               }
-              unit_store<false, 0>(&omap, col0, (int)row0, k, q, false, rraw, stg, none);
+              unit_store<false, 0>(&call.m[0].out, col0, (int)row0, k, q, false, rraw, stg, none);
             }
           }
         } else if constexpr (EPI == kEpiOut) {
           auto none = [] {};
           if (!IN32 && has_bias) add_bias(v, braw, p, col0);
           if (p.pre != nullptr) {
-            unit_store<IN32, 0>(&pmap, col0, (int)row0, 0, v, false, rraw, stg, none);
-            if (IN32 && col0 + 16 < p.n) unit_store<IN32, 1>(&pmap, col0 + 16, (int)row0, 0, v, false, rraw, stg, none);
+            unit_store<IN32, 0>(&call.m[0].pre, col0, (int)row0, 0, v, false, rraw, stg, none);
+            if (IN32 && col0 + 16 < p.n) unit_store<IN32, 1>(&call.m[0].pre, col0 + 16, (int)row0, 0, v, false, rraw, stg, none);
           }
           if (p.act == kActSilu) {
 #pragma unroll
@@ -956,13 +1014,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           }
           if constexpr (OF32) {
             const bool two = col0 + 16 < p.n;
-            unit_store<true, 0>(&omap, col0, (int)row0, x.sp, v, has_res, rraw, stg, [&]() {
+            unit_store<true, 0>(&call.m[0].out, col0, (int)row0, x.sp, v, has_res, rraw, stg, [&]() {
               if (!two) next();
               else if (has_res) load_res<true>(rraw, p, row0, col0 + 16);
             });
-            if (two) unit_store<true, 1>(&omap, col0 + 16, (int)row0, x.sp, v, has_res, rraw, stg, next);
+            if (two) unit_store<true, 1>(&call.m[0].out, col0 + 16, (int)row0, x.sp, v, has_res, rraw, stg, next);
           } else {
-            unit_store<false, 0>(&omap, col0, (int)row0, x.sp, v, has_res, rraw, stg, next);
+            unit_store<false, 0>(&call.m[0].out, col0, (int)row0, x.sp, v, has_res, rraw, stg, next);
           }
         } else if constexpr (JOIN) {
           float* mine = reinterpret_cast<float*>(sm) + (32 * (w & 3) + lane) * p.bn;
@@ -970,8 +1028,17 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           for (int j = 0; j < 8; ++j)
             *reinterpret_cast<float4*>(mine + 4 * ((8 * ch + j) ^ (lane & 7))) =
                 make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        } else if (PAIR && pq.epi == kEpiOut) {
+          const CUtensorMap* om = &call.m[PAIR ? x.q : 0].out;
+          auto none = [] {};
+          unit_store<OF32, 0>(om, col0, (int)row0, 0, v, false, rraw, stg, none);
+          if (OF32 && col0 + 16 < pq.n) unit_store<OF32, OF32 ? 1 : 0>(om, col0 + 16, (int)row0, 0, v, false, rraw, stg, none);
         } else {
           // through shared memory, 16 columns at a time: 16 lanes per row, a row per half warp
+          if (PAIR) {
+            if (lane == 0) tma_store_wait_read();
+            __syncwarp();
+          }
           float* f = reinterpret_cast<float*>(stg);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -988,8 +1055,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 const int r = 2 * i + (lane >> 4);
                 y[i] = f[r * 16 + 4 * ((cl >> 2) ^ ((r >> 1) & 3)) + (cl & 3)];
               }
-              out_rows<IN32, OF32>(p, row0 + (lane >> 4), (int)min((int64_t)32, T.m - row0) - (lane >> 4), col, y,
-                                   rahead.res[h], rahead.bias[h]);
+              out_rows<IN32, OF32, PAIR>(pq, row0 + (lane >> 4), (int)min((int64_t)32, rows_m - row0) - (lane >> 4),
+                                         col, y, rahead.res[h], rahead.bias[h]);
             }
             __syncwarp();
           }
@@ -1011,7 +1078,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       if constexpr (!FLUSH) job += jobs;
     }
     // shared memory has been read; the stores themselves end with the grid
-    if ((EPI == kEpiOut || EPI == kEpiDz) && lane == 0) tma_store_wait_read();
+    if ((EPI == kEpiOut || EPI == kEpiDz || PAIR) && lane == 0) tma_store_wait_read();
     if (!ok && lane == 0) atomicExch(p.flag, 1);
   }
   umma::fence_before_sync();
@@ -1020,7 +1087,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     // this thread's share of the tile; what its first four columns need besides the sums is loaded before the
     // barrier
     const bool any = unit < T.total;
-    const Tile x = any ? T.at(p, unit, 0, 1) : Tile{0, 0, 0, 0, 0};
+    const Tile x = any ? T.at(p, unit, 0, 1) : Tile{0, 0, 0, 0, 0, 0};
     const int row0 = x.tm * 128, rows = any ? min(128, T.m - row0) : 0, groups = p.bn / 4;
     const uint32_t base = umma::smem_u32(sm);
     const int first = part * kGemmThreads + t;
@@ -1078,14 +1145,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 
 // One CTA (or pair) per SM (or pair of SMs), at most one per tile; one cluster per tile where they join.
 template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI, bool OF32>
-cudaError_t gemm_t(const GemmParams& p, const GemmMaps& m, cudaStream_t s) {
+cudaError_t gemm_launch(const GemmCall<EPI == kEpiPair ? 2 : 1>& call, int64_t units, int cluster, cudaStream_t s) {
   using S = GemmSmem<CG, BN, NP>;
   auto kern = k_gemm<CG, BN, NP, A_MN, B_MN, EPI, OF32>;
   cudaError_t e = set_smem_cached(reinterpret_cast<const void*>(kern), (int)S::kBytes, 100);
   if (e != cudaSuccess) return e;
-  const int64_t mt = (p.m + 128 * CG - 1) / (128 * CG), nt = (p.n + p.bn - 1) / p.bn;
-  int64_t units = mt * nt * p.splits;
-  const int cluster = EPI == kEpiJoin ? p.join : CG;
   if (EPI != kEpiJoin) {
     const int sms = sm_count_cached();
     const int64_t most = (sms > 0 ? sms : 152) / CG;
@@ -1106,7 +1170,22 @@ cudaError_t gemm_t(const GemmParams& p, const GemmMaps& m, cudaStream_t s) {
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, p, m.a, m.b, m.out, m.pre);
+  return cudaLaunchKernelEx(&cfg, kern, call);
+}
+inline int64_t gemm_tiles(const GemmParams& p, int cg) {
+  return (int64_t)((p.m + 128 * cg - 1) / (128 * cg)) * ((p.n + p.bn - 1) / p.bn) * p.splits;
+}
+template <int CG, int BN, int NP, bool A_MN, bool B_MN, int EPI, bool OF32>
+cudaError_t gemm_t(const GemmParams& p, const GemmMaps& m, cudaStream_t s) {
+  GemmCall<1> call;
+  call.p[0] = p;
+  call.m[0] = m;
+  return gemm_launch<CG, BN, NP, A_MN, B_MN, EPI, OF32>(call, gemm_tiles(p, CG), EPI == kEpiJoin ? p.join : CG, s);
+}
+template <int CG, int BN, int NP>
+cudaError_t gemm_pair_t(const GemmCall<2>& call, cudaStream_t s) {
+  const int64_t tiles = gemm_tiles(call.p[0], CG) + gemm_tiles(call.p[1], CG);
+  return gemm_launch<CG, BN, NP, false, true, kEpiPair, NP == 3>(call, tiles, CG, s);
 }
 
 }  // namespace
