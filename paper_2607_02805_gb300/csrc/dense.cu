@@ -377,30 +377,47 @@ __global__ void __launch_bounds__(kThreads) k_colsum(const float* part, int rang
 }
 
 // ---- the sums of a split product ----
-// A thread adds four columns of one row over the splits, in order, and ends
-// them as the product's own output step would.
+// Four columns of one row per SLICES threads: each adds every SLICES-th split, in
+// order, with eight loads in flight, and the first adds the slices, in order, and
+// ends them as the product's own output step would. With one thread for all 64
+// splits of a small output the reads were a chain of latencies (11 us).
+template <int SLICES>
 __global__ void __launch_bounds__(kThreads) k_split_reduce(const GemmParams p, const float* part, int64_t ld) {
   pdl_sync();
+  constexpr int G = kThreads / SLICES;  // groups of four columns per CTA
+  __shared__ float4 red[SLICES][G];
   const int64_t groups = ld / 4;
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int slice = threadIdx.x / G, lg = threadIdx.x % G;
+  const int64_t idx = (int64_t)blockIdx.x * G + lg;
   const int64_t row = idx / groups;
   const int c = (int)(idx - row * groups) * 4;
   int m = p.m;
   if (p.rows_axis == 1) m = min(m, *p.rows_dev);
-  if (row >= m) return;
   if (!dguard(kSiteSplitReduce, p.out_last, p.out_extent)) return;
-  const float* at = part + row * ld + c;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = 0; i < p.splits; i += 8) {
-    float4 q[8];
+  if (row < m) {
+    const float* at = part + row * ld + c;
+    for (int i = slice; i < p.splits; i += 8 * SLICES) {
+      float4 q[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (i + j < p.splits) q[j] = *reinterpret_cast<const float4*>(at + (i + j) * p.split_stride);
+      for (int j = 0; j < 8; ++j)
+        q[j] = i + j * SLICES < p.splits ? *reinterpret_cast<const float4*>(at + (i + j * SLICES) * p.split_stride)
+                                         : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (i + j < p.splits) s.x += q[j].x, s.y += q[j].y, s.z += q[j].z, s.w += q[j].w;
+      for (int j = 0; j < 8; ++j) s.x += q[j].x, s.y += q[j].y, s.z += q[j].z, s.w += q[j].w;
+    }
   }
-  out4(p, row, c, s);
+  if constexpr (SLICES > 1) {
+    red[slice][lg] = s;
+    __syncthreads();
+    if (slice != 0) return;
+#pragma unroll
+    for (int k = 1; k < SLICES; ++k) {
+      const float4 q = red[k][lg];
+      s.x += q.x, s.y += q.y, s.z += q.z, s.w += q.w;
+    }
+  }
+  if (row < m) out4(p, row, c, s);
 }
 
 // ---- a linear layer of a few rows ----
@@ -588,7 +605,9 @@ cudaError_t launch_colsum(const float* part, int ranges, int64_t cols, void* out
 }
 cudaError_t launch_split_reduce(const GemmParams& p, const float* part, cudaStream_t s) {
   const int64_t ld = (p.n + 3) / 4 * 4, n = (int64_t)p.m * (ld / 4);
-  launch_pdl(k_split_reduce, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, p, part, ld);
+  auto grid = [&](int slices) { return dim3((unsigned)((n + kThreads / slices - 1) / (kThreads / slices))); };
+  if (p.splits > 8) launch_pdl(k_split_reduce<8>, grid(8), dim3(kThreads), 0, s, p, part, ld);
+  else launch_pdl(k_split_reduce<1>, grid(1), dim3(kThreads), 0, s, p, part, ld);
   return cudaGetLastError();
 }
 cudaError_t launch_linear_vec(const VecParams& p, cudaStream_t s) {

@@ -139,7 +139,8 @@ Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split) {
       const double a_rows = m < 128 ? (double)m : 128.0;
       const double mma = 2.0 * bn * products, load = 2.0 * pieces * (a_rows + bn / cg);
       double step = mma > load ? mma : load;
-      if (step < 300) step = 300;  // six stages in flight at a latency of about 1800 clocks
+      const double least = pieces == 3 ? 800 : 300;  // the stages in flight at a latency of about 1800 clocks
+      if (step < least) step = least;
       for (int waves = 1; waves <= 4; ++waves) {
         int64_t s = waves == 1 && !may_split ? 1 : units * waves / tiles;
         if (s < 1 || !may_split) s = 1;
@@ -206,7 +207,7 @@ PairPlan plan_pair(const int64_t (&m)[2], const int64_t (&n)[2], const int64_t (
         const double mma = 2.0 * bn * (pieces == 3 ? 6 : 1), rows = m[j] < 128 ? (double)m[j] : 128.0;
         const double load = 2.0 * pieces * (rows + bn / cg);
         double step = mma > load ? mma : load;
-        if (step < 300) step = 300;
+        if (step < (pieces == 3 ? 800 : 300)) step = pieces == 3 ? 800 : 300;
         tile[j][c] = (k[j] + 63) / 64 * step + 400;
         count[j][c] = (double)((m[j] + 128 * cg - 1) / (128 * cg)) * ((n[j] + bn - 1) / bn);
       }
@@ -337,7 +338,8 @@ cudaError_t run_out(Plan q, bool a_mn, bool b_mn, GemmParams p, const Operand& a
   return api_launched(launch_split_reduce(p, part, s), s);
 }
 
-// Both products of a gradient in one launch: out (with dz [rows][out] as A) and w.
+// Both products of a gradient in one launch: px (dz as it lies times w) and pw
+// (dz transposed times x).
 cudaError_t run_pair(const GradPlan& g, GemmParams px, GemmParams pw, const Operand& dz, const Operand& bx,
                      const Operand& bw, cudaStream_t s) {
   GemmCall<2> call;
@@ -770,7 +772,13 @@ int bdscan_linear_backward(const bdscan_linear_dims* dims, const void* x, const 
       dz = Operand{p.dz, l.N, l.T, p.ld_dz, l.pieces, p.plane};
     }
     p.part = sums;
-    e = api_launched(launch_prep(p, px, pw, s), s);
+    // A large operand is packed by a launch of its own: the gradient's pass leaves room for 24 warps per SM,
+    // packing alone has 64 (18 us against 36 for the 10016 x 1803 x of a layer of 560 outputs).
+    if (l.T * l.K + l.N * l.K > ((int64_t)1 << 24) && (px.dst != nullptr || pw.dst != nullptr)) {
+      e = api_launched(launch_pack(px, pw, s), s);
+      px = pw = kNoPack;
+    }
+    if (e == cudaSuccess) e = api_launched(launch_prep(p, px, pw, s), s);
     if (e == cudaSuccess && dbias != nullptr && !products)
       e = api_launched(launch_colsum(sums, ws.ranges, l.N, dbias, l.dtype == BDSCAN_F32, s), s);
   } else if (px.dst != nullptr || pw.dst != nullptr) {
@@ -975,6 +983,8 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
     gh.row_map = last ? rp.idx : nullptr;
     gh.row_scale = rp.gscale;
     gh.out_extent = last ? l.T * l.K : l.T * ld_acc;
+    // With several pieces the rows that count decide how the tiles of the two would have to be dealt, and only the
+    // device knows them: 16384 rows, half of them counting, took 1817 us as pairs and 1762 one after the other.
     if (e == cudaSuccess && ws.pieces == 1 && ws.g.one) {
       e = run_pair(ws.g, gh, gw, dz, bp, scaled, s);
     } else {

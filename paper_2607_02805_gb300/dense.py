@@ -26,31 +26,33 @@ def _code(dtype):
     return CODES[dtype]
 
 
-def _refuse(name, t, shape, dtype, device):
+def _refuse(name, t, shape, dtype, index):
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {shape}")
     if t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, not {dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, not on {'the CPU' if index < 0 else f'cuda:{index}'}")
     raise ValueError(f"{name} is not contiguous")
 
 
-def _whole(name, t, shape, dtype, device):
-    """Address of a contiguous tensor (None stays None). torch.Size compares with a tuple, dtypes are singletons."""
+# The checks run in every call: torch.Size compares with a tuple, dtypes are singletons, and the device's index is
+# cheaper to ask for than the device.
+def _whole(name, t, shape, dtype, index):
+    """Address of a contiguous tensor (None stays None)."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
-        _refuse(name, t, shape, dtype, device)
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+        _refuse(name, t, shape, dtype, index)
     return t.data_ptr()
 
 
-def _rows(name, t, shape, dtype, device):
+def _rows(name, t, shape, dtype, index):
     """Address and row stride of a 2-D tensor with contiguous rows."""
     if t is None:
         return None, 0
-    if t.shape != shape or t.dtype is not dtype or t.device != device:
-        _refuse(name, t, shape, dtype, device)
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+        _refuse(name, t, shape, dtype, index)
     ld, step = t.stride()
     if step != 1 and shape[1] > 1:
         raise ValueError(f"the rows of {name} are not contiguous")
@@ -62,6 +64,7 @@ class _Holder:
         self.device = torch.device(device)
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index if self.device.type == "cuda" else -1
         self._plans = {}  # (kind, row strides) -> (dims, workspace bytes)
         self._buf = {}
 
@@ -108,7 +111,7 @@ class Linear(_Holder):
     def forward(self, x, w, bias=None, residual=None, save_pre=False, out=None, stream=None):
         """y (the holder's buffer, or `out`); with save_pre the pre-activations
         are kept for backward(). Without an activation there is none to keep."""
-        dt, od, dev = self.dtype, self.out_dtype, self.device
+        dt, od, dev = self.dtype, self.out_dtype, self._index
         px, ld_x = _rows("x", x, self._x, dt, dev)
         pr, ld_r = _rows("residual", residual, self._y, od, dev)
         y = self._buffer("y", self._y, od) if out is None else out
@@ -126,7 +129,7 @@ class Linear(_Holder):
     def backward(self, x, w, dy, bias=True, need_dx=True, need_dw=True, stream=None):
         """(dx, dw, dbias) of <dy, y>; dbias None without `bias`. The
         residual's gradient is dy."""
-        dt, dev = self.dtype, self.device
+        dt, dev = self.dtype, self._index
         px, ld_x = _rows("x", x, self._x, dt, dev)
         py, ld_y = _rows("dy", dy, self._y, self.out_dtype, dev)
         pw = _whole("w", w, self._w, dt, dev)
@@ -157,10 +160,10 @@ class LmLoss(_Holder):
         return binding.make_lm_loss_dims(self.rows, self.d_model, self.vocab, _code(self.dtype), self.excluded, ld_h)
 
     def _inputs(self, h, w, target, weight):
-        ph, ld_h = _rows("h", h, self._h, self.dtype, self.device)
-        return ld_h, (ph, _whole("w", w, self._w, self.dtype, self.device),
-                      _whole("target", target, self._t, torch.int64, self.device),
-                      _whole("weight", weight, self._t, torch.float32, self.device))
+        ph, ld_h = _rows("h", h, self._h, self.dtype, self._index)
+        return ld_h, (ph, _whole("w", w, self._w, self.dtype, self._index),
+                      _whole("target", target, self._t, torch.int64, self._index),
+                      _whole("weight", weight, self._t, torch.float32, self._index))
 
     def forward(self, h, w, target, weight=None, stream=None):
         """(loss, lse), fp32 per row; zero at the rows that do not count."""
@@ -175,12 +178,12 @@ class LmLoss(_Holder):
     def backward(self, h, w, target, weight=None, dloss=None, lse=None, stream=None):
         """(dh, dw) of <dloss, loss>, from the last forward's lse or the one given."""
         ld_h, inputs = self._inputs(h, w, target, weight)
-        pd = _whole("dloss", dloss, self._t, torch.float32, self.device)
+        pd = _whole("dloss", dloss, self._t, torch.float32, self._index)
         if lse is None:
             lse = self._buf.get("lse")
             if lse is None:
                 raise ValueError("backward needs a forward or its lse")
-        pl = _whole("lse", lse, self._t, torch.float32, self.device)
+        pl = _whole("lse", lse, self._t, torch.float32, self._index)
         dh = self._buffer("dh", self._h, self.dtype)
         dw = self._buffer("dw", self._w, self.dtype)
         _, d, ws, size = self._plan(("backward", ld_h), binding.bdscan_lm_loss_backward_workspace_size)
