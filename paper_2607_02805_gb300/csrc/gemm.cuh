@@ -412,15 +412,33 @@ __device__ __forceinline__ void load_rows_ahead(RowsAhead& a, const GemmParams& 
     const int col = col0 + 16 * h + (lane & 15);
     if (p.bias != nullptr) a.bias[h] = col < p.n ? load1(p.bias, IN32, col) : 0.f;
     if (p.res == nullptr) continue;
+    const int64_t row = row0 + (lane >> 4);
+    const int left = col < p.n ? (int)min((int64_t)32, p.m - row) : 0;
+    const unsigned char* at = static_cast<const unsigned char*>(p.res) + ((row * p.ld_res + col) << (p.res_f32 ? 2 : 1));
+    const int64_t step = p.ld_res << (p.res_f32 ? 3 : 2);
+    if (p.res_f32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int64_t r = row0 + (lane >> 4) + 2 * i;
-      if (r >= p.m || col >= p.n) continue;
-      const int64_t at = r * p.ld_res + col;
-      a.res[h][i] = p.res_f32 ? static_cast<const uint32_t*>(p.res)[at]
-                              : (uint32_t)static_cast<const unsigned short*>(p.res)[at];
+      for (int i = 0; i < 16; ++i, at += step)
+        if (2 * i < left) a.res[h][i] = *reinterpret_cast<const uint32_t*>(at);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i, at += step)
+        if (2 * i < left) a.res[h][i] = *reinterpret_cast<const unsigned short*>(at);
     }
   }
+}
+// Every second row of one column from `at` on, those below `left`: addresses by
+// addition (with a 64-bit product each the rows took 36 instructions per element).
+template <bool F32>
+__device__ __forceinline__ void store_rows(void* p, int64_t row, int64_t ld, int col, int left, const float (&x)[16]) {
+  unsigned char* at = static_cast<unsigned char*>(p) + (row * ld + col) * (F32 ? 4 : 2);
+  const int64_t step = 2 * ld * (F32 ? 4 : 2);
+#pragma unroll
+  for (int i = 0; i < 16; ++i, at += step)
+    if (2 * i < left) {
+      if constexpr (F32) *reinterpret_cast<float*>(at) = x[i];
+      else *reinterpret_cast<bf16*>(at) = __float2bfloat16_rn(x[i]);
+    }
 }
 // The output step of rows row, row + 2, ... (those below row + left) of one
 // column, by plain stores. IN32: bias and pre are fp32; OF32: the output is;
@@ -433,10 +451,7 @@ __device__ __forceinline__ void out_rows(const GemmParams& p, int64_t row, int l
     for (int i = 0; i < 16; ++i) x[i] += bias;
   }
   if (!PLAIN && p.pre != nullptr) {
-    const int64_t at = row * p.ld_pre + col;
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (2 * i < left) store1(p.pre, IN32, at + 2 * i * p.ld_pre, x[i]);
+    store_rows<IN32>(p.pre, row, p.ld_pre, col, left, x);
   }
   if (!PLAIN && p.act == kActSilu) {
 #pragma unroll
@@ -457,10 +472,7 @@ __device__ __forceinline__ void out_rows(const GemmParams& p, int64_t row, int l
         store1(p.out, OF32, p.row_map[row + 2 * i] * p.ld_out + col, x[i] * p.row_scale[row + 2 * i]);
     return;
   }
-  const int64_t at = row * p.ld_out + col;
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (2 * i < left) store1(p.out, OF32, at + 2 * i * p.ld_out, x[i]);
+  store_rows<OF32>(p.out, row, p.ld_out, col, left, x);
 }
 // The same for one element (the last step of a split product).
 __device__ __forceinline__ void out1(const GemmParams& p, int64_t row, int col, float v, float bias) {
