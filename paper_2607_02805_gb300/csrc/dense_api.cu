@@ -111,7 +111,7 @@ struct Plan {
 constexpr int64_t kSms = 152;
 // The choice minimises a model of the product's time in clocks. A tile's step
 // of 64 k takes the larger of its MMAs (128 x 256 x 16 in 128 clocks per SM)
-// and its operands' way from L2 (64 bytes per clock and SM); a tile adds about
+// and its operands' way from L2 (80 bytes per clock and SM); a tile adds about
 // 400 clocks, and the epilogue of the last one 8 per column; the sums of a split
 // add a launch and their way to memory and back, a cluster that joins 5000
 // clocks; a launch of pairs of CTAs starts 1500 clocks later.
@@ -121,63 +121,76 @@ constexpr int64_t kSms = 152;
 struct Instance {
   int cg, bn;
 };
-Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split) {
+// Clocks of a tile's step of 64 k. bf16 B with rows along k (b_mn) is loaded in
+// whole groups of 64 columns. fp32 steps hold the two close together, and their
+// loads were seen at 64 bytes per clock.
+double step_clocks(int64_t m, int cg, int bn, int pieces, bool b_mn) {
+  const double mma = 2.0 * bn * (pieces == 3 ? 6 : 1);
+  const int64_t cols = b_mn && pieces == 1 ? up(bn / cg, 64) : bn / cg;
+  const double load = (pieces == 3 ? 6.0 : 1.6) * (double)((m < 128 ? m : 128) + cols);
+  const double least = pieces == 3 ? 800 : 300;  // the stages in flight at a latency of about 1800 clocks
+  const double step = mma > load ? mma : load;
+  return step > least ? step : least;
+}
+double product_clocks(const Plan& q, int64_t m, int64_t n, int64_t k) {  // q.cfg.b_mn set
+  const int cg = q.cfg.cg;
+  const int64_t nk = (k + 63) / 64, tiles = (m + 128 * cg - 1) / (128 * cg) * ((n + q.bn - 1) / q.bn);
+  const double step = step_clocks(m, cg, q.bn, q.cfg.pieces, q.cfg.b_mn);
+  if (q.join > 1) return 1500 + (nk + q.join - 1) / q.join * step + 8.0 * q.bn + 5000;
+  const int64_t waves = (tiles * q.splits + kSms / cg - 1) / (kSms / cg);
+  double cost = (cg == 2 ? 3000 : 1500) + waves * ((nk + q.splits - 1) / q.splits * step + 400) + 8.0 * q.bn;
+  if (q.splits > 1) cost += 5000 + 8.0 * q.splits * m * n / 3000;
+  return cost;
+}
+// Where the rows that count are known on the device only, m2 and k2 (not zero)
+// are the sizes with half of them, and the choice minimises the sum of both.
+Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split, bool b_mn, int64_t m2 = 0, int64_t k2 = 0) {
   static const Instance bf16_any[] = {{2, 256}, {1, 128}}, f32_any[] = {{2, 128}, {1, 128}};
   const Instance* inst = pieces == 3 ? f32_any : bf16_any;
-  const int count = 2;
-  const int64_t products = pieces == 3 ? 6 : 1, nk = (k + 63) / 64;
-  Plan best;
+  const int64_t nk = (k + 63) / 64;
+  Plan best, q;
   memset(&best, 0, sizeof(best));
-  double best_cost = -1;
-  for (int i = 0; i < count; ++i) {
+  best.cost = -1;
+  auto consider = [&]() {
+    q.cost = product_clocks(q, m, n, k);
+    if (m2 > 0) q.cost += product_clocks(q, m2, n, k2);
+    if (best.cost < 0 || q.cost < best.cost) best = q;
+  };
+  for (int i = 0; i < 2; ++i) {
     const int cg = inst[i].cg;
     if (cg == 2 && m <= 128) continue;
     const int64_t units = kSms / cg, mt = (m + 128 * cg - 1) / (128 * cg);
     for (int bn = inst[i].bn; bn >= 32; bn -= 32) {
       if (bn - 32 >= n) continue;
-      const int64_t nt = (n + bn - 1) / bn, tiles = mt * nt;
-      const double a_rows = m < 128 ? (double)m : 128.0;
-      const double mma = 2.0 * bn * products, load = 2.0 * pieces * (a_rows + bn / cg);
-      double step = mma > load ? mma : load;
-      const double least = pieces == 3 ? 800 : 300;  // the stages in flight at a latency of about 1800 clocks
-      if (step < least) step = least;
+      const int64_t tiles = mt * ((n + bn - 1) / bn);
+      memset(&q, 0, sizeof(q));
+      q.cfg.cg = cg;
+      q.cfg.bn = inst[i].bn;
+      q.cfg.pieces = pieces;
+      q.cfg.b_mn = b_mn;
+      q.bn = bn;
+      q.group_m = cg == 2 ? 8 : 12;
+      q.splits = q.join = 1;
+      consider();
+      if (!may_split) continue;
       for (int waves = 1; waves <= 4; ++waves) {
-        int64_t s = waves == 1 && !may_split ? 1 : units * waves / tiles;
-        if (s < 1 || !may_split) s = 1;
-        if (s > nk / 2) s = nk / 2 > 0 ? nk / 2 : 1;
+        int64_t s = units * waves / tiles;
+        if (s > nk / 2) s = nk / 2;
         if (s > 64) s = 64;
-        const int64_t w = (tiles * s + units - 1) / units;
-        double cost = (cg == 2 ? 3000 : 1500) + w * ((nk + s - 1) / s * step + 400) + 8.0 * bn;
-        if (s > 1) cost += 5000 + 8.0 * s * m * n / 3000;
-        if (best_cost < 0 || cost < best_cost) {
-          best_cost = cost;
-          best.cfg.cg = cg;
-          best.cfg.bn = inst[i].bn;
-          best.bn = bn;
-          best.splits = (int)s;
-          best.join = 1;
-        }
-        if (!may_split) break;
+        if (s <= 1) continue;
+        q.splits = (int)s;
+        consider();
       }
+      q.splits = 1;
       // a cluster per tile, as many as are resident together (fp32 by twos was slower than pairs without a
       // split: 2048 x 448 x 1792 training step 86 us against 82)
-      for (int j = 2; cg == 1 && pieces == 1 && may_split && j <= 8; j *= 2) {
+      for (int j = 2; cg == 1 && pieces == 1 && j <= 8; j *= 2) {
         if (tiles > (j == 2 ? 76 : j == 4 ? 36 : 15) || nk < 2 * j) break;
-        const double cost = 1500 + (nk + j - 1) / j * step + 8.0 * bn + 5000;
-        if (cost < best_cost) {
-          best_cost = cost;
-          best.cfg.cg = cg;
-          best.cfg.bn = inst[i].bn;
-          best.bn = bn;
-          best.splits = 1;
-          best.join = j;
-        }
+        q.join = j;
+        consider();
       }
     }
   }
-  best.cfg.pieces = pieces;
-  best.cost = best_cost;
-  best.group_m = best.cfg.cg == 2 ? 8 : 12;
   return best;
 }
 // Two products in one launch (the gradients of a linear layer or of the head),
@@ -204,11 +217,7 @@ PairPlan plan_pair(const int64_t (&m)[2], const int64_t (&n)[2], const int64_t (
         const int bn = 32 * (c + 1);
         count[j][c] = 0;
         if (bn > inst[i].bn || bn - 32 >= n[j]) continue;
-        const double mma = 2.0 * bn * (pieces == 3 ? 6 : 1), rows = m[j] < 128 ? (double)m[j] : 128.0;
-        const double load = 2.0 * pieces * (rows + bn / cg);
-        double step = mma > load ? mma : load;
-        if (step < (pieces == 3 ? 800 : 300)) step = pieces == 3 ? 800 : 300;
-        tile[j][c] = (k[j] + 63) / 64 * step + 400;
+        tile[j][c] = (k[j] + 63) / 64 * step_clocks(m[j], cg, bn, pieces, true) + 400;
         count[j][c] = (double)((m[j] + 128 * cg - 1) / (128 * cg)) * ((n[j] + bn - 1) / bn);
       }
     for (int c = 7; c >= 0; --c)
@@ -242,15 +251,17 @@ struct GradPlan {
   PairPlan pair;
   bool one, w_first;
 };
-GradPlan plan_grad(int64_t rows, int64_t in, int64_t out, int pieces) {
+GradPlan plan_grad(int64_t rows, int64_t in, int64_t out, int pieces, int64_t rows2 = 0) {
   GradPlan g;
-  g.x = plan(rows, in, out, pieces, true);
-  g.w = plan(out, in, rows, pieces, true);
-  const PairPlan wx = plan_pair({out, rows}, {in, in}, {rows, out}, pieces);
-  const PairPlan xw = plan_pair({rows, out}, {in, in}, {out, rows}, pieces);
+  g.x = plan(rows, in, out, pieces, true, true, rows2, out);
+  g.w = plan(out, in, rows, pieces, true, true, rows2 > 0 ? out : 0, rows2);
+  const int64_t r = rows2 > 0 ? (rows + rows2 + 1) / 2 : rows;
+  const PairPlan wx = plan_pair({out, r}, {in, in}, {r, out}, pieces);
+  const PairPlan xw = plan_pair({r, out}, {in, in}, {out, r}, pieces);
   g.w_first = xw.cost < 0 || (wx.cost >= 0 && wx.cost < xw.cost);
   g.pair = g.w_first ? wx : xw;
-  g.one = g.pair.cost >= 0 && g.pair.cost < g.x.cost + g.w.cost + 3000;
+  const double two = (g.x.cost + g.w.cost) / (rows2 > 0 ? 2 : 1) + 3000;
+  g.one = g.pair.cost >= 0 && g.pair.cost < two;
   return g;
 }
 size_t split_bytes(const Plan& q, int64_t m, int64_t n) {
@@ -436,7 +447,7 @@ LinFwdWs lin_fwd_ws(const Lin& l) {
   LinFwdWs w;
   memset(&w, 0, sizeof(w));
   if (l.T <= kVecRows) return w;
-  w.q = plan(l.T, l.N, l.K, l.pieces, true);
+  w.q = plan(l.T, l.N, l.K, l.pieces, true, false);
   size_t o = 0;
   w.x = o;
   if (!in_place(l.dtype, l.ld_x)) o += packed_bytes(l.dtype, l.T, l.K);
@@ -540,6 +551,14 @@ LossRows loss_rows_ws(const Loss& l, bool backward) {
 // Up to this many rows the product's last CTA joins their statistics, 32 at a
 // time in about 2 us each; more rows get a launch of their own, a CTA per 32.
 constexpr int64_t kJoinRows = 64;
+// How many rows count is known on the device only; any number is right. Tiles and
+// splits are chosen for all of them and for half, as a masked objective draws
+// them; of 129 to 256 rows for half alone, which then fit the 128 of a single CTA
+// (256 rows, half of them counting, over 50,021 entries: training 79 us with the
+// choice for both, 70 for half); fp32 for all alone (1000 rows, all counting: 169
+// us, for half 180).
+int64_t plan_rows(const Loss& l) { return l.pieces == 1 && l.T > 128 && l.T <= 256 ? 128 : l.T; }
+int64_t half_rows(const Loss& l) { return l.pieces == 3 || plan_rows(l) != l.T ? 0 : (l.T + 1) / 2; }
 struct LossFwdWs {
   Plan q;
   LossRows r;
@@ -549,7 +568,7 @@ struct LossFwdWs {
 LossFwdWs loss_fwd_ws(const Loss& l) {
   LossFwdWs w;
   memset(&w, 0, sizeof(w));
-  w.q = plan(l.T, l.V, l.K, l.pieces, false);
+  w.q = plan(plan_rows(l), l.V, l.K, l.pieces, false, false, half_rows(l), l.K);
   w.r = loss_rows_ws(l, false);
   size_t o = w.r.end;
   w.w = o;
@@ -562,9 +581,11 @@ LossFwdWs loss_fwd_ws(const Loss& l) {
   return w;
 }
 
-// Vocabulary entries per piece of the backward: as many as 256 MiB hold of
-// the logits' gradient, in pieces of equal size.
-constexpr int64_t kPieceBytes = (int64_t)256 << 20;
+// Vocabulary entries per piece of the backward: as many as 400 MiB hold of
+// the logits' gradient, in pieces of equal size. Fewer pieces have fewer last
+// waves and sums of dh (16384 rows over 50,304 entries: 64 MiB 2373 us, 128
+// 1915, 256 1796, 384 1779, 512 1738, 1024 1708), and each holds memory.
+constexpr int64_t kPieceBytes = (int64_t)400 << 20;
 struct LossBwdWs {
   Plan qz;
   GradPlan g;
@@ -582,8 +603,8 @@ LossBwdWs loss_bwd_ws(const Loss& l) {
   w.pieces = (int)((l.V + most - 1) / most);
   w.piece = w.pieces == 1 ? l.V : up((l.V + w.pieces - 1) / w.pieces, 256);
   w.pieces = (int)((l.V + w.piece - 1) / w.piece);
-  w.qz = plan(l.T, w.piece, l.K, l.pieces, false);
-  w.g = plan_grad(l.T, l.K, w.piece, l.pieces);
+  w.qz = plan(plan_rows(l), w.piece, l.K, l.pieces, false, false, half_rows(l), l.K);
+  w.g = plan_grad(plan_rows(l), l.K, w.piece, l.pieces, half_rows(l));
   size_t o = w.r.end;
   w.w = o;
   if (!in_place(l.dtype, l.K)) o += packed_bytes(l.dtype, l.V, l.K);

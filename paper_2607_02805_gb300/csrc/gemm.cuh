@@ -997,6 +997,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
             for (int i = 0; i < 32; ++i) v[i] = 0.f;
           }
           auto none = [] {};
+          // the product over rows reads them in steps of 64; rows behind those are read, by the product for dh, for
+          // rows that nobody keeps
+          if (row0 >= ((T.m + 63) & ~63)) continue;
           if constexpr (NP == 1) {
             unit_store<false, 0>(&call.m[0].out, col0, (int)row0, 0, v, false, rraw, stg, none);
           } else {
