@@ -65,8 +65,7 @@ struct GemmParams {
   int* flag;             // set by a bounded wait that gave up
 };
 
-// Elements of k per stage of the product with `pieces` bf16 pieces per operand.
-__host__ __device__ constexpr int gemm_bk(int pieces) { return pieces == 3 ? 32 : 64; }
+constexpr int kGemmBk = 64;  // elements of k per stage: one 128-byte swizzled row
 
 // Instances: CG 1 or 2 CTAs per tile, BN columns at most, `pieces` bf16 pieces
 // per operand (1: bf16 operands, 3: fp32 operands).

@@ -64,17 +64,16 @@ struct Operand {
   int64_t plane;
 };
 
-// Boxes of `box_inner` elements (a swizzled row of 128 or 64 bytes) x
-// `box_rows` rows; elements outside the operand read as zero.
-bool encode(CUtensorMap* m, const Operand& o, int box_inner, int box_rows) {
+// Boxes of 64 elements x `box_rows` rows, 128-byte swizzle; elements outside
+// the operand read as zero.
+bool encode(CUtensorMap* m, const Operand& o, int box_rows) {
   const cuuint64_t dims[3] = {(cuuint64_t)o.inner, (cuuint64_t)o.rows, (cuuint64_t)o.pieces};
   const int64_t plane = o.pieces > 1 ? o.plane : up(o.ld * 8, 8);  // one piece: never stepped over
   const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)plane * 2};
-  const cuuint32_t box[3] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows, 1u};
+  const cuuint32_t box[3] = {(cuuint32_t)kGemmBk, (cuuint32_t)box_rows, 1u};
   const cuuint32_t estr[3] = {1u, 1u, 1u};
   return tensor_map_encoder()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.base), dims, strides, box,
-                              estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              box_inner == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -122,12 +121,13 @@ struct Instance {
   int cg, bn;
 };
 // Clocks of a tile's step of 64 k. bf16 B with rows along k (b_mn) is loaded in
-// whole groups of 64 columns. fp32 steps hold the two close together, and their
-// loads were seen at 64 bytes per clock.
+// whole groups of 64 columns. fp32 loads count at 48 bytes per clock: over 30
+// fp32 cases that chose better than 64 or 80 (means of 49.5, 50.3 and 52.7 us),
+// since those steps hold the two closer together.
 double step_clocks(int64_t m, int cg, int bn, int pieces, bool b_mn) {
   const double mma = 2.0 * bn * (pieces == 3 ? 6 : 1);
   const int64_t cols = b_mn && pieces == 1 ? up(bn / cg, 64) : bn / cg;
-  const double load = (pieces == 3 ? 6.0 : 1.6) * (double)((m < 128 ? m : 128) + cols);
+  const double load = (pieces == 3 ? 8.0 : 1.6) * (double)((m < 128 ? m : 128) + cols);
   const double least = pieces == 3 ? 800 : 300;  // the stages in flight at a latency of about 1800 clocks
   const double step = mma > load ? mma : load;
   return step > least ? step : least;
@@ -289,9 +289,7 @@ cudaError_t run_product(const Plan& q, const GemmParams& p, const Operand& a, co
                         int64_t plane, int64_t out_rows, cudaStream_t s) {
   GemmMaps m;
   memset(&m, 0, sizeof(m));
-  const int bk = gemm_bk(q.cfg.pieces);
-  if (!(q.cfg.a_mn ? encode(&m.a, a, 64, bk) : encode(&m.a, a, bk, 128)) ||
-      !(q.cfg.b_mn ? encode(&m.b, b, 64, bk) : encode(&m.b, b, bk, q.bn / q.cfg.cg)))
+  if (!encode(&m.a, a, q.cfg.a_mn ? kGemmBk : 128) || !encode(&m.b, b, q.cfg.b_mn ? kGemmBk : q.bn / q.cfg.cg))
     return cudaErrorInvalidValue;
   const int epi = q.cfg.epi;
   if ((epi == kEpiOut || epi == kEpiDz) && !encode_out(&m.out, p.out, p.out_f32, p.n, out_rows, p.ld_out, planes, plane))
@@ -355,7 +353,6 @@ cudaError_t run_pair(const GradPlan& g, GemmParams px, GemmParams pw, const Oper
                      const Operand& bw, cudaStream_t s) {
   GemmCall<2> call;
   memset(&call, 0, sizeof(call));
-  const int bk = gemm_bk(g.x.cfg.pieces);
   for (int j = 0; j < 2; ++j) {
     const bool w = (j == 0) == g.w_first;
     const Plan& q = g.pair.q[j];
@@ -368,7 +365,7 @@ cudaError_t run_pair(const GradPlan& g, GemmParams px, GemmParams pw, const Oper
     p.epi = p.row_map == nullptr && rows16(p.ld_out, p.out_f32) && rows16(p.n, p.out_f32) ? kEpiOut : kEpiRows;
     p.out_last = p.row_map != nullptr ? p.out_extent - 1 : (p.m - 1) * p.ld_out + p.n - 1;
     GemmMaps& m = call.m[j];
-    if (!(w ? encode(&m.a, dz, 64, bk) : encode(&m.a, dz, bk, 128)) || !encode(&m.b, w ? bw : bx, 64, bk))
+    if (!encode(&m.a, dz, w ? kGemmBk : 128) || !encode(&m.b, w ? bw : bx, kGemmBk))
       return cudaErrorInvalidValue;
     if (p.epi == kEpiOut && !encode_out(&m.out, p.out, p.out_f32, p.n, p.m, p.ld_out, 1, 0)) return cudaErrorInvalidValue;
   }

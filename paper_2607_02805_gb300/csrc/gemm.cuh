@@ -13,22 +13,23 @@
 // accumulator while the MMAs fill the other (four warps per scheduler: the
 // epilogue is chains of latencies, and with two the GELU of a 16384 x 832 x
 // 3328 product took longer than its MMAs). A stage holds 64 elements of k
-// (fp32: 32) of both operands in the swizzled layouts of umma.cuh, rows along m
-// or n (K-major) or along k (MN-major), as the operand lies in memory: no operand
-// is transposed by a pass of its own.
+// of both operands in the 128-byte swizzled layouts of umma.cuh, rows along m or
+// n (K-major) or along k (MN-major), as the operand lies in memory: no operand is
+// transposed by a pass of its own.
 //
 // fp32 operands come as three bf16 pieces each (value = p0 + p1 + p2 to 24
 // bits); the six products with the largest terms are accumulated, smallest
-// first, and after every 64 elements of k (two stages of 32: with stages of 64
-// only two fit) the epilogue warps add the accumulator to fp32 registers: the tensor core's own accumulation truncates,
-// and over a long k that error would grow with k.
+// first, and after every 64 elements of k the epilogue warps add the accumulator
+// to fp32 registers: the tensor core's own accumulation truncates, and over a
+// long k that error would grow with k. A stage holds one piece of both operands,
+// three stages make a step of k. (With all pieces of 32 elements in a stage, in
+// rows of 64 bytes, the TMA unit was the limit: about a row per clock.)
 //
 // kEpiJoin splits a long k over a cluster: each of its CTAs sums a range of k of
 // the same tile, leaves its accumulators in shared memory, and ends a share of
 // the tile's elements from all of them through distributed shared memory, in
 // the order of the ranges. One launch instead of two and no way through memory
-// (32 x 3328 x 832 called
-// alone 12.0 us with a second launch, 9.3 so).
+// (32 x 3328 x 832 called alone 12.0 us with a second launch, 9.3 so).
 //
 // Every wait has a poll limit. A role that gives up sets the wait flag and
 // leaves its loop; the producer then waits for its copies in flight, and TMEM
@@ -50,20 +51,25 @@ namespace {
 constexpr int kEpiWarps = 16;
 constexpr int kGemmThreads = 128 + 32 * kEpiWarps;
 
+// The order in which a step's pieces are loaded: 1, 2, 0, so that the products
+// can begin with the smallest terms.
+template <int NP>
+constexpr int kFirstPiece = NP == 3 ? 1 : 0;
+
 template <int CG, int BN, int NP>
 struct GemmSmem {
-  static constexpr int kBk = gemm_bk(NP);                              // elements of k per stage
+  static constexpr int kBk = kGemmBk;                                  // elements of k per stage
   static constexpr uint32_t kRow = kBk * 2u;                           // bytes of a K-major row
   static constexpr uint32_t kA = 128u * kRow;                          // one piece of A
   static constexpr uint32_t kB = (uint32_t)(BN / CG) * kRow;           // one piece of B
   static constexpr uint32_t kCol = kBk * 128u;                         // 64 columns of an MN-major operand
-  static constexpr uint32_t kStage = NP * (kA + kB);
+  static constexpr uint32_t kStage = kA + kB;
   static constexpr uint32_t kEpi = kEpiWarps * 2048u;
   static constexpr int kStages = (int)((232448u - 1024u - 512u - kEpi) / kStage) > 8
                                      ? 8
                                      : (int)((232448u - 1024u - 512u - kEpi) / kStage);
   static constexpr uint32_t kBytes = kStages * kStage + kEpi + 1024u;
-  static_assert(kStages >= 2, "at least two stages");
+  static_assert(kStages > NP, "the stages of a step of k and one more");
 };
 
 // ---- cluster and two-CTA forms of the pieces of umma.cuh ----
@@ -735,34 +741,37 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
       const bool a_mn = PAIR ? pq.a_mn != 0 : A_MN;
       // columns of B that a CTA loads: its share of the tile, MN-major in whole groups of 64
       const int bcols = B_MN ? (pq.bn / CG + 63) / 64 : pq.bn / CG;
-      const uint32_t stage_tx = CG * NP * (S::kA + (uint32_t)bcols * (B_MN ? S::kCol : S::kRow));
+      const uint32_t stage_tx = CG * (S::kA + (uint32_t)bcols * (B_MN ? S::kCol : S::kRow));
       const int m0 = x.tm * 128 * CG + (int)rank * 128;
       const int n0 = x.tn * pq.bn + (CG == 2 ? (int)rank * (pq.bn / 2) : 0);
-      for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
+      const int steps = (x.k1 - x.k0) * NP;
+      for (int st = 0, kb = x.k0, q = kFirstPiece<NP>; st < steps; ++st, ++it) {
         if (!(ok = warp_wait(&empty[s], ph ^ 1))) break;
         if (leader) {
           if (rank == 0) bar_expect_tx(&full[s], stage_tx);
           const uint32_t bar = full0 + 8u * (uint32_t)s;
-          const uint32_t a = base + (uint32_t)s * S::kStage, b = a + NP * S::kA;
+          const uint32_t a = base + (uint32_t)s * S::kStage, b = a + S::kA;
+          if (a_mn) {
 #pragma unroll
-          for (int q = 0; q < NP; ++q) {
-            if (a_mn) {
+            for (int j = 0; j < 2; ++j) gtma_load<CG>(a + j * S::kCol, amap, m0 + 64 * j, kb * BK, q, bar);
+          } else {
+            gtma_load<CG>(a, amap, kb * BK, m0, q, bar);
+          }
+          if constexpr (B_MN) {
 #pragma unroll
-              for (int j = 0; j < 2; ++j)
-                gtma_load<CG>(a + q * S::kA + j * S::kCol, amap, m0 + 64 * j, kb * BK, q, bar);
-            } else {
-              gtma_load<CG>(a + q * S::kA, amap, kb * BK, m0, q, bar);
-            }
-            if constexpr (B_MN) {
-#pragma unroll
-              for (int j = 0; j < (BN / CG + 63) / 64; ++j)
-                if (j < bcols) gtma_load<CG>(b + q * S::kB + j * S::kCol, bmap, n0 + 64 * j, kb * BK, q, bar);
-            } else {
-              gtma_load<CG>(b + q * S::kB, bmap, kb * BK, n0, q, bar);
-            }
+            for (int j = 0; j < (BN / CG + 63) / 64; ++j)
+              if (j < bcols) gtma_load<CG>(b + j * S::kCol, bmap, n0 + 64 * j, kb * BK, q, bar);
+          } else {
+            gtma_load<CG>(b, bmap, kb * BK, n0, q, bar);
           }
         }
         if (++s == ST) s = 0, ph ^= 1;
+        if constexpr (NP == 3) {  // pieces 1, 2, 0 of a step of k
+          q = q == 2 ? 0 : q + 1;
+          if (q == 1) ++kb;
+        } else {
+          ++kb;
+        }
       }
     }
     // the stages in flight: consumed (their release has arrived in this CTA), or after a give-up at least landed
@@ -777,10 +786,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
       const bool leader = elect_one();
       const uint32_t base = umma::smem_u32(sm);
       auto desc = [](uint32_t at, bool mn) {
-        if (mn) return umma::sdesc(at, S::kCol, 1024u);
-        return BK == 64 ? umma::sdesc(at, 16u, 1024u) : umma::sdesc64(at, 16u, 512u);
+        return umma::sdesc(at, mn ? S::kCol : 16u, 1024u);
       };
-      const uint64_t db0 = desc(base + NP * S::kA, B_MN);
+      const uint64_t db0 = desc(base + S::kA, B_MN);
       bool ok = true;
       int job = 0, s = 0;
       uint32_t ph = 0;
@@ -793,34 +801,54 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
         const uint64_t da0 = desc(base, a_mn);
         const int k0 = x.k0, k1 = x.k1;
         for (int kb = k0; kb < k1; ++kb) {
-          const bool first = kb == k0 || (FLUSH && ((kb - k0) & 1) == 0);
-          const bool last = kb + 1 == k1 || (FLUSH && ((kb - k0) & 1) == 1);
+          const bool first = FLUSH || kb == k0, last = FLUSH || kb + 1 == k1;
           if (first) {
             if (!(ok = warp_wait(&accempty[job & 1], ((job >> 1) & 1) ^ 1))) break;
             umma::fence_after_sync();
           }
-          if (!(ok = warp_wait(&full[s], ph))) break;
           const uint32_t d = tm + (uint32_t)(job & 1) * BN;
-          const uint64_t da = umma::sdesc_adv(da0, (uint32_t)s * S::kStage), db = umma::sdesc_adv(db0, (uint32_t)s * S::kStage);
-          if (leader) {
-            if constexpr (NP == 1) {
+          // the four MMAs of 64 k from the A of stage sa and the B of stage sb
+          auto four = [&](int sa, int sb, bool fresh) {
+            const uint64_t da = umma::sdesc_adv(da0, (uint32_t)sa * S::kStage);
+            const uint64_t db = umma::sdesc_adv(db0, (uint32_t)sb * S::kStage);
+            if (leader) {
 #pragma unroll
               for (int q = 0; q < BK / 16; ++q)
-                gmma<CG>(d, umma::sdesc_adv(da, q * astep), umma::sdesc_adv(db, q * bstep), idesc, !first || q > 0);
-            } else {
-              constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};  // smallest terms first
-#pragma unroll
-              for (int c = 0; c < 6; ++c)
-#pragma unroll
-                for (int q = 0; q < BK / 16; ++q)
-                  gmma<CG>(d, umma::sdesc_adv(da, pa[c] * S::kA + q * astep),
-                           umma::sdesc_adv(db, pb[c] * S::kB + q * bstep), idesc, !first || c > 0 || q > 0);
+                gmma<CG>(d, umma::sdesc_adv(da, q * astep), umma::sdesc_adv(db, q * bstep), idesc, !fresh || q > 0);
             }
-            gcommit<CG>(&empty[s]);
-            if (last) gcommit<CG>(&accfull[job & 1]);
+          };
+          auto step = [&]() {  // the next stage once it is full
+            const int at = s;
+            ok = warp_wait(&full[s], ph);
+            if (++s == ST) s = 0, ph ^= 1;
+            return at;
+          };
+          if constexpr (NP == 1) {
+            const int s0 = step();
+            if (!ok) break;
+            four(s0, s0, first);
+            if (leader) gcommit<CG>(&empty[s0]);
+          } else {
+            const int s1 = step();
+            if (!ok) break;
+            four(s1, s1, true);
+            const int s2 = step();
+            if (!ok) break;
+            const int s0 = step();
+            if (!ok) break;
+            four(s2, s0, false);
+            four(s0, s2, false);
+            if (leader) gcommit<CG>(&empty[s2]);
+            four(s1, s0, false);
+            four(s0, s1, false);
+            if (leader) gcommit<CG>(&empty[s1]);
+            four(s0, s0, false);
+            if (leader) gcommit<CG>(&empty[s0]);
           }
-          if (++s == ST) s = 0, ph ^= 1;
-          if (last) ++job;
+          if (last) {
+            if (leader) gcommit<CG>(&accfull[job & 1]);
+            ++job;
+          }
         }
       }
       if (!ok && leader) atomicExch(p.flag, 1);
@@ -865,7 +893,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
       another = sched.get(p, p1, ++i, nx);
       const GemmParams& pq = PAIR && x.q ? p1 : p;
       const int rows_m = sched.of(x).m;
-      const int jobs = FLUSH ? (x.k1 - x.k0 + 1) / 2 : (x.k1 > x.k0 ? 1 : 0);
+      const int jobs = FLUSH ? x.k1 - x.k0 : (x.k1 > x.k0 ? 1 : 0);
       const int nend = min(pq.n, (x.tn + 1) * pq.bn);
       float acc[FLUSH ? NC * 32 : 1];
       if constexpr (FLUSH) {

@@ -36,13 +36,6 @@ __host__ __device__ constexpr uint64_t sdesc(uint32_t saddr, uint32_t lbo, uint3
          ((uint64_t)((sbo >> 4) & 0x3FFFu) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 
-// The same for rows of 64 bytes (32 bf16 of K, K-major) with the 64-byte
-// swizzle, layout type 4: 16-byte chunk j of row r sits at chunk
-// j ^ ((r >> 1) & 3), 8-row groups are 512 bytes apart.
-__host__ __device__ constexpr uint64_t sdesc64(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
-  return (sdesc(saddr, lbo, sbo) & ~((uint64_t)7 << 61)) | ((uint64_t)4 << 61);
-}
-
 // The descriptor d with its start address advanced by `bytes` (a multiple of
 // 16; the advanced address stays below 256 KB, so the 14-bit field does not
 // carry): one add in the MMA issue loops instead of rebuilding every field.
