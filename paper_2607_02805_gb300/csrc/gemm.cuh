@@ -669,12 +669,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
   using S = GemmSmem<CG, BN, NP>;
   constexpr int ST = S::kStages, BK = S::kBk;
   constexpr bool FLUSH = NP == 3;
-  constexpr uint32_t kCols = 2u * BN < 32u ? 32u : 2u * BN;
+  constexpr int NA = BN <= 128 ? 4 : 2;  // accumulators in turn
+  constexpr uint32_t kCols = NA * BN;
   // debug build: the last output element of the launch (uniform over the grid)
   if (!dguard(kSiteGemm, p.out_last, p.out_extent)) return;
   if (PAIR && !dguard(kSiteGemm, p1.out_last, p1.out_extent)) return;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ uint64_t full[8], empty[8], accfull[2], accempty[2];
+  __shared__ uint64_t full[8], empty[8], accfull[NA], accempty[NA];
   __shared__ uint32_t tslot;
   unsigned char* sm = align1024(smem_raw);
   const int t = threadIdx.x, lane = t & 31;
@@ -697,7 +698,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
       umma::bar_init(&full[i], 1);
       umma::bar_init(&empty[i], 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < NA; ++i) {
       umma::bar_init(&accfull[i], 1);
       umma::bar_init(&accempty[i], kEpiWarps * CG);
     }
@@ -790,7 +791,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
       };
       const uint64_t db0 = desc(base + S::kA, B_MN);
       bool ok = true;
-      int job = 0, s = 0;
+      uint32_t job = 0;
+      int s = 0;
       uint32_t ph = 0;
       Tile x;
       for (int i = 0; ok && sched.get(p, p1, i, x); ++i) {
@@ -803,10 +805,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
         for (int kb = k0; kb < k1; ++kb) {
           const bool first = FLUSH || kb == k0, last = FLUSH || kb + 1 == k1;
           if (first) {
-            if (!(ok = warp_wait(&accempty[job & 1], ((job >> 1) & 1) ^ 1))) break;
+            if (!(ok = warp_wait(&accempty[job % NA], ((job / NA) & 1) ^ 1))) break;
             umma::fence_after_sync();
           }
-          const uint32_t d = tm + (uint32_t)(job & 1) * BN;
+          const uint32_t d = tm + job % NA * BN;
           // the four MMAs of 64 k from the A of stage sa and the B of stage sb
           auto four = [&](int sa, int sb, bool fresh) {
             const uint64_t da = umma::sdesc_adv(da0, (uint32_t)sa * S::kStage);
@@ -846,7 +848,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
             if (leader) gcommit<CG>(&empty[s0]);
           }
           if (last) {
-            if (leader) gcommit<CG>(&accfull[job & 1]);
+            if (leader) gcommit<CG>(&accfull[job % NA]);
             ++job;
           }
         }
@@ -884,7 +886,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
     };
     auto first_row = [&](const Tile& x) { return (int64_t)x.tm * 128 * CG + rank * 128 + 32 * (w & 3); };
     bool ok = true;
-    int job = 0;
+    uint32_t job = 0;
     Tile x, nx;
     bool another = sched.get(p, p1, 0, nx);
     if (another) ahead_of(first_row(nx), nx.tn * p.bn + 32 * quarter);
@@ -918,18 +920,18 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
           }
         }
         for (int j = 0; j < jobs; ++j, ++job) {
-          if (!(ok = warp_wait(&accfull[job & 1], (job >> 1) & 1))) break;
+          if (!(ok = warp_wait(&accfull[job % NA], (job / NA) & 1))) break;
           umma::fence_after_sync();
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
             float v[32];
-            umma::tmem_ld32(lanes + (uint32_t)(job & 1) * BN + 32u * (uint32_t)(4 * c + quarter), v);
+            umma::tmem_ld32(lanes + job % NA * BN + 32u * (uint32_t)(4 * c + quarter), v);
 #pragma unroll
             for (int i = 0; i < 32; ++i) acc[c * 32 + i] += v[i];
           }
           umma::fence_before_sync();
           __syncwarp();
-          if (lane == 0) leader_arrive<CG>(&accempty[job & 1]);
+          if (lane == 0) leader_arrive<CG>(&accempty[job % NA]);
         }
       }
       const int64_t row0 = first_row(x), row = row0 + lane;
@@ -944,12 +946,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
       }
       if constexpr (!FLUSH) {
         if (jobs > 0) {
-          ok = warp_wait(&accfull[job & 1], (job >> 1) & 1);
+          ok = warp_wait(&accfull[job % NA], (job / NA) & 1);
           umma::fence_after_sync();
         }
       }
       if (!ok) break;
-      const uint32_t tacc = lanes + (uint32_t)(job & 1) * BN;
+      const uint32_t tacc = lanes + job % NA * BN;
 #pragma unroll(FLUSH ? NC : 1)
       for (int c = 0; c < NC; ++c) {
         const int ch = 4 * c + quarter;
@@ -969,7 +971,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
           if (c == NC - 1 && jobs > 0) {  // the accumulator may be overwritten
             umma::fence_before_sync();
             __syncwarp();
-            if (lane == 0) leader_arrive<CG>(&accempty[job & 1]);
+            if (lane == 0) leader_arrive<CG>(&accempty[job % NA]);
           }
         }
         // the unit after this chunk's last: the next chunk if that is live, else the next tile's first
