@@ -51,10 +51,12 @@ namespace {
 constexpr int kEpiWarps = 16;
 constexpr int kGemmThreads = 128 + 32 * kEpiWarps;
 
-// The order in which a step's pieces are loaded: 1, 2, 0, so that the products
-// can begin with the smallest terms.
+// The i-th piece of a step of k to be loaded: 1, 2, 0, so that the products can
+// begin with the smallest terms.
 template <int NP>
-constexpr int kFirstPiece = NP == 3 ? 1 : 0;
+constexpr int kPiece(int i) {
+  return NP == 3 ? (i + 1) % 3 : 0;
+}
 
 template <int CG, int BN, int NP>
 struct GemmSmem {
@@ -745,33 +747,30 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
       const uint32_t stage_tx = CG * (S::kA + (uint32_t)bcols * (B_MN ? S::kCol : S::kRow));
       const int m0 = x.tm * 128 * CG + (int)rank * 128;
       const int n0 = x.tn * pq.bn + (CG == 2 ? (int)rank * (pq.bn / 2) : 0);
-      const int steps = (x.k1 - x.k0) * NP;
-      for (int st = 0, kb = x.k0, q = kFirstPiece<NP>; st < steps; ++st, ++it) {
-        if (!(ok = warp_wait(&empty[s], ph ^ 1))) break;
-        if (leader) {
-          if (rank == 0) bar_expect_tx(&full[s], stage_tx);
-          const uint32_t bar = full0 + 8u * (uint32_t)s;
-          const uint32_t a = base + (uint32_t)s * S::kStage, b = a + S::kA;
-          if (a_mn) {
+      for (int kb = x.k0; kb < x.k1 && ok; ++kb) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) gtma_load<CG>(a + j * S::kCol, amap, m0 + 64 * j, kb * BK, q, bar);
-          } else {
-            gtma_load<CG>(a, amap, kb * BK, m0, q, bar);
-          }
-          if constexpr (B_MN) {
+        for (int i = 0; i < NP; ++i, ++it) {
+          if (!(ok = warp_wait(&empty[s], ph ^ 1))) break;
+          if (leader) {
+            const int q = kPiece<NP>(i);
+            if (rank == 0) bar_expect_tx(&full[s], stage_tx);
+            const uint32_t bar = full0 + 8u * (uint32_t)s;
+            const uint32_t a = base + (uint32_t)s * S::kStage, b = a + S::kA;
+            if (a_mn) {
 #pragma unroll
-            for (int j = 0; j < (BN / CG + 63) / 64; ++j)
-              if (j < bcols) gtma_load<CG>(b + j * S::kCol, bmap, n0 + 64 * j, kb * BK, q, bar);
-          } else {
-            gtma_load<CG>(b, bmap, kb * BK, n0, q, bar);
+              for (int j = 0; j < 2; ++j) gtma_load<CG>(a + j * S::kCol, amap, m0 + 64 * j, kb * BK, q, bar);
+            } else {
+              gtma_load<CG>(a, amap, kb * BK, m0, q, bar);
+            }
+            if constexpr (B_MN) {
+#pragma unroll
+              for (int j = 0; j < (BN / CG + 63) / 64; ++j)
+                if (j < bcols) gtma_load<CG>(b + j * S::kCol, bmap, n0 + 64 * j, kb * BK, q, bar);
+            } else {
+              gtma_load<CG>(b, bmap, kb * BK, n0, q, bar);
+            }
           }
-        }
-        if (++s == ST) s = 0, ph ^= 1;
-        if constexpr (NP == 3) {  // pieces 1, 2, 0 of a step of k
-          q = q == 2 ? 0 : q + 1;
-          if (q == 1) ++kb;
-        } else {
-          ++kb;
+          if (++s == ST) s = 0, ph ^= 1;
         }
       }
     }
@@ -819,18 +818,18 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
                 gmma<CG>(d, umma::sdesc_adv(da, q * astep), umma::sdesc_adv(db, q * bstep), idesc, !fresh || q > 0);
             }
           };
-          auto step = [&]() {  // the next stage once it is full
-            const int at = s;
-            ok = warp_wait(&full[s], ph);
-            if (++s == ST) s = 0, ph ^= 1;
-            return at;
-          };
           if constexpr (NP == 1) {
-            const int s0 = step();
-            if (!ok) break;
-            four(s0, s0, first);
-            if (leader) gcommit<CG>(&empty[s0]);
+            if (!(ok = warp_wait(&full[s], ph))) break;
+            four(s, s, first);
+            if (leader) gcommit<CG>(&empty[s]);
+            if (++s == ST) s = 0, ph ^= 1;
           } else {
+            auto step = [&]() {  // the next stage once it is full
+              const int at = s;
+              ok = warp_wait(&full[s], ph);
+              if (++s == ST) s = 0, ph ^= 1;
+              return at;
+            };
             const int s1 = step();
             if (!ok) break;
             four(s1, s1, true);
