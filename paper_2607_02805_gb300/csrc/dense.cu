@@ -55,10 +55,65 @@ struct Raw8 {
   }
 };
 
+// Eight values from p[at] on, wherever that lies: the 16-byte groups that hold
+// them are read whole and shifted into place, two or three wide loads instead of
+// eight narrow ones. The tensor has `span` elements, starts on a 16-byte boundary
+// and no group that reaches past its end is read: there, one element at a time.
+// Values from `n` on are zero.
+template <bool F32>
+struct Any8 {
+  static constexpr int kWords = F32 ? 12 : 8;
+  uint32_t w[kWords];
+  int shift;  // bytes
+  __device__ __forceinline__ void load(const void* p, int64_t at, int n, int64_t span) {
+    const int64_t first = at * (F32 ? 4 : 2);
+    shift = (int)first & 15;
+    const int groups = (F32 ? 2 : 1) + (shift != 0 ? 1 : 0);
+    const char* q = static_cast<const char*>(p) + (first - shift);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0u;
+    if (first - shift + 16 * groups <= span * (F32 ? 4 : 2)) {
+#pragma unroll
+      for (int g = 0; g < kWords / 4; ++g) {
+        if (g < groups) {
+          const uint4 u = *reinterpret_cast<const uint4*>(q + 16 * g);
+          w[4 * g] = u.x, w[4 * g + 1] = u.y, w[4 * g + 2] = u.z, w[4 * g + 3] = u.w;
+        }
+      }
+    } else {
+      shift = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (j >= n) break;
+        if (F32) w[F32 ? j : 0] = __float_as_uint(static_cast<const float*>(p)[at + j]);
+        else w[j / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(p)[at + j] << (16 * (j & 1));
+      }
+    }
+  }
+  __device__ __forceinline__ void get(float (&v)[8], int n) const {
+    uint32_t a[kWords - 2], b[kWords - 3];
+#pragma unroll
+    for (int i = 0; i < kWords - 2; ++i) a[i] = shift & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < kWords - 3; ++i) b[i] = shift & 4 ? a[i + 1] : a[i];
+    if (F32) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(b[F32 ? j : 0]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t u = __funnelshift_r(b[i], b[i + 1], (shift & 2) * 8);
+        v[2 * i] = __uint_as_float(u << 16);
+        v[2 * i + 1] = __uint_as_float(u & 0xffff0000u);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? v[j] : 0.f;
+  }
+};
+
 // ---- operand packing ----
-// A warp converts 256 columns of one row: a lane eight consecutive ones where
-// rows start on 16-byte boundaries, else every 32nd column, so that its loads
-// and stores stay contiguous over the warp. Operands that TMA can read where
+// A warp converts 256 columns of one row, a lane eight consecutive ones. Operands that TMA can read where
 // they lie never come here; the others, fp32 operands and the loss's rows cost
 // one read and one write.
 __device__ __forceinline__ void pack_store(bf16* d, int64_t plane, int pieces, const float (&v)[8]) {
@@ -73,21 +128,20 @@ __device__ __forceinline__ void pack_store(bf16* d, int64_t plane, int pieces, c
 #pragma unroll
   for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(d + k * plane) = *reinterpret_cast<const uint4*>(q[k]);
 }
-// The same for column c, c + 32, ... below `cols`.
-__device__ __forceinline__ void pack_store_strided(bf16* d, int64_t plane, int pieces, const float (&v)[8], int c,
-                                                   int cols) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    if (c + 32 * j >= cols) break;
-    if (pieces == 1) {
-      d[32 * j] = __float2bfloat16_rn(v[j]);
-    } else {
-      bf16 q0, q1, q2;
-      split3(v[j], q0, q1, q2);
-      d[32 * j] = q0;
-      d[plane + 32 * j] = q1;
-      d[2 * plane + 32 * j] = q2;
-    }
+// Eight columns of the operand's row from c on.
+__device__ __forceinline__ void pack_load(float (&v)[8], const PackParams& p, int64_t row, int c) {
+  const int64_t at = row * p.ld + c, span = (p.rows - 1) * p.ld + p.cols;
+  const int n = (int)p.cols - c;
+  if (p.ld % (p.src_f32 ? 4 : 8) == 0 && n >= 8) {
+    load8(v, p.src, p.src_f32, at);
+  } else if (p.src_f32) {
+    Any8<true> u;
+    u.load(p.src, at, n, span);
+    u.get(v, n);
+  } else {
+    Any8<false> u;
+    u.load(p.src, at, n, span);
+    u.get(v, n);
   }
 }
 __device__ __forceinline__ void pack_block(const PackParams& p, int64_t block) {
@@ -99,23 +153,11 @@ __device__ __forceinline__ void pack_block(const PackParams& p, int64_t block) {
   if (row >= p.rows) return;
   // debug build: the last element of the warp's row (no barrier follows)
   if (!dguard(kSitePack, (p.pieces - 1) * p.plane + row * p.ld_dst + p.ld_dst - 1, p.dst_extent)) return;
+  const int c = c0 + 8 * lane;
+  if (c >= p.ld_dst) return;
   float v[8];
-  if (p.ld % (p.src_f32 ? 4 : 8) == 0) {
-    const int c = c0 + 8 * lane;
-    if (c >= p.ld_dst) return;
-    if (c + 8 <= p.cols) {
-      load8(v, p.src, p.src_f32, row * p.ld + c);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = c + j < p.cols ? load1(p.src, p.src_f32, row * p.ld + c + j) : 0.f;
-    }
-    pack_store(p.dst + row * p.ld_dst + c, p.plane, p.pieces, v);
-  } else {  // columns past `cols` are outside the operand's map: never read
-    const int c = c0 + lane;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + 32 * j < p.cols ? load1(p.src, p.src_f32, row * p.ld + c + 32 * j) : 0.f;
-    pack_store_strided(p.dst + row * p.ld_dst + c, p.plane, p.pieces, v, c, (int)p.cols);
-  }
+  pack_load(v, p, row, c);
+  pack_store(p.dst + row * p.ld_dst + c, p.plane, p.pieces, v);
 }
 int64_t pack_blocks(const PackParams& p) {
   return p.dst == nullptr ? 0 : (p.rows * ((p.ld_dst + 255) / 256) + kThreads / 32 - 1) / (kThreads / 32);
@@ -123,32 +165,15 @@ int64_t pack_blocks(const PackParams& p) {
 // One row's 256 columns from c0 on, to slot `to`: h, and in the backward h times
 // the row's scale g.
 __device__ __forceinline__ void pack_row(const PackParams& p, int64_t row, int64_t to, float g, int c0) {
-  const int lane = threadIdx.x & 31;
+  const int c = c0 + 8 * (threadIdx.x & 31);
+  if (c >= p.ld_dst) return;
   float v[8];
-  if (p.ld % (p.src_f32 ? 4 : 8) == 0) {
-    const int c = c0 + 8 * lane;
-    if (c >= p.ld_dst) return;
-    if (c + 8 <= p.cols) {
-      load8(v, p.src, p.src_f32, row * p.ld + c);
-    } else {
+  pack_load(v, p, row, c);
+  pack_store(p.dst + to * p.ld_dst + c, p.plane, p.pieces, v);
+  if (p.scaled == nullptr) return;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = c + j < p.cols ? load1(p.src, p.src_f32, row * p.ld + c + j) : 0.f;
-    }
-    pack_store(p.dst + to * p.ld_dst + c, p.plane, p.pieces, v);
-    if (p.scaled == nullptr) return;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= g;
-    pack_store(p.scaled + to * p.ld_dst + c, p.plane, p.pieces, v);
-  } else {  // columns past `cols` are outside the operand's map: never read
-    const int c = c0 + lane;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + 32 * j < p.cols ? load1(p.src, p.src_f32, row * p.ld + c + 32 * j) : 0.f;
-    pack_store_strided(p.dst + to * p.ld_dst + c, p.plane, p.pieces, v, c, (int)p.cols);
-    if (p.scaled == nullptr) return;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= g;
-    pack_store_strided(p.scaled + to * p.ld_dst + c, p.plane, p.pieces, v, c, (int)p.cols);
-  }
+  for (int j = 0; j < 8; ++j) v[j] *= g;
+  pack_store(p.scaled + to * p.ld_dst + c, p.plane, p.pieces, v);
 }
 // Zeros in a slot behind the last row that counts, and in the gradient of a row that does not.
 __device__ __forceinline__ void pack_zero_slot(const PackParams& p, int64_t to, int c0) {
@@ -297,9 +322,8 @@ __device__ __forceinline__ void dact_block(const DactParams& p, int strip, int r
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int64_t r0 = p.rows * range / p.ranges, r1 = p.rows * (range + 1) / p.ranges;
   float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  // a lane's eight columns: consecutive ones where rows start on 16-byte boundaries, else every 32nd
   const bool aligned = p.ld_dy % (DYF32 ? 4 : 8) == 0 && (p.act == kActNone || p.ld_pre % (PREF32 ? 4 : 8) == 0);
-  const int c0 = strip * kDactCols, c = c0 + (aligned ? lane * 8 : lane), step = aligned ? 1 : 32;
+  const int c0 = strip * kDactCols, c = c0 + lane * 8, n = (int)p.cols - c;
   auto grad = [&](float (&e)[8], const float (&z)[8]) {
     if (p.act == kActSilu) {
 #pragma unroll
@@ -311,11 +335,11 @@ __device__ __forceinline__ void dact_block(const DactParams& p, int strip, int r
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] += e[j];
   };
-  if (aligned && c + 8 <= p.cols) {
-    auto finish = [&](int64_t r, float (&e)[8], const float (&z)[8]) {
-      grad(e, z);
-      if (p.dz != nullptr) pack_store(p.dz + r * p.ld_dz + c, p.plane, p.pieces, e);
-    };
+  auto finish = [&](int64_t r, float (&e)[8], const float (&z)[8]) {
+    grad(e, z);
+    if (p.dz != nullptr) pack_store(p.dz + r * p.ld_dz + c, p.plane, p.pieces, e);
+  };
+  if (aligned && n >= 8) {
     int64_t r = r0 + w;
     for (; r + 8 * (kDactFlight - 1) < r1; r += 8 * kDactFlight) {
       Raw8<DYF32> e[kDactFlight];
@@ -341,27 +365,34 @@ __device__ __forceinline__ void dact_block(const DactParams& p, int strip, int r
       if (p.act != kActNone) load8(z, p.pre, PREF32, r * p.ld_pre + c);
       finish(r, e, z);
     }
-  } else if (c < p.cols) {
-    for (int64_t r = r0 + w; r < r1; r += 8) {
-      float e[8], z[8];
+  } else if (n > 0) {
+    constexpr int kFlight = DYF32 ? 1 : 2;
+    const int64_t dy_span = (p.rows - 1) * p.ld_dy + p.cols, pre_span = (p.rows - 1) * p.ld_pre + p.cols;
+    for (int64_t r = r0 + w; r < r1; r += 8 * kFlight) {
+      Any8<DYF32> e[kFlight];
+      Any8<PREF32> z[kFlight];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool in = c + step * j < p.cols;
-        e[j] = in ? load1(p.dy, DYF32, r * p.ld_dy + c + step * j) : 0.f;
-        z[j] = in && p.act != kActNone ? load1(p.pre, PREF32, r * p.ld_pre + c + step * j) : 0.f;
+      for (int i = 0; i < kFlight; ++i) {
+        if (r + 8 * i >= r1) break;
+        e[i].load(p.dy, (r + 8 * i) * p.ld_dy + c, n, dy_span);
+        if (p.act != kActNone) z[i].load(p.pre, (r + 8 * i) * p.ld_pre + c, n, pre_span);
       }
-      grad(e, z);
-      if (p.dz == nullptr) continue;
-      bf16* d = p.dz + r * p.ld_dz + c;
-      if (aligned) pack_store(d, p.plane, p.pieces, e);  // rows of whole groups of 8
-      else pack_store_strided(d, p.plane, p.pieces, e, c, (int)p.cols);
+#pragma unroll 1
+      for (int i = 0; i < kFlight && r + 8 * i < r1; ++i) {
+        float ev[8], zv[8];
+        e[0].get(ev, n);
+        z[0].get(zv, n);
+        finish(r + 8 * i, ev, zv);
+#pragma unroll
+        for (int j = 0; j + 1 < kFlight; ++j) e[j] = e[j + 1], z[j] = z[j + 1];
+      }
     }
   }
   if (p.part == nullptr) return;
 #pragma unroll
   for (int j = 0; j < 8; ++j) red[w][j * 32 + lane] = sum[j];
   __syncthreads();
-  const int lc = threadIdx.x, col = c0 + (aligned ? (lc & 31) * 8 + (lc >> 5) : lc);
+  const int lc = threadIdx.x, col = c0 + (lc & 31) * 8 + (lc >> 5);
   if (col < p.cols) {
     float s = red[0][lc];
 #pragma unroll
