@@ -552,8 +552,8 @@ constexpr int64_t kJoinRows = 64;
 // splits are chosen for all of them and for half, as a masked objective draws
 // them; of 129 to 256 rows for half alone, which then fit the 128 of a single CTA
 // (256 rows, half of them counting, over 50,021 entries: training 79 us with the
-// choice for both, 70 for half); fp32 for all alone (1000 rows, all counting: 169
-// us, for half 180).
+// choice for both, 70 for half); fp32 for all alone (1000 rows, all counting: 171
+// us, for half 179).
 int64_t plan_rows(const Loss& l) { return l.pieces == 1 && l.T > 128 && l.T <= 256 ? 128 : l.T; }
 int64_t half_rows(const Loss& l) { return l.pieces == 3 || plan_rows(l) != l.T ? 0 : (l.T + 1) / 2; }
 struct LossFwdWs {
@@ -790,9 +790,10 @@ int bdscan_linear_backward(const bdscan_linear_dims* dims, const void* x, const 
       dz = Operand{p.dz, l.N, l.T, p.ld_dz, l.pieces, p.plane};
     }
     p.part = sums;
-    // A large operand is packed by a launch of its own: the gradient's pass leaves room for 24 warps per SM,
-    // packing alone has 64 (18 us against 36 for the 10016 x 1803 x of a layer of 560 outputs).
-    if (l.T * l.K + l.N * l.K > ((int64_t)1 << 24) && (px.dst != nullptr || pw.dst != nullptr)) {
+    // Large operands are packed by a launch of their own: the gradient's pass leaves room for 24 warps per SM,
+    // packing alone has 64 (training 10016 x 1803 -> 560: 131 us against 143; from 2^22 elements on the two ways
+    // are within 2 %, and below, the second launch costs up to 10 %).
+    if (l.T * l.K + l.N * l.K > ((int64_t)1 << 23) && (px.dst != nullptr || pw.dst != nullptr)) {
       e = api_launched(launch_pack(px, pw, s), s);
       px = pw = kNoPack;
     }
