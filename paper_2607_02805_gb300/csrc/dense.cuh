@@ -27,6 +27,7 @@ struct GemmParams {
   int splits;     // ranges of k, each with its own partial sums
   int join;       // kEpiJoin: CTAs of a tile's cluster, each with a range of k
   int group_m;    // row tiles walked together
+  int a_rows;     // rows that a load of A brings (K-major): 128, or what a single smaller tile has, in eights
   int epi, a_mn;  // kEpiPair: kEpiOut or kEpiRows, and how A lies
   int pair_extra; // kEpiPair, problem 0: tiles of problem 1 that take as long as one of its own
   // kEpiOut, kEpiRows: out[row_map ? row_map[i] : i][j]; kEpiOut has res of out's type

@@ -278,6 +278,7 @@ GemmParams geometry(const Plan& q, int64_t m, int64_t n, int64_t k, int* flag) {
   p.bn = q.bn;
   p.splits = 1;
   p.group_m = q.group_m;
+  p.a_rows = m < 128 ? (int)up(m, 8) : 128;
   p.excluded = -1;
   p.flag = flag;
   return p;
@@ -289,7 +290,7 @@ cudaError_t run_product(const Plan& q, const GemmParams& p, const Operand& a, co
                         int64_t plane, int64_t out_rows, cudaStream_t s) {
   GemmMaps m;
   memset(&m, 0, sizeof(m));
-  if (!encode(&m.a, a, q.cfg.a_mn ? kGemmBk : 128) || !encode(&m.b, b, q.cfg.b_mn ? kGemmBk : q.bn / q.cfg.cg))
+  if (!encode(&m.a, a, q.cfg.a_mn ? kGemmBk : p.a_rows) || !encode(&m.b, b, q.cfg.b_mn ? kGemmBk : q.bn / q.cfg.cg))
     return cudaErrorInvalidValue;
   const int epi = q.cfg.epi;
   if ((epi == kEpiOut || epi == kEpiDz) && !encode_out(&m.out, p.out, p.out_f32, p.n, out_rows, p.ld_out, planes, plane))
@@ -365,7 +366,7 @@ cudaError_t run_pair(const GradPlan& g, GemmParams px, GemmParams pw, const Oper
     p.epi = p.row_map == nullptr && rows16(p.ld_out, p.out_f32) && rows16(p.n, p.out_f32) ? kEpiOut : kEpiRows;
     p.out_last = p.row_map != nullptr ? p.out_extent - 1 : (p.m - 1) * p.ld_out + p.n - 1;
     GemmMaps& m = call.m[j];
-    if (!encode(&m.a, dz, w ? kGemmBk : 128) || !encode(&m.b, w ? bw : bx, kGemmBk))
+    if (!encode(&m.a, dz, w ? kGemmBk : p.a_rows) || !encode(&m.b, w ? bw : bx, kGemmBk))
       return cudaErrorInvalidValue;
     if (p.epi == kEpiOut && !encode_out(&m.out, p.out, p.out_f32, p.n, p.m, p.ld_out, 1, 0)) return cudaErrorInvalidValue;
   }

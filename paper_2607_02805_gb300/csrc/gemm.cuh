@@ -744,7 +744,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
       const bool a_mn = PAIR ? pq.a_mn != 0 : A_MN;
       // columns of B that a CTA loads: its share of the tile, MN-major in whole groups of 64
       const int bcols = B_MN ? (pq.bn / CG + 63) / 64 : pq.bn / CG;
-      const uint32_t stage_tx = CG * (S::kA + (uint32_t)bcols * (B_MN ? S::kCol : S::kRow));
+      const uint32_t stage_tx =
+          CG * ((a_mn ? S::kA : (uint32_t)pq.a_rows * S::kRow) + (uint32_t)bcols * (B_MN ? S::kCol : S::kRow));
       const int m0 = x.tm * 128 * CG + (int)rank * 128;
       const int n0 = x.tn * pq.bn + (CG == 2 ? (int)rank * (pq.bn / 2) : 0);
       for (int kb = x.k0; kb < x.k1 && ok; ++kb) {
