@@ -10,7 +10,7 @@
 //
 // Persistent CTAs, roles by warp: 0 issues the TMA loads of a ring of stages,
 // 1 the MMAs, 2 owns the TMEM allocation, 4 to 19 run the epilogue of one
-// accumulator while the MMAs fill the other (four warps per scheduler: the
+// accumulator while the MMAs fill another (four warps per scheduler: the
 // epilogue is chains of latencies, and with two the GELU of a 16384 x 832 x
 // 3328 product took longer than its MMAs). A stage holds 64 elements of k
 // of both operands in the 128-byte swizzled layouts of umma.cuh, rows along m or
@@ -671,7 +671,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
   using S = GemmSmem<CG, BN, NP>;
   constexpr int ST = S::kStages, BK = S::kBk;
   constexpr bool FLUSH = NP == 3;
-  constexpr int NA = BN <= 128 ? 4 : 2;  // accumulators in turn
+  // accumulators in turn (fp32 loss training 1000 x 448 x 8191: with two 172 us, with four 167)
+  constexpr int NA = BN <= 128 ? 4 : 2;
   constexpr uint32_t kCols = NA * BN;
   // debug build: the last output element of the launch (uniform over the grid)
   if (!dguard(kSiteGemm, p.out_last, p.out_extent)) return;
