@@ -669,17 +669,23 @@ def ssd_backward(dims, t, states, dy_c, dy_n, dstates, g, workspace, stream=None
 # row stride of their own (the dims carry it)
 # ---------------------------------------------------------------------------
 def _ptr2(t):
-    """Address of a 2-D tensor whose rows are contiguous (any row stride)."""
+    """Address of a 2-D tensor whose rows are contiguous and do not overlap (any row stride from their length on)."""
     if t is None:
         return None
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError("bdscan dense tensors must be 2-D with contiguous rows")
+    row_stride(t)
     return t.data_ptr()
 
 
 def row_stride(t):
-    """The row stride that bdscan_linear_dims / bdscan_lm_loss_dims take for t."""
-    return int(t.stride(0)) if t.shape[0] > 1 else max(1, int(t.shape[1]))
+    """The row stride that bdscan_linear_dims / bdscan_lm_loss_dims take for t. Rows that overlap (the stride 0 of an
+    expanded row, which the dims would take for the row length) are refused."""
+    if t.shape[0] <= 1:
+        return max(1, int(t.shape[1]))
+    if t.stride(0) < t.shape[1]:
+        raise ValueError(f"the rows of a bdscan dense tensor overlap: {t.shape[1]} elements every {t.stride(0)}")
+    return int(t.stride(0))
 
 
 def make_linear_dims(rows, d_in, d_out, act=BDSCAN_ACT_NONE, dtype=BDSCAN_BF16, out_dtype=None, ld_x=0, ld_res=0,

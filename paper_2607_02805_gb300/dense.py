@@ -48,7 +48,8 @@ def _whole(name, t, shape, dtype, index):
 
 
 def _rows(name, t, shape, dtype, index):
-    """Address and row stride of a 2-D tensor with contiguous rows."""
+    """Address and row stride of a 2-D tensor with contiguous rows, each in memory of its own: the stride 0 of an
+    expanded row would be read as "the row length"."""
     if t is None:
         return None, 0
     if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
@@ -56,7 +57,11 @@ def _rows(name, t, shape, dtype, index):
     ld, step = t.stride()
     if step != 1 and shape[1] > 1:
         raise ValueError(f"the rows of {name} are not contiguous")
-    return t.data_ptr(), ld if shape[0] > 1 else shape[1]
+    if shape[0] <= 1:
+        return t.data_ptr(), shape[1]
+    if ld < shape[1]:
+        raise ValueError(f"the rows of {name} overlap: {shape[1]} elements every {ld}")
+    return t.data_ptr(), ld
 
 
 class _Holder:
