@@ -5,7 +5,9 @@ PyTorch provides the device memory and the stream; every step of the
 computation runs in libbdscan through ``binding``. A ``Linear`` or ``LmLoss``
 holds one size's outputs, saved pre-activations, gradients and workspaces; the
 inputs and weights belong to the caller. What a call returns are the holder's
-buffers, valid until its next call; a holder serves one stream at a time.
+buffers, valid until its next call; a holder serves one stream at a time, and
+its buffers stay where they are for its life, so that a CUDA graph of its calls
+can be replayed as long as it lives.
 """
 
 from __future__ import annotations
@@ -70,25 +72,48 @@ class _Holder:
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index if self.device.type == "cuda" else -1
-        self._plans = {}  # (kind, row strides) -> (dims, workspace bytes)
+        self._plans = {}  # (kind, row strides) -> (dims, their reference, workspace address and bytes)
         self._buf = {}
+        self._outgrown = []  # workspaces that a larger one replaced
+        self._handle = self._stream = None  # of the last call
+
+    def _enter(self, stream):
+        """Handle of the call's stream. What the call allocates comes from that stream's memory, and what the holder
+        allocated on others before is marked as used on it."""
+        handle = binding._stream(stream)
+        if handle != self._handle:
+            if stream is None:
+                stream = torch.cuda.current_stream()
+            elif not isinstance(stream, torch.cuda.Stream):
+                stream = torch.cuda.ExternalStream(handle, self.device)
+            for t in [*self._buf.values(), *self._outgrown]:
+                t.record_stream(stream)
+            self._handle, self._stream = handle, stream
+        return handle
+
+    def _empty(self, shape, dtype):
+        with torch.cuda.stream(self._stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
 
     def _buffer(self, name, shape, dtype):
         t = self._buf.get(name)
         if t is None:
-            t = self._buf[name] = torch.empty(shape, dtype=dtype, device=self.device)
+            t = self._buf[name] = self._empty(shape, dtype)
         return t
 
     def _plan(self, key, size):
         """What a kind of call passes for its row strides, asked for once: the dims, and address and size of the
-        workspace. One workspace serves all calls of the holder, which run one after another."""
+        workspace. One workspace serves all calls of the holder, which run one after another. Where a kind of call
+        needs more, the smaller one is kept: work in flight or a CUDA graph may still write there."""
         plan = self._plans.get(key)
         if plan is None:
             dims = self._make_dims(*key[1:])
             need = size(dims)
             ws = self._buf.get("workspace")
             if need and (ws is None or ws.numel() < need):
-                ws = self._buf["workspace"] = torch.empty(need, dtype=torch.uint8, device=self.device)
+                if ws is not None:
+                    self._outgrown.append(ws)
+                ws = self._buf["workspace"] = self._empty(need, torch.uint8)
                 self._plans = {k: v[:2] + (ws.data_ptr(), ws.numel()) for k, v in self._plans.items()}
             plan = (dims, ctypes.byref(dims)) + ((None, 0) if ws is None else (ws.data_ptr(), ws.numel()))
             self._plans[key] = plan
@@ -119,16 +144,20 @@ class Linear(_Holder):
         dt, od, dev = self.dtype, self.out_dtype, self._index
         px, ld_x = _rows("x", x, self._x, dt, dev)
         pr, ld_r = _rows("residual", residual, self._y, od, dev)
-        y = self._buffer("y", self._y, od) if out is None else out
-        py, ld_y = _rows("out", y, self._y, od, dev)
         pw = _whole("w", w, self._w, dt, dev)
         pb = _whole("bias", bias, self._b, dt, dev)
+        py, ld_y = _rows("out", out, self._y, od, dev)
+        s = self._enter(stream)
+        y = out
+        if out is None:
+            y = self._buffer("y", self._y, od)
+            py, ld_y = y.data_ptr(), self.d_out
         self.pre = pp = None
         if save_pre and self.act != "none":
             self.pre = self._buffer("pre", self._y, dt)
             pp = self.pre.data_ptr()
         _, d, ws, size = self._plan(("forward", ld_x, ld_r, ld_y), binding.bdscan_linear_forward_workspace_size)
-        binding._call("bdscan_linear_forward", d, px, pw, pb, pr, pp, py, ws, size, binding._stream(stream))
+        binding._call("bdscan_linear_forward", d, px, pw, pb, pr, pp, py, ws, size, s)
         return y
 
     def backward(self, x, w, dy, bias=True, need_dx=True, need_dw=True, stream=None):
@@ -140,13 +169,13 @@ class Linear(_Holder):
         pw = _whole("w", w, self._w, dt, dev)
         if self.act != "none" and self.pre is None:
             raise ValueError("backward needs a forward with save_pre=True")
+        s = self._enter(stream)
         dx = self._buffer("dx", self._x, dt) if need_dx else None
         dw = self._buffer("dw", self._w, dt) if need_dw else None
         db = self._buffer("dbias", self._b, dt) if bias else None
         p = binding._ptr
         _, d, ws, size = self._plan(("backward", ld_x, 0, ld_y), binding.bdscan_linear_backward_workspace_size)
-        binding._call("bdscan_linear_backward", d, px, pw, p(self.pre), py, p(dx), p(dw), p(db), ws, size,
-                      binding._stream(stream))
+        binding._call("bdscan_linear_backward", d, px, pw, p(self.pre), py, p(dx), p(dw), p(db), ws, size, s)
         return dx, dw, db
 
 
@@ -173,11 +202,11 @@ class LmLoss(_Holder):
     def forward(self, h, w, target, weight=None, stream=None):
         """(loss, lse), fp32 per row; zero at the rows that do not count."""
         ld_h, inputs = self._inputs(h, w, target, weight)
+        s = self._enter(stream)
         loss = self._buffer("loss", self._t, torch.float32)
         lse = self._buffer("lse", self._t, torch.float32)
         _, d, ws, size = self._plan(("forward", ld_h), binding.bdscan_lm_loss_forward_workspace_size)
-        binding._call("bdscan_lm_loss_forward", d, *inputs, loss.data_ptr(), lse.data_ptr(), ws, size,
-                      binding._stream(stream))
+        binding._call("bdscan_lm_loss_forward", d, *inputs, loss.data_ptr(), lse.data_ptr(), ws, size, s)
         return loss, lse
 
     def backward(self, h, w, target, weight=None, dloss=None, lse=None, stream=None):
@@ -189,9 +218,9 @@ class LmLoss(_Holder):
             if lse is None:
                 raise ValueError("backward needs a forward or its lse")
         pl = _whole("lse", lse, self._t, torch.float32, self._index)
+        s = self._enter(stream)
         dh = self._buffer("dh", self._h, self.dtype)
         dw = self._buffer("dw", self._w, self.dtype)
         _, d, ws, size = self._plan(("backward", ld_h), binding.bdscan_lm_loss_backward_workspace_size)
-        binding._call("bdscan_lm_loss_backward", d, *inputs, pl, pd, dh.data_ptr(), dw.data_ptr(), ws, size,
-                      binding._stream(stream))
+        binding._call("bdscan_lm_loss_backward", d, *inputs, pl, pd, dh.data_ptr(), dw.data_ptr(), ws, size, s)
         return dh, dw

@@ -1,6 +1,9 @@
 """The holders of the dense operators and the marshalling below them, on the
 host: which tensors they refuse before an address reaches the library."""
 
+import gc
+import weakref
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -79,3 +82,103 @@ def test_binding_refuses_rows_that_overlap():
             b._ptr2(t)
     assert b.row_stride(torch.zeros(4, 24)[:, :8]) == 24
     assert b.row_stride(torch.zeros(1, 8).expand(1, 8)) == 8 and b.row_stride(torch.zeros(1, 1)) == 1
+
+
+# ---------------------------------------------------------------------------
+# workspaces and streams
+# ---------------------------------------------------------------------------
+class FakeStream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+@pytest.fixture
+def fake_streams(monkeypatch):
+    """Calls that reach the library are noted with their workspace and stream; a list of (stream, bytes) allocated and
+    one of (address, stream) marked."""
+    calls, allocated, marked, within = [], [], [], [None]
+    empty = torch.empty
+
+    class stream:
+        def __init__(self, s):
+            self.s = s
+
+        def __enter__(self):
+            self.before, within[0] = within[0], self.s
+
+        def __exit__(self, *exc):
+            within[0] = self.before
+
+    def note_empty(*args, **kw):
+        t = empty(*args, **kw)
+        allocated.append((within[0], t.data_ptr()))
+        return t
+
+    monkeypatch.setattr(b, "_call", lambda name, *args: calls.append((name,) + args[-3:]))
+    monkeypatch.setattr(b, "_stream", lambda s: None if s is None else s.cuda_stream)
+    monkeypatch.setattr(torch, "empty", note_empty)
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: handle)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: marked.append((t.data_ptr(), s)))
+    return calls, allocated, marked
+
+
+def _step(op, forward, backward, stream=None):
+    x, w = torch.zeros(300, 448), torch.zeros(1792, 448)
+    if forward:
+        op.forward(x, w, save_pre=True, stream=stream)
+    if backward:
+        op.backward(x, w, torch.zeros(300, 1792), stream=stream)
+
+
+def test_outgrown_workspaces_are_kept(fake_streams):
+    """The backward needs more than the forward; work of the forward, or a graph of it, may still use the first one."""
+    calls, _, _ = fake_streams
+    op = dense.Linear(300, 448, 1792, "gelu", torch.float32, device="cpu")
+    _step(op, True, False)
+    first = weakref.ref(op._buf["workspace"])
+    _step(op, False, True)
+    gc.collect()
+    (_, a, n, _), (_, c, m, _) = calls
+    assert m > n and a != c
+    assert first() is not None and first().data_ptr() == a and first().numel() == n
+    _step(op, True, True)  # later calls use the larger one
+    assert all(q[1:3] == (c, m) for q in calls[2:])
+
+
+def test_a_row_stride_that_needs_more_keeps_the_first_workspace(fake_streams):
+    calls, _, _ = fake_streams
+    op = dense.Linear(200, 64, 128, "none", B, device="cpu")
+    w = torch.zeros(128, 64, dtype=B)
+    op.forward(torch.zeros(200, 69, dtype=B)[:, :64], w)
+    first = weakref.ref(op._buf["workspace"])
+    op.backward(torch.zeros(200, 69, dtype=B)[:, :64], w, torch.zeros(200, 133, dtype=B)[:, :128])
+    gc.collect()
+    assert calls[1][2] > calls[0][2] and first() is not None
+
+
+def test_buffers_come_from_the_stream_of_the_call(fake_streams):
+    calls, allocated, marked = fake_streams
+    op = dense.Linear(300, 448, 1792, "gelu", torch.float32, device="cpu")
+    _step(op, True, False, FakeStream(5))
+    assert allocated and {s for s, _ in allocated if s is not None} == {5} and not marked
+    held = {t.data_ptr() for t in op._buf.values()}
+    assert held <= {p for s, p in allocated if s == 5}
+    before = len(allocated)
+    _step(op, True, True, FakeStream(6))  # what the first stream allocated is used on the second
+    assert held <= {p for p, s in marked if s == 6}
+    grown = {t.data_ptr() for t in op._buf.values()} - held
+    assert grown and grown <= {p for s, p in allocated[before:] if s == 6}
+    marks = len(marked)
+    _step(op, True, True, FakeStream(6))
+    assert len(marked) == marks and [c[-1] for c in calls] == [5, 6, 6, 6, 6]
+
+
+def test_loss_buffers_come_from_the_stream_of_the_call(fake_streams):
+    calls, allocated, _ = fake_streams
+    op = dense.LmLoss(40, 8, 16, B, device="cpu")
+    h, w, t = torch.zeros(40, 8, dtype=B), torch.zeros(16, 8, dtype=B), torch.zeros(40, dtype=torch.int64)
+    op.forward(h, w, t, stream=FakeStream(5))
+    op.backward(h, w, t, stream=FakeStream(5))
+    assert {t.data_ptr() for t in op._buf.values()} <= {p for s, p in allocated if s == 5}
+    assert [c[-1] for c in calls] == [5, 5]
