@@ -224,18 +224,20 @@ __device__ __forceinline__ float act_fwd(int act, float z) {
   return act == kActNone ? z : act == kActSilu ? silu_f(z) : gelu_f(z);
 }
 // The derivative; the argument is clamped to where the sigmoid is 0 or 1 in
-// fp32, so that no infinity meets a zero.
+// fp32, so that no infinity meets a zero. The clamp would also hide an argument
+// that is not finite (fmaxf of a NaN is the other operand): 0 z, added at the
+// end, is zero for every finite z and NaN for the others.
 __device__ __forceinline__ float act_grad(int act, float z) {
   if (act == kActNone) return 1.f;
   if (act == kActSilu) {
     const float c = fminf(fmaxf(z, -100.f), 100.f);
     const float s = rcp_f(1.f + ex2(-kLog2e * c));
-    return s * (1.f + c * (1.f - s));
+    return fmaf(0.f, z, s * (1.f + c * (1.f - s)));
   }
   const float c = fminf(fmaxf(z, -16.f), 16.f);
   constexpr float c1 = -2.f * kGeluA * kLog2e, c2 = c1 * kGeluB;
   const float s = rcp_f(1.f + ex2(c * fmaf(c2, c * c, c1)));
-  return s * (1.f + c * (1.f - s) * fmaf(6.f * kGeluA * kGeluB, c * c, 2.f * kGeluA));
+  return fmaf(0.f, z, s * (1.f + c * (1.f - s) * fmaf(6.f * kGeluA * kGeluB, c * c, 2.f * kGeluA)));
 }
 
 // fp32 as three bf16 pieces (8 + 8 + 8 bits). The first is cut towards zero
