@@ -72,3 +72,27 @@ def test_input_that_is_not_finite_reaches_the_gradients(t, k, n, dtype, act, val
     dx, dw, db = op.backward(x, w, dy)
     assert not torch.isfinite(dx[3]).any() and torch.isfinite(dx[rest]).all()
     assert not torch.isfinite(dw).any() and not torch.isfinite(db).any()
+
+
+# Sigmoids below 2^-60 may count as zero: |y| is then at most |z| 2^-60 for the z where that begins, -41.6 for SiLU.
+TAIL = 42.0 * 2.0 ** -60
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("t,k", [(4, 8), (200, 8), (200, 7), (40, 4096), (300, 4096)])
+def test_activations_far_out(t, k, dtype, act):
+    """z far out in both tails: zero below and z above, by the product, by few rows and by products that are split.
+    The value above is z times a sigmoid of 1 from an approximate reciprocal (2^-22), rounded to the type."""
+    z = torch.tensor([42.0, 50.0, 100.0, 1e4, 1e10, 1e19, 1e20, 1e30, 3e38])
+    z = torch.cat([z, -z]).to("cuda", dtype)
+    n = 18
+    x = torch.zeros(t, k, dtype=dtype, device="cuda")
+    x[:, k - 1] = 1.0
+    w = torch.zeros(n, k, dtype=dtype, device="cuda")
+    w[:, k - 1] = z
+    y = Linear(t, k, n, act, dtype).forward(x, w).double().cpu().numpy()
+    zz = z.double().cpu().numpy()
+    u = 2.0 ** -8 if dtype == B else 2.0 ** -22
+    assert (np.abs(y[:, :9] - zz[:9]) <= u * zz[:9]).all()
+    assert (np.abs(y[:, 9:]) <= TAIL).all()
