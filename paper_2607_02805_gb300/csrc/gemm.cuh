@@ -111,6 +111,17 @@ __device__ __forceinline__ void cluster_sync_all() {
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, umma::bar_wait(bar, parity));
 }
+// A barrier of the epilogue warps, which tells all of them whether one has given
+// up: nobody waits there for a warp that has left its loop.
+__device__ __forceinline__ bool epilogue_sync(bool gave_up) {
+  uint32_t any;
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n bar.red.or.pred q, 1, %2, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+      : "=r"(any)
+      : "r"(gave_up ? 1u : 0u), "n"(32 * kEpiWarps)
+      : "memory");
+  return any != 0;
+}
 // One arrival at the barrier at this offset in the tile's first CTA. What it
 // orders is this thread's TMEM loads, which have completed (wait::ld and the
 // tcgen05 fence before it); a release at cluster scope would also wait for the
@@ -963,7 +974,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
           umma::fence_after_sync();
         }
       }
-      if (!ok) break;
+      if (!ok) {
+        if constexpr (EPI == kEpiStats) epilogue_sync(true);  // this tile's barrier
+        break;
+      }
       const uint32_t tacc = lanes + job % NA * BN;
 #pragma unroll(FLUSH ? NC : 1)
       for (int c = 0; c < NC; ++c) {
@@ -1127,7 +1141,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
         // a warp is at most one tile ahead of the one that joins)
         float2* q = reinterpret_cast<float2*>(sm + ST * S::kStage) + 512 * (turn++ & 1);
         q[128 * quarter + 32 * (w & 3) + lane] = make_float2(rm, rs);
-        asm volatile("bar.sync 1, %0;\n" ::"n"(32 * kEpiWarps) : "memory");
+        if (!(ok = !epilogue_sync(false))) break;
         if (quarter == 0 && row < T.m) {
 #pragma unroll
           for (int k = 1; k < 4; ++k) stats_join(rm, rs, q[128 * k + 32 * w + lane - 128]);
