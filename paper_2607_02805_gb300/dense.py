@@ -79,7 +79,11 @@ class _Holder:
 
     def _enter(self, stream):
         """Handle of the call's stream. What the call allocates comes from that stream's memory, and what the holder
-        allocated on others before is marked as used on it."""
+        allocated on others before is marked as used on it. The kernels go to the current device, which has to be the
+        holder's."""
+        if self._index >= 0 and torch._C._cuda_getDevice() != self._index:
+            raise ValueError(f"the holder is on {self.device}, the current device is "
+                             f"cuda:{torch._C._cuda_getDevice()}")
         handle = binding._stream(stream)
         if handle != self._handle:
             if stream is None:

@@ -182,3 +182,19 @@ def test_loss_buffers_come_from_the_stream_of_the_call(fake_streams):
     op.backward(h, w, t, stream=FakeStream(5))
     assert {t.data_ptr() for t in op._buf.values()} <= {p for s, p in allocated if s == 5}
     assert [c[-1] for c in calls] == [5, 5]
+
+
+def test_holders_refuse_another_current_device(fake_streams, monkeypatch):
+    """Kernels are launched on the current device: a holder of another one would hand them that device's addresses."""
+    calls, allocated, _ = fake_streams
+    op = dense.Linear(4, 8, 16, "none", B, device="cuda:1")
+    ls = dense.LmLoss(4, 8, 16, B, device="cuda:1")
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(dense, "_rows", lambda name, t, shape, dtype, index: (1 << 20, shape[1]))
+    monkeypatch.setattr(dense, "_whole", lambda *args: 1 << 20)
+    for call in (lambda: op.forward(None, None), lambda: op.backward(None, None, None),
+                 lambda: ls.forward(None, None, None), lambda: ls.backward(None, None, None, lse=1),
+                 lambda: op.forward(None, None, stream=FakeStream(5))):
+        with pytest.raises(ValueError, match="holder is on cuda:1, the current device is cuda:0"):
+            call()
+    assert not calls and not allocated
