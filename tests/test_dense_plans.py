@@ -30,3 +30,13 @@ def test_blocks_of_rows_are_planned_for_all_of_them(d_model, vocab):
     for rows in (200, 256):
         assert tile_columns(rows, d_model, vocab, b.BDSCAN_BF16) > 128
     assert tile_columns(128, d_model, vocab, b.BDSCAN_BF16) <= 128
+
+
+def test_pieces_of_the_backward_fill_their_limit():
+    """The gradient at the logits of 16384 rows over 16384 entries is 512 MiB in bf16, which is one piece."""
+    rows, d_model, vocab = 16384, 448, 16384
+    n = b.bdscan_lm_loss_backward_workspace_size(b.make_lm_loss_dims(rows, d_model, vocab, b.BDSCAN_BF16))
+    n -= 256 + 5 * 4 * rows + 2 * rows * d_model * 2  # the rows that count, their h and its scaled copy
+    assert 1 << 29 <= n <= (1 << 29) + (64 << 20)
+    n = b.bdscan_lm_loss_backward_workspace_size(b.make_lm_loss_dims(rows, d_model, vocab + 1, b.BDSCAN_BF16))
+    assert n < 1 << 29  # two pieces of half the size
