@@ -12,8 +12,6 @@ cudaError_t launch_gemm_nt3(const GemmCfg& c, const GemmParams& p, const GemmMap
     return gemm_t<2, 128, 3, false, false, kEpiRows, true>(p, m, s);
   if (c.epi == kEpiRows && c.cg == 1 && c.bn == 128 && c.pieces == 3 && c.out_f32 == true)
     return gemm_t<1, 128, 3, false, false, kEpiRows, true>(p, m, s);
-  if (c.epi == kEpiJoin && c.cg == 1 && c.bn == 128 && c.pieces == 3)
-    return gemm_t<1, 128, 3, false, false, kEpiJoin, false>(p, m, s);
   return cudaErrorInvalidValue;
 }
 
