@@ -66,6 +66,12 @@ def _rows(name, t, shape, dtype, index):
     return t.data_ptr(), ld
 
 
+def _apart(name, at, *outputs):
+    """Refuses an input (its address) that the call overwrites while it reads it: what the holder returned before."""
+    if at and at in outputs:
+        raise ValueError(f"{name} is a buffer that this call writes: pass a copy, or use a holder of its own")
+
+
 class _Holder:
     def __init__(self, device):
         self.device = torch.device(device)
@@ -156,6 +162,7 @@ class Linear(_Holder):
         if out is None:
             y = self._buffer("y", self._y, od)
             py, ld_y = y.data_ptr(), self.d_out
+        _apart("x", px, py)
         self.pre = pp = None
         if save_pre and self.act != "none":
             self.pre = self._buffer("pre", self._y, dt)
@@ -178,8 +185,12 @@ class Linear(_Holder):
         dw = self._buffer("dw", self._w, dt) if need_dw else None
         db = self._buffer("dbias", self._b, dt) if bias else None
         p = binding._ptr
+        qx, qw = p(dx), p(dw)
+        _apart("x", px, qx)
+        _apart("dy", py, qx)
+        _apart("w", pw, qw)
         _, d, ws, size = self._plan(("backward", ld_x, 0, ld_y), binding.bdscan_linear_backward_workspace_size)
-        binding._call("bdscan_linear_backward", d, px, pw, p(self.pre), py, p(dx), p(dw), p(db), ws, size, s)
+        binding._call("bdscan_linear_backward", d, px, pw, p(self.pre), py, qx, qw, p(db), ws, size, s)
         return dx, dw, db
 
 
@@ -225,6 +236,8 @@ class LmLoss(_Holder):
         s = self._enter(stream)
         dh = self._buffer("dh", self._h, self.dtype)
         dw = self._buffer("dw", self._w, self.dtype)
+        _apart("h", inputs[0], dh.data_ptr())
+        _apart("w", inputs[1], dw.data_ptr())
         _, d, ws, size = self._plan(("backward", ld_h), binding.bdscan_lm_loss_backward_workspace_size)
         binding._call("bdscan_lm_loss_backward", d, *inputs, pl, pd, dh.data_ptr(), dw.data_ptr(), ws, size, s)
         return dh, dw

@@ -198,3 +198,33 @@ def test_holders_refuse_another_current_device(fake_streams, monkeypatch):
         with pytest.raises(ValueError, match="holder is on cuda:1, the current device is cuda:0"):
             call()
     assert not calls and not allocated
+
+
+def test_holders_refuse_what_the_call_writes(fake_streams):
+    """A result is the holder's buffer: as the next call's input it would be read while it is written."""
+    calls, _, _ = fake_streams
+    op = dense.Linear(4, 8, 8, "none", B, device="cpu")
+    x, w, dy = torch.zeros(4, 8, dtype=B), torch.zeros(8, 8, dtype=B), torch.zeros(4, 8, dtype=B)
+    y = op.forward(x, w)
+    dx, dw, _ = op.backward(x, w, dy)
+    ls = dense.LmLoss(4, 8, 8, B, device="cpu")
+    t = torch.zeros(4, dtype=torch.int64)
+    ls.forward(x, w, t)
+    dh, dhead = ls.backward(x, w, t)
+    n = len(calls)
+    for call, name in ((lambda: op.forward(y, w), "x"), (lambda: op.forward(x, w, out=x), "x"),
+                       (lambda: op.backward(dx, w, dy), "x"), (lambda: op.backward(x, w, dx), "dy"),
+                       (lambda: op.backward(x, dw, dy), "w"), (lambda: ls.backward(dh, w, t), "h"),
+                       (lambda: ls.backward(x, dhead, t), "w")):
+        with pytest.raises(ValueError, match=f"^{name} is a buffer that this call writes"):
+            call()
+    assert len(calls) == n
+    # read before it is written, written by no product of the call, or another holder's
+    op.forward(x, w, residual=y)
+    op.forward(dx, w)
+    op.backward(y, w, dy, need_dx=False)
+    op.backward(x, w, dx, need_dx=False)
+    dense.Linear(4, 8, 8, "none", B, device="cpu").forward(y, w)
+    empty = dense.Linear(0, 8, 8, "none", B, device="cpu")
+    empty.forward(torch.zeros(0, 8, dtype=B), w)
+    assert len(calls) == n + 6

@@ -73,3 +73,26 @@ def test_calls_on_a_given_stream():
             assert torch.equal(a, c)
         assert all((t == 7).all() for t in noise)
     assert binding.bdscan_ssd_wait_flag(1) == 0
+
+
+def test_graph_on_a_stream_of_its_own_outlives_the_warm_up():
+    """Warm-up on the current stream, capture on another: the same buffers, freed only after both."""
+    x, w, dy = _case()
+    op = Linear(300, 448, 1792, "gelu", F)
+    want = [op.forward(x, w, save_pre=True).clone()] + [t.clone() for t in op.backward(x, w, dy)]
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = [op.forward(x, w, save_pre=True), *op.backward(x, w, dy)]
+    for t in got:
+        t.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    for a, c in zip(got, want):
+        assert torch.equal(a, c)
+    del g, op, got
+    torch.cuda.synchronize()
+    again = Linear(300, 448, 1792, "gelu", F)
+    for a, c in zip([again.forward(x, w, save_pre=True), *again.backward(x, w, dy)], want):
+        assert torch.equal(a, c)
+    assert binding.bdscan_ssd_wait_flag(1) == 0
