@@ -21,6 +21,9 @@ from . import binding
 ACTS = {"none": binding.BDSCAN_ACT_NONE, "silu": binding.BDSCAN_ACT_SILU, "gelu": binding.BDSCAN_ACT_GELU}
 CODES = {torch.float32: binding.BDSCAN_F32, torch.bfloat16: binding.BDSCAN_BF16}
 
+# The current stream's handle without a Stream object, where this PyTorch has the query.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
 
 def _code(dtype):
     if dtype not in CODES:
@@ -87,10 +90,14 @@ class _Holder:
         """Handle of the call's stream. What the call allocates comes from that stream's memory, and what the holder
         allocated on others before is marked as used on it. The kernels go to the current device, which has to be the
         holder's."""
-        if self._index >= 0 and torch._C._cuda_getDevice() != self._index:
-            raise ValueError(f"the holder is on {self.device}, the current device is "
-                             f"cuda:{torch._C._cuda_getDevice()}")
-        handle = binding._stream(stream)
+        index = self._index
+        if index < 0:
+            handle = binding._stream(stream)
+        else:
+            current = torch._C._cuda_getDevice()
+            if current != index:
+                raise ValueError(f"the holder is on {self.device}, the current device is cuda:{current}")
+            handle = _raw_stream(index) if stream is None and _raw_stream is not None else binding._stream(stream)
         if handle != self._handle:
             if stream is None:
                 stream = torch.cuda.current_stream()
