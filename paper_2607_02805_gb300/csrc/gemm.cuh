@@ -590,8 +590,13 @@ __device__ __forceinline__ void join_rows(const float2* part, int parts, int64_t
       const int i = i0 + r, row = idx[i];
       const float l = (m + log2f(s)) * kLn2;
       const float zt = __ldcg(at_target + i);
+      // The loss from the target's logit and the maximum in base 2, with the product exact: the logits' own size
+      // cancels before anything is rounded (l - zt, with l rounded at that size, was off by |zt| 2^-23, and below zero
+      // for targets that are nearly certain). No probability is above one; a NaN stays.
+      float d = fmaf(-zt, kLog2e, m) + log2f(s);
+      d = d < 0.f ? 0.f : d * kLn2;
       // a target that is the excluded entry has probability zero, also where no entry is left
-      const float d = zt == -INFINITY ? INFINITY : l - zt;
+      if (zt == -INFINITY) d = INFINITY;
       lse[row] = l;
       loss[row] = weight != nullptr ? weight[row] * d : d;
     }
