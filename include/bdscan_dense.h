@@ -105,7 +105,8 @@ int bdscan_lm_loss_forward(const bdscan_lm_loss_dims* dims, const void* h, const
 /* Gradients of <dloss, loss> (dloss nullable: ones) with respect to h
  * [rows][d_model] and w [vocab][d_model], of `dtype`. lse is the forward's. The
  * logits are computed again, in pieces of the vocabulary whose gradient (rounded
- * to `dtype`; fp32: three pieces) the workspace holds, 512 MiB at most (256 entries at least). */
+ * to `dtype`; fp32: three pieces) the workspace holds, 512 MiB at most (256 entries at
+ * least). The product for dw reads h times weight and dloss, rounded likewise. */
 size_t bdscan_lm_loss_backward_workspace_size(const bdscan_lm_loss_dims* dims);
 int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, const void* w, const int64_t* target,
                             const float* weight, const float* lse, const float* dloss, void* dh, void* dw,
