@@ -4,6 +4,8 @@
  *   - the linear layer with bias, activation and residual in one product (the
  *     MLP of a block, Appendix C: ratio 4; the projections around a mixer; the
  *     logits of single tokens), forward and backward;
+ *   - the gated linear layer: both projections of a gated feed-forward block,
+ *     the activation and the product in one, forward and backward;
  *   - the weighted softmax cross entropy of the language-model head over the
  *     vocabulary (the masked objective, Sec. 3; Sec. 4.1), at the rows that
  *     count, without keeping the logits, forward and backward.
@@ -74,6 +76,37 @@ size_t bdscan_linear_backward_workspace_size(const bdscan_linear_dims* dims);
 int bdscan_linear_backward(const bdscan_linear_dims* dims, const void* x, const void* w, const void* pre,
                            const void* dy, void* dx, void* dw, void* dbias, void* workspace, size_t workspace_bytes,
                            void* stream);
+
+/* y = act(x wg^T + bg) * (x wu^T + bu), elementwise product.
+ * Layouts: x [rows][d_in] (row stride ld_x), w [2 d_hidden][d_in]: the rows of
+ * wg, then those of wu; bias [2 d_hidden] likewise (nullable), y
+ * [rows][d_hidden] (row stride ld_y). All have `dtype` (f32 or bf16). Sums,
+ * activation and product are fp32, y is rounded once. rows >= 0, d_in and
+ * d_hidden >= 1. y is no input. */
+typedef struct bdscan_gated_linear_dims {
+  int64_t rows;
+  int64_t d_in;
+  int64_t d_hidden;
+  int64_t ld_x;
+  int64_t ld_y; /* of y, and of dy in the backward */
+  int32_t act;  /* BDSCAN_ACT_* */
+  int32_t dtype;
+} bdscan_gated_linear_dims;
+
+size_t bdscan_gated_linear_forward_workspace_size(const bdscan_gated_linear_dims* dims);
+int bdscan_gated_linear_forward(const bdscan_gated_linear_dims* dims, const void* x, const void* w, const void* bias,
+                                void* y, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of <dy, y>: with g = x wg^T + bg and u = x wu^T + bu, computed
+ * again, dz = [dy u act'(g), dy act(g)] [rows][2 d_hidden], dx = dz w
+ * [rows][d_in], dw = dz^T x [2 d_hidden][d_in], dbias = column sums of dz
+ * [2 d_hidden]. Each of dx, dw, dbias is nullable and then not computed; bias
+ * is the forward's. dz enters the products rounded to `dtype` (fp32: three
+ * pieces), and dbias unrounded. No output is an input. */
+size_t bdscan_gated_linear_backward_workspace_size(const bdscan_gated_linear_dims* dims);
+int bdscan_gated_linear_backward(const bdscan_gated_linear_dims* dims, const void* x, const void* w, const void* bias,
+                                 const void* dy, void* dx, void* dw, void* dbias, void* workspace,
+                                 size_t workspace_bytes, void* stream);
 
 /* loss[t] = weight[t] (lse[t] - z[t][target[t]]), lse[t] = log sum_v exp(z[t][v]),
  * z = h w^T, at the rows that count: target inside 0 .. vocab - 1 and weight

@@ -58,6 +58,25 @@ def linear_backward(x, w, pre, dy, name="none"):
     return dz @ w, dz.T @ x, dz.sum(0)
 
 
+def gated_linear_forward(x, w, bias=None, name="silu"):
+    """y = act(gate) * up; w holds the rows of the gate's weights, then the others."""
+    z = x @ w.T
+    if bias is not None:
+        z = z + bias
+    gate, up = np.split(z, 2, axis=1)
+    return act(name, gate) * up
+
+
+def gated_linear_backward(x, w, bias, dy, name="silu"):
+    """dx, dw, dbias."""
+    z = x @ w.T
+    if bias is not None:
+        z = z + bias
+    gate, up = np.split(z, 2, axis=1)
+    dz = np.concatenate((dy * up * act_grad(name, gate), dy * act(name, gate)), axis=1)
+    return dz @ w, dz.T @ x, dz.sum(0)
+
+
 def _rows(target, weight, vocab):
     return (target >= 0) & (target < vocab) & (weight != 0)
 

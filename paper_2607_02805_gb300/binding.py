@@ -189,6 +189,21 @@ DENSE_SIGNATURES = [
      [_P(bdscan_lm_loss_dims)] + [c_void_p] * 9 + [ctypes.c_size_t, c_void_p]),
 ]
 
+class bdscan_gated_linear_dims(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d_in", ctypes.c_int64), ("d_hidden", ctypes.c_int64),
+                ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64), ("act", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+# include/bdscan_dense.h, the gated linear layer
+GATED_SIGNATURES = [
+    ("bdscan_gated_linear_forward_workspace_size", ctypes.c_size_t, [_P(bdscan_gated_linear_dims)]),
+    ("bdscan_gated_linear_forward", ctypes.c_int,
+     [_P(bdscan_gated_linear_dims)] + [c_void_p] * 5 + [ctypes.c_size_t, c_void_p]),
+    ("bdscan_gated_linear_backward_workspace_size", ctypes.c_size_t, [_P(bdscan_gated_linear_dims)]),
+    ("bdscan_gated_linear_backward", ctypes.c_int,
+     [_P(bdscan_gated_linear_dims)] + [c_void_p] * 8 + [ctypes.c_size_t, c_void_p]),
+]
+
 BDSCAN_NOALLOC_SCRATCH_BYTES = 32 << 20
 
 _lock = threading.Lock()
@@ -210,7 +225,7 @@ def load(build_if_missing: bool = True, debug=None):
             if not os.path.exists(path):
                 raise RuntimeError(f"libbdscan is not built ({path} missing); run paper_2607_02805_gb300/build.py")
             lib = ctypes.CDLL(path)
-            for name, res, args in SIGNATURES + DENSE_SIGNATURES:
+            for name, res, args in SIGNATURES + DENSE_SIGNATURES + GATED_SIGNATURES:
                 f = getattr(lib, name)
                 f.restype = res
                 f.argtypes = args
@@ -447,6 +462,23 @@ def bdscan_linear_backward_workspace_size(dims) -> int:
 
 def bdscan_linear_backward(dims, x, w, pre, dy, dx, dw, dbias, workspace, workspace_bytes, stream):
     return load().bdscan_linear_backward(_ref(dims), x, w, pre, dy, dx, dw, dbias, workspace, workspace_bytes, stream)
+
+
+def bdscan_gated_linear_forward_workspace_size(dims) -> int:
+    return load().bdscan_gated_linear_forward_workspace_size(_ref(dims))
+
+
+def bdscan_gated_linear_forward(dims, x, w, bias, y, workspace, workspace_bytes, stream):
+    return load().bdscan_gated_linear_forward(_ref(dims), x, w, bias, y, workspace, workspace_bytes, stream)
+
+
+def bdscan_gated_linear_backward_workspace_size(dims) -> int:
+    return load().bdscan_gated_linear_backward_workspace_size(_ref(dims))
+
+
+def bdscan_gated_linear_backward(dims, x, w, bias, dy, dx, dw, dbias, workspace, workspace_bytes, stream):
+    return load().bdscan_gated_linear_backward(_ref(dims), x, w, bias, dy, dx, dw, dbias, workspace, workspace_bytes,
+                                               stream)
 
 
 def bdscan_lm_loss_forward_workspace_size(dims) -> int:
@@ -702,6 +734,20 @@ def linear_forward(dims, x, w, bias, residual, pre, y, workspace, stream=None):
 def linear_backward(dims, x, w, pre, dy, dx, dw, dbias, workspace, stream=None):
     _call("bdscan_linear_backward", ctypes.byref(dims), _ptr2(x), _ptr(w), _ptr(pre), _ptr2(dy), _ptr(dx), _ptr(dw),
           _ptr(dbias), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def make_gated_linear_dims(rows, d_in, d_hidden, act=BDSCAN_ACT_SILU, dtype=BDSCAN_BF16, ld_x=0, ld_y=0):
+    return bdscan_gated_linear_dims(int(rows), int(d_in), int(d_hidden), int(ld_x), int(ld_y), int(act), int(dtype))
+
+
+def gated_linear_forward(dims, x, w, bias, y, workspace, stream=None):
+    _call("bdscan_gated_linear_forward", ctypes.byref(dims), _ptr2(x), _ptr(w), _ptr(bias), _ptr2(y), _ptr(workspace),
+          _nbytes(workspace), _stream(stream))
+
+
+def gated_linear_backward(dims, x, w, bias, dy, dx, dw, dbias, workspace, stream=None):
+    _call("bdscan_gated_linear_backward", ctypes.byref(dims), _ptr2(x), _ptr(w), _ptr(bias), _ptr2(dy), _ptr(dx),
+          _ptr(dw), _ptr(dbias), _ptr(workspace), _nbytes(workspace), _stream(stream))
 
 
 def make_lm_loss_dims(rows, d_model, vocab, dtype=BDSCAN_BF16, excluded=-1, ld_h=0):

@@ -569,6 +569,85 @@ __global__ void __launch_bounds__(128) k_linear_vec(const VecParams p) {
   store1(p.y, p.out_f32, r * p.ld_y + n, v);
 }
 
+// ---- a gated layer of a few rows ----
+// The same with NC columns of both projections per warp: one row of 832 -> 3328
+// reads 11 MB of w.
+template <typename T, int ROWS, int NC, bool VEC>
+__global__ void __launch_bounds__(128) k_gated_vec(const VecParams p) {
+  pdl_sync();
+  constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;  // elements per load
+  const int lane = threadIdx.x & 31;
+  const int64_t n0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 5)) * NC;
+  if (n0 >= p.n) return;
+  if (!dguard(kSiteLinearVec, (p.rows - 1) * p.ld_y + p.n - 1, p.out_extent)) return;
+  const T* x = static_cast<const T*>(p.x);
+  const T* w = static_cast<const T*>(p.w);
+  float acc[ROWS][2][NC];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[r][0][c] = acc[r][1][c] = 0.f;
+#pragma unroll 2
+  for (int k = lane * E; k < p.k; k += 32 * E) {
+    float wv[2][NC][E];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int64_t n = (n0 + c < p.n ? n0 + c : p.n - 1) + (int64_t)q * p.n;
+        if constexpr (VEC) {
+          const uint4 u = __ldcs(reinterpret_cast<const uint4*>(w + n * p.k + k));
+          const T* e = reinterpret_cast<const T*>(&u);
+#pragma unroll
+          for (int j = 0; j < E; ++j) wv[q][c][j] = cvt(e[j]);
+        } else {
+          wv[q][c][0] = cvt(w[n * p.k + k]);
+        }
+      }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (r < p.rows) {
+        float xv[E];
+        if constexpr (VEC) {
+          const uint4 u = *reinterpret_cast<const uint4*>(x + r * p.ld_x + k);
+          const T* e = reinterpret_cast<const T*>(&u);
+#pragma unroll
+          for (int j = 0; j < E; ++j) xv[j] = cvt(e[j]);
+        } else {
+          xv[0] = cvt(x[r * p.ld_x + k]);
+        }
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int j = 0; j < E; ++j) acc[r][q][c] = fmaf(xv[j], wv[q][c][j], acc[r][q][c]);
+      }
+    }
+  }
+  float g = 0.f, u = 0.f;  // lane r * NC + c finishes output (r, c)
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        acc[r][0][c] += __shfl_xor_sync(0xffffffffu, acc[r][0][c], o);
+        acc[r][1][c] += __shfl_xor_sync(0xffffffffu, acc[r][1][c], o);
+      }
+      if (lane == r * NC + c) g = acc[r][0][c], u = acc[r][1][c];
+    }
+  const int r = lane / NC;
+  const int64_t n = n0 + lane % NC;
+  if (lane >= ROWS * NC || r >= p.rows || n >= p.n) return;
+  const int f32 = sizeof(T) == 4;
+  if (p.bias != nullptr) {
+    g += load1(p.bias, f32, n);
+    u += load1(p.bias, f32, n + p.n);
+  }
+  store1(p.y, f32, r * p.ld_y + n, act_fwd(p.act, g) * u);
+}
+
 // ---- rows of the loss ----
 // A CTA takes `per` rows (a multiple of 1024). It counts the rows before its
 // own, all of them, rather than waiting for another CTA's count: up to 64 CTAs
@@ -635,6 +714,18 @@ void vec_t(const VecParams& p, bool vec, cudaStream_t s) {
   if (vec) launch_pdl(k_linear_vec<T, ROWS, NC, true>, grid, 128, 0, s, p);
   else launch_pdl(k_linear_vec<T, ROWS, NC, false>, grid, 128, 0, s, p);
 }
+template <typename T, int ROWS>
+void gated_t(const VecParams& p, bool vec, cudaStream_t s) {
+  const unsigned grid = (unsigned)((p.n + 3) / 4);
+  if (vec) launch_pdl(k_gated_vec<T, ROWS, 1, true>, grid, 128, 0, s, p);
+  else launch_pdl(k_gated_vec<T, ROWS, 1, false>, grid, 128, 0, s, p);
+}
+template <typename T>
+void gated_rows(const VecParams& p, bool vec, cudaStream_t s) {
+  if (p.rows == 1) gated_t<T, 1>(p, vec, s);
+  else if (p.rows <= 4) gated_t<T, 4>(p, vec, s);
+  else gated_t<T, 8>(p, vec, s);
+}
 template <typename T>
 void vec_rows(const VecParams& p, bool vec, cudaStream_t s) {
   // four columns per warp share its loads of x, once there are columns enough to fill the SMs that way
@@ -687,6 +778,13 @@ cudaError_t launch_linear_vec(const VecParams& p, cudaStream_t s) {
   const bool vec = p.k % e == 0 && p.ld_x % e == 0;
   if (p.f32) vec_rows<float>(p, vec, s);
   else vec_rows<bf16>(p, vec, s);
+  return cudaGetLastError();
+}
+cudaError_t launch_gated_vec(const VecParams& p, cudaStream_t s) {
+  const int e = p.f32 ? 4 : 8;
+  const bool vec = p.k % e == 0 && p.ld_x % e == 0;
+  if (p.f32) gated_rows<float>(p, vec, s);
+  else gated_rows<bf16>(p, vec, s);
   return cudaGetLastError();
 }
 cudaError_t launch_loss_rows(const LossRowsParams& p, cudaStream_t s) {

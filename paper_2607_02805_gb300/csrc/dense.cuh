@@ -16,6 +16,12 @@ constexpr int kEpiJoin = 4;   // the same, the ranges of k of a tile joined by a
 constexpr int kEpiPair = 5;   // two products in one launch, each kEpiOut or kEpiRows without bias, activation and residual
 constexpr int kEpiStats = 1;  // running maximum and sum of a row's logits, and the target's logit
 constexpr int kEpiDz = 2;     // the loss's gradient at the logits
+// A gated layer's tile holds the same bn / 2 columns of both projections, the gate's first; n counts both.
+constexpr int kEpiGate = 6;        // act(gate) * up, by TMA
+constexpr int kEpiGateRows = 7;    // the same by plain stores
+constexpr int kEpiGateDz = 8;      // the gradients at both projections from `res` = dy, by TMA
+constexpr int kEpiGateDzRows = 9;  // the same by plain loads and stores
+constexpr bool epi_gate(int epi) { return epi >= kEpiGate && epi <= kEpiGateDzRows; }
 
 // A [m][k] or [k][m], B [n][k] or [k][n] come as tensor maps; extents in elements.
 struct GemmParams {
@@ -63,6 +69,7 @@ struct GemmParams {
   void* sum_out;
   int64_t sum_cols;
   int sum_ranges, sum_f32;
+  float* colsum;         // kEpiGateDz: [row ranges of 32][n] column sums of the unrounded gradients, or null
   int* flag;             // set by a bounded wait that gave up
 };
 
@@ -77,7 +84,8 @@ struct GemmCfg {
   bool out_f32;     // kEpiOut, kEpiRows
 };
 
-// Tensor maps of a product; `out` and `pre` for kEpiOut, `out` for kEpiDz.
+// Tensor maps of a product; `out` and `pre` for kEpiOut, `out` for kEpiDz and kEpiGate, for kEpiGateDz `out` the
+// gate's columns and `pre` the other projection's.
 struct GemmMaps {
   CUtensorMap a, b, out, pre;
 };
@@ -136,6 +144,9 @@ struct VecParams {
   int64_t out_extent;  // elements of y (debug build)
 };
 cudaError_t launch_linear_vec(const VecParams& p, cudaStream_t s);
+
+// y = act(x wg^T + bg) * (x wu^T + bu) for a few rows; w and bias hold the gate's n rows, then the others.
+cudaError_t launch_gated_vec(const VecParams& p, cudaStream_t s);
 
 // The rows of the loss that count (weight, and dloss if given, not zero, and a
 // target inside the vocabulary), in order: their number, index, target and

@@ -22,6 +22,7 @@ cudaError_t launch_gemm_nn3(const GemmCfg&, const GemmParams&, const GemmMaps&, 
 cudaError_t launch_gemm_tn3(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
 cudaError_t launch_gemm_pair(const GemmCfg&, const GemmCall<2>&, cudaStream_t);
 cudaError_t launch_gemm_loss(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
+cudaError_t launch_gemm_gate(const GemmCfg&, const GemmParams&, const GemmMaps&, cudaStream_t);
 
 namespace {
 
@@ -78,17 +79,18 @@ bool encode(CUtensorMap* m, const Operand& o, int box_rows) {
 }
 
 // The output [planes][rows][cols] as the epilogue stores it: boxes of 32
-// rows x 64 bytes.
+// rows x 64 bytes, or of 32 where `box_cols` is 16 bf16.
 bool encode_out(CUtensorMap* m, const void* base, int f32, int64_t cols, int64_t rows, int64_t ld, int planes,
-                int64_t plane) {
+                int64_t plane, int box_cols = 0) {
   const int64_t elt = f32 ? 4 : 2;
+  if (box_cols == 0) box_cols = f32 ? 16 : 32;
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
   const cuuint64_t strides[2] = {(cuuint64_t)(ld * elt), (cuuint64_t)((planes > 1 ? plane : ld * 8) * elt)};
-  const cuuint32_t box[3] = {f32 ? 16u : 32u, 32u, 1u};
+  const cuuint32_t box[3] = {(cuuint32_t)box_cols, 32u, 1u};
   const cuuint32_t estr[3] = {1u, 1u, 1u};
   return tensor_map_encoder()(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
                               const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_64B,
+                              box_cols * elt == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // Whether rows of `ld` elements start on 16-byte boundaries.
@@ -144,7 +146,8 @@ double product_clocks(const Plan& q, int64_t m, int64_t n, int64_t k) {  // q.cf
 }
 // Where the rows that count are known on the device only, m2 and k2 (not zero)
 // are the sizes with half of them, and the choice minimises the sum of both.
-Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split, bool b_mn, int64_t m2 = 0, int64_t k2 = 0) {
+Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split, bool b_mn, int64_t m2 = 0, int64_t k2 = 0,
+          int step = 32) {  // step: columns of a tile are a multiple of it
   static const Instance bf16_any[] = {{2, 256}, {1, 128}}, f32_any[] = {{2, 128}, {1, 128}};
   const Instance* inst = pieces == 3 ? f32_any : bf16_any;
   const int64_t nk = (k + 63) / 64;
@@ -160,8 +163,8 @@ Plan plan(int64_t m, int64_t n, int64_t k, int pieces, bool may_split, bool b_mn
     const int cg = inst[i].cg;
     if (cg == 2 && m <= 128) continue;
     const int64_t units = kSms / cg, mt = (m + 128 * cg - 1) / (128 * cg);
-    for (int bn = inst[i].bn; bn >= 32; bn -= 32) {
-      if (bn - 32 >= n) continue;
+    for (int bn = inst[i].bn; bn >= step; bn -= step) {
+      if (bn - step >= n) continue;
       const int64_t tiles = mt * ((n + bn - 1) / bn);
       memset(&q, 0, sizeof(q));
       q.cfg.cg = cg;
@@ -292,16 +295,26 @@ cudaError_t run_product(const Plan& q, const GemmParams& p, const Operand& a, co
                         int64_t plane, int64_t out_rows, cudaStream_t s) {
   GemmMaps m;
   memset(&m, 0, sizeof(m));
-  if (!encode(&m.a, a, q.cfg.a_mn ? kGemmBk : p.a_rows) || !encode(&m.b, b, q.cfg.b_mn ? kGemmBk : q.bn / q.cfg.cg))
-    return cudaErrorInvalidValue;
   const int epi = q.cfg.epi;
+  // columns of B per load: a CTA's share of the tile, of a gated layer those of one projection
+  const int b_rows = epi_gate(epi) ? q.bn / 2 : q.bn / q.cfg.cg;
+  if (!encode(&m.a, a, q.cfg.a_mn ? kGemmBk : p.a_rows) || !encode(&m.b, b, q.cfg.b_mn ? kGemmBk : b_rows))
+    return cudaErrorInvalidValue;
   if ((epi == kEpiOut || epi == kEpiDz) && !encode_out(&m.out, p.out, p.out_f32, p.n, out_rows, p.ld_out, planes, plane))
     return cudaErrorInvalidValue;
   if (epi == kEpiOut && p.pre != nullptr && !encode_out(&m.pre, p.pre, p.pre_f32, p.n, out_rows, p.ld_pre, 1, 0))
     return cudaErrorInvalidValue;
   const bool f32 = q.cfg.pieces == 3;
+  const int unit = q.cfg.bn / 8;  // columns of an epilogue warp of a gated layer
+  if (epi == kEpiGate && !encode_out(&m.out, p.out, p.out_f32, p.n / 2, out_rows, p.ld_out, 1, 0, unit))
+    return cudaErrorInvalidValue;
+  if (epi == kEpiGateDz &&
+      (!encode_out(&m.out, p.out, 0, p.n / 2, out_rows, p.ld_out, planes, plane, unit) ||
+       !encode_out(&m.pre, (__nv_bfloat16*)p.out + p.n / 2, 0, p.n / 2, out_rows, p.ld_out, planes, plane, unit)))
+    return cudaErrorInvalidValue;
   cudaError_t e;
-  if (epi == kEpiStats || epi == kEpiDz) e = launch_gemm_loss(q.cfg, p, m, s);
+  if (epi_gate(epi)) e = launch_gemm_gate(q.cfg, p, m, s);
+  else if (epi == kEpiStats || epi == kEpiDz) e = launch_gemm_loss(q.cfg, p, m, s);
   else if (q.cfg.a_mn) e = f32 ? launch_gemm_tn3(q.cfg, p, m, s) : launch_gemm_tn(q.cfg, p, m, s);
   else if (q.cfg.b_mn) e = f32 ? launch_gemm_nn3(q.cfg, p, m, s) : launch_gemm_nn(q.cfg, p, m, s);
   else e = f32 ? launch_gemm_nt3(q.cfg, p, m, s) : launch_gemm_nt(q.cfg, p, m, s);
@@ -488,6 +501,81 @@ LinBwdWs lin_bwd_ws(const Lin& l) {
   o += al256((size_t)w.ranges * l.N * 4);
   w.part = o;
   const size_t a = split_bytes(w.g.x, l.T, l.K), b = split_bytes(w.g.w, l.N, l.K);
+  w.total = o + (a > b ? a : b);
+  return w;
+}
+
+// ---------------------------------------------------------------------------
+// gated linear
+// ---------------------------------------------------------------------------
+struct Gated {
+  int64_t T, K, F, ld_x, ld_y;
+  int act, dtype, pieces;
+};
+int check_gated(const bdscan_gated_linear_dims* d, Gated* l, const char* fn) {
+  api_begin();
+  if (d == nullptr) return fail_msg(BDSCAN_ERR_ARG, fn, "dims is NULL");
+  if (d->rows < 0) return fail_msg(BDSCAN_ERR_ARG, fn, "negative rows");
+  if (d->d_in <= 0 || d->d_hidden <= 0) return fail_msg(BDSCAN_ERR_ARG, fn, "d_in and d_hidden must be positive");
+  const int rc = check_types(d->dtype, d->dtype, fn);
+  if (rc) return rc;
+  if (d->act != BDSCAN_ACT_NONE && d->act != BDSCAN_ACT_SILU && d->act != BDSCAN_ACT_GELU)
+    return fail_msg(BDSCAN_ERR_ARG, fn, "bad act");
+  if (d->rows > kMaxRows || d->d_in > kMaxCols || d->d_hidden > kMaxCols / 2)
+    return fail_msg(BDSCAN_ERR_UNSUPPORTED, fn, "rows above 2^30, d_in above 2^24 or d_hidden above 2^23");
+  l->T = d->rows;
+  l->K = d->d_in;
+  l->F = d->d_hidden;
+  l->ld_x = d->ld_x ? d->ld_x : l->K;
+  l->ld_y = d->ld_y ? d->ld_y : l->F;
+  if (l->ld_x < l->K) return fail_msg(BDSCAN_ERR_ARG, fn, "ld_x is below d_in");
+  if (l->ld_y < l->F) return fail_msg(BDSCAN_ERR_ARG, fn, "ld_y is below d_hidden");
+  if (l->ld_x > kMaxCols * 64 || l->ld_y > kMaxCols * 64)
+    return fail_msg(BDSCAN_ERR_UNSUPPORTED, fn, "a row stride above 2^30");
+  l->act = d->act;
+  l->dtype = d->dtype;
+  l->pieces = d->dtype == BDSCAN_F32 ? 3 : 1;
+  return BDSCAN_OK;
+}
+// A tile has the same columns of both projections, in units of 32.
+Plan plan_gated(const Gated& l) { return plan(l.T, 2 * l.F, l.K, l.pieces, false, false, 0, 0, 64); }
+
+struct GatedFwdWs {
+  Plan q;
+  size_t x, w, total;
+};
+GatedFwdWs gated_fwd_ws(const Gated& l) {
+  GatedFwdWs w;
+  memset(&w, 0, sizeof(w));
+  if (l.T <= kVecRows) return w;
+  w.q = plan_gated(l);
+  if (!in_place(l.dtype, l.ld_x)) w.w = packed_bytes(l.dtype, l.T, l.K);
+  w.total = w.w + (in_place(l.dtype, l.K) ? 0 : packed_bytes(l.dtype, 2 * l.F, l.K));
+  return w;
+}
+struct GatedBwdWs {
+  Plan qz;
+  GradPlan g;
+  size_t x, w, dz, sums, part, total;
+  int64_t ranges;  // rows in 32s, each with its column sums
+};
+GatedBwdWs gated_bwd_ws(const Gated& l) {
+  GatedBwdWs w;
+  memset(&w, 0, sizeof(w));
+  w.qz = plan_gated(l);
+  w.g = plan_grad(l.T, l.K, 2 * l.F, l.pieces);
+  size_t o = 0;
+  w.x = o;
+  if (!in_place(l.dtype, l.ld_x)) o += packed_bytes(l.dtype, l.T, l.K);
+  w.w = o;
+  if (!in_place(l.dtype, l.K)) o += packed_bytes(l.dtype, 2 * l.F, l.K);
+  w.dz = o;
+  o += packed_bytes(l.dtype, l.T, 2 * l.F);
+  w.sums = o;
+  w.ranges = (l.T + 31) / 32;
+  o += al256((size_t)w.ranges * 2 * l.F * 4);
+  w.part = o;
+  const size_t a = split_bytes(w.g.x, l.T, l.K), b = split_bytes(w.g.w, 2 * l.F, l.K);
   w.total = o + (a > b ? a : b);
   return w;
 }
@@ -839,6 +927,142 @@ int bdscan_linear_backward(const bdscan_linear_dims* dims, const void* x, const 
   if (e == cudaSuccess && dw != nullptr) {
     add_sums(&gw);
     e = run_out(ws.g.w, true, true, gw, dz, ox, part, s);
+  }
+  return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+}
+
+size_t bdscan_gated_linear_forward_workspace_size(const bdscan_gated_linear_dims* dims) {
+  Gated l;
+  if (check_gated(dims, &l, "bdscan_gated_linear_forward_workspace_size") != BDSCAN_OK || l.T == 0) return 0;
+  return gated_fwd_ws(l).total;
+}
+
+int bdscan_gated_linear_forward(const bdscan_gated_linear_dims* dims, const void* x, const void* w, const void* bias,
+                                void* y, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "bdscan_gated_linear_forward";
+  Gated l;
+  int rc = check_gated(dims, &l, fn);
+  if (rc) return rc;
+  if (l.T == 0) return api_ok();
+  DENSE_REQ(x, fn, "x");
+  DENSE_REQ(w, fn, "w");
+  DENSE_OPT(bias, fn, "bias");
+  DENSE_REQ(y, fn, "y");
+  cudaStream_t s = (cudaStream_t)stream;
+  const int f32 = l.dtype == BDSCAN_F32;
+  if (l.T <= kVecRows) {
+    VecParams v{};
+    v.x = x, v.w = w, v.bias = bias, v.y = y;
+    v.ld_x = l.ld_x, v.ld_y = l.ld_y;
+    v.rows = (int)l.T, v.k = (int)l.K, v.n = (int)l.F, v.act = l.act;
+    v.f32 = v.out_f32 = f32;
+    v.out_extent = (l.T - 1) * l.ld_y + l.F;
+    const cudaError_t e = api_launched(launch_gated_vec(v, s), s);
+    return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+  }
+  const GatedFwdWs ws = gated_fwd_ws(l);
+  if ((rc = check_workspace(workspace, workspace_bytes, ws.total, fn))) return rc;
+  int* flag;
+  if ((rc = check_device(fn, &flag))) return rc;
+  char* base = (char*)workspace;
+  PackParams px, pw;
+  const Operand a = operand(&px, l.dtype, x, l.T, l.K, l.ld_x, base + ws.x);
+  const Operand b = operand(&pw, l.dtype, w, 2 * l.F, l.K, l.K, base + ws.w);
+  cudaError_t e = cudaSuccess;
+  if (px.dst != nullptr || pw.dst != nullptr) e = api_launched(launch_pack(px, pw, s), s);
+  if (e == cudaSuccess) {
+    Plan q = ws.q;
+    GemmParams p = geometry(q, l.T, 2 * l.F, l.K, flag);
+    p.bias = bias;
+    p.out = y;
+    p.ld_out = l.ld_y;
+    p.bias_f32 = p.out_f32 = f32;
+    p.act = l.act;
+    p.out_extent = (l.T - 1) * l.ld_y + l.F;
+    p.out_last = p.out_extent - 1;
+    q.cfg.epi = rows16(l.ld_y, f32) && rows16(l.F, f32) ? kEpiGate : kEpiGateRows;
+    e = run_product(q, p, a, b, 1, 0, l.T, s);
+  }
+  return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+}
+
+size_t bdscan_gated_linear_backward_workspace_size(const bdscan_gated_linear_dims* dims) {
+  Gated l;
+  if (check_gated(dims, &l, "bdscan_gated_linear_backward_workspace_size") != BDSCAN_OK || l.T == 0) return 0;
+  return gated_bwd_ws(l).total;
+}
+
+int bdscan_gated_linear_backward(const bdscan_gated_linear_dims* dims, const void* x, const void* w, const void* bias,
+                                 const void* dy, void* dx, void* dw, void* dbias, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  const char* fn = "bdscan_gated_linear_backward";
+  Gated l;
+  int rc = check_gated(dims, &l, fn);
+  if (rc) return rc;
+  DENSE_OPT(dx, fn, "dx");
+  DENSE_OPT(dw, fn, "dw");
+  DENSE_OPT(dbias, fn, "dbias");
+  cudaStream_t s = (cudaStream_t)stream;
+  const size_t elt = l.dtype == BDSCAN_F32 ? 4 : 2;
+  const int64_t N = 2 * l.F;
+  if (l.T == 0) {  // sums over no rows
+    cudaError_t e = cudaSuccess;
+    if (dw != nullptr) e = cudaMemsetAsync(dw, 0, (size_t)N * l.K * elt, s);
+    if (dbias != nullptr && e == cudaSuccess) e = cudaMemsetAsync(dbias, 0, (size_t)N * elt, s);
+    return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+  }
+  if (dx == nullptr && dw == nullptr && dbias == nullptr) return api_ok();
+  DENSE_REQ(x, fn, "x");
+  DENSE_REQ(w, fn, "w");
+  DENSE_OPT(bias, fn, "bias");
+  DENSE_REQ(dy, fn, "dy");
+  const GatedBwdWs ws = gated_bwd_ws(l);
+  if ((rc = check_workspace(workspace, workspace_bytes, ws.total, fn))) return rc;
+  int* flag;
+  if ((rc = check_device(fn, &flag))) return rc;
+  char* base = (char*)workspace;
+  float* part = (float*)(base + ws.part);
+  const int f32 = l.dtype == BDSCAN_F32;
+  PackParams px, pw;
+  const Operand a = operand(&px, l.dtype, x, l.T, l.K, l.ld_x, base + ws.x);
+  const Operand b = operand(&pw, l.dtype, w, N, l.K, l.K, base + ws.w);
+  cudaError_t e = cudaSuccess;
+  if (px.dst != nullptr || pw.dst != nullptr) e = api_launched(launch_pack(px, pw, s), s);
+  // both projections again, and from them the gradients there
+  const int64_t ld_dz = up(N, 8), plane = l.T * ld_dz;
+  const Operand dz{base + ws.dz, N, l.T, ld_dz, l.pieces, plane};
+  float* sums = dbias != nullptr ? (float*)(base + ws.sums) : nullptr;
+  if (e == cudaSuccess) {
+    Plan q = ws.qz;
+    GemmParams p = geometry(q, l.T, N, l.K, flag);
+    p.bias = bias;
+    p.res = dy;
+    p.ld_res = l.ld_y;
+    p.bias_f32 = p.res_f32 = f32;
+    p.out = base + ws.dz;
+    p.ld_out = ld_dz;
+    p.split_stride = plane;
+    p.act = l.act;
+    p.colsum = sums;
+    p.out_extent = l.pieces * plane;
+    p.out_last = (l.pieces - 1) * plane + (l.T - 1) * ld_dz + N - 1;
+    q.cfg.epi = rows16(l.ld_y, f32) && l.F % 8 == 0 ? kEpiGateDz : kEpiGateDzRows;
+    e = run_product(q, p, a, b, l.pieces, plane, l.T, s);
+  }
+  if (e == cudaSuccess && dbias != nullptr)
+    e = api_launched(launch_colsum(sums, (int)ws.ranges, N, dbias, f32, s), s);
+  GemmParams gx = geometry(ws.g.x, l.T, l.K, N, flag), gw = geometry(ws.g.w, N, l.K, l.T, flag);
+  gx.out = dx;
+  gw.out = dw;
+  gx.ld_out = gw.ld_out = l.K;
+  gx.out_f32 = gw.out_f32 = f32;
+  gx.out_extent = l.T * l.K;
+  gw.out_extent = N * l.K;
+  if (e == cudaSuccess && dx != nullptr && dw != nullptr && ws.g.one) {
+    e = run_pair(ws.g, gx, gw, dz, b, a, s);
+  } else {
+    if (e == cudaSuccess && dx != nullptr) e = run_out(ws.g.x, false, true, gx, dz, b, part, s);
+    if (e == cudaSuccess && dw != nullptr) e = run_out(ws.g.w, true, true, gw, dz, a, part, s);
   }
   return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
 }

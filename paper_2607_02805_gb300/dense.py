@@ -2,8 +2,8 @@
 (include/bdscan_dense.h) from PyTorch.
 
 PyTorch provides the device memory and the stream; every step of the
-computation runs in libbdscan through ``binding``. A ``Linear`` or ``LmLoss``
-holds one size's outputs, saved pre-activations, gradients and workspaces; the
+computation runs in libbdscan through ``binding``. A ``Linear``, ``GatedLinear``
+or ``LmLoss`` holds one size's outputs, saved pre-activations, gradients and workspaces; the
 inputs and weights belong to the caller. What a call returns are the holder's
 buffers, valid until its next call; a holder serves one stream at a time, and
 its buffers stay where they are for its life, so that a CUDA graph of its calls
@@ -198,6 +198,61 @@ class Linear(_Holder):
         _apart("w", pw, qw)
         _, d, ws, size = self._plan(("backward", ld_x, 0, ld_y), binding.bdscan_linear_backward_workspace_size)
         binding._call("bdscan_linear_backward", d, px, pw, p(self.pre), py, qx, qw, p(db), ws, size, s)
+        return dx, dw, db
+
+
+class GatedLinear(_Holder):
+    """y = act(x wg^T + bg) * (x wu^T + bu) for x [rows, d_in]; w [2 d_hidden, d_in] holds the rows of wg, then those
+    of wu, bias [2 d_hidden] likewise."""
+
+    def __init__(self, rows, d_in, d_hidden, act="silu", dtype=torch.bfloat16, device="cuda"):
+        if act not in ACTS:
+            raise ValueError(f"unknown activation {act!r}")
+        _code(dtype)
+        super().__init__(device)
+        self.rows, self.d_in, self.d_hidden, self.act = int(rows), int(d_in), int(d_hidden), act
+        self.dtype = dtype
+        self._x, self._w, self._y = (self.rows, self.d_in), (2 * self.d_hidden, self.d_in), (self.rows, self.d_hidden)
+        self._b = (2 * self.d_hidden,)
+
+    def _make_dims(self, ld_x, ld_y):
+        return binding.make_gated_linear_dims(self.rows, self.d_in, self.d_hidden, ACTS[self.act], _code(self.dtype),
+                                              ld_x, ld_y)
+
+    def forward(self, x, w, bias=None, out=None, stream=None):
+        """y (the holder's buffer, or `out`). Nothing is kept for backward()."""
+        dt, dev = self.dtype, self._index
+        px, ld_x = _rows("x", x, self._x, dt, dev)
+        pw = _whole("w", w, self._w, dt, dev)
+        pb = _whole("bias", bias, self._b, dt, dev)
+        py, ld_y = _rows("out", out, self._y, dt, dev)
+        s = self._enter(stream)
+        y = out
+        if out is None:
+            y = self._buffer("y", self._y, dt)
+            py, ld_y = y.data_ptr(), self.d_hidden
+        _apart("x", px, py)
+        _, d, ws, size = self._plan(("forward", ld_x, ld_y), binding.bdscan_gated_linear_forward_workspace_size)
+        binding._call("bdscan_gated_linear_forward", d, px, pw, pb, py, ws, size, s)
+        return y
+
+    def backward(self, x, w, dy, bias=None, need_dx=True, need_dw=True, stream=None):
+        """(dx, dw, dbias) of <dy, y>, from the forward's inputs; dbias None without `bias`."""
+        dt, dev = self.dtype, self._index
+        px, ld_x = _rows("x", x, self._x, dt, dev)
+        py, ld_y = _rows("dy", dy, self._y, dt, dev)
+        pw = _whole("w", w, self._w, dt, dev)
+        pb = _whole("bias", bias, self._b, dt, dev)
+        s = self._enter(stream)
+        dx = self._buffer("dx", self._x, dt) if need_dx else None
+        dw = self._buffer("dw", self._w, dt) if need_dw else None
+        db = self._buffer("dbias", self._b, dt) if bias is not None else None
+        p = binding._ptr
+        qx, qw, qb = p(dx), p(dw), p(db)
+        for name, at in (("x", px), ("dy", py), ("w", pw), ("bias", pb)):
+            _apart(name, at, qx, qw, qb)
+        _, d, ws, size = self._plan(("backward", ld_x, ld_y), binding.bdscan_gated_linear_backward_workspace_size)
+        binding._call("bdscan_gated_linear_backward", d, px, pw, pb, py, qx, qw, qb, ws, size, s)
         return dx, dw, db
 
 
