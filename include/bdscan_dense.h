@@ -8,8 +8,11 @@
  *     the activation and the product in one, forward and backward;
  *   - the weighted softmax cross entropy of the language-model head over the
  *     vocabulary (the masked objective, Sec. 3; Sec. 4.1), at the rows that
- *     count, without keeping the logits, forward and backward.
- * Both run on the tcgen05 tensor cores (bf16 operands, fp32 accumulation in
+ *     count, without keeping the logits, forward and backward;
+ *   - token scores of given logits: log probabilities of tokens, entropies and
+ *     the likeliest entries (what a denoising step chooses its tokens by, and
+ *     what a teacher hands on), forward and backward.
+ * The products run on the tcgen05 tensor cores (bf16 operands, fp32 accumulation in
  * TMEM); fp32 inputs are computed to fp32 accuracy from three bf16 pieces per
  * value.
  *
@@ -144,6 +147,49 @@ size_t bdscan_lm_loss_backward_workspace_size(const bdscan_lm_loss_dims* dims);
 int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, const void* w, const int64_t* target,
                             const float* weight, const float* lse, const float* dloss, void* dh, void* dw,
                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Scores of rows of logits z, with p = softmax(z / temperature):
+ *   logp[t] = log p[token[t]],  entropy[t] = -sum_v p_v log p_v,
+ *   top_ids, top_logp [rows][top]: the `top` entries of the largest
+ *   probability, largest first, of equal logits the lower index first, and
+ *   their log probabilities.
+ * `excluded` names an entry of probability zero, whatever its logit (-1: none);
+ * a logit of minus infinity is one too. Such entries are never among the
+ * likeliest (places left over hold -1 and minus infinity), and as a token have
+ * logp minus infinity. A row without any other entry has entropy 0, no likeliest
+ * entries and no gradient. A row whose token is outside 0 .. vocab - 1 does not
+ * count: its logits are not read, logp, entropy, stats and gradient are 0, and
+ * it has no likeliest entries. A row with NaN or plus infinity at an entry that
+ * is not excluded has NaN everywhere and -1 for the likeliest entries.
+ * Layouts: logits [rows][vocab] (row stride ld_logits) and dlogits (ld_dlogits)
+ * of `dtype` (f32 or bf16); token [rows] int64; stats [rows][2]: the largest
+ * logit and the logarithm of the sum of exponentials relative to it, which the
+ * backward reads. Everything else fp32, top_ids int64. top 0 .. 64, temperature
+ * 2^-20 .. 2^20. No workspace. */
+typedef struct bdscan_token_scores_dims {
+  int64_t rows;
+  int64_t vocab;
+  int64_t ld_logits;
+  int64_t ld_dlogits;
+  int64_t excluded;
+  int32_t top;
+  int32_t dtype;
+  float temperature;
+} bdscan_token_scores_dims;
+
+/* token and logp are nullable together, entropy and stats each, top_ids and
+ * top_logp where top is 0. Outputs may not be inputs. */
+int bdscan_token_scores_forward(const bdscan_token_scores_dims* dims, const void* logits, const int64_t* token,
+                                float* logp, float* entropy, float* stats, int64_t* top_ids, float* top_logp,
+                                void* stream);
+
+/* dlogits: gradient of <dlogp, logp> + <dentropy, entropy> at the logits. dlogp
+ * and dentropy are nullable (zero); token is the forward's, nullable where dlogp
+ * is; stats and entropy (read where dentropy is given) are the forward's.
+ * dlogits may be the logits themselves (same stride). */
+int bdscan_token_scores_backward(const bdscan_token_scores_dims* dims, const void* logits, const int64_t* token,
+                                 const float* stats, const float* entropy, const float* dlogp, const float* dentropy,
+                                 void* dlogits, void* stream);
 
 #ifdef __cplusplus
 }

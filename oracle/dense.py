@@ -109,3 +109,61 @@ def lm_loss_backward(h, w, target, weight, dloss, excluded=-1):
         dh[t] = dz @ w
         dw += np.outer(dz, h[t])
     return dh, dw
+
+
+def token_scores_forward(z, token=None, top=0, excluded=-1, temperature=1.0):
+    """logp (None without token), entropy, ids and log probabilities of the likeliest entries of rows of logits."""
+    rows, vocab = z.shape
+    logp, entropy = np.zeros(rows), np.zeros(rows)
+    ids, best = np.full((rows, top), -1), np.full((rows, top), -np.inf)
+    for t in range(rows):
+        if token is not None and not 0 <= token[t] < vocab:
+            continue
+        v = z[t].astype(np.float64) / temperature
+        if excluded >= 0:
+            v[excluded] = -np.inf
+        if np.isnan(v).any() or (v == np.inf).any():
+            logp[t] = entropy[t] = best[t] = np.nan
+            continue
+        if (v == -np.inf).all():
+            logp[t] = -np.inf
+            continue
+        v -= v.max()
+        v -= np.log(np.exp(v).sum())
+        there = v > -np.inf
+        entropy[t] = -(np.exp(v[there]) * v[there]).sum()
+        if token is not None:
+            logp[t] = v[token[t]]
+        # the logits themselves decide the order; a stable sort keeps the lower index first
+        order = np.argsort(-np.where(there, z[t].astype(np.float64), -np.inf), kind="stable")[:top]
+        order = order[there[order]]
+        ids[t, :len(order)], best[t, :len(order)] = order, v[order]
+    return (None if token is None else logp), entropy, ids, best
+
+
+def token_scores_backward(z, token, dlogp, dentropy, excluded=-1, temperature=1.0):
+    """Gradient at the logits; token, dlogp and dentropy may be None."""
+    rows, vocab = z.shape
+    dz = np.zeros(z.shape)
+    for t in range(rows):
+        if token is not None and not 0 <= token[t] < vocab:
+            continue
+        v = z[t].astype(np.float64) / temperature
+        if excluded >= 0:
+            v[excluded] = -np.inf
+        if (v == -np.inf).all():
+            continue
+        v = v - v.max()
+        v = v - np.log(np.exp(v).sum())
+        p = np.exp(v)
+        there = p > 0
+        plogp = np.where(there, p * np.where(there, v, 0.0), 0.0)
+        if dentropy is not None:
+            dz[t] -= dentropy[t] * (plogp + p * -plogp.sum())
+        if dlogp is not None:
+            dz[t] -= dlogp[t] * p
+            dz[t, token[t]] += dlogp[t]
+        dz[t] /= temperature
+        if excluded >= 0:
+            dz[t, excluded] = 0.0
+    return dz

@@ -204,6 +204,18 @@ GATED_SIGNATURES = [
      [_P(bdscan_gated_linear_dims)] + [c_void_p] * 8 + [ctypes.c_size_t, c_void_p]),
 ]
 
+class bdscan_token_scores_dims(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("ld_logits", ctypes.c_int64),
+                ("ld_dlogits", ctypes.c_int64), ("excluded", ctypes.c_int64), ("top", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+
+# include/bdscan_dense.h, token scores
+SCORES_SIGNATURES = [
+    ("bdscan_token_scores_forward", ctypes.c_int, [_P(bdscan_token_scores_dims)] + [c_void_p] * 8),
+    ("bdscan_token_scores_backward", ctypes.c_int, [_P(bdscan_token_scores_dims)] + [c_void_p] * 8),
+]
+
 BDSCAN_NOALLOC_SCRATCH_BYTES = 32 << 20
 
 _lock = threading.Lock()
@@ -225,7 +237,7 @@ def load(build_if_missing: bool = True, debug=None):
             if not os.path.exists(path):
                 raise RuntimeError(f"libbdscan is not built ({path} missing); run paper_2607_02805_gb300/build.py")
             lib = ctypes.CDLL(path)
-            for name, res, args in SIGNATURES + DENSE_SIGNATURES + GATED_SIGNATURES:
+            for name, res, args in SIGNATURES + DENSE_SIGNATURES + GATED_SIGNATURES + SCORES_SIGNATURES:
                 f = getattr(lib, name)
                 f.restype = res
                 f.argtypes = args
@@ -478,6 +490,16 @@ def bdscan_gated_linear_backward_workspace_size(dims) -> int:
 
 def bdscan_gated_linear_backward(dims, x, w, bias, dy, dx, dw, dbias, workspace, workspace_bytes, stream):
     return load().bdscan_gated_linear_backward(_ref(dims), x, w, bias, dy, dx, dw, dbias, workspace, workspace_bytes,
+                                               stream)
+
+
+def bdscan_token_scores_forward(dims, logits, token, logp, entropy, stats, top_ids, top_logp, stream):
+    return load().bdscan_token_scores_forward(_ref(dims), logits, token, logp, entropy, stats, top_ids, top_logp,
+                                              stream)
+
+
+def bdscan_token_scores_backward(dims, logits, token, stats, entropy, dlogp, dentropy, dlogits, stream):
+    return load().bdscan_token_scores_backward(_ref(dims), logits, token, stats, entropy, dlogp, dentropy, dlogits,
                                                stream)
 
 
@@ -762,3 +784,19 @@ def lm_loss_forward(dims, h, w, target, weight, loss, lse, workspace, stream=Non
 def lm_loss_backward(dims, h, w, target, weight, lse, dloss, dh, dw, workspace, stream=None):
     _call("bdscan_lm_loss_backward", ctypes.byref(dims), _ptr2(h), _ptr(w), _ptr(target), _ptr(weight), _ptr(lse),
           _ptr(dloss), _ptr(dh), _ptr(dw), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def make_token_scores_dims(rows, vocab, top=0, dtype=BDSCAN_BF16, excluded=-1, temperature=1.0, ld_logits=0,
+                           ld_dlogits=0):
+    return bdscan_token_scores_dims(int(rows), int(vocab), int(ld_logits), int(ld_dlogits), int(excluded), int(top),
+                                    int(dtype), float(temperature))
+
+
+def token_scores_forward(dims, logits, token, logp, entropy, stats, top_ids, top_logp, stream=None):
+    _call("bdscan_token_scores_forward", ctypes.byref(dims), _ptr2(logits), _ptr(token), _ptr(logp), _ptr(entropy),
+          _ptr(stats), _ptr(top_ids), _ptr(top_logp), _stream(stream))
+
+
+def token_scores_backward(dims, logits, token, stats, entropy, dlogp, dentropy, dlogits, stream=None):
+    _call("bdscan_token_scores_backward", ctypes.byref(dims), _ptr2(logits), _ptr(token), _ptr(stats), _ptr(entropy),
+          _ptr(dlogp), _ptr(dentropy), _ptr2(dlogits), _stream(stream))

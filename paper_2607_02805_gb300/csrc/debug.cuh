@@ -44,6 +44,7 @@ enum DebugSite : int {
   kSiteSplitReduce,
   kSiteLinearVec,
   kSitePack,
+  kSiteScores,
   kSiteCount
 };
 

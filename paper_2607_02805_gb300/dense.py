@@ -2,8 +2,8 @@
 (include/bdscan_dense.h) from PyTorch.
 
 PyTorch provides the device memory and the stream; every step of the
-computation runs in libbdscan through ``binding``. A ``Linear``, ``GatedLinear``
-or ``LmLoss`` holds one size's outputs, saved pre-activations, gradients and workspaces; the
+computation runs in libbdscan through ``binding``. A ``Linear``, ``GatedLinear``,
+``LmLoss`` or ``TokenScores`` holds one size's outputs, saved pre-activations, gradients and workspaces; the
 inputs and weights belong to the caller. What a call returns are the holder's
 buffers, valid until its next call; a holder serves one stream at a time, and
 its buffers stay where they are for its life, so that a CUDA graph of its calls
@@ -303,3 +303,60 @@ class LmLoss(_Holder):
         _, d, ws, size = self._plan(("backward", ld_h), binding.bdscan_lm_loss_backward_workspace_size)
         binding._call("bdscan_lm_loss_backward", d, *inputs, pl, pd, dh.data_ptr(), dw.data_ptr(), ws, size, s)
         return dh, dw
+
+
+class TokenScores(_Holder):
+    """Log probabilities of tokens, entropies and the `top` likeliest entries of rows of logits [rows, vocab], of
+    softmax(logits / temperature); include/bdscan_dense.h has the rules."""
+
+    def __init__(self, rows, vocab, top=0, dtype=torch.bfloat16, excluded=-1, temperature=1.0, device="cuda"):
+        _code(dtype)
+        super().__init__(device)
+        self.rows, self.vocab, self.top, self.dtype = int(rows), int(vocab), int(top), dtype
+        self.excluded, self.temperature = int(excluded), float(temperature)
+        self._z, self._t, self._k = (self.rows, self.vocab), (self.rows,), (self.rows, self.top)
+
+    def _make_dims(self, ld, ld_out):
+        return binding.make_token_scores_dims(self.rows, self.vocab, self.top, _code(self.dtype), self.excluded,
+                                              self.temperature, ld, ld_out)
+
+    def _dims(self, ld, ld_out):
+        return self._plan(("", ld, ld_out), lambda dims: 0)[1]
+
+    def forward(self, logits, token=None, stream=None):
+        """(logp, entropy, top_ids, top_logp); logp None without `token`, the last two None where top is 0."""
+        pz, ld = _rows("logits", logits, self._z, self.dtype, self._index)
+        pt = _whole("token", token, self._t, torch.int64, self._index)
+        s = self._enter(stream)
+        logp = self._buffer("logp", self._t, torch.float32) if token is not None else None
+        entropy = self._buffer("entropy", self._t, torch.float32)
+        stats = self._buffer("stats", (self.rows, 2), torch.float32)
+        ids = self._buffer("ids", self._k, torch.int64) if self.top else None
+        top = self._buffer("top", self._k, torch.float32) if self.top else None
+        p = binding._ptr
+        binding._call("bdscan_token_scores_forward", self._dims(ld, 0), pz, pt, p(logp), entropy.data_ptr(),
+                      stats.data_ptr(), p(ids), p(top), s)
+        return logp, entropy, ids, top
+
+    def backward(self, logits, token=None, dlogp=None, dentropy=None, out=None, stream=None):
+        """Gradient of <dlogp, logp> + <dentropy, entropy> at the logits of the last forward (the holder's buffer, or
+        `out`, which may be the logits)."""
+        f32, dev = torch.float32, self._index
+        pz, ld = _rows("logits", logits, self._z, self.dtype, dev)
+        po, ld_out = _rows("out", out, self._z, self.dtype, dev)
+        pt = _whole("token", token, self._t, torch.int64, dev)
+        pl = _whole("dlogp", dlogp, self._t, f32, dev)
+        ph = _whole("dentropy", dentropy, self._t, f32, dev)
+        if "stats" not in self._buf:
+            raise ValueError("backward needs a forward")
+        s = self._enter(stream)
+        dz = out
+        if out is None:
+            dz = self._buffer("dlogits", self._z, self.dtype)
+            po, ld_out = dz.data_ptr(), self.vocab
+            _apart("logits", pz, po)
+        elif po == pz and ld_out != ld:
+            raise ValueError("out begins where the logits do, with another row stride")
+        binding._call("bdscan_token_scores_backward", self._dims(ld, ld_out), pz, pt, self._buf["stats"].data_ptr(),
+                      self._buf["entropy"].data_ptr(), pl, ph, po, s)
+        return dz
