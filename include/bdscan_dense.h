@@ -9,6 +9,8 @@
  *   - the weighted softmax cross entropy of the language-model head over the
  *     vocabulary (the masked objective, Sec. 3; Sec. 4.1), at the rows that
  *     count, without keeping the logits, forward and backward;
+ *   - the distillation loss: how far the head's distribution is from a
+ *     teacher's, of which the likeliest entries are known, the same way;
  *   - token scores of given logits: log probabilities of tokens, entropies and
  *     the likeliest entries (what a denoising step chooses its tokens by, and
  *     what a teacher hands on), forward and backward.
@@ -147,6 +149,44 @@ size_t bdscan_lm_loss_backward_workspace_size(const bdscan_lm_loss_dims* dims);
 int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, const void* w, const int64_t* target,
                             const float* weight, const float* lse, const float* dloss, void* dh, void* dw,
                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* loss[t] = weight[t] sum_v q_tv (log q_tv - log p_tv), the divergence of the
+ * student's p_t = softmax(h w^T / temperature) over the whole vocabulary from the
+ * teacher's q_t = softmax(teacher[t] / temperature) over the row's known entries:
+ * those whose id is inside 0 .. vocab - 1 and not `excluded`, with a teacher's
+ * logit above minus infinity. An id that comes twice has both shares. lse[t] = log sum_v exp(z[t][v] /
+ * temperature). A row counts where its weight is not zero and an entry is known;
+ * the others get loss = lse = 0 and no gradient, whatever h holds there, and cost
+ * no product. `excluded` as in the vocabulary loss.
+ * Layouts: h, w, weight, loss, lse, dloss as in the vocabulary loss; ids
+ * [rows][top] int64, teacher [rows][top] fp32, top 1 .. 64; z [rows][top] fp32
+ * receives h w^T at the known entries of the rows that count, else 0, which the
+ * backward reads. temperature 2^-20 .. 2^20. */
+typedef struct bdscan_distill_loss_dims {
+  int64_t rows;
+  int64_t d_model;
+  int64_t vocab;
+  int64_t ld_h;
+  int64_t excluded;
+  int32_t top;
+  int32_t dtype;
+  float temperature;
+} bdscan_distill_loss_dims;
+
+/* weight is nullable (ones). */
+size_t bdscan_distill_loss_forward_workspace_size(const bdscan_distill_loss_dims* dims);
+int bdscan_distill_loss_forward(const bdscan_distill_loss_dims* dims, const void* h, const void* w, const int64_t* ids,
+                                const float* teacher, const float* weight, float* loss, float* lse, float* z,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of <dloss, loss> (dloss nullable: ones) with respect to h
+ * [rows][d_model] and w [vocab][d_model], of `dtype`, as in the vocabulary loss
+ * with p - q at the logits, over the temperature. lse and z are the forward's. */
+size_t bdscan_distill_loss_backward_workspace_size(const bdscan_distill_loss_dims* dims);
+int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const void* h, const void* w,
+                                 const int64_t* ids, const float* teacher, const float* weight, const float* lse,
+                                 const float* z, const float* dloss, void* dh, void* dw, void* workspace,
+                                 size_t workspace_bytes, void* stream);
 
 /* Scores of rows of logits z, with p = softmax(z / temperature):
  *   logp[t] = log p[token[t]],  entropy[t] = -sum_v p_v log p_v,

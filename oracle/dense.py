@@ -111,6 +111,55 @@ def lm_loss_backward(h, w, target, weight, dloss, excluded=-1):
     return dh, dw
 
 
+def _teacher(ids, logits, vocab, excluded, temperature):
+    """Known entries of a row, and their q."""
+    known = (ids >= 0) & (ids < vocab) & (ids != excluded) & (logits != -np.inf)
+    q = np.zeros(len(ids))
+    if known.any():
+        t = logits[known] / temperature
+        e = np.exp(t - t.max())
+        q[known] = e / e.sum()
+    return known, q
+
+
+def distill_loss_forward(h, w, ids, teacher, weight, excluded=-1, temperature=1.0):
+    """loss, log sum and the student's logits at the known entries, per row."""
+    loss, lse, at = np.zeros(h.shape[0]), np.zeros(h.shape[0]), np.zeros(ids.shape)
+    for t in range(h.shape[0]):
+        known, q = _teacher(ids[t], teacher[t], w.shape[0], excluded, temperature)
+        if weight[t] == 0 or not known.any():
+            continue
+        raw = w @ h[t]
+        z = raw / temperature
+        if excluded >= 0:
+            z[excluded] = -np.inf
+        lse[t] = z.max() + np.log(np.exp(z - z.max()).sum())
+        at[t, known] = raw[ids[t, known]]
+        full = np.zeros(w.shape[0])
+        np.add.at(full, ids[t, known], q[known])
+        some = full > 0
+        loss[t] = weight[t] * (full[some] * (np.log(full[some]) - z[some] + lse[t])).sum()
+    return loss, lse, at
+
+
+def distill_loss_backward(h, w, ids, teacher, weight, dloss, excluded=-1, temperature=1.0):
+    """dh, dw."""
+    dh, dw = np.zeros_like(h), np.zeros_like(w)
+    _, lse, _ = distill_loss_forward(h, w, ids, teacher, weight, excluded, temperature)
+    for t in range(h.shape[0]):
+        known, q = _teacher(ids[t], teacher[t], w.shape[0], excluded, temperature)
+        if weight[t] == 0 or dloss[t] == 0 or not known.any():
+            continue
+        dz = np.exp(w @ h[t] / temperature - lse[t])
+        if excluded >= 0:
+            dz[excluded] = 0.0
+        np.subtract.at(dz, ids[t, known], q[known])
+        dz *= weight[t] * dloss[t] / temperature
+        dh[t] = dz @ w
+        dw += np.outer(dz, h[t])
+    return dh, dw
+
+
 def token_scores_forward(z, token=None, top=0, excluded=-1, temperature=1.0):
     """logp (None without token), entropy, ids and log probabilities of the likeliest entries of rows of logits."""
     rows, vocab = z.shape

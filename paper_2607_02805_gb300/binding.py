@@ -204,6 +204,23 @@ GATED_SIGNATURES = [
      [_P(bdscan_gated_linear_dims)] + [c_void_p] * 8 + [ctypes.c_size_t, c_void_p]),
 ]
 
+class bdscan_distill_loss_dims(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d_model", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("ld_h", ctypes.c_int64), ("excluded", ctypes.c_int64), ("top", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+
+# include/bdscan_dense.h, the distillation loss
+DISTILL_SIGNATURES = [
+    ("bdscan_distill_loss_forward_workspace_size", ctypes.c_size_t, [_P(bdscan_distill_loss_dims)]),
+    ("bdscan_distill_loss_forward", ctypes.c_int,
+     [_P(bdscan_distill_loss_dims)] + [c_void_p] * 9 + [ctypes.c_size_t, c_void_p]),
+    ("bdscan_distill_loss_backward_workspace_size", ctypes.c_size_t, [_P(bdscan_distill_loss_dims)]),
+    ("bdscan_distill_loss_backward", ctypes.c_int,
+     [_P(bdscan_distill_loss_dims)] + [c_void_p] * 11 + [ctypes.c_size_t, c_void_p]),
+]
+
+
 class bdscan_token_scores_dims(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("ld_logits", ctypes.c_int64),
                 ("ld_dlogits", ctypes.c_int64), ("excluded", ctypes.c_int64), ("top", ctypes.c_int32),
@@ -237,7 +254,8 @@ def load(build_if_missing: bool = True, debug=None):
             if not os.path.exists(path):
                 raise RuntimeError(f"libbdscan is not built ({path} missing); run paper_2607_02805_gb300/build.py")
             lib = ctypes.CDLL(path)
-            for name, res, args in SIGNATURES + DENSE_SIGNATURES + GATED_SIGNATURES + SCORES_SIGNATURES:
+            for name, res, args in (SIGNATURES + DENSE_SIGNATURES + GATED_SIGNATURES + DISTILL_SIGNATURES
+                                    + SCORES_SIGNATURES):
                 f = getattr(lib, name)
                 f.restype = res
                 f.argtypes = args
@@ -491,6 +509,25 @@ def bdscan_gated_linear_backward_workspace_size(dims) -> int:
 def bdscan_gated_linear_backward(dims, x, w, bias, dy, dx, dw, dbias, workspace, workspace_bytes, stream):
     return load().bdscan_gated_linear_backward(_ref(dims), x, w, bias, dy, dx, dw, dbias, workspace, workspace_bytes,
                                                stream)
+
+
+def bdscan_distill_loss_forward_workspace_size(dims) -> int:
+    return load().bdscan_distill_loss_forward_workspace_size(_ref(dims))
+
+
+def bdscan_distill_loss_forward(dims, h, w, ids, teacher, weight, loss, lse, z, workspace, workspace_bytes, stream):
+    return load().bdscan_distill_loss_forward(_ref(dims), h, w, ids, teacher, weight, loss, lse, z, workspace,
+                                              workspace_bytes, stream)
+
+
+def bdscan_distill_loss_backward_workspace_size(dims) -> int:
+    return load().bdscan_distill_loss_backward_workspace_size(_ref(dims))
+
+
+def bdscan_distill_loss_backward(dims, h, w, ids, teacher, weight, lse, z, dloss, dh, dw, workspace, workspace_bytes,
+                                 stream):
+    return load().bdscan_distill_loss_backward(_ref(dims), h, w, ids, teacher, weight, lse, z, dloss, dh, dw,
+                                               workspace, workspace_bytes, stream)
 
 
 def bdscan_token_scores_forward(dims, logits, token, logp, entropy, stats, top_ids, top_logp, stream):
@@ -784,6 +821,22 @@ def lm_loss_forward(dims, h, w, target, weight, loss, lse, workspace, stream=Non
 def lm_loss_backward(dims, h, w, target, weight, lse, dloss, dh, dw, workspace, stream=None):
     _call("bdscan_lm_loss_backward", ctypes.byref(dims), _ptr2(h), _ptr(w), _ptr(target), _ptr(weight), _ptr(lse),
           _ptr(dloss), _ptr(dh), _ptr(dw), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def make_distill_loss_dims(rows, d_model, vocab, top, dtype=BDSCAN_BF16, excluded=-1, temperature=1.0, ld_h=0):
+    return bdscan_distill_loss_dims(int(rows), int(d_model), int(vocab), int(ld_h), int(excluded), int(top),
+                                    int(dtype), float(temperature))
+
+
+def distill_loss_forward(dims, h, w, ids, teacher, weight, loss, lse, z, workspace, stream=None):
+    _call("bdscan_distill_loss_forward", ctypes.byref(dims), _ptr2(h), _ptr(w), _ptr(ids), _ptr(teacher), _ptr(weight),
+          _ptr(loss), _ptr(lse), _ptr(z), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def distill_loss_backward(dims, h, w, ids, teacher, weight, lse, z, dloss, dh, dw, workspace, stream=None):
+    _call("bdscan_distill_loss_backward", ctypes.byref(dims), _ptr2(h), _ptr(w), _ptr(ids), _ptr(teacher),
+          _ptr(weight), _ptr(lse), _ptr(z), _ptr(dloss), _ptr(dh), _ptr(dw), _ptr(workspace), _nbytes(workspace),
+          _stream(stream))
 
 
 def make_token_scores_dims(rows, vocab, top=0, dtype=BDSCAN_BF16, excluded=-1, temperature=1.0, ld_logits=0,

@@ -45,6 +45,7 @@ enum DebugSite : int {
   kSiteLinearVec,
   kSitePack,
   kSiteScores,
+  kSiteDistill,
   kSiteCount
 };
 

@@ -226,7 +226,7 @@ __device__ __forceinline__ void loss_row(const LossRowsParams& p, int64_t i, flo
   wt = in && p.weight != nullptr ? p.weight[i] : 1.f;
   const float dl = in && p.dloss != nullptr ? p.dloss[i] : 1.f;
   if (wt == 0.f || dl == 0.f || tg >= p.vocab || tg < 0) tg = -1;
-  wt *= dl;
+  wt *= dl * p.scale;
 }
 // The slot's bookkeeping of a row that counts, the outputs of one that does not.
 __device__ __forceinline__ void loss_row_out(const LossRowsParams& p, int64_t i, int to, float wt, int64_t tg) {

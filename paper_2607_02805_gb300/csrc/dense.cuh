@@ -51,6 +51,7 @@ struct GemmParams {
   int64_t out_last, out_extent;  // last element written and elements of `out` or `part` (debug build)
   // kEpiStats / kEpiDz: rows i are the rows that count; column j is entry v0 + j
   int v0, excluded;
+  float scale;           // of the logits before the softmax: 1 / temperature
   const int* target;     // [rows] of the rows that count
   float2* part;          // [column tiles][rows] (maximum, sum of exponentials), base 2
   float* at_target;      // [rows]
@@ -158,6 +159,7 @@ struct LossRowsParams {
   int *count, *idx, *tgt, *pos;  // count [2]: rows that count, and a zero; pos [rows]: slot, or -1
   float *gscale, *lse_c;
   float *loss, *lse;
+  float scale;  // of the gradient scales: 1 / temperature
 };
 cudaError_t launch_loss_rows(const LossRowsParams& p, cudaStream_t s);
 // launch_loss_rows and launch_pack_rows in one, for up to small_loss_rows() rows.
@@ -166,6 +168,31 @@ cudaError_t launch_loss_prep(const LossRowsParams& l, const PackParams& p, const
 cudaError_t launch_loss_combine(const float2* part, int parts, int64_t rows_ld, const float* at_target,
                                 const int* count, const int* idx, const float* weight, float* loss, float* lse,
                                 int64_t rows, cudaStream_t s);
+// The distillation loss around the vocabulary loss's products (distill.cu).
+struct DistillParams {
+  const int64_t* ids;    // [rows][top], with the teacher's logits
+  const float* teacher;
+  const float* weight;   // [rows] or null
+  int64_t rows, vocab, excluded;
+  int top;
+  float scale, scale2;   // 1 / temperature, and log2(e) / temperature
+  int64_t* target;       // launch_distill_rows: [rows] the first known entry, or -1
+  // launch_distill_join: slots of the rows that count, their partial statistics and the operands as they lie
+  const int *count, *idx;
+  const float2* part;
+  int parts, d_model;
+  int64_t rows_ld, ld_h;
+  const void *h, *w;
+  float *z, *loss, *lse;  // [rows][top], [rows]; z null: launch_distill_rows leaves it alone
+  // launch_distill_dz: entries v0 .. v0 + n - 1 in `pieces` planes
+  const float *lse_in, *z_in;
+  __nv_bfloat16* dz;
+  int64_t ld_dz, plane, dz_extent;
+  int v0, n, pieces;
+};
+cudaError_t launch_distill_rows(const DistillParams& p, cudaStream_t s);
+cudaError_t launch_distill_join(const DistillParams& p, int f32, cudaStream_t s);
+cudaError_t launch_distill_dz(const DistillParams& p, cudaStream_t s);
 int* ssd_wait_flag_ptr();  // ssd.cu
 
 }  // namespace bds

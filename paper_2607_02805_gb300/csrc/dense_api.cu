@@ -285,6 +285,7 @@ GemmParams geometry(const Plan& q, int64_t m, int64_t n, int64_t k, int* flag) {
   // 24); in the last of several tiles, smaller boxes brought nothing (300 x 1024 x 4000: 8.7 us against 7.1)
   p.a_rows = m < 128 ? (int)up(m, 8) : 128;
   p.excluded = -1;
+  p.scale = 1.f;
   p.flag = flag;
   return p;
 }
@@ -586,6 +587,7 @@ GatedBwdWs gated_bwd_ws(const Gated& l) {
 struct Loss {
   int64_t T, K, V, ld_h, excluded;
   int dtype, pieces;
+  float scale;  // 1 / temperature
 };
 int check_loss(const bdscan_lm_loss_dims* d, Loss* l, const char* fn) {
   api_begin();
@@ -607,6 +609,7 @@ int check_loss(const bdscan_lm_loss_dims* d, Loss* l, const char* fn) {
   l->excluded = d->excluded;
   l->dtype = d->dtype;
   l->pieces = d->dtype == BDSCAN_F32 ? 3 : 1;
+  l->scale = 1.f;
   return BDSCAN_OK;
 }
 
@@ -740,6 +743,108 @@ cudaError_t prepare_rows(const Loss& l, const LossRows& r, const LossRowsParams&
   return e != cudaSuccess ? e : api_launched(launch_pack_rows(p, pw, s), s);
 }
 
+// Where the rows that count go; the outputs' pointers are the caller's.
+LossRowsParams rows_params(const Loss& l, const LossRows& r, const int64_t* target, const float* weight, char* base) {
+  LossRowsParams rp;
+  memset(&rp, 0, sizeof(rp));
+  rp.target = target;
+  rp.weight = weight;
+  rp.rows = l.T;
+  rp.vocab = l.V;
+  rp.count = (int*)(base + r.count);
+  rp.idx = (int*)(base + r.idx);
+  rp.tgt = (int*)(base + r.tgt);
+  rp.pos = (int*)(base + r.pos);
+  rp.scale = l.scale;
+  return rp;
+}
+// The forward's product: partial statistics of the rows that count.
+GemmParams stats_params(const Loss& l, const LossFwdWs& ws, const LossRowsParams& rp, char* base, int* flag) {
+  GemmParams p = geometry(ws.q, l.T, l.V, l.K, flag);
+  p.rows_dev = rp.count;
+  p.rows_axis = 1;
+  p.target = rp.tgt;
+  p.excluded = (int)l.excluded;
+  p.scale = l.scale;
+  p.part = (float2*)(base + ws.part);
+  p.at_target = (float*)(base + ws.at);
+  p.rows_ld = ws.r.rows;
+  p.out_last = (ws.parts - 1) * p.rows_ld + l.T - 1;
+  p.out_extent = ws.parts * p.rows_ld;
+  return p;
+}
+
+// The backward, piece by piece of the vocabulary: the gradient at the logits
+// (p - 1 at the target, as the epilogue leaves it; `mend(v0, n, dz)` may launch
+// what changes it), then both products.
+template <typename F>
+cudaError_t loss_backward(const Loss& l, const LossBwdWs& ws, LossRowsParams rp, const void* h, const void* w, void* dh,
+                          void* dw, char* base, int* flag, cudaStream_t s, F mend) {
+  const size_t elt = l.dtype == BDSCAN_F32 ? 4 : 2;
+  rp.gscale = (float*)(base + ws.r.gscale);
+  rp.lse_c = (float*)(base + ws.r.lse);
+  Operand a, scaled;
+  PackParams pw;
+  const Operand b = operand(&pw, l.dtype, w, l.V, l.K, l.K, base + ws.w);
+  cudaError_t e = prepare_rows(l, ws.r, rp, h, base, dh, pw, &a, &scaled, s);
+  const int64_t ld_dz = up(ws.piece, 8), ld_acc = up(l.K, 4);
+  const int f32 = l.dtype == BDSCAN_F32;
+  float* part = (float*)(base + ws.part);
+  float* acc = (float*)(base + ws.acc);
+  for (int i = 0; i < ws.pieces && e == cudaSuccess; ++i) {
+    const int64_t v0 = i * ws.piece, n = l.V - v0 < ws.piece ? l.V - v0 : ws.piece;
+    Operand bp = b;  // this piece's rows of w
+    bp.base = (const char*)b.base + v0 * b.ld * 2;
+    bp.rows = n;
+    const Operand dz{base + ws.dz, n, ws.r.rows, ld_dz, l.pieces, ws.r.rows * ld_dz};
+    // the logits' gradient
+    Plan q = ws.qz;
+    q.cfg.epi = kEpiDz;
+    GemmParams p = geometry(q, l.T, n, l.K, flag);
+    p.rows_dev = rp.count;
+    p.rows_axis = 1;
+    p.target = rp.tgt;
+    p.v0 = (int)v0;
+    p.excluded = (int)l.excluded;
+    p.scale = l.scale;
+    p.lse = rp.lse_c;
+    p.out = base + ws.dz;
+    p.ld_out = ld_dz;
+    p.out_last = (l.pieces - 1) * ws.r.rows * ld_dz + (ws.r.rows - 1) * ld_dz + n - 1;
+    p.out_extent = l.pieces * ws.r.rows * ld_dz;
+    e = run_product(q, p, a, bp, l.pieces, ws.r.rows * ld_dz, ws.r.rows, s);
+    if (e == cudaSuccess) e = mend(v0, n, dz);
+    // this piece's rows of dw, and its part of dh: fp32 sums over the pieces, the last one writes dh
+    const bool last = i + 1 == ws.pieces;
+    GemmParams gw = geometry(ws.g.w, n, l.K, ws.r.rows, flag), gh = geometry(ws.g.x, l.T, l.K, n, flag);
+    gw.rows_dev = gh.rows_dev = rp.count;
+    gw.rows_axis = 2;
+    gw.out = (char*)dw + (size_t)v0 * l.K * elt;
+    gw.ld_out = l.K;
+    gw.out_f32 = f32;
+    gw.out_extent = n * l.K;
+    gh.rows_axis = 1;
+    gh.res = i > 0 ? acc : nullptr;
+    gh.ld_res = ld_acc;
+    gh.res_f32 = 1;
+    gh.out = last ? dh : acc;
+    gh.ld_out = last ? l.K : ld_acc;
+    gh.out_f32 = last ? f32 : 1;
+    gh.row_map = last ? rp.idx : nullptr;
+    gh.row_scale = rp.gscale;
+    gh.out_extent = last ? l.T * l.K : l.T * ld_acc;
+    // With several pieces the rows that count decide how the tiles of the two would have to be dealt, and only the
+    // device knows them: 16384 rows, half of them counting, took 1817 us as pairs and 1762 one after the other.
+    if (e == cudaSuccess && ws.pieces == 1 && ws.g.one) {
+      e = run_pair(ws.g, gh, gw, dz, bp, scaled, s);
+    } else {
+      if (e == cudaSuccess) e = run_out(ws.g.w, true, true, gw, dz, scaled, part, s);
+      if (e == cudaSuccess) e = run_out(ws.g.x, false, true, gh, dz, bp, part, s, !last);
+    }
+  }
+  return e;
+}
+
 int check_workspace(const void* ws, size_t have, size_t need, const char* fn) {
   if (need == 0) return BDSCAN_OK;
   DENSE_REQ(ws, fn, "workspace");
@@ -755,6 +860,45 @@ int check_device(const char* fn, int** flag) {
     return fail_msg(BDSCAN_ERR_UNSUPPORTED, fn, "the driver has no tensor-map encoder");
   *flag = ssd_wait_flag_ptr();
   return *flag != nullptr ? BDSCAN_OK : fail_msg(BDSCAN_ERR_CUDA, fn, "cannot locate the device wait flag");
+}
+
+// ---------------------------------------------------------------------------
+// distillation: the loss above from a teacher's entries
+// ---------------------------------------------------------------------------
+constexpr int kMaxEntries = 64;
+int check_distill(const bdscan_distill_loss_dims* d, Loss* l, const char* fn) {
+  api_begin();
+  if (d == nullptr) return fail_msg(BDSCAN_ERR_ARG, fn, "dims is NULL");
+  const bdscan_lm_loss_dims loss = {d->rows, d->d_model, d->vocab, d->ld_h, d->excluded, d->dtype};
+  const int rc = check_loss(&loss, l, fn);
+  if (rc) return rc;
+  if (d->top <= 0) return fail_msg(BDSCAN_ERR_ARG, fn, "top must be positive");
+  if (d->top > kMaxEntries) return fail_msg(BDSCAN_ERR_UNSUPPORTED, fn, "top above 64");
+  if (!(d->temperature >= 0x1p-20f && d->temperature <= 0x1p20f))
+    return fail_msg(BDSCAN_ERR_ARG, fn, "temperature is not between 2^-20 and 2^20");
+  l->scale = 1.f / d->temperature;
+  return BDSCAN_OK;
+}
+// The entries that stand for the rows' targets, behind the loss's own workspace.
+size_t target_bytes(const Loss& l) { return al256((size_t)l.T * 8); }
+
+DistillParams distill_params(const Loss& l, const LossRowsParams& rp, int top, const int64_t* ids,
+                             const float* teacher) {
+  DistillParams p;
+  memset(&p, 0, sizeof(p));
+  p.ids = ids;
+  p.teacher = teacher;
+  p.weight = rp.weight;
+  p.rows = l.T;
+  p.vocab = l.V;
+  p.excluded = l.excluded;
+  p.top = top;
+  p.scale = l.scale;
+  p.scale2 = 1.4426950408889634f * l.scale;
+  p.target = const_cast<int64_t*>(rp.target);
+  p.count = rp.count;
+  p.idx = rp.idx;
+  return p;
 }
 
 }  // namespace
@@ -1093,16 +1237,7 @@ int bdscan_lm_loss_forward(const bdscan_lm_loss_dims* dims, const void* h, const
   if ((rc = check_device(fn, &flag))) return rc;
   cudaStream_t s = (cudaStream_t)stream;
   char* base = (char*)workspace;
-  LossRowsParams rp;
-  memset(&rp, 0, sizeof(rp));
-  rp.target = target;
-  rp.weight = weight;
-  rp.rows = l.T;
-  rp.vocab = l.V;
-  rp.count = (int*)(base + ws.r.count);
-  rp.idx = (int*)(base + ws.r.idx);
-  rp.tgt = (int*)(base + ws.r.tgt);
-  rp.pos = (int*)(base + ws.r.pos);
+  LossRowsParams rp = rows_params(l, ws.r, target, weight, base);
   rp.loss = loss;
   rp.lse = lse;
   Operand a;
@@ -1113,16 +1248,7 @@ int bdscan_lm_loss_forward(const bdscan_lm_loss_dims* dims, const void* h, const
   if (e == cudaSuccess) {
     Plan q = ws.q;
     q.cfg.epi = kEpiStats;
-    GemmParams p = geometry(q, l.T, l.V, l.K, flag);
-    p.rows_dev = rp.count;
-    p.rows_axis = 1;
-    p.target = rp.tgt;
-    p.excluded = (int)l.excluded;
-    p.part = (float2*)(base + ws.part);
-    p.at_target = (float*)(base + ws.at);
-    p.rows_ld = ws.r.rows;
-    p.out_last = (ws.parts - 1) * p.rows_ld + l.T - 1;
-    p.out_extent = ws.parts * p.rows_ld;
+    GemmParams p = stats_params(l, ws, rp, base, flag);
     if (last_joins) {
       p.ticket = rp.count + 1;
       p.row_idx = rp.idx;
@@ -1171,77 +1297,126 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
   int* flag;
   if ((rc = check_device(fn, &flag))) return rc;
   char* base = (char*)workspace;
-  LossRowsParams rp;
-  memset(&rp, 0, sizeof(rp));
-  rp.target = target;
-  rp.weight = weight;
+  LossRowsParams rp = rows_params(l, ws.r, target, weight, base);
   rp.dloss = dloss;
   rp.lse_in = lse;
-  rp.rows = l.T;
-  rp.vocab = l.V;
-  rp.count = (int*)(base + ws.r.count);
-  rp.idx = (int*)(base + ws.r.idx);
-  rp.tgt = (int*)(base + ws.r.tgt);
-  rp.pos = (int*)(base + ws.r.pos);
-  rp.gscale = (float*)(base + ws.r.gscale);
-  rp.lse_c = (float*)(base + ws.r.lse);
-  Operand a, scaled;
+  const cudaError_t e = loss_backward(l, ws, rp, h, w, dh, dw, base, flag, (cudaStream_t)stream,
+                                      [](int64_t, int64_t, const Operand&) { return cudaSuccess; });
+  return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+}
+
+size_t bdscan_distill_loss_forward_workspace_size(const bdscan_distill_loss_dims* dims) {
+  Loss l;
+  if (check_distill(dims, &l, "bdscan_distill_loss_forward_workspace_size") != BDSCAN_OK || l.T == 0) return 0;
+  return loss_fwd_ws(l).total + target_bytes(l);
+}
+
+int bdscan_distill_loss_forward(const bdscan_distill_loss_dims* dims, const void* h, const void* w, const int64_t* ids,
+                                const float* teacher, const float* weight, float* loss, float* lse, float* z,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "bdscan_distill_loss_forward";
+  Loss l;
+  int rc = check_distill(dims, &l, fn);
+  if (rc) return rc;
+  if (l.T == 0) return api_ok();
+  DENSE_REQ(h, fn, "h");
+  DENSE_REQ(w, fn, "w");
+  DENSE_REQ(ids, fn, "ids");
+  DENSE_REQ(teacher, fn, "teacher");
+  DENSE_OPT(weight, fn, "weight");
+  DENSE_REQ(loss, fn, "loss");
+  DENSE_REQ(lse, fn, "lse");
+  DENSE_REQ(z, fn, "z");
+  const LossFwdWs ws = loss_fwd_ws(l);
+  if ((rc = check_workspace(workspace, workspace_bytes, ws.total + target_bytes(l), fn))) return rc;
+  int* flag;
+  if ((rc = check_device(fn, &flag))) return rc;
+  cudaStream_t s = (cudaStream_t)stream;
+  char* base = (char*)workspace;
+  LossRowsParams rp = rows_params(l, ws.r, (const int64_t*)(base + ws.total), weight, base);
+  rp.loss = loss;
+  rp.lse = lse;
+  DistillParams d = distill_params(l, rp, dims->top, ids, teacher);
+  d.z = z;
+  cudaError_t e = api_launched(launch_distill_rows(d, s), s);
+  Operand a;
   PackParams pw;
   const Operand b = operand(&pw, l.dtype, w, l.V, l.K, l.K, base + ws.w);
-  cudaError_t e = prepare_rows(l, ws.r, rp, h, base, dh, pw, &a, &scaled, s);
-  const int64_t ld_dz = up(ws.piece, 8), ld_acc = up(l.K, 4);
-  const int f32 = l.dtype == BDSCAN_F32;
-  float* part = (float*)(base + ws.part);
-  float* acc = (float*)(base + ws.acc);
-  for (int i = 0; i < ws.pieces && e == cudaSuccess; ++i) {
-    const int64_t v0 = i * ws.piece, n = l.V - v0 < ws.piece ? l.V - v0 : ws.piece;
-    Operand bp = b;  // this piece's rows of w
-    bp.base = (const char*)b.base + v0 * b.ld * 2;
-    bp.rows = n;
-    const Operand dz{base + ws.dz, n, ws.r.rows, ld_dz, l.pieces, ws.r.rows * ld_dz};
-    // the logits' gradient
-    Plan q = ws.qz;
-    q.cfg.epi = kEpiDz;
-    GemmParams p = geometry(q, l.T, n, l.K, flag);
-    p.rows_dev = rp.count;
-    p.rows_axis = 1;
-    p.target = rp.tgt;
-    p.v0 = (int)v0;
-    p.excluded = (int)l.excluded;
-    p.lse = rp.lse_c;
-    p.out = base + ws.dz;
-    p.ld_out = ld_dz;
-    p.out_last = (l.pieces - 1) * ws.r.rows * ld_dz + (ws.r.rows - 1) * ld_dz + n - 1;
-    p.out_extent = l.pieces * ws.r.rows * ld_dz;
-    e = run_product(q, p, a, bp, l.pieces, ws.r.rows * ld_dz, ws.r.rows, s);
-    // this piece's rows of dw, and its part of dh: fp32 sums over the pieces, the last one writes dh
-    const bool last = i + 1 == ws.pieces;
-    GemmParams gw = geometry(ws.g.w, n, l.K, ws.r.rows, flag), gh = geometry(ws.g.x, l.T, l.K, n, flag);
-    gw.rows_dev = gh.rows_dev = rp.count;
-    gw.rows_axis = 2;
-    gw.out = (char*)dw + (size_t)v0 * l.K * elt;
-    gw.ld_out = l.K;
-    gw.out_f32 = f32;
-    gw.out_extent = n * l.K;
-    gh.rows_axis = 1;
-    gh.res = i > 0 ? acc : nullptr;
-    gh.ld_res = ld_acc;
-    gh.res_f32 = 1;
-    gh.out = last ? dh : acc;
-    gh.ld_out = last ? l.K : ld_acc;
-    gh.out_f32 = last ? f32 : 1;
-    gh.row_map = last ? rp.idx : nullptr;
-    gh.row_scale = rp.gscale;
-    gh.out_extent = last ? l.T * l.K : l.T * ld_acc;
-    // With several pieces the rows that count decide how the tiles of the two would have to be dealt, and only the
-    // device knows them: 16384 rows, half of them counting, took 1817 us as pairs and 1762 one after the other.
-    if (e == cudaSuccess && ws.pieces == 1 && ws.g.one) {
-      e = run_pair(ws.g, gh, gw, dz, bp, scaled, s);
-    } else {
-      if (e == cudaSuccess) e = run_out(ws.g.w, true, true, gw, dz, scaled, part, s);
-      if (e == cudaSuccess) e = run_out(ws.g.x, false, true, gh, dz, bp, part, s, !last);
-    }
+  if (e == cudaSuccess) e = prepare_rows(l, ws.r, rp, h, base, nullptr, pw, &a, nullptr, s);
+  if (e == cudaSuccess) {
+    Plan q = ws.q;
+    q.cfg.epi = kEpiStats;
+    e = run_product(q, stats_params(l, ws, rp, base, flag), a, b, 1, 0, l.T, s);
   }
+  if (e == cudaSuccess) {
+    d.part = (const float2*)(base + ws.part);
+    d.parts = ws.parts;
+    d.rows_ld = ws.r.rows;
+    d.d_model = (int)l.K;
+    d.ld_h = l.ld_h;
+    d.h = h;
+    d.w = w;
+    d.loss = loss;
+    d.lse = lse;
+    e = api_launched(launch_distill_join(d, l.dtype == BDSCAN_F32, s), s);
+  }
+  return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+}
+
+size_t bdscan_distill_loss_backward_workspace_size(const bdscan_distill_loss_dims* dims) {
+  Loss l;
+  if (check_distill(dims, &l, "bdscan_distill_loss_backward_workspace_size") != BDSCAN_OK || l.T == 0) return 0;
+  return loss_bwd_ws(l).total + target_bytes(l);
+}
+
+int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const void* h, const void* w,
+                                 const int64_t* ids, const float* teacher, const float* weight, const float* lse,
+                                 const float* z, const float* dloss, void* dh, void* dw, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  const char* fn = "bdscan_distill_loss_backward";
+  Loss l;
+  int rc = check_distill(dims, &l, fn);
+  if (rc) return rc;
+  cudaStream_t s = (cudaStream_t)stream;
+  DENSE_REQ(dw, fn, "dw");
+  if (l.T == 0) {
+    const cudaError_t e = cudaMemsetAsync(dw, 0, (size_t)l.V * l.K * (l.dtype == BDSCAN_F32 ? 4 : 2), s);
+    return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
+  }
+  DENSE_REQ(h, fn, "h");
+  DENSE_REQ(w, fn, "w");
+  DENSE_REQ(ids, fn, "ids");
+  DENSE_REQ(teacher, fn, "teacher");
+  DENSE_OPT(weight, fn, "weight");
+  DENSE_REQ(lse, fn, "lse");
+  DENSE_REQ(z, fn, "z");
+  DENSE_OPT(dloss, fn, "dloss");
+  DENSE_REQ(dh, fn, "dh");
+  const LossBwdWs ws = loss_bwd_ws(l);
+  if ((rc = check_workspace(workspace, workspace_bytes, ws.total + target_bytes(l), fn))) return rc;
+  int* flag;
+  if ((rc = check_device(fn, &flag))) return rc;
+  char* base = (char*)workspace;
+  LossRowsParams rp = rows_params(l, ws.r, (const int64_t*)(base + ws.total), weight, base);
+  rp.dloss = dloss;
+  rp.lse_in = lse;
+  DistillParams d = distill_params(l, rp, dims->top, ids, teacher);
+  d.lse_in = lse;
+  d.z_in = z;
+  cudaError_t e = api_launched(launch_distill_rows(d, s), s);
+  // the epilogue takes 1 off at the row's target, which is a known entry: what is written there below covers it
+  if (e == cudaSuccess)
+    e = loss_backward(l, ws, rp, h, w, dh, dw, base, flag, s, [&](int64_t v0, int64_t n, const Operand& dz) {
+      DistillParams q = d;
+      q.dz = (__nv_bfloat16*)dz.base;
+      q.ld_dz = dz.ld;
+      q.plane = dz.plane;
+      q.pieces = dz.pieces;
+      q.dz_extent = dz.pieces * dz.plane;
+      q.v0 = (int)v0;
+      q.n = (int)n;
+      return api_launched(launch_distill_dz(q, s), s);
+    });
   return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
 }
 

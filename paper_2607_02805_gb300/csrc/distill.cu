@@ -1,0 +1,233 @@
+// distill.cu -- the passes of the distillation loss (include/bdscan_dense.h)
+// around the vocabulary loss's products: which rows count, the student's logits at
+// the teacher's entries with the loss, and the gradient at those entries.
+//
+// q = softmax(teacher / T) over a row's known entries (inside the vocabulary, not
+// the excluded one, not minus infinity), p = softmax(h w^T / T) over the whole
+// vocabulary, of which the product's epilogue has left partial maxima and sums:
+// loss = weight sum_v q_v (log q_v - log p_v). A row has 64 entries at most, two
+// per lane; q is formed again from the teacher's logits wherever it is needed.
+// Entries of the same id are one entry of the vocabulary, with their shares added.
+#include "dense.cuh"
+#include "gemm.cuh"
+
+namespace bds {
+namespace {
+
+constexpr int kThreads = 256, kRowWarps = kThreads / 32;
+
+// A row's entries, lane l those at l and l + 32: id (-1 where not known), q and log2 q.
+struct Entries {
+  int id[2];
+  float q[2], l2[2];
+};
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ void load_ids(Entries& e, float (&t)[2], const DistillParams& p, int64_t row) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int j = lane + 32 * k;
+    const int64_t id = j < p.top ? p.ids[row * p.top + j] : -1;
+    t[k] = j < p.top ? p.teacher[row * p.top + j] : -INFINITY;
+    e.id[k] = id >= 0 && id < p.vocab && id != p.excluded && t[k] != -INFINITY ? (int)id : -1;
+  }
+}
+__device__ __forceinline__ void load_entries(Entries& e, const DistillParams& p, int64_t row) {
+  float t[2];
+  load_ids(e, t, p, row);
+  float m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (e.id[k] >= 0) m = fmaxf(m, t[k]);
+  m = warp_max(m);
+  float s = 0.f;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    e.l2[k] = (t[k] - m) * p.scale2;  // NaN stays, and plus infinity becomes that
+    e.q[k] = e.id[k] >= 0 ? ex2(e.l2[k]) : 0.f;
+    s += e.q[k];
+  }
+  s = warp_sum(s);
+  const float l2 = log2f(s), r = 1.f / s;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    e.q[k] *= r;
+    e.l2[k] -= l2;
+  }
+}
+
+// The shares of an entry's id in all places, and their logarithm in base 2.
+__device__ __forceinline__ void merge_ids(Entries& e, float (&share)[2], int top) {
+  share[0] = share[1] = 0.f;
+  int times[2] = {0, 0};
+  for (int j = 0; j < top; ++j) {
+    const int id = __shfl_sync(0xffffffffu, j < 32 ? e.id[0] : e.id[1], j & 31);
+    const float q = __shfl_sync(0xffffffffu, j < 32 ? e.q[0] : e.q[1], j & 31);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (id == e.id[k]) share[k] += q, ++times[k];
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (times[k] > 1) e.l2[k] = log2f(share[k]);
+}
+
+// A warp per row: its first known entry as the target of the loss's row
+// bookkeeping, -1 where there is none, and zeros in z (forward) where the row
+// does not count.
+__global__ void __launch_bounds__(kThreads) k_distill_rows(const DistillParams p) {
+  pdl_sync();
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+  if (row >= p.rows) return;
+  if (!dguard(kSiteDistill, row, p.rows)) return;
+  Entries e;
+  float t[2];
+  load_ids(e, t, p, row);
+  const uint32_t lo = __ballot_sync(0xffffffffu, e.id[0] >= 0), hi = __ballot_sync(0xffffffffu, e.id[1] >= 0);
+  const int first = lo != 0 ? __shfl_sync(0xffffffffu, e.id[0], __ffs(lo) - 1)
+                            : hi != 0 ? __shfl_sync(0xffffffffu, e.id[1], __ffs(hi) - 1) : -1;
+  if (lane == 0) p.target[row] = first;
+  if (p.z != nullptr && (first < 0 || (p.weight != nullptr && p.weight[row] == 0.f)))
+    for (int j = lane; j < p.top; j += 32) p.z[row * p.top + j] = 0.f;
+}
+
+// One row's product with a row of w, by a warp.
+template <typename T, bool VEC>
+__device__ __forceinline__ float dot_row(const T* a, const T* b, int k) {
+  constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
+  const int lane = threadIdx.x & 31;
+  float s = 0.f;
+#pragma unroll 4
+  for (int i = lane * E; i < k; i += 32 * E) {
+    if constexpr (VEC) {
+      const uint4 u = *reinterpret_cast<const uint4*>(a + i), v = *reinterpret_cast<const uint4*>(b + i);
+      const T *x = reinterpret_cast<const T*>(&u), *y = reinterpret_cast<const T*>(&v);
+#pragma unroll
+      for (int j = 0; j < E; ++j) s = fmaf(cvt(x[j]), cvt(y[j]), s);
+    } else {
+      s = fmaf(cvt(a[i]), cvt(b[i]), s);
+    }
+  }
+  return warp_sum(s);
+}
+
+// A CTA per row that counts: the partial statistics joined, the student's logits
+// at the row's entries (a warp per entry; rows of w come from L2 mostly), and the
+// loss, formed in base 2 before anything is rounded at the logits' own size.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) k_distill_join(const DistillParams p) {
+  pdl_sync();
+  __shared__ float2 red[kRowWarps];
+  __shared__ float zs[64];
+  __shared__ int ids[64];
+  const int slot = blockIdx.x, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  if (slot >= *p.count) return;
+  const int64_t row = p.idx[slot];
+  Entries e;
+  if (w == 0) {
+    load_entries(e, p, row);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) ids[lane + 32 * k] = e.id[k];
+    float share[2];
+    merge_ids(e, share, p.top);
+  }
+  float m = -INFINITY, s = 0.f;
+  for (int k = threadIdx.x; k < p.parts; k += kThreads) stats_join(m, s, p.part[(int64_t)k * p.rows_ld + slot]);
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1)
+    stats_join(m, s, make_float2(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o)));
+  if (lane == 0) red[w] = make_float2(m, s);
+  __syncthreads();
+  const T* h = static_cast<const T*>(p.h) + row * p.ld_h;
+  for (int j = w; j < p.top; j += kRowWarps) {
+    const int id = ids[j];
+    const float z = id >= 0 ? dot_row<T, VEC>(h, static_cast<const T*>(p.w) + (int64_t)id * p.d_model, p.d_model) : 0.f;
+    if (lane == 0) zs[j] = z;
+  }
+  __syncthreads();
+  if (w != 0) return;
+  m = red[0].x, s = red[0].y;
+#pragma unroll
+  for (int k = 1; k < kRowWarps; ++k) stats_join(m, s, red[k]);
+  const float l2 = log2f(s);
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int j = lane + 32 * k;
+    if (j < p.top) {
+      const float z = zs[j];
+      p.z[row * p.top + j] = z;
+      // an entry too unlikely for fp32 adds nothing
+      if (e.id[k] >= 0 && e.q[k] != 0.f) sum = fmaf(e.q[k], e.l2[k] - (fmaf(z, p.scale2, -m) - l2), sum);
+    }
+  }
+  sum = warp_sum(sum);
+  if (lane == 0) {
+    const float d = sum < 0.f ? 0.f : sum * kLn2;  // no divergence is below zero; a NaN stays
+    p.loss[row] = p.weight != nullptr ? p.weight[row] * d : d;
+    p.lse[row] = (m + l2) * kLn2;
+  }
+}
+
+// The gradient at the logits, p - q, of the entries inside a piece of the
+// vocabulary, over what the product's epilogue left there. Formed again from the
+// row's own logit, so that it is rounded once. An id that comes twice takes both
+// shares; each of its lanes writes the same value.
+__global__ void __launch_bounds__(kThreads) k_distill_dz(const DistillParams p) {
+  pdl_sync();
+  const int lane = threadIdx.x & 31;
+  const int64_t slot = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+  if (slot >= *p.count) return;
+  if (!dguard(kSiteDistill, (p.pieces - 1) * p.plane + slot * p.ld_dz + p.n - 1, p.dz_extent)) return;
+  const int64_t row = p.idx[slot];
+  Entries e;
+  load_entries(e, p, row);
+  float share[2];
+  merge_ids(e, share, p.top);
+  const float lse = p.lse_in[row];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int at = e.id[k] - p.v0;
+    if (e.id[k] < 0 || at < 0 || at >= p.n) continue;
+    float v = ex2(fmaf(p.z_in[row * p.top + lane + 32 * k], p.scale, -lse) * kLog2e) - share[k];
+    bf16* to = p.dz + slot * p.ld_dz + at;
+    for (int i = 0; i < p.pieces; ++i) {
+      const float part = p.pieces == 1 ? v : bf16_part(v);
+      to[i * p.plane] = __float2bfloat16_rn(part);
+      v -= part;
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_distill_rows(const DistillParams& p, cudaStream_t s) {
+  launch_pdl(k_distill_rows, dim3((unsigned)((p.rows + kRowWarps - 1) / kRowWarps)), dim3(kThreads), 0, s, p);
+  return cudaGetLastError();
+}
+cudaError_t launch_distill_join(const DistillParams& p, int f32, cudaStream_t s) {
+  const int e = f32 ? 4 : 8;
+  const bool vec = p.d_model % e == 0 && p.ld_h % e == 0;
+  const dim3 grid((unsigned)p.rows), block(kThreads);
+  if (f32) vec ? launch_pdl(k_distill_join<float, true>, grid, block, 0, s, p)
+               : launch_pdl(k_distill_join<float, false>, grid, block, 0, s, p);
+  else vec ? launch_pdl(k_distill_join<bf16, true>, grid, block, 0, s, p)
+           : launch_pdl(k_distill_join<bf16, false>, grid, block, 0, s, p);
+  return cudaGetLastError();
+}
+cudaError_t launch_distill_dz(const DistillParams& p, cudaStream_t s) {
+  launch_pdl(k_distill_dz, dim3((unsigned)((p.rows + kRowWarps - 1) / kRowWarps)), dim3(kThreads), 0, s, p);
+  return cudaGetLastError();
+}
+
+}  // namespace bds

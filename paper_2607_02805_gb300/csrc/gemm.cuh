@@ -1372,10 +1372,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
           float mx = v[0];
 #pragma unroll
           for (int i = 1; i < 32; ++i) mx = fmaxf(mx, v[i]);
-          const float nm = fmaxf(rm, mx * kLog2e);
+          const float c = kLog2e * p.scale, nm = fmaxf(rm, mx * c);
           float add = 0.f;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) add += ex2(fmaf(v[i], kLog2e, -nm));
+          for (int i = 0; i < 32; ++i) add += ex2(fmaf(v[i], c, -nm));
           // a row with nothing so far (every entry excluded or past the end) stays at sum 0
           // (or at NaN, which the maximum passes over)
           if (nm != -INFINITY) {
@@ -1389,7 +1389,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant_
           const int vcol = p.v0 + col0;
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            float d = ex2((v[i] - rlse) * kLog2e);
+            float d = ex2(fmaf(v[i], p.scale, -rlse) * kLog2e);
             d = vcol + i == rt ? d - 1.f : d;
             v[i] = vcol + i == p.excluded ? 0.f : d;
           }

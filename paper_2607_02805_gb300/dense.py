@@ -3,7 +3,7 @@
 
 PyTorch provides the device memory and the stream; every step of the
 computation runs in libbdscan through ``binding``. A ``Linear``, ``GatedLinear``,
-``LmLoss`` or ``TokenScores`` holds one size's outputs, saved pre-activations, gradients and workspaces; the
+``LmLoss``, ``DistillLoss`` or ``TokenScores`` holds one size's outputs, saved pre-activations, gradients and workspaces; the
 inputs and weights belong to the caller. What a call returns are the holder's
 buffers, valid until its next call; a holder serves one stream at a time, and
 its buffers stay where they are for its life, so that a CUDA graph of its calls
@@ -302,6 +302,60 @@ class LmLoss(_Holder):
         _apart("w", inputs[1], dw.data_ptr())
         _, d, ws, size = self._plan(("backward", ld_h), binding.bdscan_lm_loss_backward_workspace_size)
         binding._call("bdscan_lm_loss_backward", d, *inputs, pl, pd, dh.data_ptr(), dw.data_ptr(), ws, size, s)
+        return dh, dw
+
+
+class DistillLoss(_Holder):
+    """Divergence of softmax(h w^T / temperature) from a teacher's distribution over `top` entries per row, for
+    h [rows, d_model], w [vocab, d_model], ids and teacher (its logits) [rows, top]; include/bdscan_dense.h has the
+    rules. What TokenScores gives as the likeliest entries and their log probabilities is such a teacher."""
+
+    def __init__(self, rows, d_model, vocab, top, dtype=torch.bfloat16, excluded=-1, temperature=1.0, device="cuda"):
+        _code(dtype)
+        super().__init__(device)
+        self.rows, self.d_model, self.vocab, self.top = int(rows), int(d_model), int(vocab), int(top)
+        self.dtype, self.excluded, self.temperature = dtype, int(excluded), float(temperature)
+        self._h, self._w = (self.rows, self.d_model), (self.vocab, self.d_model)
+        self._t, self._k = (self.rows,), (self.rows, self.top)
+
+    def _make_dims(self, ld_h):
+        return binding.make_distill_loss_dims(self.rows, self.d_model, self.vocab, self.top, _code(self.dtype),
+                                              self.excluded, self.temperature, ld_h)
+
+    def _inputs(self, h, w, ids, teacher, weight):
+        f32, dev = torch.float32, self._index
+        ph, ld_h = _rows("h", h, self._h, self.dtype, dev)
+        return ld_h, (ph, _whole("w", w, self._w, self.dtype, dev), _whole("ids", ids, self._k, torch.int64, dev),
+                      _whole("teacher", teacher, self._k, f32, dev), _whole("weight", weight, self._t, f32, dev))
+
+    def forward(self, h, w, ids, teacher, weight=None, stream=None):
+        """(loss, lse), fp32 per row; zero at the rows that do not count."""
+        ld_h, inputs = self._inputs(h, w, ids, teacher, weight)
+        s = self._enter(stream)
+        loss = self._buffer("loss", self._t, torch.float32)
+        lse = self._buffer("lse", self._t, torch.float32)
+        z = self._buffer("z", self._k, torch.float32)
+        for name, at in (("teacher", inputs[3]), ("weight", inputs[4])):
+            _apart(name, at, loss.data_ptr(), lse.data_ptr(), z.data_ptr())
+        _, d, ws, size = self._plan(("forward", ld_h), binding.bdscan_distill_loss_forward_workspace_size)
+        binding._call("bdscan_distill_loss_forward", d, *inputs, loss.data_ptr(), lse.data_ptr(), z.data_ptr(), ws,
+                      size, s)
+        return loss, lse
+
+    def backward(self, h, w, ids, teacher, weight=None, dloss=None, stream=None):
+        """(dh, dw) of <dloss, loss>, of the last forward."""
+        ld_h, inputs = self._inputs(h, w, ids, teacher, weight)
+        pd = _whole("dloss", dloss, self._t, torch.float32, self._index)
+        if "z" not in self._buf:
+            raise ValueError("backward needs a forward")
+        s = self._enter(stream)
+        dh = self._buffer("dh", self._h, self.dtype)
+        dw = self._buffer("dw", self._w, self.dtype)
+        for name, at in (("h", inputs[0]), ("w", inputs[1])):
+            _apart(name, at, dh.data_ptr(), dw.data_ptr())
+        _, d, ws, size = self._plan(("backward", ld_h), binding.bdscan_distill_loss_backward_workspace_size)
+        binding._call("bdscan_distill_loss_backward", d, *inputs, self._buf["lse"].data_ptr(),
+                      self._buf["z"].data_ptr(), pd, dh.data_ptr(), dw.data_ptr(), ws, size, s)
         return dh, dw
 
 
