@@ -227,6 +227,7 @@ __device__ __forceinline__ void loss_row(const LossRowsParams& p, int64_t i, flo
   const float dl = in && p.dloss != nullptr ? p.dloss[i] : 1.f;
   if (wt == 0.f || dl == 0.f || tg >= p.vocab || tg < 0) tg = -1;
   wt *= dl * p.scale;
+  if (p.dz_scale != nullptr && tg >= 0) wt /= p.dz_scale[i];
 }
 // The slot's bookkeeping of a row that counts, the outputs of one that does not.
 __device__ __forceinline__ void loss_row_out(const LossRowsParams& p, int64_t i, int to, float wt, int64_t tg) {
@@ -236,6 +237,7 @@ __device__ __forceinline__ void loss_row_out(const LossRowsParams& p, int64_t i,
     if (p.gscale != nullptr) {
       p.gscale[to] = wt;
       p.lse_c[to] = p.lse_in[i];
+      if (p.dz_scale != nullptr) p.dz_scale_c[to] = p.dz_scale[i];
     }
   } else if (p.loss != nullptr) {
     p.loss[i] = 0.f;

@@ -57,6 +57,7 @@ struct GemmParams {
   float* at_target;      // [rows]
   int64_t rows_ld;       // rows of `part`
   const float* lse;      // [rows] of the rows that count
+  const float* dz_scale; // kEpiDz: [rows] factors of the gradient that is kept, or null (ones)
   // kEpiStats with few rows: the last CTA to end (by `ticket`, zero before)
   // joins the partial statistics into the outputs; null: launch_loss_combine does
   int* ticket;
@@ -160,6 +161,9 @@ struct LossRowsParams {
   float *gscale, *lse_c;
   float *loss, *lse;
   float scale;  // of the gradient scales: 1 / temperature
+  // factors that the gradient at the logits takes from the rows' scales ([rows], null: none), and those of the slots
+  const float* dz_scale;
+  float* dz_scale_c;
 };
 cudaError_t launch_loss_rows(const LossRowsParams& p, cudaStream_t s);
 // launch_loss_rows and launch_pack_rows in one, for up to small_loss_rows() rows.
@@ -177,6 +181,8 @@ struct DistillParams {
   int top;
   float scale, scale2;   // 1 / temperature, and log2(e) / temperature
   int64_t* target;       // launch_distill_rows: [rows] the first known entry, or -1
+  const float* dloss;    // and in a bf16 backward the factor that the row's gradient takes from its scale
+  float* row_scale;
   // launch_distill_join: slots of the rows that count, their partial statistics and the operands as they lie
   const int *count, *idx;
   const float2* part;
@@ -185,7 +191,7 @@ struct DistillParams {
   const void *h, *w;
   float *z, *loss, *lse;  // [rows][top], [rows]; z null: launch_distill_rows leaves it alone
   // launch_distill_dz: entries v0 .. v0 + n - 1 in `pieces` planes
-  const float *lse_in, *z_in;
+  const float *lse_in, *z_in, *dz_scale;  // dz_scale: of the slots, or null
   __nv_bfloat16* dz;
   int64_t ld_dz, plane, dz_extent;
   int v0, n, pieces;

@@ -808,6 +808,7 @@ cudaError_t loss_backward(const Loss& l, const LossBwdWs& ws, LossRowsParams rp,
     p.excluded = (int)l.excluded;
     p.scale = l.scale;
     p.lse = rp.lse_c;
+    p.dz_scale = rp.dz_scale_c;
     p.out = base + ws.dz;
     p.ld_out = ld_dz;
     p.out_last = (l.pieces - 1) * ws.r.rows * ld_dz + (ws.r.rows - 1) * ld_dz + n - 1;
@@ -879,8 +880,11 @@ int check_distill(const bdscan_distill_loss_dims* d, Loss* l, const char* fn) {
   l->scale = 1.f / d->temperature;
   return BDSCAN_OK;
 }
-// The entries that stand for the rows' targets, behind the loss's own workspace.
+// Behind the loss's own workspace: the entries that stand for the rows' targets, and in the backward the factors that
+// the gradient at the logits takes, of the rows and of the slots.
 size_t target_bytes(const Loss& l) { return al256((size_t)l.T * 8); }
+size_t row_scale_bytes(const Loss& l) { return al256((size_t)up(l.T, 256) * 4); }
+size_t distill_bwd_bytes(const Loss& l) { return target_bytes(l) + 2 * row_scale_bytes(l); }
 
 DistillParams distill_params(const Loss& l, const LossRowsParams& rp, int top, const int64_t* ids,
                              const float* teacher) {
@@ -1366,7 +1370,7 @@ int bdscan_distill_loss_forward(const bdscan_distill_loss_dims* dims, const void
 size_t bdscan_distill_loss_backward_workspace_size(const bdscan_distill_loss_dims* dims) {
   Loss l;
   if (check_distill(dims, &l, "bdscan_distill_loss_backward_workspace_size") != BDSCAN_OK || l.T == 0) return 0;
-  return loss_bwd_ws(l).total + target_bytes(l);
+  return loss_bwd_ws(l).total + distill_bwd_bytes(l);
 }
 
 int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const void* h, const void* w,
@@ -1393,7 +1397,7 @@ int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const voi
   DENSE_OPT(dloss, fn, "dloss");
   DENSE_REQ(dh, fn, "dh");
   const LossBwdWs ws = loss_bwd_ws(l);
-  if ((rc = check_workspace(workspace, workspace_bytes, ws.total + target_bytes(l), fn))) return rc;
+  if ((rc = check_workspace(workspace, workspace_bytes, ws.total + distill_bwd_bytes(l), fn))) return rc;
   int* flag;
   if ((rc = check_device(fn, &flag))) return rc;
   char* base = (char*)workspace;
@@ -1403,6 +1407,13 @@ int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const voi
   DistillParams d = distill_params(l, rp, dims->top, ids, teacher);
   d.lse_in = lse;
   d.z_in = z;
+  if (l.pieces == 1) {  // fp32: three pieces round nothing off
+    char* at = base + ws.total + target_bytes(l);
+    d.dloss = dloss;
+    d.row_scale = (float*)at;
+    rp.dz_scale = d.row_scale;
+    d.dz_scale = rp.dz_scale_c = (float*)(at + row_scale_bytes(l));
+  }
   cudaError_t e = api_launched(launch_distill_rows(d, s), s);
   // the epilogue takes 1 off at the row's target, which is a known entry: what is written there below covers it
   if (e == cudaSuccess)
