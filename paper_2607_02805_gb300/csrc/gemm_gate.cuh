@@ -90,15 +90,17 @@ __device__ __forceinline__ void rows_out(void* out, int64_t ld, int64_t m, int64
     *reinterpret_cast<float4*>(f + lane * 16 + 4 * (j ^ ((lane >> 1) & 3))) =
         make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
   __syncwarp();
-  if (col + cl >= n) return;
-  float y[16];
+  if (col + cl < n) {
+    float y[16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int r = 2 * i + (lane >> 4);
-    y[i] = f[r * 16 + 4 * ((cl >> 2) ^ ((r >> 1) & 3)) + (cl & 3)];
+    for (int i = 0; i < 16; ++i) {
+      const int r = 2 * i + (lane >> 4);
+      y[i] = f[r * 16 + 4 * ((cl >> 2) ^ ((r >> 1) & 3)) + (cl & 3)];
+    }
+    const int64_t row = row0 + (lane >> 4);
+    store_rows<F32>(out, row, ld, at + col + cl, (int)min((int64_t)32, m - row), y);
   }
-  const int64_t row = row0 + (lane >> 4);
-  store_rows<F32>(out, row, ld, at + col + cl, (int)min((int64_t)32, m - row), y);
+  __syncwarp();
 }
 // Bias of 16 columns from col on, added to them.
 template <bool F32, bool ROWS>
@@ -187,6 +189,7 @@ __device__ __forceinline__ bool gate_epilogue(const GemmParams& p, const GemmMap
         if (!(ok = warp_wait(&accfull[job % NA], (job / NA) & 1))) break;
         umma::fence_after_sync();
         if (live) {
+          __syncwarp();  // TMEM is read by whole warps
           float a[16], b[16];
           umma::tmem_ld16x2(lanes + job % NA * BN + c0, a, lanes + job % NA * BN + h + c0, b);
 #pragma unroll
@@ -219,6 +222,7 @@ __device__ __forceinline__ bool gate_epilogue(const GemmParams& p, const GemmMap
     for (int hf = 0; hf < NH; ++hf) {
       const int col = col0 + 16 * hf;
       if constexpr (!FLUSH) {
+        __syncwarp();  // TMEM is read by whole warps
         const uint32_t at = lanes + job % NA * BN + (uint32_t)(c0 + 16 * hf);
         umma::tmem_ld16x2(at, g, at + (uint32_t)h, u);
         if (hf == NH - 1) release();

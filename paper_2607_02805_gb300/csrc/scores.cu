@@ -8,17 +8,21 @@
 // overflow. One pass: a thread keeps the maximum of what it has seen and s, t
 // relative to it, and rescales them once per batch of four 16-byte loads.
 //
-// The likeliest entries come without sorting. The threads of a CTA form 64
+// The likeliest entries come without sorting. The threads of a CTA form 128
 // groups; the top-th largest of the groups' maxima is a bound that at least
-// `top` entries reach, and only groups that reach it can hold one. Those read
-// their entries again (from L2) and list what reaches the bound, on average
-// little more than `top`; the rank of each in the list, by value and then by
-// lower index, is its place in the output. Rows with so many equal entries that
-// the list overflows are searched once per place instead.
+// `top` entries reach, and only groups that reach it can hold one. A warp each
+// reads such a group's entries again (from L2) and lists what reaches the bound:
+// of independent entries -128 log(1 - top / 128) on average, 17 for 16 and 89
+// for 64. The rank of each in the list, by value and then by lower index, is its
+// place in the output. Rows with so many equal entries that the list overflows
+// are searched once per place instead.
 //
-// One CTA per row. Where that leaves SMs idle, a cluster of CTAs shares a row:
-// each leaves its statistics and its own likeliest entries in the first one's
-// shared memory.
+// One CTA per row, six of 256 threads per SM. Where that leaves SMs idle, a
+// cluster of CTAs shares a row: each leaves its statistics and its own likeliest
+// entries in the first one's shared memory. 16384 rows of 50304 bf16 (1.65 GB):
+// 240 us without likeliest entries, the copy rate, 275 with one, 313 with 16 (an
+// eighth of each row read again, and its latency), 485 with 64. The gradient is
+// one read and one write at the copy rate (477 us).
 #include <cstdio>
 #include <cstring>
 
@@ -26,12 +30,13 @@
 #include "debug.cuh"
 #include "device.cuh"
 #include "params.h"
+#include "ssd_common.cuh"
 
 namespace bds {
 namespace {
 
 constexpr int kMaxTop = 64;
-constexpr int kGroups = 64;
+constexpr int kGroups = 128;
 constexpr int kList = 512;     // entries of a CTA's list; eight CTAs' kMaxTop each
 constexpr int kMaxParts = 8;   // CTAs of a row's cluster
 constexpr int kNone = 1 << 30; // stands for the index of a place without an entry, another for each place
@@ -96,6 +101,27 @@ struct Vec {
     if constexpr (E == 4) return make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
     else return make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
   }
+  // The larger of the first or the second half.
+  __device__ __forceinline__ float half_max(int h) const {
+    if constexpr (E == 4) {
+      return fmaxf(__uint_as_float(w[2 * h]), __uint_as_float(w[2 * h + 1]));
+    } else {
+      const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&w[2 * h]),
+                                       *reinterpret_cast<const __nv_bfloat162*>(&w[2 * h + 1]));
+      const float2 f = __bfloat1622float2(m);
+      return fmaxf(f.x, f.y);
+    }
+  }
+  // Which entries, not minus infinity, are `tau` or more.
+  __device__ __forceinline__ uint32_t reach(float tau) const {
+    uint32_t hit = 0;
+#pragma unroll
+    for (int k = 0; k < E / 2; ++k) {
+      const float2 v = two(k);
+      hit |= (v.x >= tau && v.x != -INFINITY ? 1u : 0u) << 2 * k | (v.y >= tau && v.y != -INFINITY ? 2u : 0u) << 2 * k;
+    }
+    return hit;
+  }
   __device__ __forceinline__ void none() {
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = E == 4 ? 0xff800000u : 0xff80ff80u;
@@ -145,29 +171,35 @@ struct Row {
   }
   __device__ __forceinline__ const uint4* group(int i) const { return reinterpret_cast<const uint4*>(at + lead) + i; }
   __device__ __forceinline__ int first(int i) const { return lead + i * E; }  // entry index of group i
+  __device__ __forceinline__ int begin(int part, int parts) const { return (int)((int64_t)n * part / parts); }
+  __device__ __forceinline__ void exclude(Vec<T>& q, int i, int excluded) const {
+    if ((unsigned)(excluded - first(i)) < (unsigned)E) q.exclude(excluded - first(i));
+  }
 };
 
 // The entries of part `part` of `parts` of a row that this thread of THREADS
-// takes: batch(U groups, the first's number; the others follow in steps of
+// takes: batch(U groups or one, the first's number; the others follow in steps of
 // THREADS), one(value, index) at the ends of the row. The excluded entry is minus
-// infinity, and so is what fills up the last batch.
+// infinity.
 template <typename T, int THREADS, int U, typename FV, typename FB>
 __device__ __forceinline__ void for_entries(const Row<T>& r, int part, int parts, int excluded, FV one, FB batch) {
   constexpr int E = Vec<T>::E;
   const int t = threadIdx.x;
-  const int a = (int)((int64_t)r.n * part / parts), b = (int)((int64_t)r.n * (part + 1) / parts);
+  const int a = r.begin(part, parts), b = r.begin(part + 1, parts);
   int i = a + t;
-  for (; i < b; i += U * THREADS) {
+  // whole batches, then single groups
+  for (; i + (U - 1) * THREADS < b; i += U * THREADS) {
     Vec<T> q[U];
 #pragma unroll
-    for (int j = 0; j < U; ++j)
-      if (i + j * THREADS < b) q[j].load(r.group(i + j * THREADS));
+    for (int j = 0; j < U; ++j) q[j].load(r.group(i + j * THREADS));
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const int at = r.first(i + j * THREADS);
-      if (i + j * THREADS >= b) q[j].none();
-      else if ((unsigned)(excluded - at) < (unsigned)E) q[j].exclude(excluded - at);
-    }
+    for (int j = 0; j < U; ++j) r.exclude(q[j], i + j * THREADS, excluded);
+    batch(q, i);
+  }
+  for (; i < b; i += THREADS) {
+    Vec<T> q[1];
+    q[0].load(r.group(i));
+    r.exclude(q[0], i, excluded);
     batch(q, i);
   }
   // the few entries before and behind the groups, by threads of the first and the last part
@@ -203,9 +235,7 @@ __device__ __forceinline__ void stat_add(Stat& a, float v, float c) {
   a.t = fmaf(e, fmaxf(d, -200.f), a.t);
 }
 template <typename T, int U>
-__device__ __forceinline__ void stat_add(Stat& a, const Vec<T> (&q)[U], float c) {
-  const float m = vec_max(q);
-  if (m > a.m) stat_move(a, m, c);
+__device__ __forceinline__ void stat_sum(Stat& a, const Vec<T> (&q)[U], float c) {  // none above a.m
   const float ref = -ref_of(a.m);
   const f32x2 mm = pair(ref, ref), cc = pair(c, c);
   f32x2 s = pair(a.s, 0.f), t = pair(a.t, 0.f);
@@ -221,6 +251,12 @@ __device__ __forceinline__ void stat_add(Stat& a, const Vec<T> (&q)[U], float c)
     }
   a.s = halves(s).x + halves(s).y;
   a.t = halves(t).x + halves(t).y;
+}
+template <typename T, int U>
+__device__ __forceinline__ void stat_add(Stat& a, const Vec<T> (&q)[U], float c) {
+  const float m = vec_max(q);
+  if (m > a.m) stat_move(a, m, c);
+  stat_sum(a, q, c);
 }
 
 __device__ __forceinline__ uint32_t my_rank() {
@@ -239,38 +275,87 @@ __device__ __forceinline__ void put_cluster(uint32_t at, float v) {
 __device__ __forceinline__ void put_cluster(uint32_t at, int v) {
   asm volatile("st.shared::cluster.s32 [%0], %1;\n" ::"r"(at), "r"(v) : "memory");
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory"); }
+// Each thread by itself: what comes before may have left the warp's threads at different places, and the aligned forms
+// would count such a warp more than once.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;\n" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;\n" ::: "memory"); }
 
+// Keys that order like the floats they stand for (one zero); 0 is below all.
+__device__ __forceinline__ uint32_t key_of(float v) {
+  const uint32_t u = __float_as_uint(v + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 // Whether entry (v, i) comes before (w, j).
 __device__ __forceinline__ bool before(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
 
 template <int THREADS>
 struct ScoresSmem {
-  float gmax[kGroups];
+  alignas(16) float gmax[kGroups];
   Stat warp[THREADS / 32];
   float lv[kList], pv[kList];  // the list, and what the parts of a row found
   int li[kList], pi[kList];
   Stat part[kMaxParts];
-  int count;
+  float tau[kGroups / 32];
+  int sel[kGroups];  // groups that reach the bound
+  int count, selected;
 };
+
+// The outputs of a row from its statistics. Nothing left: no entry has a
+// probability. NaN or plus infinity anywhere: everything is NaN.
+struct RowOut {
+  const ScoresParams& p;
+  int64_t row;
+  float m, s, ln;
+  bool bad;
+  __device__ __forceinline__ RowOut(const ScoresParams& p_, int64_t row_, const Stat& a)
+      : p(p_), row(row_), m(a.m), s(a.s), ln(log2f(a.s) * kLn2), bad(isnan(a.s)) {}
+  __device__ __forceinline__ float logp(float z) const {
+    const float d = fmaf(z - m, p.inv_t, -ln);
+    return bad ? s : z == -INFINITY ? z : d > 0.f ? 0.f : d;
+  }
+  // by one thread; zt: the token's logit
+  __device__ __forceinline__ void scores(const Stat& a, float zt) const {
+    if (p.logp != nullptr) p.logp[row] = logp(zt);
+    const float h = (log2f(s) - a.t / s) * kLn2;
+    if (p.entropy != nullptr) p.entropy[row] = m == -INFINITY && !bad ? 0.f : h < 0.f ? 0.f : h;
+    if (p.stats != nullptr) p.stats[row] = make_float2(bad ? s : m, ln);
+  }
+  __device__ __forceinline__ void place(int k, float v, int at) const {
+    p.top_logp[row * p.top + k] = logp(v);
+    p.top_ids[row * p.top + k] = bad || v == -INFINITY ? -1 : at;
+  }
+};
+// Of a row that does not count, by thread t of n.
+__device__ __forceinline__ void out_none(const ScoresParams& p, int64_t row, int t, int n) {
+  if (t == 0) {
+    if (p.logp != nullptr) p.logp[row] = 0.f;
+    if (p.entropy != nullptr) p.entropy[row] = 0.f;
+    if (p.stats != nullptr) p.stats[row] = make_float2(0.f, 0.f);
+  }
+  for (int i = t; i < p.top; i += n) {
+    p.top_ids[row * p.top + i] = -1;
+    p.top_logp[row * p.top + i] = -INFINITY;
+  }
+}
 
 // The `top` first entries of the list in order: emit(place, value, index), then minus infinity for what is missing.
 template <int THREADS, typename F>
 __device__ __forceinline__ void rank_list(const float* lv, const int* li, int n, int top, F emit) {
-  for (int i = threadIdx.x; i < n; i += THREADS) {
+  const int t = threadIdx.x % THREADS;
+  for (int i = t; i < n; i += THREADS) {
     const float v = lv[i];
     const int at = li[i];
     int rank = 0;
     for (int j = 0; j < n; ++j) rank += before(lv[j], li[j], v, at) ? 1 : 0;
     if (rank < top) emit(rank, v, at);
   }
-  for (int i = threadIdx.x; i < top; i += THREADS)
+  for (int i = t; i < top; i += THREADS)
     if (i >= n) emit(i, -INFINITY, kNone);
 }
 
 template <typename T, int THREADS, bool CLUSTER>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const ScoresParams p) {
+__global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_scores(const ScoresParams p) {
   pdl_sync();
   constexpr int E = Vec<T>::E, U = 4, W = THREADS / 32;
   __shared__ ScoresSmem<THREADS> sm;
@@ -281,17 +366,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Scores
   if (CLUSTER) cluster_arrive();
   int64_t token = p.token != nullptr ? p.token[row] : 0;
   if (token < 0 || token >= p.vocab) {  // a row that does not count (the same for its whole cluster)
-    if (part == 0) {
-      if (t == 0) {
-        if (p.logp != nullptr) p.logp[row] = 0.f;
-        if (p.entropy != nullptr) p.entropy[row] = 0.f;
-        if (p.stats != nullptr) p.stats[row] = make_float2(0.f, 0.f);
-      }
-      for (int i = t; i < p.top; i += THREADS) {
-        p.top_ids[row * p.top + i] = -1;
-        p.top_logp[row * p.top + i] = -INFINITY;
-      }
-    }
+    if (part == 0) out_none(p, row, t, THREADS);
     if (CLUSTER) cluster_wait();
     return;
   }
@@ -300,9 +375,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Scores
   float zt = 0.f;
   if (t == 0 && part == 0 && p.token != nullptr) zt = token == p.excluded ? -INFINITY : cvt(r.at[token]);
   auto each_of = [&](auto f) {  // a batch entry by entry
-    return [&r, f](const Vec<T>(&q)[U], int i) {
+    return [&r, f](const auto& q, int i) {
 #pragma unroll
-      for (int j = 0; j < U; ++j)
+      for (int j = 0; j < (int)(sizeof(q) / sizeof(Vec<T>)); ++j)
 #pragma unroll
         for (int k = 0; k < E / 2; ++k) {
           const float2 v = q[j].two(k);
@@ -314,22 +389,35 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Scores
   Stat a = {-INFINITY, 0.f, 0.f};
   for_entries<T, THREADS, U>(
       r, part, parts, p.excluded, [&](float v, int) { stat_add(a, v, c); },
-      [&](const Vec<T>(&q)[U], int) { stat_add(a, q, c); });
+      [&](const auto& q, int) { stat_add(a, q, c); });
 
   // the groups' maxima, then the CTA's
   constexpr int G = THREADS / kGroups;  // threads of a group
   float m = a.m;
 #pragma unroll
   for (int o = 1; o < G; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  const float gm = m;
-  if (t % G == 0) sm.gmax[t / G] = gm;
-  if (t == 0) sm.count = 0;
+  if (t % G == 0) sm.gmax[t / G] = m;
+  if (t == 0) sm.count = sm.selected = 0;
   __syncthreads();
-  const float g0 = sm.gmax[lane], g1 = sm.gmax[lane + 32];
-  m = fmaxf(g0, g1);
+  const float4 g4 = reinterpret_cast<const float4*>(sm.gmax)[lane];
+  m = fmaxf(fmaxf(g4.x, g4.y), fmaxf(g4.z, g4.w));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  // all threads' sums relative to that, added in a fixed order
+  // the bound, the top-th largest of the groups' maxima: the smallest that fewer than `top` exceed
+  if (p.top > 0 && t < kGroups) {
+    const float of = sm.gmax[t];
+    int above = 0;
+#pragma unroll 8
+    for (int j = 0; j < kGroups / 4; ++j) {
+      const float4 q = reinterpret_cast<const float4*>(sm.gmax)[j];
+      above += (q.x > of) + (q.y > of) + (q.z > of) + (q.w > of);
+    }
+    float tau = above < p.top ? of : INFINITY;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) tau = fminf(tau, __shfl_xor_sync(0xffffffffu, tau, o));
+    if (lane == 0) sm.tau[w] = tau;
+  }
+  // all threads' sums relative to the maximum, added in a fixed order
   stat_move(a, m, c);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -337,27 +425,47 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Scores
     a.t += __shfl_xor_sync(0xffffffffu, a.t, o);
   }
   if (lane == 0) sm.warp[w] = a;
+  __syncthreads();
   if (p.top > 0) {
-    // the bound: the top-th largest of the groups' maxima (every warp finds it for itself)
-    int r0 = 0, r1 = 0;
-#pragma unroll 8
-    for (int j = 0; j < kGroups; ++j) {
-      const float q = sm.gmax[j];
-      r0 += before(q, j, g0, lane) ? 1 : 0;
-      r1 += before(q, j, g1, lane + 32) ? 1 : 0;
-    }
-    float tau = r0 == p.top - 1 ? g0 : r1 == p.top - 1 ? g1 : -INFINITY;
+    float tau = sm.tau[0];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) tau = fmaxf(tau, __shfl_xor_sync(0xffffffffu, tau, o));
-    if (gm >= tau && a.m != -INFINITY) {
-      auto keep = [&](float v, int at) {
-        if (v >= tau && v != -INFINITY) {
-          const int to = atomicAdd(&sm.count, 1);
-          if (to < kList) sm.lv[to] = v, sm.li[to] = at;
+    for (int k = 1; k < kGroups / 32; ++k) tau = fminf(tau, sm.tau[k]);
+    auto keep = [&](float v, int at) {
+      if (v >= tau && v != -INFINITY) {
+        const int to = atomicAdd(&sm.count, 1);
+        if (to < kList) sm.lv[to] = v, sm.li[to] = at;
+      }
+    };
+    // the groups that reach it, listed in any order; all threads share their entries (a warp those of its own groups:
+    // 16384 x 50304 with 16 entries 327 us, 2048 x 131072 fp32 211; so 316 and 189)
+    if (t < kGroups && sm.gmax[t] >= tau && sm.gmax[t] != -INFINITY) sm.sel[atomicAdd(&sm.selected, 1)] = t;
+    __syncthreads();
+    const int begin = r.begin(part, parts), end = r.begin(part + 1, parts), ns = sm.selected;
+    const int per = (end - begin + THREADS - 1) / THREADS * G;  // 16-byte groups of each, the last ones past the end
+    for (int x = t; x < ns * per; x += U * THREADS) {
+      Vec<T> q[U];
+      int at[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int y = x + j * THREADS, k = y / per, e = y - k * per;
+        at[j] = k < ns ? begin + sm.sel[k] * G + e % G + e / G * THREADS : end;
+        if (at[j] < end) q[j].load(r.group(at[j]));
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if (at[j] >= end) continue;
+        r.exclude(q[j], at[j], p.excluded);
+        const Vec<T> one[1] = {q[j]};
+        if (vec_max(one) < tau) continue;
+        for (uint32_t hit = q[j].reach(tau); hit != 0; hit &= hit - 1) {
+          const int i = r.first(at[j]) + __ffs(hit) - 1;
+          keep(cvt(r.at[i]), i);
         }
-      };
-      for_entries<T, THREADS, U>(r, part, parts, p.excluded, keep, each_of(keep));
+      }
     }
+    if (part == 0 && t < r.lead && t != p.excluded) keep(cvt(r.at[t]), t);
+    const int last = r.lead + r.n * E + t;
+    if (part == parts - 1 && t < r.tail && last != p.excluded) keep(cvt(r.at[last]), last);
   }
   __syncthreads();
   // the part's sums (every thread: the same)
@@ -397,6 +505,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Scores
   const float *lv = sm.lv;
   const int* li = sm.li;
   if constexpr (CLUSTER) {
+    __syncthreads();
     cluster_wait();  // the first CTA has begun
     if (t == 0) {
       const uint32_t to = first_cta(&sm.part[part]);
@@ -409,6 +518,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Scores
       put_cluster(tv + 4 * k, v);
       put_cluster(ti + 4 * k, v == -INFINITY ? kNone + part * p.top + k : at);
     });
+    __syncthreads();
     cluster_arrive();
     cluster_wait();
     if (part != 0) return;
@@ -423,55 +533,255 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Scores
     lv = sm.pv, li = sm.pi;
     n = parts * p.top;
   }
-  // nothing left: no entry has a probability; NaN or plus infinity anywhere: everything is NaN
-  const float l2 = log2f(a.s), ln = l2 * kLn2;
-  const bool bad = isnan(a.s);
-  auto logp = [&](float z) {
-    const float d = fmaf(z - a.m, p.inv_t, -ln);
-    return bad ? a.s : z == -INFINITY ? z : d > 0.f ? 0.f : d;
+  const RowOut out(p, row, a);
+  if (t == 0) out.scores(a, zt);
+  if (p.top > 0) rank_list<THREADS>(lv, li, n, p.top, [&](int k, float v, int at) { out.place(k, v, at); });
+}
+
+// ---- short rows: a warp each ----
+// The whole row stays in registers, NV 16-byte groups and two single entries per
+// lane: the maximum first, then the sums. The bound is the top-th largest of 128
+// groups' maxima, four per lane (of 256 in the shortest rows, whose groups would
+// be fewer than `top`), taken off one by one; what reaches it is ranked as above,
+// in the warp's own list. 16384 rows of 2000 bf16: 21 us, with 16 entries 55 (by
+// CTAs of 128 threads: 36 and 68); the loop that takes the maxima off is most of
+// the difference.
+constexpr int kWarpList = 256;
+constexpr int kWarpsPerCta = 4;
+template <typename T, int NV>
+__global__ void __launch_bounds__(32 * kWarpsPerCta) k_scores_warp(const ScoresParams p) {
+  pdl_sync();
+  constexpr int E = Vec<T>::E;
+  __shared__ float lists[kWarpsPerCta][kWarpList];
+  __shared__ int places[kWarpsPerCta][kWarpList], counts[kWarpsPerCta];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int64_t row = (int64_t)blockIdx.x * kWarpsPerCta + w;
+  if (row >= p.rows) return;
+  if (!dguard(kSiteScores, row * p.ld + p.vocab - 1, (p.rows - 1) * p.ld + p.vocab)) return;
+  const int64_t token = p.token != nullptr ? p.token[row] : 0;
+  if (token < 0 || token >= p.vocab) {
+    out_none(p, row, lane, 32);
+    return;
+  }
+  const Row<T> r(p.logits, row, p.ld, p.vocab);
+  const float c = p.scale;
+  Vec<T> q[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if (lane + 32 * j < r.n) q[j].load(r.group(lane + 32 * j));
+    else q[j].none();
+  }
+  const int last = r.lead + r.n * E + lane;
+  float one[2] = {-INFINITY, -INFINITY};
+  if (lane < r.lead && lane != p.excluded) one[0] = cvt(r.at[lane]);
+  if (lane < r.tail && last != p.excluded) one[1] = cvt(r.at[last]);
+  float zt = 0.f;
+  if (lane == 0 && p.token != nullptr) zt = token == p.excluded ? -INFINITY : cvt(r.at[token]);
+  if (lane == 0) counts[w] = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) r.exclude(q[j], lane + 32 * j, p.excluded);
+  // a lane's groups: every fourth of its 16-byte groups, or half a one, the single entries with the first
+  constexpr int NG = NV == 4 ? 8 : 4;
+  float g[NG];
+#pragma unroll
+  for (int k = 0; k < NG; ++k) {
+    if constexpr (NG == 8) {
+      g[k] = q[k / 2].half_max(k % 2);
+    } else {
+      Vec<T> mine[NV / 4];
+#pragma unroll
+      for (int j = 0; j < NV / 4; ++j) mine[j] = q[4 * j + k];
+      g[k] = vec_max(mine);
+    }
+  }
+  g[0] = fmaxf(g[0], fmaxf(one[0], one[1]));
+  Stat a = {g[0], 0.f, 0.f};
+#pragma unroll
+  for (int k = 1; k < NG; ++k) a.m = fmaxf(a.m, g[k]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(0xffffffffu, a.m, o));
+  stat_sum(a, q, c);
+  stat_add(a, one[0], c);
+  stat_add(a, one[1], c);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+    a.t += __shfl_xor_sync(0xffffffffu, a.t, o);
+  }
+  const RowOut out(p, row, a);
+  if (lane == 0) out.scores(a, zt);
+  if (p.top == 0) return;
+  uint32_t keys[NG], bound = 0;
+#pragma unroll
+  for (int k = 0; k < NG; ++k) keys[k] = g[k] > -INFINITY ? key_of(g[k]) : 0u;  // NaN (all of a group) is none either
+  for (int i = 0; i < p.top; ++i) {
+    uint32_t mine = keys[0];
+#pragma unroll
+    for (int k = 1; k < NG; ++k) mine = max(mine, keys[k]);
+    bound = __reduce_max_sync(0xffffffffu, mine);
+    if (bound == 0) break;  // fewer groups than places: everything is listed
+    const uint32_t who = __ballot_sync(0xffffffffu, mine == bound);
+    if (lane == __ffs(who) - 1) {
+      bool gone = false;
+#pragma unroll
+      for (int k = 0; k < NG; ++k)
+        if (!gone && keys[k] == bound) keys[k] = 0, gone = true;
+    }
+  }
+  const float tau = bound != 0 ? of_key(bound) : -INFINITY;
+  float* lv = lists[w];
+  int* li = places[w];
+  auto keep = [&](float v, int at) {
+    if (v >= tau && v != -INFINITY) {
+      const int to = atomicAdd(&counts[w], 1);
+      if (to < kWarpList) lv[to] = v, li[to] = at;
+    }
   };
-  if (t == 0) {
-    if (p.logp != nullptr) p.logp[row] = logp(zt);
-    const float h = (l2 - a.t / a.s) * kLn2;
-    if (p.entropy != nullptr) p.entropy[row] = a.m == -INFINITY && !bad ? 0.f : h < 0.f ? 0.f : h;
-    if (p.stats != nullptr) p.stats[row] = make_float2(bad ? a.s : a.m, ln);
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const Vec<T> v[1] = {q[j]};
+    if (vec_max(v) >= tau) {
+      for (uint32_t hit = v[0].reach(tau); hit != 0; hit &= hit - 1) {
+        const int i = r.first(lane + 32 * j) + __ffs(hit) - 1;
+        keep(cvt(r.at[i]), i);
+      }
+    }
   }
-  if (p.top > 0) {
-    float* lo = p.top_logp + row * p.top;
-    int64_t* id = p.top_ids + row * p.top;
-    rank_list<THREADS>(lv, li, n, p.top, [&](int k, float v, int at) {
-      if (k < p.top) lo[k] = logp(v), id[k] = bad || v == -INFINITY ? -1 : at;
-    });
+  keep(one[0], lane);
+  keep(one[1], last);
+  __syncwarp();
+  int n = counts[w];
+  if (n > kWarpList) {  // place by place, as above
+    float pv = INFINITY;
+    int pi = -1;
+    for (int k = 0; k < p.top; ++k) {
+      float bv = -INFINITY;
+      int bi = 0x7fffffff;
+      for (int i = lane; i < p.vocab; i += 32) {
+        const float v = i == p.excluded ? -INFINITY : cvt(r.at[i]);
+        if (v != -INFINITY && before(pv, pi, v, i) && before(v, i, bv, bi)) bv = v, bi = i;
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const float v = __shfl_xor_sync(0xffffffffu, bv, o);
+        const int i = __shfl_xor_sync(0xffffffffu, bi, o);
+        if (before(v, i, bv, bi)) bv = v, bi = i;
+      }
+      if (lane == 0) out.place(k, bv, bi);
+      pv = bv, pi = bi;
+    }
+    return;
   }
+  rank_list<32>(lv, li, n, p.top, [&](int k, float v, int at) { out.place(k, v, at); });
 }
 
 // ---- gradient of the logits ----
 // dz_v = -p_v (dlogp + dentropy (entropy + log p_v)) / T, at the token plus dlogp
-// / T: one read and one write, with p from the forward's statistics.
+// / T: one read and one write in 16-byte groups of the output's rows, with p from
+// the forward's statistics. Where the logits' rows lie on other boundaries
+// (SHIFT), a group comes from the two that hold it.
 template <typename T>
-__global__ void __launch_bounds__(256) k_scores_bwd(const ScoresParams p) {
+__device__ __forceinline__ void load_shifted(Vec<T>& v, const T* at, const T* end) {
+  const int shift = (int)(reinterpret_cast<uintptr_t>(at) & 15);
+  const uint4* g = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(at) - shift);
+  uint32_t w[8];
+  if (shift == 0 || reinterpret_cast<const T*>(g + 2) <= end) {
+    const uint4 a = __ldg(g), b = shift == 0 ? make_uint4(0, 0, 0, 0) : __ldg(g + 1);
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+  } else {  // the second one reaches past the last entry
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (Vec<T>::E == 4) {
+        v.w[j] = reinterpret_cast<const uint32_t*>(at)[j];
+      } else {
+        const unsigned short* h = reinterpret_cast<const unsigned short*>(at);
+        v.w[j] = (uint32_t)h[2 * j] | (uint32_t)h[2 * j + 1] << 16;
+      }
+    }
+    return;
+  }
+  uint32_t a[6], b[5];
+#pragma unroll
+  for (int i = 0; i < 6; ++i) a[i] = shift & 8 ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) b[i] = shift & 4 ? a[i + 1] : a[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v.w[i] = __funnelshift_r(b[i], b[i + 1], (shift & 2) * 8);
+}
+template <typename T, bool SHIFT>
+__global__ void __launch_bounds__(256, 6) k_scores_bwd(const ScoresParams p) {
   pdl_sync();
-  constexpr int E = Vec<T>::E, THREADS = 256;
+  constexpr int E = Vec<T>::E, THREADS = 256, U = SHIFT ? 2 : 4;
   const int t = threadIdx.x, part = (int)(blockIdx.x % p.parts);
   const int64_t row = blockIdx.x / p.parts;
   if (!dguard(kSiteScores, row * p.ld_out + p.vocab - 1, (p.rows - 1) * p.ld_out + p.vocab)) return;
   T* out = static_cast<T*>(p.dlogits) + row * p.ld_out;
+  const T* in = static_cast<const T*>(p.logits) + row * p.ld;
+  const T* end = static_cast<const T*>(p.logits) + (p.rows - 1) * p.ld + p.vocab;
   const int64_t token = p.token != nullptr ? p.token[row] : 0;
   const float2 st = p.stats_in[row];
   const bool counts = token >= 0 && token < p.vocab && st.x != -INFINITY;
-  const Row<T> r(p.logits, row, p.ld, p.vocab);
-  const float ls = st.y * kLog2e, ref = ref_of(st.x);
+  const Row<T> r(p.dlogits, row, p.ld_out, p.vocab);
+  const float ls = -st.y * kLog2e, ref = -ref_of(st.x);
   const float dl = (p.dlogp != nullptr ? p.dlogp[row] : 0.f) * p.inv_t;
   const float dh = (p.dentropy != nullptr ? p.dentropy[row] : 0.f) * p.inv_t;
-  const float base = dl + (p.dentropy != nullptr ? dh * p.entropy_in[row] : 0.f), slope = dh * kLn2;
+  const float base = -dl - (p.dentropy != nullptr ? dh * p.entropy_in[row] : 0.f), slope = -dh * kLn2;
+  const int tk = p.token != nullptr ? (int)token : -1;
+  auto special = [&](float g, int at) { return at == p.excluded ? 0.f : at == tk ? g + dl : g; };
   auto grad = [&](float z, int at) {
-    const float d = (z - ref) * p.scale - ls;
-    float g = -ex2(d) * fmaf(slope, fmaxf(d, -200.f), base);
-    if (p.token != nullptr && at == (int)token) g += dl;
-    return at == p.excluded || !counts ? 0.f : g;
+    const float d = fmaf(z + ref, p.scale, ls);
+    return special(ex2(d) * fmaf(slope, fmaxf(d, -200.f), base), at);
   };
-  const int a = (int)((int64_t)p.vocab * part / p.parts), b = (int)((int64_t)p.vocab * (part + 1) / p.parts);
-  for (int i = a + t; i < b; i += THREADS) out[i] = to_out<T>(grad(counts ? cvt(r.at[i]) : 0.f, i));
+  const int a = r.begin(part, p.parts), b = r.begin(part + 1, p.parts);
+  auto store = [&](int i, const float (&g)[E]) {
+    uint4 u;
+    if constexpr (E == 4) u = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
+    else u = make_uint4(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[E / 2], g[E / 2 + 1]), pack_bf16(g[E - 2], g[E - 1]));
+    *reinterpret_cast<uint4*>(out + r.first(i)) = u;
+  };
+  if (!counts) {
+    const float zero[E] = {};
+    for (int i = a + t; i < b; i += THREADS) store(i, zero);
+  } else {
+    for (int i = a + t; i < b; i += U * THREADS) {
+      Vec<T> q[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if (i + j * THREADS >= b) continue;
+        const T* at = in + r.first(i + j * THREADS);
+        if constexpr (SHIFT) {
+          load_shifted(q[j], at, end);
+        } else {  // not through the read-only path: the output may be the input
+          const uint4 u = *reinterpret_cast<const uint4*>(at);
+          q[j].w[0] = u.x, q[j].w[1] = u.y, q[j].w[2] = u.z, q[j].w[3] = u.w;
+        }
+      }
+      const f32x2 rr = pair(ref, ref), cc = pair(p.scale, p.scale), ll = pair(ls, ls), ss = pair(slope, slope),
+                  bb = pair(base, base);
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if (i + j * THREADS >= b) continue;
+        float g[E];
+#pragma unroll
+        for (int k = 0; k < E / 2; ++k) {
+          const float2 v = q[j].two(k);
+          const float2 d = halves(fma2(add2(pair(v.x, v.y), rr), cc, ll));
+          const float2 e = halves(mul2(pair(ex2(d.x), ex2(d.y)), fma2(pair(fmaxf(d.x, -200.f), fmaxf(d.y, -200.f)), ss, bb)));
+          g[2 * k] = e.x, g[2 * k + 1] = e.y;
+        }
+        const int at = r.first(i + j * THREADS);
+        if ((unsigned)(tk - at) < (unsigned)E || (unsigned)(p.excluded - at) < (unsigned)E) {
+#pragma unroll
+          for (int k = 0; k < E; ++k) g[k] = special(g[k], at + k);
+        }
+        store(i + j * THREADS, g);
+      }
+    }
+  }
+  if (part == 0 && t < r.lead) out[t] = to_out<T>(counts ? grad(cvt(in[t]), t) : 0.f);
+  const int last = r.lead + r.n * E + t;
+  if (part == p.parts - 1 && t < r.tail) out[last] = to_out<T>(counts ? grad(cvt(in[last]), last) : 0.f);
 }
 
 template <typename T, int THREADS>
@@ -490,6 +800,39 @@ cudaError_t scores_t(const ScoresParams& p, cudaStream_t s) {
   cfg.numAttrs = p.parts > 1 ? 2 : 1;
   return p.parts > 1 ? cudaLaunchKernelEx(&cfg, k_scores<T, THREADS, true>, p)
                      : cudaLaunchKernelEx(&cfg, k_scores<T, THREADS, false>, p);
+}
+
+template <typename T, int NV>
+cudaError_t scores_warp_t(const ScoresParams& p, cudaStream_t s) {
+  return launch_pdl(k_scores_warp<T, NV>, dim3((unsigned)((p.rows + kWarpsPerCta - 1) / kWarpsPerCta)),
+                    dim3(32 * kWarpsPerCta), 0, s, p);
+}
+template <typename T>
+cudaError_t scores(ScoresParams p, cudaStream_t s) {
+  const int64_t bytes = (int64_t)p.vocab * sizeof(T);
+  // a row's 16-byte groups beside its single entries: 512 NV bytes at most
+  if (bytes <= 2048) return scores_warp_t<T, 4>(p, s);
+  if (bytes <= 4096) return scores_warp_t<T, 8>(p, s);
+  if (bytes <= 8192) return scores_warp_t<T, 16>(p, s);
+  // a row's cluster: as many CTAs as leave no SM idle, each with 2048 entries at least
+  while (p.parts < kMaxParts && p.rows * p.parts < 152 && p.vocab >= 2048 * 2 * p.parts) p.parts *= 2;
+  // 1536 threads per SM either way. Small CTAs overlap one row's passes with another's loads (16384 rows of 24000 bf16,
+  // 16 entries: 177 us by 128 threads, 216 by 256), but the rows in flight should stay in L2 until their likeliest
+  // entries are listed: 912 rows of 100 KB do (50304 bf16: 363 by 128, 313 by 256), of fp32 456 (8192 rows 314 by 256,
+  // 283 by 512).
+  if (bytes <= 64 * 1024) return scores_t<T, 128>(p, s);
+  if (bytes <= 160 * 1024 || p.parts > 1) return scores_t<T, 256>(p, s);
+  return scores_t<T, 512>(p, s);
+}
+template <typename T>
+cudaError_t scores_bwd(ScoresParams p, cudaStream_t s) {
+  // a row over several CTAs where there are few: four groups per thread at least
+  while (p.parts < 64 && p.rows * p.parts < 912 && (int64_t)p.vocab * sizeof(T) >= 2 * 16384 * p.parts) p.parts *= 2;
+  const dim3 grid((unsigned)(p.rows * p.parts)), block(256);
+  // rows of both on the same boundaries: the first ones are
+  const bool same = p.rows == 1 || (p.ld - p.ld_out) * sizeof(T) % 16 == 0;
+  return same ? launch_pdl(k_scores_bwd<T, false>, grid, block, 0, s, p)
+              : launch_pdl(k_scores_bwd<T, true>, grid, block, 0, s, p);
 }
 
 int fail(int code, const char* fn, const char* what) {
@@ -580,14 +923,8 @@ int bdscan_token_scores_forward(const bdscan_token_scores_dims* dims, const void
   p.stats = (float2*)stats;
   p.top_ids = top_ids;
   p.top_logp = top_logp;
-  const bool small = p.vocab <= 4096;
-  // a row's cluster: as many CTAs as leave no SM idle, each with 2048 entries at least
-  while (p.parts < kMaxParts && p.rows * p.parts < 152 && p.vocab >= 2048 * 2 * p.parts) p.parts *= 2;
   cudaStream_t s = (cudaStream_t)stream;
-  const bool f32 = dims->dtype == BDSCAN_F32;
-  const cudaError_t e = small ? (f32 ? scores_t<float, 128>(p, s) : scores_t<bf16, 128>(p, s))
-                              : (f32 ? scores_t<float, 512>(p, s) : scores_t<bf16, 512>(p, s));
-  return done(e, fn, s);
+  return done(dims->dtype == BDSCAN_F32 ? scores<float>(p, s) : scores<bf16>(p, s), fn, s);
 }
 
 int bdscan_token_scores_backward(const bdscan_token_scores_dims* dims, const void* logits, const int64_t* token,
@@ -613,12 +950,8 @@ int bdscan_token_scores_backward(const bdscan_token_scores_dims* dims, const voi
   p.dlogp = dlogp;
   p.dentropy = dentropy;
   p.dlogits = dlogits;
-  while (p.parts < 64 && p.rows * p.parts < 608 && p.vocab >= 2048 * p.parts) p.parts *= 2;
   cudaStream_t s = (cudaStream_t)stream;
-  const dim3 grid((unsigned)(p.rows * p.parts)), block(256);
-  const cudaError_t e = dims->dtype == BDSCAN_F32 ? launch_pdl(k_scores_bwd<float>, grid, block, 0, s, p)
-                                                  : launch_pdl(k_scores_bwd<bf16>, grid, block, 0, s, p);
-  return done(e, fn, s);
+  return done(dims->dtype == BDSCAN_F32 ? scores_bwd<float>(p, s) : scores_bwd<bf16>(p, s), fn, s);
 }
 
 }  // extern "C"
