@@ -161,10 +161,18 @@ struct LossRowsParams {
   float *gscale, *lse_c;
   float *loss, *lse;
   float scale;  // of the gradient scales: 1 / temperature
+  // instead of targets, the distillation's entries [rows][top]: the first known one stands for the target, and the
+  // student's logits of rows that do not count are zeroed (z null: they are not written)
+  const int64_t* ids;
+  const float* teacher;
+  int top;
+  int64_t excluded;
+  float* z;
   // factors that the gradient at the logits takes from the rows' scales ([rows], null: none), and those of the slots
   const float* dz_scale;
   float* dz_scale_c;
 };
+cudaError_t launch_loss_targets(const LossRowsParams& p, int64_t* target, cudaStream_t s);  // the first known entries
 cudaError_t launch_loss_rows(const LossRowsParams& p, cudaStream_t s);
 // launch_loss_rows and launch_pack_rows in one, for up to small_loss_rows() rows.
 int64_t small_loss_rows();
@@ -180,23 +188,24 @@ struct DistillParams {
   int64_t rows, vocab, excluded;
   int top;
   float scale, scale2;   // 1 / temperature, and log2(e) / temperature
-  int64_t* target;       // launch_distill_rows: [rows] the first known entry, or -1
-  const float* dloss;    // and in a bf16 backward the factor that the row's gradient takes from its scale
-  float* row_scale;
+  // launch_distill_grad: the gradient at the entries, [rows][top], and in bf16 the factor that it takes from the row's
+  // scale, [rows]
+  const float* dloss;
+  float *grad, *row_scale;
   // launch_distill_join: slots of the rows that count, their partial statistics and the operands as they lie
   const int *count, *idx;
   const float2* part;
   int parts, d_model;
   int64_t rows_ld, ld_h;
   const void *h, *w;
-  float *z, *loss, *lse;  // [rows][top], [rows]; z null: launch_distill_rows leaves it alone
+  float *z, *loss, *lse;  // [rows][top], [rows]
   // launch_distill_dz: entries v0 .. v0 + n - 1 in `pieces` planes
-  const float *lse_in, *z_in, *dz_scale;  // dz_scale: of the slots, or null
+  const float *lse_in, *z_in;
   __nv_bfloat16* dz;
   int64_t ld_dz, plane, dz_extent;
   int v0, n, pieces;
 };
-cudaError_t launch_distill_rows(const DistillParams& p, cudaStream_t s);
+cudaError_t launch_distill_grad(const DistillParams& p, cudaStream_t s);
 cudaError_t launch_distill_join(const DistillParams& p, int f32, cudaStream_t s);
 cudaError_t launch_distill_dz(const DistillParams& p, cudaStream_t s);
 int* ssd_wait_flag_ptr();  // ssd.cu

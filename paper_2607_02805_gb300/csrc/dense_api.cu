@@ -880,14 +880,31 @@ int check_distill(const bdscan_distill_loss_dims* d, Loss* l, const char* fn) {
   l->scale = 1.f / d->temperature;
   return BDSCAN_OK;
 }
-// Behind the loss's own workspace: the entries that stand for the rows' targets, and in the backward the factors that
-// the gradient at the logits takes, of the rows and of the slots.
-size_t target_bytes(const Loss& l) { return al256((size_t)l.T * 8); }
+// Behind the loss's own workspace: the targets that the entries stand for, where there are too many rows to look for
+// them while they are numbered, and in the backward the gradient at the entries and the factors that the gradient at the
+// logits takes, of the rows and of the slots.
+size_t target_bytes(const Loss& l) { return l.T > small_loss_rows() ? al256((size_t)l.T * 8) : 0; }
 size_t row_scale_bytes(const Loss& l) { return al256((size_t)up(l.T, 256) * 4); }
-size_t distill_bwd_bytes(const Loss& l) { return target_bytes(l) + 2 * row_scale_bytes(l); }
+size_t entry_bytes(const Loss& l, int top) { return al256((size_t)l.T * top * 4); }
+size_t distill_bwd_bytes(const Loss& l, int top) {
+  return target_bytes(l) + entry_bytes(l, top) + 2 * row_scale_bytes(l);
+}
 
-DistillParams distill_params(const Loss& l, const LossRowsParams& rp, int top, const int64_t* ids,
-                             const float* teacher) {
+cudaError_t find_targets(const Loss& l, LossRowsParams* rp, void* target, cudaStream_t s) {
+  if (l.T <= small_loss_rows()) return cudaSuccess;
+  const cudaError_t e = api_launched(launch_loss_targets(*rp, (int64_t*)target, s), s);
+  rp->target = (const int64_t*)target;
+  rp->ids = nullptr;
+  rp->z = nullptr;
+  return e;
+}
+// Its parameters, and the entries in the row bookkeeping's.
+DistillParams distill_params(const Loss& l, LossRowsParams& rp, int top, const int64_t* ids, const float* teacher) {
+  rp.ids = ids;
+  rp.teacher = teacher;
+  rp.top = top;
+  rp.excluded = l.excluded;
+
   DistillParams p;
   memset(&p, 0, sizeof(p));
   p.ids = ids;
@@ -899,7 +916,6 @@ DistillParams distill_params(const Loss& l, const LossRowsParams& rp, int top, c
   p.top = top;
   p.scale = l.scale;
   p.scale2 = 1.4426950408889634f * l.scale;
-  p.target = const_cast<int64_t*>(rp.target);
   p.count = rp.count;
   p.idx = rp.idx;
   return p;
@@ -1337,15 +1353,15 @@ int bdscan_distill_loss_forward(const bdscan_distill_loss_dims* dims, const void
   if ((rc = check_device(fn, &flag))) return rc;
   cudaStream_t s = (cudaStream_t)stream;
   char* base = (char*)workspace;
-  LossRowsParams rp = rows_params(l, ws.r, (const int64_t*)(base + ws.total), weight, base);
+  LossRowsParams rp = rows_params(l, ws.r, nullptr, weight, base);
   rp.loss = loss;
   rp.lse = lse;
   DistillParams d = distill_params(l, rp, dims->top, ids, teacher);
-  d.z = z;
-  cudaError_t e = api_launched(launch_distill_rows(d, s), s);
+  d.z = rp.z = z;
   Operand a;
   PackParams pw;
   const Operand b = operand(&pw, l.dtype, w, l.V, l.K, l.K, base + ws.w);
+  cudaError_t e = find_targets(l, &rp, base + ws.total, s);
   if (e == cudaSuccess) e = prepare_rows(l, ws.r, rp, h, base, nullptr, pw, &a, nullptr, s);
   if (e == cudaSuccess) {
     Plan q = ws.q;
@@ -1370,7 +1386,7 @@ int bdscan_distill_loss_forward(const bdscan_distill_loss_dims* dims, const void
 size_t bdscan_distill_loss_backward_workspace_size(const bdscan_distill_loss_dims* dims) {
   Loss l;
   if (check_distill(dims, &l, "bdscan_distill_loss_backward_workspace_size") != BDSCAN_OK || l.T == 0) return 0;
-  return loss_bwd_ws(l).total + distill_bwd_bytes(l);
+  return loss_bwd_ws(l).total + distill_bwd_bytes(l, dims->top);
 }
 
 int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const void* h, const void* w,
@@ -1397,24 +1413,27 @@ int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const voi
   DENSE_OPT(dloss, fn, "dloss");
   DENSE_REQ(dh, fn, "dh");
   const LossBwdWs ws = loss_bwd_ws(l);
-  if ((rc = check_workspace(workspace, workspace_bytes, ws.total + distill_bwd_bytes(l), fn))) return rc;
+  if ((rc = check_workspace(workspace, workspace_bytes, ws.total + distill_bwd_bytes(l, dims->top), fn))) return rc;
   int* flag;
   if ((rc = check_device(fn, &flag))) return rc;
   char* base = (char*)workspace;
-  LossRowsParams rp = rows_params(l, ws.r, (const int64_t*)(base + ws.total), weight, base);
+  LossRowsParams rp = rows_params(l, ws.r, nullptr, weight, base);
   rp.dloss = dloss;
   rp.lse_in = lse;
   DistillParams d = distill_params(l, rp, dims->top, ids, teacher);
   d.lse_in = lse;
   d.z_in = z;
+  d.dloss = dloss;
+  char* at = base + ws.total + target_bytes(l);
+  d.grad = (float*)at;
   if (l.pieces == 1) {  // fp32: three pieces round nothing off
-    char* at = base + ws.total + target_bytes(l);
-    d.dloss = dloss;
+    at += entry_bytes(l, dims->top);
     d.row_scale = (float*)at;
     rp.dz_scale = d.row_scale;
-    d.dz_scale = rp.dz_scale_c = (float*)(at + row_scale_bytes(l));
+    rp.dz_scale_c = (float*)(at + row_scale_bytes(l));
   }
-  cudaError_t e = api_launched(launch_distill_rows(d, s), s);
+  cudaError_t e = api_launched(launch_distill_grad(d, s), s);
+  if (e == cudaSuccess) e = find_targets(l, &rp, base + ws.total, s);
   // the epilogue takes 1 off at the row's target, which is a known entry: what is written there below covers it
   if (e == cudaSuccess)
     e = loss_backward(l, ws, rp, h, w, dh, dw, base, flag, s, [&](int64_t v0, int64_t n, const Operand& dz) {

@@ -67,6 +67,21 @@ __device__ __forceinline__ void load_entries(Entries& e, const DistillParams& p,
 
 // The shares of an entry's id in all places, and their logarithm in base 2.
 __device__ __forceinline__ void merge_ids(Entries& e, float (&share)[2], int top) {
+  const int lane = threadIdx.x & 31;
+  // no two lanes with the same id: an entry that is not known stands for itself
+  const int own[2] = {e.id[0] >= 0 ? e.id[0] : -1 - lane, e.id[1] >= 0 ? e.id[1] : -1 - lane};
+  bool twice = __popc(__match_any_sync(0xffffffffu, own[0])) > 1;
+  if (top > 32) {
+    twice |= __popc(__match_any_sync(0xffffffffu, own[1])) > 1;
+#pragma unroll 8
+    for (int j = 0; j < 32; ++j) {
+      const int id = __shfl_sync(0xffffffffu, e.id[0], j);
+      twice |= id >= 0 && id == e.id[1];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) share[k] = e.q[k];
+  if (!__any_sync(0xffffffffu, twice)) return;
   share[0] = share[1] = 0.f;
   int times[2] = {0, 0};
   for (int j = 0; j < top; ++j) {
@@ -122,103 +137,121 @@ __device__ __forceinline__ float pick_scale(const Entries& e, const float (&s)[2
   return err_1 < err_m ? one : mant;
 }
 
-// A warp per row: its first known entry as the target of the loss's row
-// bookkeeping, -1 where there is none, and zeros in z (forward) where the row
-// does not count.
-__global__ void __launch_bounds__(kThreads) k_distill_rows(const DistillParams p) {
+// A warp per row: the gradient at its entries, which k_distill_dz puts in place
+// piece by piece of the vocabulary, and what it takes of the row's scale.
+__global__ void __launch_bounds__(kThreads) k_distill_grad(const DistillParams p) {
   pdl_sync();
   const int lane = threadIdx.x & 31;
   const int64_t row = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
   if (row >= p.rows) return;
   if (!dguard(kSiteDistill, row, p.rows)) return;
+  const float g = (p.weight != nullptr ? p.weight[row] : 1.f) * (p.dloss != nullptr ? p.dloss[row] : 1.f) * p.scale;
+  Entries e;
+  float share[2], s[2] = {0.f, 0.f};
+  load_entries(e, p, row);
+  if (g == 0.f || !__any_sync(0xffffffffu, e.id[0] >= 0 || e.id[1] >= 0)) return;  // a row that does not count
+  merge_ids(e, share, p.top);
+  const float lse = p.lse_in[row];
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (e.id[k] >= 0) s[k] = entry_grad(p, p.z_in[row * p.top + lane + 32 * k], lse, share[k]);
+  const float a = p.row_scale != nullptr ? pick_scale(e, s, g) : 1.f;
+  if (lane == 0 && p.row_scale != nullptr) p.row_scale[row] = a;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (lane + 32 * k < p.top) p.grad[row * p.top + lane + 32 * k] = a * s[k];
+}
+
+// A row's products with J rows of w (null: none), by a warp, J loads of w and one of the row in flight.
+template <typename T, bool VEC, int J>
+__device__ __forceinline__ void dot_rows(float (&s)[J], const T* a, const T* const (&b)[J], int k) {
+  constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int j = 0; j < J; ++j) s[j] = 0.f;
+#pragma unroll 2
+  for (int i = lane * E; i < k; i += 32 * E) {
+    if constexpr (VEC) {
+      const uint4 u = *reinterpret_cast<const uint4*>(a + i);
+      uint4 v[J];
+#pragma unroll
+      for (int j = 0; j < J; ++j) v[j] = b[j] != nullptr ? *reinterpret_cast<const uint4*>(b[j] + i) : make_uint4(0, 0, 0, 0);
+      const T* x = reinterpret_cast<const T*>(&u);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const T* y = reinterpret_cast<const T*>(&v[j]);
+#pragma unroll
+        for (int q = 0; q < E; ++q) s[j] = fmaf(cvt(x[q]), cvt(y[q]), s[j]);
+      }
+    } else {
+      const float x = cvt(a[i]);
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (b[j] != nullptr) s[j] = fmaf(x, cvt(b[j][i]), s[j]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j) s[j] = warp_sum(s[j]);
+}
+
+// WPR warps per row that counts: the student's logits at the row's entries, four
+// of them per warp at a time (rows of w come from L2 mostly), the partial
+// statistics joined, and the loss, formed in base 2 before anything is rounded at
+// the logits' own size. It is a chain of latencies: with many rows one warp each
+// (8192 rows, 32 entries of 832 bf16, 436 MB), a CTA each where there are few.
+template <typename T, bool VEC, int WPR>
+__global__ void __launch_bounds__(kThreads) k_distill_join(const DistillParams p) {
+  pdl_sync();
+  constexpr int J = 4, R = kRowWarps / WPR;
+  __shared__ float2 red[kRowWarps];
+  __shared__ float zs[R][64];
+  const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) % WPR, r = (threadIdx.x >> 5) / WPR;
+  const int slot = blockIdx.x * R + r;
+  if (slot >= *p.count) return;  // all warps of the row
+  const int64_t row = p.idx[slot];
   Entries e;
   float t[2];
   load_ids(e, t, p, row);
-  const uint32_t lo = __ballot_sync(0xffffffffu, e.id[0] >= 0), hi = __ballot_sync(0xffffffffu, e.id[1] >= 0);
-  const int first = lo != 0 ? __shfl_sync(0xffffffffu, e.id[0], __ffs(lo) - 1)
-                            : hi != 0 ? __shfl_sync(0xffffffffu, e.id[1], __ffs(hi) - 1) : -1;
-  if (lane == 0) p.target[row] = first;
-  if (p.row_scale != nullptr && first >= 0) {
-    const float g = (p.weight != nullptr ? p.weight[row] : 1.f) * (p.dloss != nullptr ? p.dloss[row] : 1.f) * p.scale;
-    float share[2], s[2] = {0.f, 0.f};
-    load_entries(e, p, row);
-    merge_ids(e, share, p.top);
-    const float lse = p.lse_in[row];
+  const T* h = static_cast<const T*>(p.h) + row * p.ld_h;
+  for (int j0 = J * w; j0 < p.top; j0 += J * WPR) {
+    const T* at[J];
+    float z[J];
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-      if (e.id[k] >= 0) s[k] = entry_grad(p, p.z_in[row * p.top + lane + 32 * k], lse, share[k]);
-    const float a = pick_scale(e, s, g);
-    if (lane == 0) p.row_scale[row] = a;
-  }
-  if (p.z != nullptr && (first < 0 || (p.weight != nullptr && p.weight[row] == 0.f)))
-    for (int j = lane; j < p.top; j += 32) p.z[row * p.top + j] = 0.f;
-}
-
-// One row's product with a row of w, by a warp.
-template <typename T, bool VEC>
-__device__ __forceinline__ float dot_row(const T* a, const T* b, int k) {
-  constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
-  const int lane = threadIdx.x & 31;
-  float s = 0.f;
-#pragma unroll 4
-  for (int i = lane * E; i < k; i += 32 * E) {
-    if constexpr (VEC) {
-      const uint4 u = *reinterpret_cast<const uint4*>(a + i), v = *reinterpret_cast<const uint4*>(b + i);
-      const T *x = reinterpret_cast<const T*>(&u), *y = reinterpret_cast<const T*>(&v);
-#pragma unroll
-      for (int j = 0; j < E; ++j) s = fmaf(cvt(x[j]), cvt(y[j]), s);
-    } else {
-      s = fmaf(cvt(a[i]), cvt(b[i]), s);
+    for (int j = 0; j < J; ++j) {
+      const int id = __shfl_sync(0xffffffffu, j0 + j < 32 ? e.id[0] : e.id[1], (j0 + j) & 31);
+      at[j] = id >= 0 && j0 + j < p.top ? static_cast<const T*>(p.w) + (int64_t)id * p.d_model : nullptr;
     }
-  }
-  return warp_sum(s);
-}
-
-// A CTA per row that counts: the partial statistics joined, the student's logits
-// at the row's entries (a warp per entry; rows of w come from L2 mostly), and the
-// loss, formed in base 2 before anything is rounded at the logits' own size.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_distill_join(const DistillParams p) {
-  pdl_sync();
-  __shared__ float2 red[kRowWarps];
-  __shared__ float zs[64];
-  __shared__ int ids[64];
-  const int slot = blockIdx.x, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  if (slot >= *p.count) return;
-  const int64_t row = p.idx[slot];
-  Entries e;
-  if (w == 0) {
-    load_entries(e, p, row);
+    dot_rows<T, VEC, J>(z, h, at, p.d_model);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) ids[lane + 32 * k] = e.id[k];
-    float share[2];
-    merge_ids(e, share, p.top);
+    for (int j = 0; j < J; ++j)
+      if (lane == j && j0 + j < p.top) zs[r][j0 + j] = z[j];
   }
   float m = -INFINITY, s = 0.f;
-  for (int k = threadIdx.x; k < p.parts; k += kThreads) stats_join(m, s, p.part[(int64_t)k * p.rows_ld + slot]);
+  for (int k = w * 32 + lane; k < p.parts; k += 32 * WPR) stats_join(m, s, p.part[(int64_t)k * p.rows_ld + slot]);
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1)
     stats_join(m, s, make_float2(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o)));
-  if (lane == 0) red[w] = make_float2(m, s);
-  __syncthreads();
-  const T* h = static_cast<const T*>(p.h) + row * p.ld_h;
-  for (int j = w; j < p.top; j += kRowWarps) {
-    const int id = ids[j];
-    const float z = id >= 0 ? dot_row<T, VEC>(h, static_cast<const T*>(p.w) + (int64_t)id * p.d_model, p.d_model) : 0.f;
-    if (lane == 0) zs[j] = z;
-  }
-  __syncthreads();
-  if (w != 0) return;
-  m = red[0].x, s = red[0].y;
+  if constexpr (WPR > 1) {
+    static_assert(R == 1, "the barrier is the CTA's");
+    if (lane == 0) red[w] = make_float2(m, s);
+    __syncthreads();
+    if (w != 0) return;
+    m = red[0].x, s = red[0].y;
 #pragma unroll
-  for (int k = 1; k < kRowWarps; ++k) stats_join(m, s, red[k]);
+    for (int k = 1; k < WPR; ++k) stats_join(m, s, red[k]);
+  } else {
+    __syncwarp();
+  }
+  float share[2];
+  load_entries(e, p, row);
+  merge_ids(e, share, p.top);
   const float l2 = log2f(s);
   float sum = 0.f;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int j = lane + 32 * k;
     if (j < p.top) {
-      const float z = zs[j];
+      const float z = zs[r][j];
       p.z[row * p.top + j] = z;
       // an entry too unlikely for fp32 adds nothing
       if (e.id[k] >= 0 && e.q[k] != 0.f) sum = fmaf(e.q[k], e.l2[k] - (fmaf(z, p.scale2, -m) - l2), sum);
@@ -232,54 +265,49 @@ __global__ void __launch_bounds__(kThreads) k_distill_join(const DistillParams p
   }
 }
 
-// The gradient at the logits, p - q, of the entries inside a piece of the
-// vocabulary, over what the product's epilogue left there. Formed again from the
-// row's own logit, so that it is rounded once. An id that comes twice takes both
-// shares; each of its lanes writes the same value.
+// The gradient at the logits of the entries inside a piece of the vocabulary,
+// over what the product's epilogue left there: rounded once, from the row's own
+// logit. A thread per entry; those of an id that comes twice write the same value.
 __global__ void __launch_bounds__(kThreads) k_distill_dz(const DistillParams p) {
   pdl_sync();
-  const int lane = threadIdx.x & 31;
-  const int64_t slot = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+  const int64_t x = (int64_t)blockIdx.x * kThreads + threadIdx.x, slot = x / p.top;
   if (slot >= *p.count) return;
   if (!dguard(kSiteDistill, (p.pieces - 1) * p.plane + slot * p.ld_dz + p.n - 1, p.dz_extent)) return;
-  const int64_t row = p.idx[slot];
-  Entries e;
-  load_entries(e, p, row);
-  float share[2];
-  merge_ids(e, share, p.top);
-  const float lse = p.lse_in[row], a = p.dz_scale != nullptr ? p.dz_scale[slot] : 1.f;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int at = e.id[k] - p.v0;
-    if (e.id[k] < 0 || at < 0 || at >= p.n) continue;
-    float v = a * entry_grad(p, p.z_in[row * p.top + lane + 32 * k], lse, share[k]);
-    bf16* to = p.dz + slot * p.ld_dz + at;
-    for (int i = 0; i < p.pieces; ++i) {
-      const float part = p.pieces == 1 ? v : bf16_part(v);
-      to[i * p.plane] = __float2bfloat16_rn(part);
-      v -= part;
-    }
+  const int64_t at = (int64_t)p.idx[slot] * p.top + (x - slot * p.top);
+  const int64_t id = p.ids[at], to = id - p.v0;
+  if (id < 0 || id == p.excluded || to < 0 || to >= p.n || p.teacher[at] == -INFINITY) return;
+  float v = p.grad[at];
+  bf16* d = p.dz + slot * p.ld_dz + to;
+  for (int i = 0; i < p.pieces; ++i) {
+    const float part = p.pieces == 1 ? v : bf16_part(v);
+    d[i * p.plane] = __float2bfloat16_rn(part);
+    v -= part;
   }
 }
 
 }  // namespace
 
-cudaError_t launch_distill_rows(const DistillParams& p, cudaStream_t s) {
-  launch_pdl(k_distill_rows, dim3((unsigned)((p.rows + kRowWarps - 1) / kRowWarps)), dim3(kThreads), 0, s, p);
+cudaError_t launch_distill_grad(const DistillParams& p, cudaStream_t s) {
+  launch_pdl(k_distill_grad, dim3((unsigned)((p.rows + kRowWarps - 1) / kRowWarps)), dim3(kThreads), 0, s, p);
   return cudaGetLastError();
 }
+namespace {
+template <typename T, bool VEC>
+void join_t(const DistillParams& p, cudaStream_t s) {
+  // 8192 of 16384 rows, 32 entries of 832 bf16: a CTA per row 145 us, two warps 111, one 97
+  if (p.rows >= 2048) launch_pdl(k_distill_join<T, VEC, 1>, dim3((unsigned)((p.rows + 7) / 8)), dim3(kThreads), 0, s, p);
+  else launch_pdl(k_distill_join<T, VEC, 8>, dim3((unsigned)p.rows), dim3(kThreads), 0, s, p);
+}
+}  // namespace
 cudaError_t launch_distill_join(const DistillParams& p, int f32, cudaStream_t s) {
   const int e = f32 ? 4 : 8;
   const bool vec = p.d_model % e == 0 && p.ld_h % e == 0;
-  const dim3 grid((unsigned)p.rows), block(kThreads);
-  if (f32) vec ? launch_pdl(k_distill_join<float, true>, grid, block, 0, s, p)
-               : launch_pdl(k_distill_join<float, false>, grid, block, 0, s, p);
-  else vec ? launch_pdl(k_distill_join<bf16, true>, grid, block, 0, s, p)
-           : launch_pdl(k_distill_join<bf16, false>, grid, block, 0, s, p);
+  if (f32) vec ? join_t<float, true>(p, s) : join_t<float, false>(p, s);
+  else vec ? join_t<bf16, true>(p, s) : join_t<bf16, false>(p, s);
   return cudaGetLastError();
 }
 cudaError_t launch_distill_dz(const DistillParams& p, cudaStream_t s) {
-  launch_pdl(k_distill_dz, dim3((unsigned)((p.rows + kRowWarps - 1) / kRowWarps)), dim3(kThreads), 0, s, p);
+  launch_pdl(k_distill_dz, dim3((unsigned)((p.rows * p.top + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, p);
   return cudaGetLastError();
 }
 
