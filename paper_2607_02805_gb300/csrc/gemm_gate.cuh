@@ -79,9 +79,10 @@ __device__ __forceinline__ void rows_in(float (&v)[16], const GemmParams& p, int
     v[4 * j] = q.x, v[4 * j + 1] = q.y, v[4 * j + 2] = q.z, v[4 * j + 3] = q.w;
   }
 }
-template <bool F32>
+// PIECES: to as many planes of bf16, `plane` elements apart, the largest piece of what is left of the value each.
+template <bool F32, int PIECES = 1>
 __device__ __forceinline__ void rows_out(void* out, int64_t ld, int64_t m, int64_t row0, int col, int n, int at,
-                                         const float (&v)[16], unsigned char* stg) {
+                                         const float (&v)[16], unsigned char* stg, int64_t plane = 0) {
   const int lane = threadIdx.x & 31, cl = lane & 15;
   float* f = reinterpret_cast<float*>(stg);
   __syncwarp();
@@ -98,7 +99,15 @@ __device__ __forceinline__ void rows_out(void* out, int64_t ld, int64_t m, int64
       y[i] = f[r * 16 + 4 * ((cl >> 2) ^ ((r >> 1) & 3)) + (cl & 3)];
     }
     const int64_t row = row0 + (lane >> 4);
-    store_rows<F32>(out, row, ld, at + col + cl, (int)min((int64_t)32, m - row), y);
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+      float part[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) part[i] = PIECES == 1 ? y[i] : bf16_part(y[i]);
+      store_rows<F32>(static_cast<bf16*>(out) + k * plane, row, ld, at + col + cl, (int)min((int64_t)32, m - row), part);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] -= part[i];
+    }
   }
   __syncwarp();
 }
@@ -286,6 +295,11 @@ __device__ __forceinline__ bool gate_epilogue(const GemmParams& p, const GemmMap
           const int c = col + (lane >> 1);
           if (c < n) p.colsum[(row0 >> 5) * p.n + c + (lane & 1) * n] = (lane & 1) ? b : a;
         }
+        if constexpr (ROWS) {
+          rows_out<false, NP>(p.out, p.ld_out, p.m, row0, col, n, 0, g, stg, p.split_stride);
+          rows_out<false, NP>(p.out, p.ld_out, p.m, row0, col, n, n, u, stg, p.split_stride);
+          continue;
+        }
         // the pieces of both gradients (fp32: the largest of what is left, three times)
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
@@ -298,11 +312,7 @@ __device__ __forceinline__ bool gate_epilogue(const GemmParams& p, const GemmMap
               g[j] -= dg[j], u[j] -= du[j];
             }
           }
-          if constexpr (ROWS) {
-            bf16* out = static_cast<bf16*>(p.out) + k * p.split_stride;
-            rows_out<false>(out, p.ld_out, p.m, row0, col, n, 0, dg, stg);
-            rows_out<false>(out, p.ld_out, p.m, row0, col, n, n, du, stg);
-          } else if constexpr (NP == 3) {
+          if constexpr (NP == 3) {
             unsigned char* at = stg + 2048 * (k & 1);
             if (k == 2) {  // the first piece's two stores have read this half
               if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 2;\n" ::: "memory");
