@@ -20,8 +20,8 @@
 // One CTA per row, six of 256 threads per SM. Where that leaves SMs idle, a
 // cluster of CTAs shares a row: each leaves its statistics and its own likeliest
 // entries in the first one's shared memory. 16384 rows of 50304 bf16 (1.65 GB):
-// 240 us without likeliest entries, the copy rate, 275 with one, 313 with 16 (an
-// eighth of each row read again, and its latency), 485 with 64. The gradient is
+// 240 us without likeliest entries, the copy rate, 260 with one, 300 with 16 (an
+// eighth of each row read again, and its latency), 473 with 64. The gradient is
 // one read and one write at the copy rate (477 us).
 #include <cstdio>
 #include <cstring>
@@ -37,6 +37,7 @@ namespace {
 
 constexpr int kMaxTop = 64;
 constexpr int kGroups = 128;
+constexpr int kTakeOff = 32;   // up to so many places one warp finds the bound
 constexpr int kList = 512;     // entries of a CTA's list; eight CTAs' kMaxTop each
 constexpr int kMaxParts = 8;   // CTAs of a row's cluster
 constexpr int kNone = 1 << 30; // stands for the index of a place without an entry, another for each place
@@ -286,6 +287,29 @@ __device__ __forceinline__ uint32_t key_of(float v) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+// A bound that the top-th largest of a warp's N values per lane reaches, and no
+// more than it: the values' keys, taken off one by one. In their last bits the
+// keys carry their place, so that no two are equal and a round is a maximum, a
+// reduction and N selects (with a ballot for the first of equal keys a round took
+// twice as long); the bound is the key without them. Minus infinity (where there
+// are fewer values than `top`) and NaN count as none.
+template <int N>
+__device__ __forceinline__ float take_off(const float (&v)[N], int top) {
+  constexpr uint32_t kPlace = 32 * N - 1;
+  const int lane = threadIdx.x & 31;
+  uint32_t keys[N], bound = 0;
+#pragma unroll
+  for (int k = 0; k < N; ++k) keys[k] = v[k] > -INFINITY ? (key_of(v[k]) & ~kPlace) | (uint32_t)(N * lane + k) : 0u;
+  for (int i = 0; i < top; ++i) {
+    uint32_t mine = keys[0];
+#pragma unroll
+    for (int k = 1; k < N; ++k) mine = max(mine, keys[k]);
+    bound = __reduce_max_sync(0xffffffffu, mine);
+#pragma unroll
+    for (int k = 0; k < N; ++k) keys[k] = keys[k] == bound ? 0u : keys[k];
+  }
+  return bound != 0 ? of_key(bound & ~kPlace) : -INFINITY;
+}
 // Whether entry (v, i) comes before (w, j).
 __device__ __forceinline__ bool before(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
 
@@ -347,6 +371,7 @@ __device__ __forceinline__ void rank_list(const float* lv, const int* li, int n,
     const float v = lv[i];
     const int at = li[i];
     int rank = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) rank += before(lv[j], li[j], v, at) ? 1 : 0;
     if (rank < top) emit(rank, v, at);
   }
@@ -403,8 +428,16 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_scores(const Scores
   m = fmaxf(fmaxf(g4.x, g4.y), fmaxf(g4.z, g4.w));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  // the bound, the top-th largest of the groups' maxima: the smallest that fewer than `top` exceed
-  if (p.top > 0 && t < kGroups) {
+  // The bound, the top-th largest of the groups' maxima. For few places one warp takes the maxima off, while the others
+  // wait (issue slots are what many rows share); for many a thread per group counts those above its own, and the bound is
+  // the smallest that fewer than `top` exceed.
+  if (p.top > 0 && p.top <= kTakeOff) {
+    if (w == 0) {
+      const float four[4] = {g4.x, g4.y, g4.z, g4.w};
+      const float tau = take_off(four, p.top);
+      if (lane < kGroups / 32) sm.tau[lane] = tau;
+    }
+  } else if (p.top > 0 && t < kGroups) {
     const float of = sm.gmax[t];
     int above = 0;
 #pragma unroll 8
@@ -442,14 +475,17 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_scores(const Scores
     __syncthreads();
     const int begin = r.begin(part, parts), end = r.begin(part + 1, parts), ns = sm.selected;
     const int per = (end - begin + THREADS - 1) / THREADS * G;  // 16-byte groups of each, the last ones past the end
-    for (int x = t; x < ns * per; x += U * THREADS) {
+    int k = per > 0 ? t / per : ns, e = t - k * per;  // group and its e-th
+    const int dk = per > 0 ? THREADS / per : 0, de = THREADS - dk * per;
+    while (k < ns) {
       Vec<T> q[U];
       int at[U];
 #pragma unroll
       for (int j = 0; j < U; ++j) {
-        const int y = x + j * THREADS, k = y / per, e = y - k * per;
         at[j] = k < ns ? begin + sm.sel[k] * G + e % G + e / G * THREADS : end;
         if (at[j] < end) q[j].load(r.group(at[j]));
+        k += dk, e += de;
+        if (e >= per) e -= per, ++k;
       }
 #pragma unroll
       for (int j = 0; j < U; ++j) {
@@ -502,8 +538,6 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_scores(const Scores
     n = p.top;
     __syncthreads();
   }
-  const float *lv = sm.lv;
-  const int* li = sm.li;
   if constexpr (CLUSTER) {
     __syncthreads();
     cluster_wait();  // the first CTA has begun
@@ -530,12 +564,16 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_scores(const Scores
       stat_move(q, nm, c);
       a.s += q.s, a.t += q.t;
     }
-    lv = sm.pv, li = sm.pi;
-    n = parts * p.top;
   }
   const RowOut out(p, row, a);
   if (t == 0) out.scores(a, zt);
-  if (p.top > 0) rank_list<THREADS>(lv, li, n, p.top, [&](int k, float v, int at) { out.place(k, v, at); });
+  if (p.top > 0) {
+    // the parts' lists again as one (searching the other lists by halving instead: a few percent more for 16 entries of
+    // one row, a quarter less for 64)
+    const float* lv = CLUSTER ? sm.pv : sm.lv;
+    const int* li = CLUSTER ? sm.pi : sm.li;
+    rank_list<THREADS>(lv, li, CLUSTER ? parts * p.top : n, p.top, [&](int k, float v, int at) { out.place(k, v, at); });
+  }
 }
 
 // ---- short rows: a warp each ----
@@ -543,7 +581,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_scores(const Scores
 // lane: the maximum first, then the sums. The bound is the top-th largest of 128
 // groups' maxima, four per lane (of 256 in the shortest rows, whose groups would
 // be fewer than `top`), taken off one by one; what reaches it is ranked as above,
-// in the warp's own list. 16384 rows of 2000 bf16: 21 us, with 16 entries 55 (by
+// in the warp's own list. 16384 rows of 2000 bf16: 21 us, with 16 entries 46 (by
 // CTAs of 128 threads: 36 and 68); the loop that takes the maxima off is most of
 // the difference.
 constexpr int kWarpList = 256;
@@ -611,24 +649,7 @@ __global__ void __launch_bounds__(32 * kWarpsPerCta) k_scores_warp(const ScoresP
   const RowOut out(p, row, a);
   if (lane == 0) out.scores(a, zt);
   if (p.top == 0) return;
-  uint32_t keys[NG], bound = 0;
-#pragma unroll
-  for (int k = 0; k < NG; ++k) keys[k] = g[k] > -INFINITY ? key_of(g[k]) : 0u;  // NaN (all of a group) is none either
-  for (int i = 0; i < p.top; ++i) {
-    uint32_t mine = keys[0];
-#pragma unroll
-    for (int k = 1; k < NG; ++k) mine = max(mine, keys[k]);
-    bound = __reduce_max_sync(0xffffffffu, mine);
-    if (bound == 0) break;  // fewer groups than places: everything is listed
-    const uint32_t who = __ballot_sync(0xffffffffu, mine == bound);
-    if (lane == __ffs(who) - 1) {
-      bool gone = false;
-#pragma unroll
-      for (int k = 0; k < NG; ++k)
-        if (!gone && keys[k] == bound) keys[k] = 0, gone = true;
-    }
-  }
-  const float tau = bound != 0 ? of_key(bound) : -INFINITY;
+  const float tau = take_off(g, p.top);  // minus infinity: fewer groups than places, and everything is listed
   float* lv = lists[w];
   int* li = places[w];
   auto keep = [&](float v, int at) {
