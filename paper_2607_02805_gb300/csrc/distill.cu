@@ -145,11 +145,13 @@ __global__ void __launch_bounds__(kThreads) k_distill_grad(const DistillParams p
   const int64_t row = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
   if (row >= p.rows) return;
   if (!dguard(kSiteDistill, row, p.rows)) return;
-  const float g = (p.weight != nullptr ? p.weight[row] : 1.f) * (p.dloss != nullptr ? p.dloss[row] : 1.f) * p.scale;
+  const float wt = p.weight != nullptr ? p.weight[row] : 1.f, dl = p.dloss != nullptr ? p.dloss[row] : 1.f;
+  const float g = wt * (dl * p.scale);  // may be zero where neither is
   Entries e;
   float share[2], s[2] = {0.f, 0.f};
   load_entries(e, p, row);
-  if (g == 0.f || !__any_sync(0xffffffffu, e.id[0] >= 0 || e.id[1] >= 0)) return;  // a row that does not count
+  // the rows that count, as loss_row() has them
+  if (wt == 0.f || dl == 0.f || !__any_sync(0xffffffffu, e.id[0] >= 0 || e.id[1] >= 0)) return;
   merge_ids(e, share, p.top);
   const float lse = p.lse_in[row];
 #pragma unroll
@@ -209,6 +211,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_join(const DistillParams p
   const int slot = blockIdx.x * R + r;
   if (slot >= *p.count) return;  // all warps of the row
   const int64_t row = p.idx[slot];
+  if (!dguard(kSiteDistill, row * p.top + p.top - 1, p.rows * p.top)) return;
   Entries e;
   float t[2];
   load_ids(e, t, p, row);

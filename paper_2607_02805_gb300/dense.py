@@ -388,8 +388,10 @@ class TokenScores(_Holder):
         ids = self._buffer("ids", self._k, torch.int64) if self.top else None
         top = self._buffer("top", self._k, torch.float32) if self.top else None
         p = binding._ptr
+        pi = p(ids)
+        _apart("token", pt, pi)
         binding._call("bdscan_token_scores_forward", self._dims(ld, 0), pz, pt, p(logp), entropy.data_ptr(),
-                      stats.data_ptr(), p(ids), p(top), s)
+                      stats.data_ptr(), pi, p(top), s)
         return logp, entropy, ids, top
 
     def backward(self, logits, token=None, dlogp=None, dentropy=None, out=None, stream=None):

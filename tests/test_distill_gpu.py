@@ -157,6 +157,22 @@ def test_entries_that_are_not_known(dtype):
 
 
 @pytest.mark.parametrize("dtype", [B, F])
+def test_scales_that_vanish_in_their_product(dtype):
+    """A weight and a dloss whose product is below fp32: the row counts, its gradient is zero, and nothing that was
+    left in memory comes into it."""
+    h, w, ids, teacher, weight, dloss = case(60, 64, 300, 4, dtype, counted=1.0, ragged=False)
+    weight[3], dloss[3] = 1e-30, 1e-30
+    weight[4], dloss[5] = 1e30, 1e-35
+    op = DistillLoss(60, 64, 300, 4, dtype)
+    op.forward(h, w, ids, teacher, weight)
+    op.backward(h, w, ids, teacher, weight, dloss)
+    for t in [op._buf["workspace"], *op._outgrown]:
+        t.fill_(255)  # NaN as bf16 and as fp32
+    dh, dw = op.backward(h, w, ids, teacher, weight, dloss)
+    assert torch.isfinite(dh).all() and torch.isfinite(dw).all() and not dh[3].any()
+
+
+@pytest.mark.parametrize("dtype", [B, F])
 @pytest.mark.parametrize("v", [1, 40, 700])
 def test_ids_that_come_twice(dtype, v):
     h, w, ids, teacher, weight, dloss = case(50, 32, v, 64, dtype, counted=1.0, ragged=False)
@@ -245,6 +261,45 @@ def test_vocabulary_in_several_pieces(dtype):
     out = torch.ones(t, dtype=torch.bool, device="cuda")
     out[at] = False
     assert not loss[out].any() and not dh[out].any()
+
+
+def test_offsets_past_32_bits():
+    """h is columns of a buffer of 70,000 rows of 40,000 elements: row offsets pass 2^31 elements."""
+    t, k, v, n, ld = 70000, 16, 300, 4, 40000
+    wide = torch.zeros((t, ld), dtype=B, device="cuda")
+    h = wide[:, 64:64 + k]
+    h.copy_(torch.randn(t, k, device="cuda").to(B))
+    w = torch.randn(v, k, device="cuda").to(B)
+    ids = torch.randint(0, v, (t, n), device="cuda")
+    teacher = torch.randn(t, n, device="cuda")
+    at = torch.tensor([0, 53686, 53688, 69999], device="cuda")  # both sides of 2^31 elements
+    weight = torch.zeros(t, device="cuda")
+    weight[at] = 1.0
+    op = DistillLoss(t, k, v, n, B)
+    loss, _ = op.forward(h, w, ids, teacher, weight)
+    dh, dw = op.backward(h, w, ids, teacher, weight)
+    args = (f64(h[at]), f64(w), ids[at].cpu().numpy(), f64(teacher[at]), np.ones(4))
+    within("loss", loss[at], od.distill_loss_forward(*args)[0], 1e-4)
+    gh, gw = od.distill_loss_backward(*args, np.ones(4))
+    parity.assert_close("dh", dh[at].double().cpu().numpy(), gh, parity.GRAD_TOL, parity.BF16_U)
+    parity.assert_close("dw", dw.double().cpu().numpy(), gw, parity.GRAD_TOL, parity.BF16_U)
+    assert int((loss != 0).sum()) <= 4
+
+
+def test_two_streams_with_a_holder_each():
+    args = [case(200, 64, 700, 9, B, seed=i) for i in (1, 2)]
+    ops = [DistillLoss(200, 64, 700, 9, B, 3, 2.0) for _ in args]
+
+    def step(o, a, s=None):
+        return (*o.forward(*a[:5], stream=s), *o.backward(*a, stream=s))
+
+    want = [[t.clone() for t in step(o, a)] for o, a in zip(ops, args)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in args]
+    for _ in range(8):
+        got = [step(o, a, s) for o, a, s in zip(ops, args, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for g, v in zip(got, want) for p, q in zip(g, v))
 
 
 def test_no_rows():

@@ -244,6 +244,23 @@ def test_two_streams_with_a_holder_each():
         assert all(torch.equal(p, q) for g, v in zip(got, want) for p, q in zip(g, v))
 
 
+def test_offsets_past_32_bits():
+    """x and y are columns of a buffer of 70,000 rows of 40,000 elements: row offsets pass 2^31 elements."""
+    t, k, n, ld = 70000, 64, 48, 40000
+    wide = torch.zeros((t, ld), dtype=B, device="cuda")
+    x, y = wide[:, 64:64 + k], wide[:, 1024:1024 + n]
+    x.copy_(torch.randn(t, k, device="cuda").to(B))
+    w = (torch.randn(2 * n, k, device="cuda") / 8).to(B)
+    op = GatedLinear(t, k, n)
+    op.forward(x, w, out=y)
+    at = torch.tensor([0, 53686, 53688, 69999], device="cuda")  # both sides of 2^31 elements
+    close("y", y[at], od.gated_linear_forward(f64(x[at]), f64(w)), 0)
+    assert not wide[:, 128:1024].any() and not wide[:, 1024 + n:].any()
+    dx, _, _ = op.backward(x, w, y)
+    gx, _, _ = od.gated_linear_backward(f64(x[at]), f64(w), None, f64(y[at]))
+    close("dx", dx[at], gx, 0, True)
+
+
 def test_gated_block_with_its_down_projection():
     """A whole feed-forward block: gated layer, down projection onto the residual stream, and back."""
     t, k, n = 260, 96, 256

@@ -103,6 +103,10 @@ def test_holder_refuses(monkeypatch):
     wide = torch.zeros(4, 12, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="another row stride"):
         op.backward(wide.flatten()[:40].view(4, 10), out=wide[:, :10])
+    one = TokenScores(4, 10, 1, device="cpu")
+    one._buf["ids"] = t.view(4, 1)
+    with pytest.raises(ValueError, match="token is a buffer that this call writes"):
+        one.forward(z, t)
     op._buf["dlogits"] = z
     with pytest.raises(ValueError, match="logits is a buffer that this call writes"):
         op.backward(z)

@@ -222,6 +222,67 @@ def test_gradient_in_place_and_alone():
     assert out.data_ptr() == z.data_ptr() and torch.equal(z, both)
 
 
+def test_offsets_past_32_bits():
+    """Logits are columns of a buffer of 60,000 rows of 40,000 elements, the gradient of another."""
+    t, v, ld = 60000, 300, 40000
+    wide = torch.zeros((t, ld), dtype=B, device="cuda")
+    z = wide[:, 64:64 + v]
+    z.copy_((torch.randn(t, v, device="cuda") * 3).to(B))
+    token = torch.randint(0, v, (t,), device="cuda")
+    op = TokenScores(t, v, 3, B)
+    got = [x.clone() for x in op.forward(z, token)]
+    dl = torch.randn(t, device="cuda")
+    dz = op.backward(z, token, dl, out=wide[:, 1024:1024 + v])
+    # the copy's rows lie on other boundaries, so that sums add up in another order: each side is off by the bounds above
+    same = TokenScores(t, v, 3, B)
+    close = z.contiguous()
+    want = same.forward(close, token)
+    e = (v / 128 + 64) * 2.0 ** -24 + 2.0 ** -21
+    assert torch.equal(got[2], want[2])
+    for i in (0, 3):
+        assert ((got[i] - want[i]).abs() <= 2 * (e + 2.0 ** -21 * want[i].abs())).all()
+    assert ((got[1] - want[1]).abs() <= 4 * e * (1 + math.log(v))).all()
+    grad = same.backward(close, token, dl).float()
+    size = (e + 2.0 ** -21 * (2 + math.log(v))) * dl.abs()[:, None]
+    assert ((dz.float() - grad).abs() <= 2 * (size + 2.0 ** -8 * grad.abs())).all()
+    assert not wide[:, :64].any() and not wide[:, 64 + v:1024].any() and not wide[:, 1024 + v:].any()
+
+
+def test_two_streams_with_a_holder_each():
+    args = [draw(70, 9001, B, seed=i) for i in (1, 2)]
+    ops = [TokenScores(70, 9001, 5, B) for _ in args]
+
+    def step(o, a, s=None):
+        return (*o.forward(a[0], a[1], stream=s), o.backward(*a, stream=s))
+
+    want = [[t.clone() for t in step(o, a)] for o, a in zip(ops, args)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in args]
+    for _ in range(8):
+        got = [step(o, a, s) for o, a, s in zip(ops, args, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for g, v in zip(got, want) for p, q in zip(g, v))
+
+
+@pytest.mark.parametrize("vocab", [100, 5000, 90000])
+@pytest.mark.parametrize("rows", [2, 300])
+@pytest.mark.parametrize("dtype", [B, F])
+def test_same_scores_however_a_row_lies(vocab, rows, dtype):
+    """Rows on other boundaries, with neighbours that must not be read: the same entries, and scores to rounding."""
+    z, token, dl, dh = draw(rows, vocab, dtype)
+    op = TokenScores(rows, vocab, 8, dtype)
+    want = [t.clone() for t in op.forward(z, token)]
+    grad = op.backward(z, token, dl, dh).clone()
+    wide = torch.full((rows, vocab + 11), math.nan, device="cuda", dtype=dtype)
+    y = wide[:, :vocab]
+    y.copy_(z)
+    got = op.forward(y, token)
+    assert torch.equal(got[2], want[2])
+    for i in (0, 1, 3):
+        torch.testing.assert_close(got[i], want[i], rtol=2e-6, atol=2e-6 * math.log(vocab + 1))
+    torch.testing.assert_close(op.backward(y, token, dl, dh), grad, rtol=2.0 ** -7 if dtype == B else 1e-5, atol=1e-6)
+
+
 def test_gradients_against_differences():
     z, token, dl, dh = draw(3, 12, F, std=1.0)
     op = TokenScores(3, 12, 0, F, 4, 0.8)
