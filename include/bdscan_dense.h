@@ -198,13 +198,13 @@ int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const voi
  * likeliest (places left over hold -1 and minus infinity), and as a token have
  * logp minus infinity. A row without any other entry has entropy 0, no likeliest
  * entries and no gradient. A row whose token is outside 0 .. vocab - 1 does not
- * count: its logits are not read, logp, entropy, stats and gradient are 0, and
- * it has no likeliest entries. A row with NaN or plus infinity at an entry that
+ * count: its logits are not read, logp, entropy and gradient are 0, and it has
+ * no likeliest entries. A row with NaN or plus infinity at an entry that
  * is not excluded has NaN everywhere and -1 for the likeliest entries.
  * Layouts: logits [rows][vocab] (row stride ld_logits) and dlogits (ld_dlogits)
  * of `dtype` (f32 or bf16); token [rows] int64; stats [rows][2]: the largest
  * logit and the logarithm of the sum of exponentials relative to it, which the
- * backward reads. Everything else fp32, top_ids int64. top 0 .. 64, temperature
+ * backward reads (minus infinity first: no gradient). Everything else fp32, top_ids int64. top 0 .. 64, temperature
  * 2^-20 .. 2^20. No workspace. */
 typedef struct bdscan_token_scores_dims {
   int64_t rows;

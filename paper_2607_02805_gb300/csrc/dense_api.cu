@@ -538,6 +538,10 @@ int check_gated(const bdscan_gated_linear_dims* d, Gated* l, const char* fn) {
   l->pieces = d->dtype == BDSCAN_F32 ? 3 : 1;
   return BDSCAN_OK;
 }
+// Rows up to which a forward streams the weights once, a warp per column of both projections. The product is faster from
+// three rows on where its operands need no packing (832 -> 3328 bf16: 4 rows 7.2 us, 8 rows 14.6, by the product 5.5;
+// fp32, whose operands are packed: 8 rows 9.8, by the product 23.7).
+int64_t gated_vec_rows(const Gated& l) { return in_place(l.dtype, l.ld_x) && in_place(l.dtype, l.K) ? 2 : kVecRows; }
 // A tile has the same columns of both projections, in units of 32.
 Plan plan_gated(const Gated& l) { return plan(l.T, 2 * l.F, l.K, l.pieces, false, false, 0, 0, 64); }
 
@@ -548,7 +552,7 @@ struct GatedFwdWs {
 GatedFwdWs gated_fwd_ws(const Gated& l) {
   GatedFwdWs w;
   memset(&w, 0, sizeof(w));
-  if (l.T <= kVecRows) return w;
+  if (l.T <= gated_vec_rows(l)) return w;
   w.q = plan_gated(l);
   if (!in_place(l.dtype, l.ld_x)) w.w = packed_bytes(l.dtype, l.T, l.K);
   w.total = w.w + (in_place(l.dtype, l.K) ? 0 : packed_bytes(l.dtype, 2 * l.F, l.K));
@@ -1114,7 +1118,7 @@ int bdscan_gated_linear_forward(const bdscan_gated_linear_dims* dims, const void
   DENSE_REQ(y, fn, "y");
   cudaStream_t s = (cudaStream_t)stream;
   const int f32 = l.dtype == BDSCAN_F32;
-  if (l.T <= kVecRows) {
+  if (l.T <= gated_vec_rows(l)) {
     VecParams v{};
     v.x = x, v.w = w, v.bias = bias, v.y = y;
     v.ld_x = l.ld_x, v.ld_y = l.ld_y;

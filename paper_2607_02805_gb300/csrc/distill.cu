@@ -297,9 +297,13 @@ cudaError_t launch_distill_grad(const DistillParams& p, cudaStream_t s) {
 namespace {
 template <typename T, bool VEC>
 void join_t(const DistillParams& p, cudaStream_t s) {
-  // 8192 of 16384 rows, 32 entries of 832 bf16: a CTA per row 145 us, two warps 111, one 97
-  if (p.rows >= 2048) launch_pdl(k_distill_join<T, VEC, 1>, dim3((unsigned)((p.rows + 7) / 8)), dim3(kThreads), 0, s, p);
-  else launch_pdl(k_distill_join<T, VEC, 8>, dim3((unsigned)p.rows), dim3(kThreads), 0, s, p);
+  // 8192 of 16384 rows, 32 entries of 832 bf16: a CTA per row 145 us, two warps 111, one 97; 2048 rows, 16 entries: 18 by
+  // CTAs, 14 by warps; 1024 rows 11 and 12. A warp takes four entries in turn, so that it needs the more rows beside it
+  // the more entries.
+  if (p.rows >= 2048 && p.rows >= 64 * p.top)
+    launch_pdl(k_distill_join<T, VEC, 1>, dim3((unsigned)((p.rows + 7) / 8)), dim3(kThreads), 0, s, p);
+  else
+    launch_pdl(k_distill_join<T, VEC, 8>, dim3((unsigned)p.rows), dim3(kThreads), 0, s, p);
 }
 }  // namespace
 cudaError_t launch_distill_join(const DistillParams& p, int f32, cudaStream_t s) {

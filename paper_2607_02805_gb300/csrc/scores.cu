@@ -355,7 +355,7 @@ __device__ __forceinline__ void out_none(const ScoresParams& p, int64_t row, int
   if (t == 0) {
     if (p.logp != nullptr) p.logp[row] = 0.f;
     if (p.entropy != nullptr) p.entropy[row] = 0.f;
-    if (p.stats != nullptr) p.stats[row] = make_float2(0.f, 0.f);
+    if (p.stats != nullptr) p.stats[row] = make_float2(-INFINITY, 0.f);  // as of a row without entries: no gradient
   }
   for (int i = t; i < p.top; i += n) {
     p.top_ids[row * p.top + i] = -1;

@@ -202,11 +202,23 @@ def test_rows_that_do_not_count(vocab, rows):
     for r in (1, 3, 4):
         assert logp[r] == 0 and entropy[r] == 0 and (ids[r] == -1).all() and (best[r] == -math.inf).all()
         assert not dz[r].any()
+    # nor have they one where the gradient is of the entropy alone and the tokens are not given again
+    alone = op.backward(z, None, None, dh)
+    assert not alone[[1, 3, 4]].any() and torch.isfinite(alone).all()
+    dz = op.backward(z, token, dl, dh)
     keep = torch.tensor([i for i in range(rows) if i not in (1, 3, 4)], device="cuda")
     part = TokenScores(len(keep), vocab, 3, F)
     want = [t.clone() for t in part.forward(z[keep], token[keep])] + [part.backward(z[keep], token[keep], dl[keep], dh[keep])]
     for a, b in zip((logp, entropy, ids, best, dz), want):
         torch.testing.assert_close(a[keep], b, rtol=1e-5, atol=1e-6)
+
+
+def test_no_rows():
+    op = TokenScores(0, 50, 3)
+    z, token = torch.zeros(0, 50, device="cuda", dtype=B), torch.zeros(0, device="cuda", dtype=torch.int64)
+    logp, entropy, ids, best = op.forward(z, token)
+    assert logp.shape == entropy.shape == (0,) and ids.shape == best.shape == (0, 3)
+    assert op.backward(z, token, logp, entropy).shape == (0, 50)
 
 
 def test_gradient_in_place_and_alone():
