@@ -37,7 +37,6 @@ namespace {
 
 constexpr int kMaxTop = 64;
 constexpr int kGroups = 128;
-constexpr int kTakeOff = 32;   // up to so many places one warp finds the bound
 constexpr int kList = 512;     // entries of a CTA's list; eight CTAs' kMaxTop each
 constexpr int kMaxParts = 8;   // CTAs of a row's cluster
 constexpr int kNone = 1 << 30; // stands for the index of a place without an entry, another for each place
@@ -367,6 +366,23 @@ __device__ __forceinline__ void out_none(const ScoresParams& p, int64_t row, int
 template <int THREADS, typename F>
 __device__ __forceinline__ void rank_list(const float* lv, const int* li, int n, int top, F emit) {
   const int t = threadIdx.x % THREADS;
+  if (THREADS >= 128 && 2 * n <= THREADS) {  // a short list: four or two lanes of a warp per entry
+    const int lanes = 4 * n <= THREADS ? 4 : 2, i = t / lanes;
+    float v = 0.f;
+    int at = 0, rank = 0;
+    if (i < n) {
+      v = lv[i], at = li[i];
+#pragma unroll 4
+      for (int j = t % lanes; j < n; j += lanes) rank += before(lv[j], li[j], v, at) ? 1 : 0;
+    }
+    __syncwarp();
+    rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+    const int more = __shfl_xor_sync(0xffffffffu, rank, 2);
+    if (lanes == 4) rank += more;
+    if (i < n && t % lanes == 0 && rank < top) emit(rank, v, at);
+    for (int k = n + t; k < top; k += THREADS) emit(k, -INFINITY, kNone);
+    return;
+  }
   for (int i = t; i < n; i += THREADS) {
     const float v = lv[i];
     const int at = li[i];
@@ -380,7 +396,7 @@ __device__ __forceinline__ void rank_list(const float* lv, const int* li, int n,
 }
 
 template <typename T, int THREADS, bool CLUSTER>
-__global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_scores(const ScoresParams p) {
+__global__ void __launch_bounds__(THREADS, CLUSTER ? 512 / THREADS : 1536 / THREADS) k_scores(const ScoresParams p) {
   pdl_sync();
   constexpr int E = Vec<T>::E, U = 4, W = THREADS / 32;
   __shared__ ScoresSmem<THREADS> sm;
@@ -412,9 +428,28 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_scores(const Scores
     };
   };
   Stat a = {-INFINITY, 0.f, 0.f};
-  for_entries<T, THREADS, U>(
-      r, part, parts, p.excluded, [&](float v, int) { stat_add(a, v, c); },
-      [&](const auto& q, int) { stat_add(a, q, c); });
+  // a part of a row that is shared fits the threads' registers mostly: it is not read again then
+  constexpr int NR = CLUSTER ? 8 : 1;
+  Vec<T> held[NR];
+  const bool hold = CLUSTER && r.begin(part + 1, parts) - r.begin(part, parts) <= NR * THREADS;
+  if (hold) {
+    const int begin = r.begin(part, parts) + t, end = r.begin(part + 1, parts);
+#pragma unroll
+    for (int j = 0; j < NR; ++j) {
+      if (begin + j * THREADS < end) held[j].load(r.group(begin + j * THREADS));
+      else held[j].none();
+    }
+#pragma unroll
+    for (int j = 0; j < NR; ++j) r.exclude(held[j], begin + j * THREADS, p.excluded);
+    stat_add(a, held, c);
+    if (part == 0 && t < r.lead && t != p.excluded) stat_add(a, cvt(r.at[t]), c);
+    const int last = r.lead + r.n * E + t;
+    if (part == parts - 1 && t < r.tail && last != p.excluded) stat_add(a, cvt(r.at[last]), c);
+  } else {
+    for_entries<T, THREADS, U>(
+        r, part, parts, p.excluded, [&](float v, int) { stat_add(a, v, c); },
+        [&](const auto& q, int) { stat_add(a, q, c); });
+  }
 
   // the groups' maxima, then the CTA's
   constexpr int G = THREADS / kGroups;  // threads of a group
@@ -430,7 +465,9 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_scores(const Scores
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   // The bound, the top-th largest of the groups' maxima. For few places one warp takes the maxima off, while the others
   // wait (issue slots are what many rows share); for many a thread per group counts those above its own, and the bound is
-  // the smallest that fewer than `top` exceed.
+  // the smallest that fewer than `top` exceed. A row that several CTAs share has the SMs to itself, and the count is
+  // sooner done (16 entries of one row: 7.9 us by taking off).
+  constexpr int kTakeOff = CLUSTER ? 4 : 32;
   if (p.top > 0 && p.top <= kTakeOff) {
     if (w == 0) {
       const float four[4] = {g4.x, g4.y, g4.z, g4.w};
@@ -469,33 +506,46 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_scores(const Scores
         if (to < kList) sm.lv[to] = v, sm.li[to] = at;
       }
     };
-    // the groups that reach it, listed in any order; all threads share their entries (a warp those of its own groups:
-    // 16384 x 50304 with 16 entries 327 us, 2048 x 131072 fp32 211; so 316 and 189)
-    if (t < kGroups && sm.gmax[t] >= tau && sm.gmax[t] != -INFINITY) sm.sel[atomicAdd(&sm.selected, 1)] = t;
-    __syncthreads();
-    const int begin = r.begin(part, parts), end = r.begin(part + 1, parts), ns = sm.selected;
-    const int per = (end - begin + THREADS - 1) / THREADS * G;  // 16-byte groups of each, the last ones past the end
-    int k = per > 0 ? t / per : ns, e = t - k * per;  // group and its e-th
-    const int dk = per > 0 ? THREADS / per : 0, de = THREADS - dk * per;
-    while (k < ns) {
-      Vec<T> q[U];
-      int at[U];
+    if (hold) {
+      const int begin = r.begin(part, parts) + t;
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
-        at[j] = k < ns ? begin + sm.sel[k] * G + e % G + e / G * THREADS : end;
-        if (at[j] < end) q[j].load(r.group(at[j]));
-        k += dk, e += de;
-        if (e >= per) e -= per, ++k;
-      }
-#pragma unroll
-      for (int j = 0; j < U; ++j) {
-        if (at[j] >= end) continue;
-        r.exclude(q[j], at[j], p.excluded);
-        const Vec<T> one[1] = {q[j]};
+      for (int j = 0; j < NR; ++j) {
+        const Vec<T> one[1] = {held[j]};
         if (vec_max(one) < tau) continue;
-        for (uint32_t hit = q[j].reach(tau); hit != 0; hit &= hit - 1) {
-          const int i = r.first(at[j]) + __ffs(hit) - 1;
+        for (uint32_t hit = held[j].reach(tau); hit != 0; hit &= hit - 1) {
+          const int i = r.first(begin + j * THREADS) + __ffs(hit) - 1;
           keep(cvt(r.at[i]), i);
+        }
+      }
+    } else {
+      // the groups that reach it, listed in any order; all threads share their entries (a warp those of its own groups:
+      // 16384 x 50304 with 16 entries 327 us, 2048 x 131072 fp32 211; so 316 and 189, by the rest of that time)
+      if (t < kGroups && sm.gmax[t] >= tau && sm.gmax[t] != -INFINITY) sm.sel[atomicAdd(&sm.selected, 1)] = t;
+      __syncthreads();
+      const int begin = r.begin(part, parts), end = r.begin(part + 1, parts), ns = sm.selected;
+      const int per = (end - begin + THREADS - 1) / THREADS * G;  // 16-byte groups of each, the last ones past the end
+      int k = per > 0 ? t / per : ns, e = t - k * per;  // group and its e-th
+      const int dk = per > 0 ? THREADS / per : 0, de = THREADS - dk * per;
+      while (k < ns) {
+        Vec<T> q[U];
+        int at[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+          at[j] = k < ns ? begin + sm.sel[k] * G + e % G + e / G * THREADS : end;
+          if (at[j] < end) q[j].load(r.group(at[j]));
+          k += dk, e += de;
+          if (e >= per) e -= per, ++k;
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+          if (at[j] >= end) continue;
+          r.exclude(q[j], at[j], p.excluded);
+          const Vec<T> one[1] = {q[j]};
+          if (vec_max(one) < tau) continue;
+          for (uint32_t hit = q[j].reach(tau); hit != 0; hit &= hit - 1) {
+            const int i = r.first(at[j]) + __ffs(hit) - 1;
+            keep(cvt(r.at[i]), i);
+          }
         }
       }
     }
