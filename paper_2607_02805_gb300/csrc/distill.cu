@@ -177,7 +177,8 @@ __device__ __forceinline__ void dot_rows(float (&s)[J], const T* a, const T* con
       const uint4 u = *reinterpret_cast<const uint4*>(a + i);
       uint4 v[J];
 #pragma unroll
-      for (int j = 0; j < J; ++j) v[j] = b[j] != nullptr ? *reinterpret_cast<const uint4*>(b[j] + i) : make_uint4(0, 0, 0, 0);
+      for (int j = 0; j < J; ++j)
+        v[j] = b[j] != nullptr ? *reinterpret_cast<const uint4*>(b[j] + i) : make_uint4(0, 0, 0, 0);
       const T* x = reinterpret_cast<const T*>(&u);
 #pragma unroll
       for (int j = 0; j < J; ++j) {
@@ -297,9 +298,9 @@ cudaError_t launch_distill_grad(const DistillParams& p, cudaStream_t s) {
 namespace {
 template <typename T, bool VEC>
 void join_t(const DistillParams& p, cudaStream_t s) {
-  // 8192 of 16384 rows, 32 entries of 832 bf16: a CTA per row 145 us, two warps 111, one 97; 2048 rows, 16 entries: 18 by
-  // CTAs, 14 by warps; 1024 rows 11 and 12. A warp takes four entries in turn, so that it needs the more rows beside it
-  // the more entries.
+  // 8192 of 16384 rows, 32 entries of 832 bf16: a CTA per row 145 us, two warps 111, one 97; 2048 rows, 16 entries: 18
+  // by CTAs, 14 by warps; 1024 rows 11 and 12. A warp takes four entries in turn, so that it needs the more rows beside
+  // it the more entries.
   if (p.rows >= 2048 && p.rows >= 64 * p.top)
     launch_pdl(k_distill_join<T, VEC, 1>, dim3((unsigned)((p.rows + 7) / 8)), dim3(kThreads), 0, s, p);
   else

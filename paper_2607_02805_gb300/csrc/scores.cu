@@ -464,9 +464,9 @@ __global__ void __launch_bounds__(THREADS, CLUSTER ? 512 / THREADS : 1536 / THRE
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   // The bound, the top-th largest of the groups' maxima. For few places one warp takes the maxima off, while the others
-  // wait (issue slots are what many rows share); for many a thread per group counts those above its own, and the bound is
-  // the smallest that fewer than `top` exceed. A row that several CTAs share has the SMs to itself, and the count is
-  // sooner done (16 entries of one row: 7.9 us by taking off).
+  // wait (issue slots are what many rows share); for many a thread per group counts those above its own, and the bound
+  // is the smallest that fewer than `top` exceed. A row that several CTAs share has the SMs to itself, and the count is
+  // sooner done (16 entries of one row 7.4 us, by taking off 7.9).
   constexpr int kTakeOff = CLUSTER ? 4 : 32;
   if (p.top > 0 && p.top <= kTakeOff) {
     if (w == 0) {
@@ -618,11 +618,30 @@ __global__ void __launch_bounds__(THREADS, CLUSTER ? 512 / THREADS : 1536 / THRE
   const RowOut out(p, row, a);
   if (t == 0) out.scores(a, zt);
   if (p.top > 0) {
-    // the parts' lists again as one (searching the other lists by halving instead: a few percent more for 16 entries of
-    // one row, a quarter less for 64)
-    const float* lv = CLUSTER ? sm.pv : sm.lv;
-    const int* li = CLUSTER ? sm.pi : sm.li;
-    rank_list<THREADS>(lv, li, CLUSTER ? parts * p.top : n, p.top, [&](int k, float v, int at) { out.place(k, v, at); });
+    const float* lv = sm.lv;
+    const int* li = sm.li;
+    if constexpr (CLUSTER) {
+      // The parts' lists again as one. Of long ones first those that reach a bound: as many of each list as add up to
+      // `top` do (one row, 64 entries: 24 us ranking all 512).
+      lv = sm.pv, li = sm.pi;
+      n = parts * p.top;
+      if (n > 128) {
+        const int deep = (p.top + parts - 1) / parts - 1;
+        float tau = sm.pv[deep];
+        for (int q = 1; q < parts; ++q) tau = fminf(tau, sm.pv[q * p.top + deep]);
+        if (t == 0) sm.count = 0;
+        __syncthreads();
+        for (int x = t; x < n; x += THREADS) {
+          if (!(sm.pv[x] >= tau) || sm.pv[x] == -INFINITY) continue;
+          const int to = atomicAdd(&sm.count, 1);
+          sm.lv[to] = sm.pv[x], sm.li[to] = sm.pi[x];
+        }
+        __syncthreads();
+        lv = sm.lv, li = sm.li;
+        n = sm.count;
+      }
+    }
+    rank_list<THREADS>(lv, li, n, p.top, [&](int k, float v, int at) { out.place(k, v, at); });
   }
 }
 
@@ -807,8 +826,11 @@ __global__ void __launch_bounds__(256, 6) k_scores_bwd(const ScoresParams p) {
   const int a = r.begin(part, p.parts), b = r.begin(part + 1, p.parts);
   auto store = [&](int i, const float (&g)[E]) {
     uint4 u;
-    if constexpr (E == 4) u = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
-    else u = make_uint4(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[E / 2], g[E / 2 + 1]), pack_bf16(g[E - 2], g[E - 1]));
+    if constexpr (E == 4)
+      u = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
+    else
+      u = make_uint4(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[E / 2], g[E / 2 + 1]),
+                     pack_bf16(g[E - 2], g[E - 1]));
     *reinterpret_cast<uint4*>(out + r.first(i)) = u;
   };
   if (!counts) {
@@ -838,7 +860,8 @@ __global__ void __launch_bounds__(256, 6) k_scores_bwd(const ScoresParams p) {
         for (int k = 0; k < E / 2; ++k) {
           const float2 v = q[j].two(k);
           const float2 d = halves(fma2(add2(pair(v.x, v.y), rr), cc, ll));
-          const float2 e = halves(mul2(pair(ex2(d.x), ex2(d.y)), fma2(pair(fmaxf(d.x, -200.f), fmaxf(d.y, -200.f)), ss, bb)));
+          const f32x2 by = fma2(pair(fmaxf(d.x, -200.f), fmaxf(d.y, -200.f)), ss, bb);
+          const float2 e = halves(mul2(pair(ex2(d.x), ex2(d.y)), by));
           g[2 * k] = e.x, g[2 * k + 1] = e.y;
         }
         const int at = r.first(i + j * THREADS);
