@@ -104,7 +104,8 @@ __device__ __forceinline__ void rows_out(void* out, int64_t ld, int64_t m, int64
       float part[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) part[i] = PIECES == 1 ? y[i] : bf16_part(y[i]);
-      store_rows<F32>(static_cast<bf16*>(out) + k * plane, row, ld, at + col + cl, (int)min((int64_t)32, m - row), part);
+      const int left = (int)min((int64_t)32, m - row);
+      store_rows<F32>(static_cast<bf16*>(out) + k * plane, row, ld, at + col + cl, left, part);
 #pragma unroll
       for (int i = 0; i < 16; ++i) y[i] -= part[i];
     }
@@ -151,8 +152,9 @@ __device__ __forceinline__ void unit_put(unsigned char* unit, int hf, const floa
                    pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
 }
 template <int CG, int BN, int NP, int EPI, int NA, typename SCHED>
-__device__ __forceinline__ bool gate_epilogue(const GemmParams& p, const GemmMaps& maps, const SCHED& sched, uint32_t tm,
-                                              unsigned char* stage, uint64_t* accfull, uint64_t* accempty, int rank) {
+__device__ __forceinline__ bool gate_epilogue(const GemmParams& p, const GemmMaps& maps, const SCHED& sched,
+                                              uint32_t tm, unsigned char* stage, uint64_t* accfull, uint64_t* accempty,
+                                              int rank) {
   using S = GemmSmem<CG, BN, NP, EPI>;
   constexpr bool FLUSH = NP == 3, F32 = NP == 3;
   constexpr bool DZ = EPI == kEpiGateDz || EPI == kEpiGateDzRows;

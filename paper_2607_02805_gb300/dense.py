@@ -2,12 +2,13 @@
 (include/bdscan_dense.h) from PyTorch.
 
 PyTorch provides the device memory and the stream; every step of the
-computation runs in libbdscan through ``binding``. A ``Linear``, ``GatedLinear``,
-``LmLoss``, ``DistillLoss`` or ``TokenScores`` holds one size's outputs, saved pre-activations, gradients and workspaces; the
-inputs and weights belong to the caller. What a call returns are the holder's
-buffers, valid until its next call; a holder serves one stream at a time, and
-its buffers stay where they are for its life, so that a CUDA graph of its calls
-can be replayed as long as it lives.
+computation runs in libbdscan through ``binding``. A ``Linear``,
+``GatedLinear``, ``LmLoss``, ``DistillLoss`` or ``TokenScores`` holds one
+size's outputs, saved pre-activations, gradients and workspaces; the inputs and
+weights belong to the caller. What a call returns are the holder's buffers,
+valid until its next call; a holder serves one stream at a time, and its
+buffers stay where they are for its life, so that a CUDA graph of its calls can
+be replayed as long as it lives.
 """
 
 from __future__ import annotations

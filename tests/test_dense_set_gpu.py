@@ -103,7 +103,8 @@ def test_functions_of_the_binding():
 
     h, head = draw(100, 72), draw(300, 72, std=0.2)
     d = binding.make_distill_loss_dims(100, 72, 300, 4, excluded=299, temperature=1.1)
-    loss, lse, zs, dh, dhead = empty(100, dtype=F), empty(100, dtype=F), empty(100, 4, dtype=F), empty(100, 72), empty(300, 72)
+    loss, lse, zs = empty(100, dtype=F), empty(100, dtype=F), empty(100, 4, dtype=F)
+    dh, dhead = empty(100, 72), empty(300, 72)
     binding.distill_loss_forward(d, h, head, ids, best, None, loss, lse, zs,
                                  space(binding.bdscan_distill_loss_forward_workspace_size(d)))
     binding.distill_loss_backward(d, h, head, ids, best, None, lse, zs, None, dh, dhead,

@@ -141,7 +141,7 @@ def test_options():
 
 @pytest.mark.parametrize("dtype", [B, F])
 def test_entries_that_are_not_known(dtype):
-    """Ids outside the vocabulary, the excluded one, logits of minus infinity; rows without any; rows with hidden garbage."""
+    """Ids outside the vocabulary, the excluded one, logits of minus infinity; rows without any, with hidden garbage."""
     h, w, ids, teacher, weight, dloss = case(60, 64, 300, 4, dtype, counted=1.0, ragged=False)
     ids[0] = -1
     ids[1] = torch.tensor([300, -7, 2 ** 40, -2 ** 40], device="cuda")
@@ -370,7 +370,8 @@ def test_teacher_to_student():
     logits = torch.randn(t, v, generator=g, device="cuda") * 3
     weight = (torch.rand(t, generator=g, device="cuda") < 0.5).float() / t
     _, _, ids, best = TokenScores(t, v, top, F, v - 1).forward(logits)
-    block, down, loss = GatedLinear(t, k, n, "silu", F), Linear(t, n, k, dtype=F), DistillLoss(t, k, v, top, F, v - 1, 2.0)
+    block, down = GatedLinear(t, k, n, "silu", F), Linear(t, n, k, dtype=F)
+    loss = DistillLoss(t, k, v, top, F, v - 1, 2.0)
     a = block.forward(x, wg)
     h = down.forward(a, wd, residual=x)
     per_row, _ = loss.forward(h, head, ids, best, weight)

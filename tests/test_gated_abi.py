@@ -120,8 +120,8 @@ def test_holder_refuses(monkeypatch):
 def test_waits_of_the_epilogue_are_bounded():
     """By reading: no loop around a poll without a limit, no barrier that would wait for a warp that has given up, and
     every way out of the loop over tiles says whether one has."""
-    code = re.sub(r"//[^\n]*", "", open(os.path.join(os.path.dirname(HEADER), os.pardir, "paper_2607_02805_gb300", "csrc",
-                                                     "gemm_gate.cuh")).read())
+    root = os.path.dirname(os.path.dirname(HEADER))
+    code = re.sub(r"//[^\n]*", "", open(os.path.join(root, "paper_2607_02805_gb300", "csrc", "gemm_gate.cuh")).read())
     assert "try_wait" not in code and "bar.sync" not in code and "__syncthreads" not in code
     assert not re.search(r"while\s*\(", code) and not re.search(r"for\s*\(\s*;\s*;", code)
     assert code.count("warp_wait(") == 2 and "if (!ok) break;" in code and "return ok;" in code

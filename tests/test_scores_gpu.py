@@ -208,7 +208,8 @@ def test_rows_that_do_not_count(vocab, rows):
     dz = op.backward(z, token, dl, dh)
     keep = torch.tensor([i for i in range(rows) if i not in (1, 3, 4)], device="cuda")
     part = TokenScores(len(keep), vocab, 3, F)
-    want = [t.clone() for t in part.forward(z[keep], token[keep])] + [part.backward(z[keep], token[keep], dl[keep], dh[keep])]
+    want = [t.clone() for t in part.forward(z[keep], token[keep])]
+    want.append(part.backward(z[keep], token[keep], dl[keep], dh[keep]))
     for a, b in zip((logp, entropy, ids, best, dz), want):
         torch.testing.assert_close(a[keep], b, rtol=1e-5, atol=1e-6)
 
@@ -245,7 +246,7 @@ def test_offsets_past_32_bits():
     got = [x.clone() for x in op.forward(z, token)]
     dl = torch.randn(t, device="cuda")
     dz = op.backward(z, token, dl, out=wide[:, 1024:1024 + v])
-    # the copy's rows lie on other boundaries, so that sums add up in another order: each side is off by the bounds above
+    # the copy's rows lie on other boundaries, and sums add up in another order: each side is off by the bounds above
     same = TokenScores(t, v, 3, B)
     close = z.contiguous()
     want = same.forward(close, token)
