@@ -154,10 +154,11 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
  * student's p_t = softmax(h w^T / temperature) over the whole vocabulary from the
  * teacher's q_t = softmax(teacher[t] / temperature) over the row's known entries:
  * those whose id is inside 0 .. vocab - 1 and not `excluded`, with a teacher's
- * logit above minus infinity. An id that comes twice has both shares. lse[t] = log sum_v exp(z[t][v] /
- * temperature). A row counts where its weight is not zero and an entry is known;
- * the others get loss = lse = 0 and no gradient, whatever h holds there, and cost
- * no product. `excluded` as in the vocabulary loss.
+ * logit above minus infinity. An id that comes twice has both shares.
+ * lse[t] = log sum_v exp(z[t][v] / temperature). A row counts where its weight is
+ * not zero and an entry is known; the others get loss = lse = 0 and no gradient,
+ * whatever h holds there, and cost no product. `excluded` as in the vocabulary
+ * loss.
  * Layouts: h, w, weight, loss, lse, dloss as in the vocabulary loss; ids
  * [rows][top] int64, teacher [rows][top] fp32, top 1 .. 64; z [rows][top] fp32
  * receives h w^T at the known entries of the rows that count, else 0, which the
@@ -204,8 +205,8 @@ int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const voi
  * Layouts: logits [rows][vocab] (row stride ld_logits) and dlogits (ld_dlogits)
  * of `dtype` (f32 or bf16); token [rows] int64; stats [rows][2]: the largest
  * logit and the logarithm of the sum of exponentials relative to it, which the
- * backward reads (minus infinity first: no gradient). Everything else fp32, top_ids int64. top 0 .. 64, temperature
- * 2^-20 .. 2^20. No workspace. */
+ * backward reads (minus infinity first: no gradient). Everything else fp32,
+ * top_ids int64. top 0 .. 64, temperature 2^-20 .. 2^20. No workspace. */
 typedef struct bdscan_token_scores_dims {
   int64_t rows;
   int64_t vocab;
@@ -226,7 +227,7 @@ int bdscan_token_scores_forward(const bdscan_token_scores_dims* dims, const void
 /* dlogits: gradient of <dlogp, logp> + <dentropy, entropy> at the logits. dlogp
  * and dentropy are nullable (zero); token is the forward's, nullable where dlogp
  * is; stats and entropy (read where dentropy is given) are the forward's.
- * dlogits may be the logits themselves (same stride). */
+ * dlogits may be the logits themselves; another stride is then refused. */
 int bdscan_token_scores_backward(const bdscan_token_scores_dims* dims, const void* logits, const int64_t* token,
                                  const float* stats, const float* entropy, const float* dlogp, const float* dentropy,
                                  void* dlogits, void* stream);

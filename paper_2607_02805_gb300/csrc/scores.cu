@@ -1037,6 +1037,8 @@ int bdscan_token_scores_backward(const bdscan_token_scores_dims* dims, const voi
   if (dlogp != nullptr && token == nullptr) return fail(BDSCAN_ERR_ARG, fn, "dlogp without token");
   if (dentropy != nullptr) SCORES_REQ(entropy, fn, "entropy");
   SCORES_REQ(dlogits, fn, "dlogits");
+  if (dlogits == logits && p.rows > 1 && p.ld != p.ld_out)
+    return fail(BDSCAN_ERR_ARG, fn, "dlogits is logits, with another row stride");
   p.logits = logits;
   p.token = token;
   p.stats_in = (const float2*)stats;

@@ -77,6 +77,8 @@ def test_refuses_bad_pointers():
                     (dict(dl=FAKE + 4), "dlogp is not"), (dict(dh=FAKE + 4), "dentropy is not"),
                     (dict(dz=None), "dlogits is NULL")):
         assert _bwd(d, **kw) == b.BDSCAN_ERR_ARG and msg in b.bdscan_last_error(), kw
+    # in place, rows that would be written before they are read
+    assert _bwd(_dims(ld_dlogits=104)) == b.BDSCAN_ERR_ARG and "another row stride" in b.bdscan_last_error()
     # no rows: no pointer is looked at
     assert _fwd(_dims(rows=0), *[None] * 7) == b.BDSCAN_OK and _bwd(_dims(rows=0), *[None] * 7) == b.BDSCAN_OK
 
