@@ -204,7 +204,13 @@ struct DistillParams {
   __nv_bfloat16* dz;
   int64_t ld_dz, plane, dz_extent;
   int v0, n, pieces;
+  // launch_distill_dw: that piece's gradient at the logits as the products read it, the slots' scales, and dw
+  const float* gscale;
+  void* dw;
 };
+constexpr int kFewRows = 16;      // rows that count, up to which launch_distill_dw writes
+constexpr int kFewRowsCall = 128; // rows up to which it is launched
+cudaError_t launch_distill_dw(const DistillParams& p, cudaStream_t s);
 cudaError_t launch_distill_grad(const DistillParams& p, cudaStream_t s);
 cudaError_t launch_distill_join(const DistillParams& p, int f32, cudaStream_t s);
 cudaError_t launch_distill_dz(const DistillParams& p, cudaStream_t s);

@@ -780,10 +780,10 @@ GemmParams stats_params(const Loss& l, const LossFwdWs& ws, const LossRowsParams
 
 // The backward, piece by piece of the vocabulary: the gradient at the logits
 // (p - 1 at the target, as the epilogue leaves it; `mend(v0, n, dz)` may launch
-// what changes it), then both products.
-template <typename F>
+// what changes it), then both products and what `settle(v0, n, dz)` launches.
+template <typename F, typename G>
 cudaError_t loss_backward(const Loss& l, const LossBwdWs& ws, LossRowsParams rp, const void* h, const void* w, void* dh,
-                          void* dw, char* base, int* flag, cudaStream_t s, F mend) {
+                          void* dw, char* base, int* flag, cudaStream_t s, F mend, G settle) {
   const size_t elt = l.dtype == BDSCAN_F32 ? 4 : 2;
   rp.gscale = (float*)(base + ws.r.gscale);
   rp.lse_c = (float*)(base + ws.r.lse);
@@ -846,6 +846,7 @@ cudaError_t loss_backward(const Loss& l, const LossBwdWs& ws, LossRowsParams rp,
       if (e == cudaSuccess) e = run_out(ws.g.w, true, true, gw, dz, scaled, part, s);
       if (e == cudaSuccess) e = run_out(ws.g.x, false, true, gh, dz, bp, part, s, !last);
     }
+    if (e == cudaSuccess) e = settle(v0, n, dz);
   }
   return e;
 }
@@ -1324,8 +1325,8 @@ int bdscan_lm_loss_backward(const bdscan_lm_loss_dims* dims, const void* h, cons
   LossRowsParams rp = rows_params(l, ws.r, target, weight, base);
   rp.dloss = dloss;
   rp.lse_in = lse;
-  const cudaError_t e = loss_backward(l, ws, rp, h, w, dh, dw, base, flag, (cudaStream_t)stream,
-                                      [](int64_t, int64_t, const Operand&) { return cudaSuccess; });
+  const auto none = [](int64_t, int64_t, const Operand&) { return cudaSuccess; };
+  const cudaError_t e = loss_backward(l, ws, rp, h, w, dh, dw, base, flag, (cudaStream_t)stream, none, none);
   return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
 }
 
@@ -1439,18 +1440,32 @@ int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const voi
   cudaError_t e = api_launched(launch_distill_grad(d, s), s);
   if (e == cudaSuccess) e = find_targets(l, &rp, base + ws.total, s);
   // the epilogue takes 1 off at the row's target, which is a known entry: what is written there below covers it
+  const auto piece = [&](int64_t v0, int64_t n, const Operand& dz) {
+    DistillParams q = d;
+    q.dz = (__nv_bfloat16*)dz.base;
+    q.ld_dz = dz.ld;
+    q.plane = dz.plane;
+    q.pieces = dz.pieces;
+    q.dz_extent = dz.pieces * dz.plane;
+    q.v0 = (int)v0;
+    q.n = (int)n;
+    return q;
+  };
+  d.d_model = (int)l.K;
+  d.ld_h = l.ld_h;
+  d.h = h;
+  d.dw = dw;
+  d.gscale = (const float*)(base + ws.r.gscale);
   if (e == cudaSuccess)
-    e = loss_backward(l, ws, rp, h, w, dh, dw, base, flag, s, [&](int64_t v0, int64_t n, const Operand& dz) {
-      DistillParams q = d;
-      q.dz = (__nv_bfloat16*)dz.base;
-      q.ld_dz = dz.ld;
-      q.plane = dz.plane;
-      q.pieces = dz.pieces;
-      q.dz_extent = dz.pieces * dz.plane;
-      q.v0 = (int)v0;
-      q.n = (int)n;
-      return api_launched(launch_distill_dz(q, s), s);
-    });
+    e = loss_backward(
+        l, ws, rp, h, w, dh, dw, base, flag, s,
+        [&](int64_t v0, int64_t n, const Operand& dz) {
+          return api_launched(launch_distill_dz(piece(v0, n, dz), s), s);
+        },
+        [&](int64_t v0, int64_t n, const Operand& dz) {
+          if (l.pieces != 1 || l.T > kFewRowsCall) return cudaSuccess;
+          return api_launched(launch_distill_dw(piece(v0, n, dz), s), s);
+        });
   return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);
 }
 

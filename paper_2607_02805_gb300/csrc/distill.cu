@@ -112,11 +112,14 @@ __device__ __forceinline__ float entry_grad(const DistillParams& p, float z, flo
 //     rounded instead, by 2^-16 / 3 * 0.54 in square, element by element.
 // (With the second rounding always there, dw was off by 2.9e-3 where the plain
 // form, rounded once, is by 1.7e-3; so by 2.4e-3.)
+// Calls of a few rows have the entries' rows of dw from k_distill_dw, and only dh
+// reads their rounded gradients: there the best of a lane's factor each is taken
+// too, and what h loses does not count.
 __device__ __forceinline__ float rounding(float v) {
   const float d = __bfloat162float(__float2bfloat16_rn(v)) - v;
   return d * d;
 }
-__device__ __forceinline__ float pick_scale(const Entries& e, const float (&s)[2], float g) {
+__device__ __forceinline__ float pick_scale(const Entries& e, const float (&s)[2], float g, bool few, int top) {
   if (!isfinite(g) || g == 0.f) return 1.f;
   int exp2;
   const float mant = 2.f * frexpf(g, &exp2);
@@ -133,7 +136,20 @@ __device__ __forceinline__ float pick_scale(const Entries& e, const float (&s)[2
   for (int k = 0; k < 2; ++k)
     if (e.id[k] >= 0) err_m += rounding(s[k] * mant), err_1 += rounding(s[k] * one);
   err_m = warp_sum(err_m) / (mant * mant);
-  err_1 = warp_sum(err_1) + 0x1p-16f / 3.f * 0.54f * size;
+  err_1 = warp_sum(err_1);
+  if (few) {
+    const float mine = ex2((float)(threadIdx.x & 31) / 32.f), r = 1.f / (mine * mine);
+    float err = 0.f;
+    for (int j = 0; j < top; ++j) {
+      const float v = __shfl_sync(0xffffffffu, j < 32 ? s[0] : s[1], j & 31);  // zero where not known
+      err += rounding(v * mine) * r;
+    }
+    const float best = -warp_max(-err);
+    const float of = __shfl_sync(0xffffffffu, mine, __ffs(__ballot_sync(0xffffffffu, err == best)) - 1 & 31);
+    if (best < err_m && best < err_1) return of;
+  } else {
+    err_1 += 0x1p-16f / 3.f * 0.54f * size;
+  }
   return err_1 < err_m ? one : mant;
 }
 
@@ -157,7 +173,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_grad(const DistillParams p
 #pragma unroll
   for (int k = 0; k < 2; ++k)
     if (e.id[k] >= 0) s[k] = entry_grad(p, p.z_in[row * p.top + lane + 32 * k], lse, share[k]);
-  const float a = p.row_scale != nullptr ? pick_scale(e, s, g) : 1.f;
+  const float a = p.row_scale != nullptr ? pick_scale(e, s, g, p.rows <= kFewRows, p.top) : 1.f;
   if (lane == 0 && p.row_scale != nullptr) p.row_scale[row] = a;
 #pragma unroll
   for (int k = 0; k < 2; ++k)
@@ -289,8 +305,49 @@ __global__ void __launch_bounds__(kThreads) k_distill_dz(const DistillParams p) 
   }
 }
 
+// Where a few rows count, the rows of dw at their entries once more, from the
+// gradients before any rounding: dw[v] = sum_r g_r (p - q)_rv h_r, with what the
+// products read where v is no entry of row r. Over many rows the roundings of
+// g (p - q) and of the scaled copy of h are as likely up as down; of two rows
+// whose shares lie badly they left dw off by 2.5e-3 where the plain form is by
+// 1.7e-3. A CTA per entry; several entries of one id write the same sums.
+__global__ void __launch_bounds__(kThreads) k_distill_dw(const DistillParams p) {
+  pdl_sync();
+  __shared__ float coef[kFewRows];
+  __shared__ const bf16* rows[kFewRows];
+  static_assert(kThreads == 16 * kFewRows, "sixteen threads per row look for the entry");
+  const int count = *p.count, slot = blockIdx.x / p.top;
+  if (count > kFewRows || slot >= count) return;
+  const int64_t at = (int64_t)p.idx[slot] * p.top + blockIdx.x % p.top, id = p.ids[at], to = id - p.v0;
+  if (id < 0 || id == p.excluded || to < 0 || to >= p.n || p.teacher[at] == -INFINITY) return;
+  if (!dguard(kSiteDistill, (count - 1) * p.ld_dz + to, p.dz_extent)) return;
+  const int r = threadIdx.x / 16;
+  if (r < count && threadIdx.x % 16 == 0) {
+    coef[r] = __bfloat162float(p.dz[r * p.ld_dz + to]) * p.gscale[r];
+    rows[r] = static_cast<const bf16*>(p.h) + p.idx[r] * p.ld_h;
+  }
+  __syncthreads();
+  if (r < count)
+    for (int j = threadIdx.x % 16; j < p.top; j += 16) {
+      const int64_t x = (int64_t)p.idx[r] * p.top + j;
+      if (p.ids[x] == id && p.teacher[x] != -INFINITY) coef[r] = p.grad[x] * p.gscale[r];
+    }
+  __syncthreads();
+  bf16* out = static_cast<bf16*>(p.dw) + id * p.d_model;
+  for (int c = threadIdx.x; c < p.d_model; c += kThreads) {
+    float sum = 0.f;
+    for (int k = 0; k < count; ++k) sum = fmaf(coef[k], __bfloat162float(rows[k][c]), sum);
+    out[c] = __float2bfloat16_rn(sum);
+  }
+}
+
 }  // namespace
 
+cudaError_t launch_distill_dw(const DistillParams& p, cudaStream_t s) {
+  const int64_t slots = p.rows < kFewRows ? p.rows : kFewRows;
+  launch_pdl(k_distill_dw, dim3((unsigned)(slots * p.top)), dim3(kThreads), 0, s, p);
+  return cudaGetLastError();
+}
 cudaError_t launch_distill_grad(const DistillParams& p, cudaStream_t s) {
   launch_pdl(k_distill_grad, dim3((unsigned)((p.rows + kRowWarps - 1) / kRowWarps)), dim3(kThreads), 0, s, p);
   return cudaGetLastError();

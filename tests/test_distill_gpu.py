@@ -206,6 +206,36 @@ def test_one_entry_is_the_vocabulary_loss():
             assert ((x.double() - y.double()).abs() <= 4 * u * size + 2 * u * y.double().abs() + 1e-7).all()
 
 
+@pytest.mark.parametrize("t", [1, 2, 3, 7, 16, 17, 40, 128])
+def test_gradients_of_a_few_rows_are_rounded_once(t):
+    # Up to 16 rows count, and dw's rows at their entries are sums of at most 16 fp32 terms, rounded once: off by 2^-8
+    # of their value at most, and by the terms' own share of them. A term's p - q is off by s = (2 e(k) M + 4e-6 (1 + M))
+    # of p + q <= 2, and each sum by 16 x 2^-24; entries that are no row's own come from p rounded to bf16, 2^-8 of p, times
+    # a copy of h rounded likewise: both at most 2^-8 of the terms.
+    k, v, n = 448, 5000, 8
+    for seed in range(6):
+        h, w, ids, teacher, weight, dloss = case(t, k, v, n, B, min(1.0, 5 / t), False, 100 + seed)
+        weight[torch.nonzero(weight)[16:, 0]] = 0.0
+        op = DistillLoss(t, k, v, n)
+        op.forward(h, w, ids, teacher, weight)
+        dw = op.backward(h, w, ids, teacher, weight, dloss)[1].double().cpu()
+        hd, wd, wt = h.double().cpu(), w.double().cpu(), (weight * dloss).double().cpu()
+        z = hd @ wd.T
+        p = torch.softmax(z, 1)
+        q = torch.zeros(t, v, dtype=torch.float64)
+        q.scatter_add_(1, ids.cpu(), torch.softmax(teacher.double().cpu(), 1))
+        want = (wt[:, None] * (p - q)).T @ hd
+        m = float(z.abs().max())
+        share = 2 * (2 * e32(k) * m + 4e-6 * (1 + m)) + 16 * 2.0 ** -24
+        own = torch.zeros(t, v, dtype=torch.bool).scatter_(1, ids.cpu(), True) & (wt != 0)[:, None]
+        sizes = (wt.abs()[:, None] * (p + q)).T @ hd.abs()
+        others = (wt.abs()[:, None] * p * ~own).T @ hd.abs()
+        tol = 2.0 ** -8 * want.abs() + share * sizes + 2 * 2.0 ** -8 * others
+        at = own.any(0)
+        bad = ((dw - want).abs() - tol)[at]
+        assert not at.any() or bad.max() <= 0, (seed, float(bad.max()))
+
+
 def test_a_student_that_agrees_has_no_loss():
     """Teacher and student the same over a vocabulary of which all entries are known."""
     for dtype in (B, F):
