@@ -290,9 +290,12 @@ __device__ __forceinline__ bool gate_epilogue(const GemmParams& p, const GemmMap
           u[j] = e[j] * a;
         }
         if (p.colsum != nullptr && row0 < p.m) {
+          // Rows behind the last one add nothing: dy = 0 there is not enough, since below 128 rows their accumulators
+          // come from rows of A that no load has written, and zero times a NaN left there is NaN.
+          const bool in = row0 + lane < p.m;
           float sg[16], su[16];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) sg[j] = g[j], su[j] = u[j];
+          for (int j = 0; j < 16; ++j) sg[j] = in ? g[j] : 0.f, su[j] = in ? u[j] : 0.f;
           const float a = colsum16(sg), b = colsum16(su);
           const int c = col + (lane >> 1);
           if (c < n) p.colsum[(row0 >> 5) * p.n + c + (lane & 1) * n] = (lane & 1) ? b : a;

@@ -18,6 +18,7 @@ Tolerances (per tensor, tests/parity.py: max |err| - u |oracle| over max
 
 import math
 
+import numpy as np
 import pytest
 
 import parity
@@ -170,6 +171,30 @@ def test_values_that_are_not_finite_stay_visible(rows, dtype):
         assert torch.isfinite(y[rest]).all() and torch.isfinite(dx[rest]).all()
         assert not torch.isfinite(dx[1]).any() and not torch.isfinite(dw[:, 3]).any()
         assert not torch.isfinite(db).all()
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("n", [9728, 9731])
+@pytest.mark.parametrize("dtype", [B, F])
+def test_bias_gradient_of_a_few_rows_behind_values_that_are_not_finite(bad, n, dtype):
+    """A product of fewer than 128 rows reads whole tiles of 128, whose other rows hold what an earlier kernel left in
+    shared memory. Here that is a product of 128 rows of NaN or infinity with the same layout, on every SM (9728 columns
+    of both projections are a tile each): nothing of it comes into the sums of the rows."""
+    k = 136
+    x, w, b, dy = case(100, k, n, dtype)
+    full, dy128 = torch.full((128, k), bad, device="cuda", dtype=dtype), torch.ones(128, n, device="cuda", dtype=dtype)
+    before = GatedLinear(128, k, n, "silu", dtype)
+    for rows in (1, 5, 8, 9, 24, 33, 40, 70, 100):
+        op = GatedLinear(rows, k, n, "silu", dtype)
+        a, e = x[:rows], dy[:rows]
+        _, _, db = before.backward(full, w, dy128, b, need_dx=False, need_dw=False)
+        assert not torch.isfinite(db).any()
+        _, _, db = op.backward(a, w, e, b, need_dx=False, need_dw=False)
+        z = f64(a) @ f64(w).T + f64(b)
+        g, u, s = z[:, :n], z[:, n:], 1 / (1 + np.exp(-z[:, :n]))
+        want = np.concatenate(((f64(e) * u * s * (1 + g * (1 - s))).sum(0), (f64(e) * g * s).sum(0)))
+        assert torch.isfinite(db).all(), rows
+        close("dbias", db, want, e32(rows) + 10 * e32(k), True)
 
 
 def test_no_rows():
