@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_join(const DistillParams p
     dot_rows<T, VEC, J>(z, h, at, p.d_model);
 #pragma unroll
     for (int j = 0; j < J; ++j)
-      if (lane == j && j0 + j < p.top) zs[r][j0 + j] = z[j];
+      if (lane == j && j0 + j < p.top) zs[r][j0 + j] = at[j] != nullptr ? z[j] : 0.f;  // 0 times a NaN of h is NaN
   }
   float m = -INFINITY, s = 0.f;
   for (int k = w * 32 + lane; k < p.parts; k += 32 * WPR) stats_join(m, s, p.part[(int64_t)k * p.rows_ld + slot]);

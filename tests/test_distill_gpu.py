@@ -332,6 +332,27 @@ def test_two_streams_with_a_holder_each():
         assert all(torch.equal(p, q) for g, v in zip(got, want) for p, q in zip(g, v))
 
 
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("k,ld", [(72, 0), (72, 3), (71, 0)])
+@pytest.mark.parametrize("rows", [40, 2100])
+def test_student_logits_of_entries_that_are_not_known(rows, k, ld, dtype):
+    """Zero, also beside a NaN or an infinity in the row, whatever way the rows are read; what is known shows it."""
+    h, w, ids, teacher, weight, _ = case(rows, k, 300, 6, dtype, counted=1.0, ragged=False, ld=ld)
+    ids[3, 2], ids[3, 5], ids[4, 0], ids[5, 1:] = -1, 300, 299, -1
+    teacher[4, 3] = -math.inf
+    h[3, 1], h[4, 2], h[5, 3] = math.nan, math.inf, -math.inf
+    op = DistillLoss(rows, k, 300, 6, dtype, 299)
+    loss, _ = op.forward(h, w, ids, teacher, weight)
+    z = op._buf["z"]
+    known = (ids >= 0) & (ids < 299) & (teacher != -math.inf)
+    at = torch.tensor([3, 4, 5], device="cuda")
+    assert not z[~known].any()
+    assert not torch.isfinite(z[at][known[at]]).any() and not torch.isfinite(loss[at]).any()
+    rest = torch.ones(rows, dtype=torch.bool, device="cuda")
+    rest[at] = False
+    assert torch.isfinite(z[rest]).all() and torch.isfinite(loss[rest]).all()
+
+
 def test_no_rows():
     op = DistillLoss(0, 64, 100, 4)
     h, w = torch.zeros(0, 64, device="cuda", dtype=B), torch.ones(100, 64, device="cuda", dtype=B)
