@@ -22,7 +22,10 @@
  * memory with a caller workspace (sizes from the *_workspace_size queries; a
  * query that returns 0 for valid dims needs none, and the workspace may then
  * be NULL), asynchronous on `stream`, gradients overwritten, return codes and
- * bdscan_last_error(). A wait on tensor-core work that gives up sets the flag
+ * bdscan_last_error(). An output that shares memory with an input is refused
+ * where the two are not one operand computed in place, said so below; columns
+ * side by side in a wider buffer share none. (Not checked by the linear
+ * layer's and the vocabulary loss's backward and the loss's forward.) A wait on tensor-core work that gives up sets the flag
  * of bdscan_ssd_wait_flag(). Calls need the driver's tensor-map encoder and
  * return BDSCAN_ERR_UNSUPPORTED without it. A value that is not finite makes
  * every output that reads it non-finite (with fp32 inputs: NaN where the exact
@@ -87,7 +90,7 @@ int bdscan_linear_backward(const bdscan_linear_dims* dims, const void* x, const 
  * wg, then those of wu; bias [2 d_hidden] likewise (nullable), y
  * [rows][d_hidden] (row stride ld_y). All have `dtype` (f32 or bf16). Sums,
  * activation and product are fp32, y is rounded once. rows >= 0, d_in and
- * d_hidden >= 1. y is no input. */
+ * d_hidden >= 1. */
 typedef struct bdscan_gated_linear_dims {
   int64_t rows;
   int64_t d_in;
@@ -107,7 +110,7 @@ int bdscan_gated_linear_forward(const bdscan_gated_linear_dims* dims, const void
  * [rows][d_in], dw = dz^T x [2 d_hidden][d_in], dbias = column sums of dz
  * [2 d_hidden]. Each of dx, dw, dbias is nullable and then not computed; bias
  * is the forward's. dz enters the products rounded to `dtype` (fp32: three
- * pieces), and dbias unrounded. No output is an input. */
+ * pieces), and dbias unrounded. */
 size_t bdscan_gated_linear_backward_workspace_size(const bdscan_gated_linear_dims* dims);
 int bdscan_gated_linear_backward(const bdscan_gated_linear_dims* dims, const void* x, const void* w, const void* bias,
                                  const void* dy, void* dx, void* dw, void* dbias, void* workspace,
@@ -219,7 +222,7 @@ typedef struct bdscan_token_scores_dims {
 } bdscan_token_scores_dims;
 
 /* token and logp are nullable together, entropy and stats each, top_ids and
- * top_logp where top is 0. Outputs may not be inputs. */
+ * top_logp where top is 0. */
 int bdscan_token_scores_forward(const bdscan_token_scores_dims* dims, const void* logits, const int64_t* token,
                                 float* logp, float* entropy, float* stats, int64_t* top_ids, float* top_logp,
                                 void* stream);

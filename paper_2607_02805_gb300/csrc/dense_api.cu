@@ -8,6 +8,7 @@
 
 #include "bdscan_dense.h"
 #include "dense.cuh"
+#include "overlap.h"
 #include "params.h"
 
 namespace bds {
@@ -851,6 +852,11 @@ cudaError_t loss_backward(const Loss& l, const LossBwdWs& ws, LossRowsParams rp,
   return e;
 }
 
+// Refuses a call that would read what it writes.
+int check_apart(const char* fn, std::initializer_list<Span> reads, std::initializer_list<Span> writes) {
+  char msg[128];
+  return any_overlap(reads, writes, msg, sizeof(msg)) ? fail_msg(BDSCAN_ERR_ARG, fn, msg) : BDSCAN_OK;
+}
 int check_workspace(const void* ws, size_t have, size_t need, const char* fn) {
   if (need == 0) return BDSCAN_OK;
   DENSE_REQ(ws, fn, "workspace");
@@ -954,6 +960,16 @@ int bdscan_linear_forward(const bdscan_linear_dims* dims, const void* x, const v
   DENSE_OPT(pre, fn, "pre");
   DENSE_REQ(y, fn, "y");
   cudaStream_t s = (cudaStream_t)stream;
+  const int64_t elt = l.dtype == BDSCAN_F32 ? 4 : 2, oelt = l.out == BDSCAN_F32 ? 4 : 2;
+  const Span to{"y", y, l.T, l.N * oelt, l.ld_y * oelt};
+  rc = check_apart(fn,
+                   {Span{"x", x, l.T, l.K * elt, l.ld_x * elt}, dense_span("w", w, l.N * l.K * elt),
+                    dense_span("bias", bias, l.N * elt)},
+                   {to, dense_span("pre", pre, l.T * l.N * elt)});
+  // y may be the residual itself
+  if (!rc && (residual != y || (l.T > 1 && l.ld_res != l.ld_y)))
+    rc = check_apart(fn, {Span{"residual", residual, l.T, l.N * oelt, l.ld_res * oelt}}, {to});
+  if (rc) return rc;
   if (l.T <= kVecRows) {
     VecParams v{};
     v.x = x, v.w = w, v.bias = bias, v.res = residual, v.y = y, v.pre = pre;
@@ -1119,6 +1135,12 @@ int bdscan_gated_linear_forward(const bdscan_gated_linear_dims* dims, const void
   DENSE_REQ(y, fn, "y");
   cudaStream_t s = (cudaStream_t)stream;
   const int f32 = l.dtype == BDSCAN_F32;
+  const int64_t elt = f32 ? 4 : 2;
+  rc = check_apart(fn,
+                   {Span{"x", x, l.T, l.K * elt, l.ld_x * elt}, dense_span("w", w, 2 * l.F * l.K * elt),
+                    dense_span("bias", bias, 2 * l.F * elt)},
+                   {Span{"y", y, l.T, l.F * elt, l.ld_y * elt}});
+  if (rc) return rc;
   if (l.T <= gated_vec_rows(l)) {
     VecParams v{};
     v.x = x, v.w = w, v.bias = bias, v.y = y;
@@ -1187,6 +1209,13 @@ int bdscan_gated_linear_backward(const bdscan_gated_linear_dims* dims, const voi
   DENSE_REQ(dy, fn, "dy");
   const GatedBwdWs ws = gated_bwd_ws(l);
   if ((rc = check_workspace(workspace, workspace_bytes, ws.total, fn))) return rc;
+  rc = check_apart(fn,
+                   {Span{"x", x, l.T, (int64_t)(l.K * elt), (int64_t)(l.ld_x * elt)}, dense_span("w", w, N * l.K * elt),
+                    dense_span("bias", bias, N * elt),
+                    Span{"dy", dy, l.T, (int64_t)(l.F * elt), (int64_t)(l.ld_y * elt)}},
+                   {dense_span("dx", dx, l.T * l.K * elt), dense_span("dw", dw, N * l.K * elt),
+                    dense_span("dbias", dbias, N * elt)});
+  if (rc) return rc;
   int* flag;
   if ((rc = check_device(fn, &flag))) return rc;
   char* base = (char*)workspace;
@@ -1354,6 +1383,13 @@ int bdscan_distill_loss_forward(const bdscan_distill_loss_dims* dims, const void
   DENSE_REQ(z, fn, "z");
   const LossFwdWs ws = loss_fwd_ws(l);
   if ((rc = check_workspace(workspace, workspace_bytes, ws.total + target_bytes(l), fn))) return rc;
+  const int64_t elt = l.dtype == BDSCAN_F32 ? 4 : 2, entries = l.T * dims->top;
+  rc = check_apart(fn,
+                   {Span{"h", h, l.T, l.K * elt, l.ld_h * elt}, dense_span("w", w, l.V * l.K * elt),
+                    dense_span("ids", ids, entries * 8), dense_span("teacher", teacher, entries * 4),
+                    dense_span("weight", weight, l.T * 4)},
+                   {dense_span("loss", loss, l.T * 4), dense_span("lse", lse, l.T * 4), dense_span("z", z, entries * 4)});
+  if (rc) return rc;
   int* flag;
   if ((rc = check_device(fn, &flag))) return rc;
   cudaStream_t s = (cudaStream_t)stream;
@@ -1419,6 +1455,14 @@ int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const voi
   DENSE_REQ(dh, fn, "dh");
   const LossBwdWs ws = loss_bwd_ws(l);
   if ((rc = check_workspace(workspace, workspace_bytes, ws.total + distill_bwd_bytes(l, dims->top), fn))) return rc;
+  const int64_t elt = l.dtype == BDSCAN_F32 ? 4 : 2, entries = l.T * dims->top;
+  rc = check_apart(fn,
+                   {Span{"h", h, l.T, l.K * elt, l.ld_h * elt}, dense_span("w", w, l.V * l.K * elt),
+                    dense_span("ids", ids, entries * 8), dense_span("teacher", teacher, entries * 4),
+                    dense_span("weight", weight, l.T * 4), dense_span("lse", lse, l.T * 4),
+                    dense_span("z", z, entries * 4), dense_span("dloss", dloss, l.T * 4)},
+                   {dense_span("dh", dh, l.T * l.K * elt), dense_span("dw", dw, l.V * l.K * elt)});
+  if (rc) return rc;
   int* flag;
   if ((rc = check_device(fn, &flag))) return rc;
   char* base = (char*)workspace;

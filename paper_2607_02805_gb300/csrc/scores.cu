@@ -29,6 +29,7 @@
 #include "bdscan_dense.h"
 #include "debug.cuh"
 #include "device.cuh"
+#include "overlap.h"
 #include "params.h"
 #include "ssd_common.cuh"
 
@@ -980,6 +981,10 @@ int check_scores(const bdscan_token_scores_dims* d, ScoresParams* p, const char*
   p->parts = 1;
   return BDSCAN_OK;
 }
+int check_apart(const char* fn, std::initializer_list<Span> reads, std::initializer_list<Span> writes) {
+  char msg[128];
+  return any_overlap(reads, writes, msg, sizeof(msg)) ? fail(BDSCAN_ERR_ARG, fn, msg) : BDSCAN_OK;
+}
 int done(cudaError_t e, const char* fn, cudaStream_t s) {
   e = api_launched(e, s);
   return e == cudaSuccess ? api_ok() : fail(BDSCAN_ERR_CUDA, fn, cudaGetErrorString(e));
@@ -1010,6 +1015,13 @@ int bdscan_token_scores_forward(const bdscan_token_scores_dims* dims, const void
     SCORES_REQ(top_ids, fn, "top_ids");
     SCORES_REQ(top_logp, fn, "top_logp");
   }
+  const int64_t elt = dims->dtype == BDSCAN_F32 ? 4 : 2, t = p.rows;
+  const int apart = check_apart(
+      fn, {Span{"logits", logits, t, p.vocab * elt, p.ld * elt}, dense_span("token", token, t * 8)},
+      {dense_span("logp", logp, t * 4), dense_span("entropy", entropy, t * 4), dense_span("stats", stats, t * 8),
+       dense_span("top_ids", p.top > 0 ? top_ids : nullptr, t * p.top * 8),
+       dense_span("top_logp", p.top > 0 ? top_logp : nullptr, t * p.top * 4)});
+  if (apart) return apart;
   p.logits = logits;
   p.token = token;
   p.logp = logp;
@@ -1039,6 +1051,16 @@ int bdscan_token_scores_backward(const bdscan_token_scores_dims* dims, const voi
   SCORES_REQ(dlogits, fn, "dlogits");
   if (dlogits == logits && p.rows > 1 && p.ld != p.ld_out)
     return fail(BDSCAN_ERR_ARG, fn, "dlogits is logits, with another row stride");
+  const int64_t elt = dims->dtype == BDSCAN_F32 ? 4 : 2, t = p.rows;
+  const Span to{"dlogits", dlogits, t, p.vocab * elt, p.ld_out * elt};
+  int apart = check_apart(fn,
+                          {dense_span("token", token, t * 8), dense_span("stats", stats, t * 8),
+                           dense_span("entropy", dentropy != nullptr ? entropy : nullptr, t * 4),
+                           dense_span("dlogp", dlogp, t * 4), dense_span("dentropy", dentropy, t * 4)},
+                          {to});
+  // in place, or nowhere near
+  if (!apart && dlogits != logits) apart = check_apart(fn, {Span{"logits", logits, t, p.vocab * elt, p.ld * elt}}, {to});
+  if (apart) return apart;
   p.logits = logits;
   p.token = token;
   p.stats_in = (const float2*)stats;

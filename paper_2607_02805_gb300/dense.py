@@ -71,7 +71,8 @@ def _rows(name, t, shape, dtype, index):
 
 
 def _apart(name, at, *outputs):
-    """Refuses an input (its address) that the call overwrites while it reads it: what the holder returned before."""
+    """Refuses an input (its address) that the call overwrites while it reads it: what the holder returned before.
+    Views that share a part of their memory with an output are refused by the library."""
     if at and at in outputs:
         raise ValueError(f"{name} is a buffer that this call writes: pass a copy, or use a holder of its own")
 

@@ -14,7 +14,7 @@ import test_distill_gpu  # noqa: E402
 import test_gated_gpu  # noqa: E402
 import test_scores_gpu  # noqa: E402
 from paper_2607_02805_gb300 import binding  # noqa: E402
-from paper_2607_02805_gb300.dense import DistillLoss, GatedLinear, TokenScores  # noqa: E402
+from paper_2607_02805_gb300.dense import DistillLoss, GatedLinear, Linear, TokenScores  # noqa: E402
 
 B, F = torch.bfloat16, torch.float32
 
@@ -112,3 +112,25 @@ def test_functions_of_the_binding():
     op = DistillLoss(100, 72, 300, 4, excluded=299, temperature=1.1)
     assert all(torch.equal(p, q) for p, q in zip((loss, lse), op.forward(h, head, ids, best)))
     assert all(torch.equal(p, q) for p, q in zip((dh, dhead), op.backward(h, head, ids, best)))
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("rows", [2, 40])
+def test_columns_side_by_side_share_nothing(rows, dtype):
+    """Inputs and outputs between one another's columns of one buffer: as with buffers of their own."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    wide = torch.randn(rows, 200, generator=g, device="cuda").to(dtype)
+    w = torch.randn(128, 64, generator=g, device="cuda").to(dtype) / 8
+    x, y = wide[:, 8:72], wide[:, 72:136]  # directly behind one another
+    for op, weights in ((GatedLinear(rows, 64, 64, dtype=dtype), w), (Linear(rows, 64, 64, dtype=dtype), w[:64])):
+        want = op.forward(x.clone(), weights).clone()
+        assert torch.equal(op.forward(x, weights, out=y), want)
+    linear = Linear(rows, 64, 64, dtype=dtype)
+    want = linear.forward(x, w[:64], residual=y.clone()).clone()
+    assert torch.equal(linear.forward(x, w[:64], residual=y, out=y), want)  # in place
+    scores = TokenScores(rows, 64, 4, dtype)
+    dh = torch.ones(rows, device="cuda")
+    scores.forward(x)
+    want = scores.backward(x, dentropy=dh).clone()
+    assert torch.equal(scores.backward(x, dentropy=dh, out=y), want)
+    assert torch.equal(scores.backward(x, dentropy=dh, out=x), want)
