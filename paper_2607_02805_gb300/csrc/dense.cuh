@@ -208,8 +208,7 @@ struct DistillParams {
   const float* gscale;
   void* dw;
 };
-constexpr int kFewRows = 16;      // rows that count, up to which launch_distill_dw writes
-constexpr int kFewRowsCall = 128; // rows up to which it is launched
+constexpr int kFewRows = 32;  // rows that count, up to which launch_distill_dw writes
 cudaError_t launch_distill_dw(const DistillParams& p, cudaStream_t s);
 cudaError_t launch_distill_grad(const DistillParams& p, cudaStream_t s);
 cudaError_t launch_distill_join(const DistillParams& p, int f32, cudaStream_t s);

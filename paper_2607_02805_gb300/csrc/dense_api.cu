@@ -1507,7 +1507,7 @@ int bdscan_distill_loss_backward(const bdscan_distill_loss_dims* dims, const voi
           return api_launched(launch_distill_dz(piece(v0, n, dz), s), s);
         },
         [&](int64_t v0, int64_t n, const Operand& dz) {
-          if (l.pieces != 1 || l.T > kFewRowsCall) return cudaSuccess;
+          if (l.pieces != 1) return cudaSuccess;
           return api_launched(launch_distill_dw(piece(v0, n, dz), s), s);
         });
   return e == cudaSuccess ? api_ok() : cuda_fail(e, fn);

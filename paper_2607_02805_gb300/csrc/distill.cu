@@ -112,7 +112,7 @@ __device__ __forceinline__ float entry_grad(const DistillParams& p, float z, flo
 //     rounded instead, by 2^-16 / 3 * 0.54 in square, element by element.
 // (With the second rounding always there, dw was off by 2.9e-3 where the plain
 // form, rounded once, is by 1.7e-3; so by 2.4e-3.)
-// Calls of a few rows have the entries' rows of dw from k_distill_dw, and only dh
+// Where few rows count, the entries' rows of dw come from k_distill_dw, and only dh
 // reads their rounded gradients: there the best of a lane's factor each is taken
 // too, and what h loses does not count.
 __device__ __forceinline__ float rounding(float v) {
@@ -153,6 +153,39 @@ __device__ __forceinline__ float pick_scale(const Entries& e, const float (&s)[2
   return err_1 < err_m ? one : mant;
 }
 
+// Rows of 32 U from `first` on whose scales are not zero, by the lane. The loads are unconditional, so that all are in
+// flight.
+template <int U>
+__device__ __forceinline__ int some_scales(const DistillParams& p, int64_t first) {
+  const int64_t r0 = first + (threadIdx.x & 31), last = p.rows - 1;
+  float a[U], b[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) a[u] = b[u] = 1.f;
+  if (p.weight != nullptr) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) a[u] = p.weight[min(r0 + 32 * u, last)];
+  }
+  if (p.dloss != nullptr) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) b[u] = p.dloss[min(r0 + 32 * u, last)];
+  }
+  int c = 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) c += (r0 + 32 * u <= last) & (a[u] != 0.f) & (b[u] != 0.f);
+  return c;
+}
+// Whether up to kFewRows rows count, by a bound that all warps agree on: rows whose scales are not zero (some may know
+// no entry). The warps of a call of many are done with its first rows, c of the lane's among them; where they are few,
+// few warps go through all.
+constexpr int kFirstScales = 8;
+__device__ __forceinline__ bool few_scales(const DistillParams& p, int c) {
+  constexpr int U = 32;
+  int n = __reduce_add_sync(0xffffffffu, c);
+  for (int64_t first = 32 * kFirstScales; n <= kFewRows && first < p.rows; first += 32 * U)
+    n += __reduce_add_sync(0xffffffffu, some_scales<U>(p, first));
+  return n <= kFewRows;
+}
+
 // A warp per row: the gradient at its entries, which k_distill_dz puts in place
 // piece by piece of the vocabulary, and what it takes of the row's scale.
 __global__ void __launch_bounds__(kThreads) k_distill_grad(const DistillParams p) {
@@ -163,6 +196,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_grad(const DistillParams p
   if (!dguard(kSiteDistill, row, p.rows)) return;
   const float wt = p.weight != nullptr ? p.weight[row] : 1.f, dl = p.dloss != nullptr ? p.dloss[row] : 1.f;
   const float g = wt * (dl * p.scale);  // may be zero where neither is
+  const int scales = p.row_scale != nullptr ? some_scales<kFirstScales>(p, 0) : 0;
   Entries e;
   float share[2], s[2] = {0.f, 0.f};
   load_entries(e, p, row);
@@ -173,7 +207,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_grad(const DistillParams p
 #pragma unroll
   for (int k = 0; k < 2; ++k)
     if (e.id[k] >= 0) s[k] = entry_grad(p, p.z_in[row * p.top + lane + 32 * k], lse, share[k]);
-  const float a = p.row_scale != nullptr ? pick_scale(e, s, g, p.rows <= kFewRows, p.top) : 1.f;
+  const float a = p.row_scale != nullptr ? pick_scale(e, s, g, few_scales(p, scales), p.top) : 1.f;
   if (lane == 0 && p.row_scale != nullptr) p.row_scale[row] = a;
 #pragma unroll
   for (int k = 0; k < 2; ++k)
@@ -305,39 +339,98 @@ __global__ void __launch_bounds__(kThreads) k_distill_dz(const DistillParams p) 
   }
 }
 
-// Where a few rows count, the rows of dw at their entries once more, from the
-// gradients before any rounding: dw[v] = sum_r g_r (p - q)_rv h_r, with what the
-// products read where v is no entry of row r. Over many rows the roundings of
-// g (p - q) and of the scaled copy of h are as likely up as down; of two rows
-// whose shares lie badly they left dw off by 2.5e-3 where the plain form is by
-// 1.7e-3. A CTA per entry; several entries of one id write the same sums.
+// Where up to kFewRows rows count, the rows of dw at their entries once more, from
+// the gradients before any rounding: dw[v] = sum_r g_r (p - q)_rv h_r, with what
+// the products read where v is no entry of row r. Over many rows the roundings of
+// g (p - q) and of the scaled copy of h are as likely up as down; few do not
+// average them out. dw's error over the plain form's (rounded once), the largest of
+// 24 draws of 24 entries of 21,707, whatever the number of rows in the call:
+//   rows that count      1     5    16    20    32    48   128
+//   by the products   1.64  1.51  1.57  1.49  1.43  1.41  1.36
+//   with this         1.02  1.12  1.03  1.03  1.02
+// (64 entries of 5000: 1.59 to 1.42, so 1.27 to 1.13.) From 32 rows on the error no
+// longer falls much, and the time rises: a step of 256 rows, 448 x 50021, takes 92 us
+// with 5 rows (without 88), 113 with 32 of 64 entries (98), and the 2 us of an empty
+// launch, 93.6 for 91.2, where more rows count.
+// A CTA takes four entries of a row, looks for their ids among all known ones, and
+// reads h once for the four: a chain of six latencies. Several entries of one id
+// write the same sums.
+constexpr int kDwEntries = 4;
 __global__ void __launch_bounds__(kThreads) k_distill_dw(const DistillParams p) {
   pdl_sync();
-  __shared__ float coef[kFewRows];
-  __shared__ const bf16* rows[kFewRows];
-  static_assert(kThreads == 16 * kFewRows, "sixteen threads per row look for the entry");
-  const int count = *p.count, slot = blockIdx.x / p.top;
+  constexpr int M = kDwEntries;
+  __shared__ float coef[M][kFewRows], scale[kFewRows];
+  __shared__ bool own[M][kFewRows];  // coef is that of the row's own entry
+  __shared__ int index[kFewRows];
+  static_assert(M * kFewRows <= kThreads, "a thread per gradient");
+  static_assert(kFewRows % 8 == 0, "coef[] in eights");
+  const int t = threadIdx.x, groups = (p.top + M - 1) / M, slot = blockIdx.x / groups, j0 = blockIdx.x % groups * M;
+  // read without waiting for the count: both have room for a tile of rows
+  const int mine = t < kFewRows ? p.idx[t] : 0;
+  const float by = t < kFewRows ? p.gscale[t] : 0.f;
+  const int count = *p.count;
   if (count > kFewRows || slot >= count) return;
-  const int64_t at = (int64_t)p.idx[slot] * p.top + blockIdx.x % p.top, id = p.ids[at], to = id - p.v0;
-  if (id < 0 || id == p.excluded || to < 0 || to >= p.n || p.teacher[at] == -INFINITY) return;
-  if (!dguard(kSiteDistill, (count - 1) * p.ld_dz + to, p.dz_extent)) return;
-  const int r = threadIdx.x / 16;
-  if (r < count && threadIdx.x % 16 == 0) {
-    coef[r] = __bfloat162float(p.dz[r * p.ld_dz + to]) * p.gscale[r];
-    rows[r] = static_cast<const bf16*>(p.h) + p.idx[r] * p.ld_h;
+  if (t < count) index[t] = mine, scale[t] = by;
+  if (t < M * kFewRows) own[t / kFewRows][t % kFewRows] = false;
+  __syncthreads();
+  int to[M];  // this piece's columns of the four, -1 where it is not known or not there
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    const int64_t at = (int64_t)index[slot] * p.top + min(j0 + m, p.top - 1), id = p.ids[at];
+    const bool known = p.teacher[at] != -INFINITY && id != p.excluded && id >= p.v0 && id < p.v0 + p.n;
+    to[m] = known ? (int)(id - p.v0) : -1;
+  }
+  if ((to[0] & to[1] & to[2] & to[3]) < 0) return;  // none; the whole CTA
+  // what the products read, and over it the rows' own entries
+  float read = 0.f;
+#pragma unroll
+  for (int m = 0; m < M; ++m)
+    if (to[m] >= 0 && t / kFewRows == m && t % kFewRows < count) {
+      const int64_t at = t % kFewRows * p.ld_dz + to[m];
+      if (dguard(kSiteDistill, at, p.dz_extent)) read = __bfloat162float(p.dz[at]);
+    }
+#pragma unroll 2
+  for (int x = t; x < count * p.top; x += kThreads) {
+    const int r = x / p.top;
+    const int64_t at = (int64_t)index[r] * p.top + (x - r * p.top), id = p.ids[at] - p.v0;
+    const float teacher = p.teacher[at], grad = p.grad[at];
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+      if (to[m] >= 0 && id == to[m] && teacher != -INFINITY) coef[m][r] = grad * scale[r], own[m][r] = true;
   }
   __syncthreads();
-  if (r < count)
-    for (int j = threadIdx.x % 16; j < p.top; j += 16) {
-      const int64_t x = (int64_t)p.idx[r] * p.top + j;
-      if (p.ids[x] == id && p.teacher[x] != -INFINITY) coef[r] = p.grad[x] * p.gscale[r];
-    }
+  if (t < M * kFewRows && t % kFewRows < count && !own[t / kFewRows][t % kFewRows])
+    coef[t / kFewRows][t % kFewRows] = read * scale[t % kFewRows];
   __syncthreads();
-  bf16* out = static_cast<bf16*>(p.dw) + id * p.d_model;
-  for (int c = threadIdx.x; c < p.d_model; c += kThreads) {
-    float sum = 0.f;
-    for (int k = 0; k < count; ++k) sum = fmaf(coef[k], __bfloat162float(rows[k][c]), sum);
-    out[c] = __float2bfloat16_rn(sum);
+  const bf16* h = static_cast<const bf16*>(p.h);
+  bf16* out = static_cast<bf16*>(p.dw);
+  constexpr int U = 2, K = 8;  // columns of a thread, and rows of them in flight
+  for (int c0 = t; c0 < p.d_model; c0 += U * kThreads) {
+    float sum[M][U] = {};
+    for (int k0 = 0; k0 < count; k0 += K) {
+      float v[K][U];  // no branch between the loads and their use: all are in flight
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const bf16* row = h + index[min(k0 + k, count - 1)] * p.ld_h;
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[k][u] = __bfloat162float(row[min(c0 + u * kThreads, p.d_model - 1)]);
+      }
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          const float by = coef[m][k0 + k];
+#pragma unroll
+          for (int u = 0; u < U; ++u) sum[m][u] = k0 + k < count ? fmaf(by, v[k][u], sum[m][u]) : sum[m][u];
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * kThreads;
+        if (to[m] >= 0 && c < p.d_model) out[(p.v0 + to[m]) * (int64_t)p.d_model + c] = __float2bfloat16_rn(sum[m][u]);
+      }
   }
 }
 
@@ -345,7 +438,8 @@ __global__ void __launch_bounds__(kThreads) k_distill_dw(const DistillParams p) 
 
 cudaError_t launch_distill_dw(const DistillParams& p, cudaStream_t s) {
   const int64_t slots = p.rows < kFewRows ? p.rows : kFewRows;
-  launch_pdl(k_distill_dw, dim3((unsigned)(slots * p.top)), dim3(kThreads), 0, s, p);
+  const int64_t groups = (p.top + kDwEntries - 1) / kDwEntries;
+  launch_pdl(k_distill_dw, dim3((unsigned)(slots * groups)), dim3(kThreads), 0, s, p);
   return cudaGetLastError();
 }
 cudaError_t launch_distill_grad(const DistillParams& p, cudaStream_t s) {

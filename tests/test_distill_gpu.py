@@ -236,6 +236,43 @@ def test_gradients_of_a_few_rows_are_rounded_once(t):
         assert not at.any() or bad.max() <= 0, (seed, float(bad.max()))
 
 
+@pytest.mark.parametrize("t", [32, 129, 256, 2500])
+@pytest.mark.parametrize("count", [1, 5, 17, 32])
+def test_few_rows_that_count_whatever_the_call_holds(t, count):
+    """dw rounded once as above, for any number of other rows, and dh as of a call of those rows alone: with the same
+    statistics the same gradients are rounded at the entries, so that what is between the two calls is each result's
+    rounding, 2^-8 of it, that of p elsewhere, 2^-8 of the terms in each, and fp32 sums over the vocabulary."""
+    k, v, n = 448, 5000, 24
+    for seed in range(3):
+        h, w, ids, teacher, _, dloss = case(t, k, v, n, B, 1.0, False, 200 + seed)
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        at = torch.randperm(t, generator=g, device="cuda")[:count].sort().values
+        weight = torch.zeros(t, device="cuda")
+        weight[at] = torch.rand(count, generator=g, device="cuda") + 0.1
+        op, alone = DistillLoss(t, k, v, n), DistillLoss(count, k, v, n)
+        op.forward(h, w, ids, teacher, weight)
+        dh, dw = op.backward(h, w, ids, teacher, weight, dloss)
+        few = [u[at].contiguous() for u in (h, ids, teacher, weight, dloss)]
+        alone.forward(few[0], w, *few[1:4])
+        alone._buf["lse"].copy_(op._buf["lse"][at])
+        alone._buf["z"].copy_(op._buf["z"][at])
+        dh_alone = alone.backward(few[0], w, *few[1:])[0].double().cpu()
+        hd, wd, wt = few[0].double().cpu(), w.double().cpu(), (few[3] * few[4]).double().cpu()
+        z, where = hd @ wd.T, few[1].cpu()
+        p, q = torch.softmax(z, 1), torch.zeros(count, v, dtype=torch.float64)
+        q.scatter_add_(1, where, torch.softmax(few[2].double().cpu(), 1))
+        own = torch.zeros(count, v, dtype=torch.bool).scatter_(1, where, True)
+        rest, both = wt[:, None] * p * ~own, wt[:, None] * (p + q)
+        share = 2 * (2 * e32(k) * float(z.abs().max()) + 4e-6 * (1 + float(z.abs().max())))
+        want, got = (wt[:, None] * (p - q)).T @ hd, dw.double().cpu()
+        tol = 2.0 ** -8 * (want.abs() + 2 * rest.T @ hd.abs()) + (share + 32 * 2.0 ** -24) * (both.T @ hd.abs())
+        assert ((got - want).abs() - tol)[own.any(0)].max() <= 0, (seed, "dw")
+        got, want = dh[at].double().cpu(), dh_alone
+        tol = 2 * 2.0 ** -8 * (want.abs() + rest @ wd.abs()) + 2 * e32(v) * want.abs().max() + 1e-9
+        assert ((got - want).abs() - tol).max() <= 0, (seed, "dh")
+        assert not dh[weight == 0].any()
+
+
 def test_a_student_that_agrees_has_no_loss():
     """Teacher and student the same over a vocabulary of which all entries are known."""
     for dtype in (B, F):
