@@ -284,6 +284,7 @@ GemmParams geometry(const Plan& q, int64_t m, int64_t n, int64_t k, int* flag) {
   p.group_m = q.group_m;
   // rows outside the operand are filled at a row's cost too (24 rows, 832 x 50304, w in L2: 21.8 us by 128, 12.8 by
   // 24); in the last of several tiles, smaller boxes brought nothing (300 x 1024 x 4000: 8.7 us against 7.1)
+  // The tile's other rows are what an earlier kernel left in shared memory, NaN among it: no epilogue may use them.
   p.a_rows = m < 128 ? (int)up(m, 8) : 128;
   p.excluded = -1;
   p.scale = 1.f;
